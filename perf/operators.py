@@ -26,7 +26,7 @@ H_14B = dict(Hq=40, Hkv=8, d=128)
 H_13B = dict(Hq=40, Hkv=40, d=128)  # no grouped queries
 H_D64 = dict(Hq=32, Hkv=8, d=64)
 H_TINY = dict(Hq=8, Hkv=8, d=64)
-E_MIN, E_MAX = 27, 238  # the exponent bytes that a write chooses from
+E_MIN, E_MAX = 27, 214  # the exponent bytes that a write chooses from
 MIN32 = -(1 << 31)
 
 
