@@ -31,6 +31,12 @@
  *                         pool, flattened into the tree the three calls above
  *                         verify (section 3.2, "Candidate Token Selection").
  *
+ * A KV cache held in 8 bits has the same cycle with calls of its own
+ * (ltd_kv_append_q8, ltd_tree_verify_attn_q8, ltd_kv_compact_q8), and a
+ * request's sampling rules (penalties, biases, a grammar's mask) stand between
+ * the target's logits and acceptance (ltd_token_counts,
+ * ltd_tree_process_logits, ltd_tree_accept_processed).
+ *
  * Conventions for every call
  * --------------------------
  * - All array pointers are DEVICE pointers, owned by the caller.  The library
@@ -78,6 +84,7 @@ extern "C" {
 #define LTD_STATUS_BAD_BLOCK 4  /* a block id the sequence uses is outside [0, num_blocks) */
 #define LTD_STATUS_BAD_PATH 5   /* accepted path not 0 = p_0 < p_1 < ..., or n_accepted out of range */
 #define LTD_STATUS_BAD_SCORE 6  /* a pool score is NaN or above its parent's */
+#define LTD_STATUS_BAD_RULE 7   /* a penalty is not finite, a repetition penalty <= 0, or n_bias out of range */
 
 #define LTD_MAX_NODES 256 /* largest Nmax (the paper's size policy spans V in [20, 240]) */
 #define LTD_MAX_POOL 1024 /* largest draft pool (1 + W + (D-2) W^2 = 1011 at W = 10, D = 12) */
@@ -87,6 +94,8 @@ extern "C" {
 #define LTD_EXPAND_MAX_W 16          /* children per frontier node (the paper's W is 10) */
 #define LTD_EXPAND_MAX_CHUNKS 64     /* vocabulary up to 64 * 4096 = 262144 entries */
 #define LTD_EXPAND_MAX_CHILDREN 256  /* F * W per round */
+
+#define LTD_MAX_BIAS 1024            /* biased tokens per sequence */
 
 #define LTD_POLICY_SIZE 0          /* state [D, L, score of every pool candidate, pad ...] */
 #define LTD_POLICY_DEPTH 1         /* state [scores of the newest in_dim-2 candidates, D, L] */
@@ -376,6 +385,168 @@ int ltd_policy_forward(int layout, const float* scores, const int32_t* pool_size
                        int h2, const float* wo, const float* bo, int n_out, int action_offset,
                        int action_scale, float* logits, int32_t* action, void* workspace,
                        size_t workspace_bytes, void* stream);
+
+/*
+ * The 8-bit KV cache.
+ *
+ * K and V rows are stored as OCP e4m3 codes (4 exponent and 3 fraction bits,
+ * largest value 448, no infinity, one NaN code), one byte per element, in the
+ * layouts of the attention call:
+ *   codes   contiguous [B][Hkv][kv_rows][d], paged [num_blocks][Hkv][kv_rows][d];
+ *   scales  [B or num_blocks][Hkv][ceil(kv_rows / scale_rows)] bytes, for K and
+ *           V apart: row r of a cache (row r of its block when paged) and head g
+ *           shares byte r / scale_rows with its neighbours.  A byte E stands for
+ *           the power of two 2^(E - 127), and a code c for c * 2^(E - 127).
+ * Powers of two keep all of a code's fraction bits: a value is exact in
+ * bfloat16 and float32, and a block whose scale grows loses bits only where a
+ * code falls below the format's normal range.
+ *   scale_rows  16, 32, 64 or 128; a paged cache's kv_rows is a multiple of it.
+ *   d           64 or 128.
+ * Anything else is LTD_EUNSUPPORTED.  Codes and rows passed to these calls are
+ * 16-byte aligned (LTD_EINVAL otherwise).  Scale bytes of rows in use lie in
+ * [27, 214], as ltd_kv_append_q8 writes them: values of up to 2^96, so that
+ * float32 sums of them under softmax weights stay finite.
+ */
+
+/*
+ * Appends rows to an 8-bit KV cache: a prompt's, or a draft tree's before its
+ * verification.
+ *
+ * For every sequence b, kv head g and K and V apart, rows i < n_rows[b] of the
+ * input become logical rows P_b + i of the cache (P_b = prefix_len[b]).  A
+ * block of scale_rows rows that receives rows takes the smallest scale byte in
+ * [27, 214] under which the block's new values are at most 448 in magnitude; if
+ * it also holds rows below P_b, its scale is not lowered, and when it grows
+ * those rows are encoded again.  Codes are rounded to nearest even.  NaN is
+ * stored as NaN and has no part in the scale; infinities, and values above
+ * 448 * 2^87, are stored as the largest code.  Other rows keep their bytes,
+ * but rows past P_b + n_rows[b] in a block that receives rows stand for
+ * undefined values afterwards (their scale may have changed).
+ *
+ *   k_new, v_new  [B][Nmax][Hkv][d] (dtype), with new_row_stride elements from
+ *                 one row to the next (at least Hkv * d; rows may be views into
+ *                 a fused projection's output); row i of sequence b starts at
+ *                 (b * Nmax + i) * new_row_stride.  Each row is 16-byte aligned.
+ *   n_rows        [B] int32 in [0, Nmax]; Nmax >= 1 has no upper limit here.
+ *   prefix_len    [B] int32 (read only).
+ * No two sequences may append to the same block.  With validate != 0:
+ * LTD_STATUS_BAD_NNODES (n_rows), LTD_STATUS_BAD_PREFIX (P_b < 0 or rows past
+ * the capacity) and LTD_STATUS_BAD_BLOCK (ids of the blocks that are written).
+ */
+int ltd_kv_append_q8(const void* k_new, const void* v_new, int64_t new_row_stride, void* k_cache,
+                     void* v_cache, uint8_t* k_scale, uint8_t* v_scale, const int32_t* block_table,
+                     const int32_t* prefix_len, const int32_t* n_rows, int B, int Nmax, int Hkv,
+                     int d, int kv_rows, int max_blocks, int num_blocks, int scale_rows, int dtype,
+                     int validate, int32_t* status, void* stream);
+
+/*
+ * Tree attention over an 8-bit KV cache: ltd_tree_verify_attn with K and V the
+ * values their codes and scales stand for.  dtype is that of q and out.  The
+ * other arguments, limits and results are that call's; the workspace is sized by
+ * ltd_tree_verify_attn_q8_workspace_size().  A NaN code in a tree row reaches
+ * the outputs of the nodes that see the row, and no others: a NaN in a visible
+ * row's V may make every dimension of those outputs NaN.
+ */
+size_t ltd_tree_verify_attn_q8_workspace_size(int B, int Nmax, int Hq, int Hkv, int d,
+                                              int max_prefix, int dtype);
+
+int ltd_tree_verify_attn_q8(const void* q, const void* k_cache, const void* v_cache,
+                            const uint8_t* k_scale, const uint8_t* v_scale,
+                            const int32_t* block_table, const int32_t* prefix_len,
+                            const int32_t* parents, const int32_t* n_nodes, void* out, int B,
+                            int Nmax, int Hq, int Hkv, int d, int max_prefix, int kv_rows,
+                            int max_blocks, int num_blocks, int scale_rows, float scale, int dtype,
+                            void* workspace, size_t workspace_bytes, int validate, int32_t* status,
+                            void* stream);
+
+/*
+ * Compaction of an 8-bit KV cache: ltd_kv_compact on codes and scales.
+ *
+ * Rows move as there.  A block that receives rows (or keeps accepted ones)
+ * takes the largest of their scale bytes, and its own if it holds rows below
+ * P_b; every row of it below P_b + n_accepted[b] whose scale byte was smaller is
+ * encoded again (rounded to nearest even), others keep their codes.  Rows >=
+ * P_b + n_accepted[b] stand for undefined values afterwards.
+ *   layer_stride_elems  codes from one layer to the next (K and V);
+ *   scale_stride_elems  scale bytes from one layer to the next; both > 0 with
+ *                       more than one layer.
+ */
+int ltd_kv_compact_q8(void* k_cache, void* v_cache, uint8_t* k_scale, uint8_t* v_scale,
+                      const int32_t* block_table, const int32_t* prefix_len,
+                      int32_t* new_prefix_len, const int32_t* accepted_nodes,
+                      const int32_t* n_accepted, int B, int Nmax, int Hkv, int d, int kv_rows,
+                      int max_blocks, int num_blocks, int scale_rows, int num_layers,
+                      int64_t layer_stride_elems, int64_t scale_stride_elems, int validate,
+                      int32_t* status, void* stream);
+
+/*
+ * The table of token occurrences that penalties read, kept by the caller from
+ * one cycle to the next.
+ *
+ *   counts    [B][Voc] int32: bits 0 .. 30 count how often the token was
+ *             emitted, bit 31 is set when it occurs in the prompt.
+ *   tokens    [B][T] int32, the first n_tokens[b] of row b are taken
+ *             (n_tokens[b] is clamped into [0, T]; tokens outside [0, Voc) are
+ *             skipped).  prompt == 0: each occurrence adds one to its count (the
+ *             out_tokens and n_accepted of an acceptance call); prompt != 0: sets
+ *             bit 31.
+ *   reset     != 0: the table is zeroed first (a new request).
+ */
+int ltd_token_counts(const int32_t* tokens, const int32_t* n_tokens, int B, int T, int Voc,
+                     int prompt, int reset, int32_t* counts, void* stream);
+
+/*
+ * A request's sampling rules on the target's logits, at every tree node.
+ *
+ * For node i < n_nodes[b] and token v let c be v's emitted count (counts) plus
+ * its occurrences among the draft tokens of node i's root path, node i included
+ * and the root left out (the root was emitted: counts has it).  With
+ * (r, f, p) = penalties[b], x = logits[b][i][v] becomes, in float32 with every
+ * step rounded,
+ *     x > 0 ? x / r : x * r     if c > 0 or v occurs in the prompt,
+ *     x - f * c, then x - p     if c > 0,
+ *     x + bias                  if v is in the bias list (entries of one token
+ *                               are added to each other in list order first),
+ *     -infinity                 if v's bit of the node's mask is 0.
+ * Tokens that no rule touches keep their bits.  A node whose mask allows
+ * nothing gets -infinity everywhere.
+ *
+ *   logits, out  [B][Nmax][Voc] float32; out may be logits (in place), but no
+ *                other overlap.  Rows i >= n_nodes[b] are not written.
+ *   draft_tokens [B][Nmax]; tokens outside [0, Voc) occur nowhere.
+ *   counts       [B][Voc] as kept by ltd_token_counts, or NULL (all zero).
+ *   penalties    [B][3] float32: repetition (> 0; 1 = none), frequency and
+ *                presence (0 = none), all finite; NULL = none, and counts is then not read.
+ *   bias_tokens, bias_values [B][max_bias], n_bias [B] int32 in [0, max_bias]:
+ *                the lists; NULL with max_bias == 0 (max_bias <=
+ *                LTD_MAX_BIAS).  Tokens outside [0, Voc) are skipped.
+ *   mask         [B][Nmax][ceil(Voc / 32)] uint32: bit v % 32 of word v / 32
+ *                allows token v; NULL = everything is allowed.
+ * With validate != 0: LTD_STATUS_BAD_NNODES, LTD_STATUS_BAD_PARENT and
+ * LTD_STATUS_BAD_RULE.
+ */
+int ltd_tree_process_logits(const float* logits, const int32_t* draft_tokens,
+                            const int32_t* parents, const int32_t* n_nodes, const int32_t* counts,
+                            const float* penalties, const int32_t* bias_tokens,
+                            const float* bias_values, const int32_t* n_bias, const uint32_t* mask,
+                            int B, int Nmax, int Voc, int max_bias, float* out, int validate,
+                            int32_t* status, void* stream);
+
+/*
+ * Greedy acceptance (ltd_tree_accept) on the logits that
+ * ltd_tree_process_logits would write, without writing them.  The rules are that
+ * call's arguments, the outputs and the workspace
+ * (ltd_tree_accept_workspace_size()) ltd_tree_accept's.  A node whose mask
+ * allows nothing predicts token 0.
+ */
+int ltd_tree_accept_processed(const float* logits, const int32_t* draft_tokens,
+                              const int32_t* parents, const int32_t* n_nodes,
+                              const int32_t* counts, const float* penalties,
+                              const int32_t* bias_tokens, const float* bias_values,
+                              const int32_t* n_bias, const uint32_t* mask, int B, int Nmax,
+                              int Voc, int max_bias, int32_t* pred, int32_t* accepted_nodes,
+                              int32_t* out_tokens, int32_t* n_accepted, void* workspace,
+                              size_t workspace_bytes, int validate, int32_t* status, void* stream);
 
 /* Library version string. */
 const char* ltd_version(void);

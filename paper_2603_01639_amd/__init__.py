@@ -33,8 +33,10 @@ STATUS_BAD_PREFIX = 3
 STATUS_BAD_BLOCK = 4
 STATUS_BAD_PATH = 5
 STATUS_BAD_SCORE = 6
+STATUS_BAD_RULE = 7
 
 MAX_NODES = 256
+MAX_BIAS = 1024
 MAX_POOL = 1024
 POLICY_SIZE = 0
 POLICY_DEPTH = 1
@@ -56,6 +58,13 @@ EXPORTED = (
     "ltd_tree_accept_sampling",
     "ltd_tree_accept_noalloc_max_bytes",
     "ltd_tree_accept_noalloc",
+    "ltd_kv_append_q8",
+    "ltd_tree_verify_attn_q8_workspace_size",
+    "ltd_tree_verify_attn_q8",
+    "ltd_kv_compact_q8",
+    "ltd_token_counts",
+    "ltd_tree_process_logits",
+    "ltd_tree_accept_processed",
 )
 
 
@@ -110,6 +119,20 @@ def lib() -> ctypes.CDLL:
         L.ltd_tree_accept_sampling.argtypes = [P] * 6 + [i32] * 3 + [f32] + [P] * 4 + [sz, i32, P,
                                                                                      P]
         L.ltd_tree_accept_sampling.restype = i32
+        L.ltd_kv_append_q8.argtypes = [P, P, i64] + [P] * 7 + [i32] * 10 + [P, P]
+        L.ltd_kv_append_q8.restype = i32
+        L.ltd_tree_verify_attn_q8_workspace_size.argtypes = [i32] * 7
+        L.ltd_tree_verify_attn_q8_workspace_size.restype = sz
+        L.ltd_tree_verify_attn_q8.argtypes = [P] * 10 + [i32] * 10 + [f32, i32, P, sz, i32, P, P]
+        L.ltd_tree_verify_attn_q8.restype = i32
+        L.ltd_kv_compact_q8.argtypes = [P] * 9 + [i32] * 9 + [i64, i64, i32, P, P]
+        L.ltd_kv_compact_q8.restype = i32
+        L.ltd_token_counts.argtypes = [P, P] + [i32] * 5 + [P, P]
+        L.ltd_token_counts.restype = i32
+        L.ltd_tree_process_logits.argtypes = [P] * 10 + [i32] * 4 + [P, i32, P, P]
+        L.ltd_tree_process_logits.restype = i32
+        L.ltd_tree_accept_processed.argtypes = [P] * 10 + [i32] * 4 + [P] * 5 + [sz, i32, P, P]
+        L.ltd_tree_accept_processed.restype = i32
         L.ltd_version.argtypes = []
         L.ltd_version.restype = ctypes.c_char_p
         _lib = L
@@ -322,3 +345,259 @@ def tree_accept_sampling(logits, draft_probs, draft_tokens, parents, n_nodes, un
         _p(workspace), workspace.numel() * workspace.element_size(), int(validate), _p(status),
         _stream(stream))
     _check("ltd_tree_accept_sampling", rc)
+
+
+# ---- the 8-bit KV cache and the sampling rules.  These calls check their
+# tensors (types, shapes, layouts, one device) before they pass pointers on, and
+# run on the tensors' GPU whichever is current.
+
+def _want(name, t, dtypes, shape):
+    """t has one of the types and the shape (None in it: any size) and is contiguous."""
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} has type {t.dtype}, not {' or '.join(map(str, dtypes))}")
+    if len(t.shape) != len(shape) or any(w is not None and w != h for w, h in zip(shape, t.shape)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not "
+                         f"({', '.join('*' if w is None else str(w) for w in shape)})")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+
+
+def _int32(shape, **tensors):
+    import torch
+    for name, t in tensors.items():
+        if t is not None:
+            _want(name, t, (torch.int32,), shape)
+
+
+def _run(fn, args, tensors, stream):
+    """Calls ltd_<fn>(*args, stream) on the GPU that holds the tensors."""
+    import torch
+    dev = tensors[0].device
+    if dev.type != "cuda":
+        raise ValueError(f"{fn} needs tensors on a GPU, not on {dev}")
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError(f"{fn}: tensors on {dev} and on {t.device}")
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"{fn}: tensors on {dev}, a stream of {stream.device}")
+    call = getattr(lib(), fn)
+    if torch.cuda.current_device() == dev.index:
+        rc = call(*args, _stream(stream))
+    else:
+        with torch.cuda.device(dev):
+            rc = call(*args, _stream(stream))
+    _check(fn, rc)
+
+
+def _q8_cache(k_cache, v_cache, k_scale, v_scale, block_table, num_blocks, scale_rows, lead):
+    """The geometry of an 8-bit cache of `lead` leading dimensions (layers):
+    kv heads, rows of a page, head size, blocks a sequence."""
+    import torch
+    if scale_rows not in (16, 32, 64, 128):
+        raise ValueError(f"scale_rows is {scale_rows}, not 16, 32, 64 or 128")
+    if k_cache.dim() != lead + 4:
+        raise ValueError(f"k_cache has {k_cache.dim()} dimensions, not {lead + 4}")
+    pages, Hkv, kv_rows, d = k_cache.shape[lead:]
+    codes = (torch.float8_e4m3fn, torch.uint8)
+    scales = (torch.uint8, torch.float8_e8m0fnu)
+    shape = tuple(k_cache.shape)
+    _want("k_cache", k_cache, codes, shape)
+    _want("v_cache", v_cache, codes, shape)
+    sshape = shape[:lead + 2] + (-(-kv_rows // scale_rows),)
+    _want("k_scale", k_scale, scales, sshape)
+    _want("v_scale", v_scale, scales, sshape)
+    max_blocks = 0
+    if block_table is not None:
+        _int32((None, None), block_table=block_table)
+        max_blocks = block_table.shape[1]
+        if num_blocks > pages:
+            raise ValueError(f"num_blocks is {num_blocks}, the cache holds {pages}")
+    return pages, Hkv, kv_rows, d, max_blocks
+
+
+def _batch_pages(B, pages, block_table):
+    """A contiguous cache holds a page per sequence, a block table a row."""
+    if block_table is None and pages < B:
+        raise ValueError(f"the cache holds {pages} sequences, the batch {B}")
+    if block_table is not None and block_table.shape[0] != B:
+        raise ValueError(f"block_table has {block_table.shape[0]} rows for {B} sequences")
+
+
+def _row_stride(name, t):
+    """Elements from one [Hkv][d] row of t [B][Nmax][Hkv][d] to the next."""
+    B, N, Hkv, d = t.shape
+    if d > 1 and t.stride(3) != 1 or Hkv > 1 and t.stride(2) != d:
+        raise ValueError(f"{name}: a row's heads and dims are not contiguous")
+    stride = t.stride(1) if N > 1 else t.stride(0) if B > 1 else Hkv * d
+    if B > 1 and t.stride(0) != N * stride:
+        raise ValueError(f"{name}: rows are not evenly spaced over the batch")
+    return stride
+
+
+def kv_append_q8(k_new, v_new, k_cache, v_cache, k_scale, v_scale, prefix_len, n_rows, *,
+                 scale_rows: int, block_table=None, num_blocks: int = 0, validate: bool = False,
+                 status=None, stream=None):
+    """Rows of a prompt or a draft tree into an 8-bit KV cache; see
+    ``ltd_kv_append_q8``.  k_new, v_new ``[B][Nmax][Hkv][d]`` (bfloat16 or
+    float32, views with evenly spaced rows welcome), caches ``[pages][Hkv][rows][d]``
+    float8_e4m3fn or uint8, scales ``[pages][Hkv][ceil(rows / scale_rows)]`` uint8."""
+    pages, Hkv, kv_rows, d, max_blocks = _q8_cache(k_cache, v_cache, k_scale, v_scale, block_table,
+                                                   num_blocks, scale_rows, 0)
+    dtype = _dtype_code(k_new)
+    if v_new.dtype != k_new.dtype:
+        raise TypeError(f"k_new has type {k_new.dtype}, v_new {v_new.dtype}")
+    if k_new.dim() != 4 or k_new.shape != v_new.shape or tuple(k_new.shape[2:]) != (Hkv, d):
+        raise ValueError(f"k_new {tuple(k_new.shape)} and v_new {tuple(v_new.shape)} are not both "
+                         f"(*, *, {Hkv}, {d})")
+    B, Nmax = k_new.shape[:2]
+    _batch_pages(B, pages, block_table)
+    _int32((B,), prefix_len=prefix_len, n_rows=n_rows)
+    if B == 0 or Nmax == 0:
+        return
+    stride = _row_stride("k_new", k_new)
+    if _row_stride("v_new", v_new) != stride:
+        raise ValueError("k_new and v_new have rows of different strides")
+    _run("ltd_kv_append_q8",
+         (_p(k_new), _p(v_new), stride, _p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale),
+          _p(block_table), _p(prefix_len), _p(n_rows), B, Nmax, Hkv, d, kv_rows, max_blocks,
+          int(num_blocks), int(scale_rows), dtype, int(validate), _p(status)),
+         (k_new, v_new, k_cache, v_cache, k_scale, v_scale, block_table, prefix_len, n_rows, status),
+         stream)
+
+
+def attn_q8_workspace_size(B, Nmax, Hq, Hkv, d, max_prefix, dtype) -> int:
+    return int(lib().ltd_tree_verify_attn_q8_workspace_size(B, Nmax, Hq, Hkv, d, max_prefix, dtype))
+
+
+def tree_verify_attn_q8(q, k_cache, v_cache, k_scale, v_scale, prefix_len, parents, n_nodes, out, *,
+                        max_prefix: int, scale_rows: int, block_table=None, num_blocks: int = 0,
+                        scale: Optional[float] = None, workspace=None, validate: bool = False,
+                        status=None, stream=None):
+    """Tree attention over an 8-bit KV cache; see ``ltd_tree_verify_attn_q8``.
+    q/out ``[B][Nmax][Hq][d]`` bfloat16 or float32, the cache as for
+    ``kv_append_q8``.  A single token a sequence is a tree of one node."""
+    pages, Hkv, kv_rows, d, max_blocks = _q8_cache(k_cache, v_cache, k_scale, v_scale, block_table,
+                                                   num_blocks, scale_rows, 0)
+    dtype = _dtype_code(q)
+    _want("q", q, (q.dtype,), (None, None, None, d))
+    _want("out", out, (q.dtype,), tuple(q.shape))
+    B, Nmax, Hq, _ = q.shape
+    _batch_pages(B, pages, block_table)
+    _int32((B,), prefix_len=prefix_len, n_nodes=n_nodes)
+    _int32((B, Nmax), parents=parents)
+    if scale is None:
+        scale = d ** -0.5
+    if workspace is None:
+        workspace = _alloc_workspace(attn_q8_workspace_size(B, Nmax, Hq, Hkv, d, max_prefix, dtype),
+                                     q.device)
+    _run("ltd_tree_verify_attn_q8",
+         (_p(q), _p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale), _p(block_table),
+          _p(prefix_len), _p(parents), _p(n_nodes), _p(out), B, Nmax, Hq, Hkv, d, int(max_prefix),
+          kv_rows, max_blocks, int(num_blocks), int(scale_rows), float(scale), dtype,
+          _p(workspace), workspace.numel() * workspace.element_size(), int(validate), _p(status)),
+         (q, k_cache, v_cache, k_scale, v_scale, block_table, prefix_len, parents, n_nodes, out,
+          workspace, status), stream)
+    return out
+
+
+def kv_compact_q8(k_cache, v_cache, k_scale, v_scale, prefix_len, new_prefix_len, accepted_nodes,
+                  n_accepted, *, scale_rows: int, block_table=None, num_blocks: int = 0,
+                  num_layers: int = 1, layer_stride_elems: int = 0, scale_stride_elems: int = 0,
+                  validate: bool = False, status=None, stream=None):
+    """In-place compaction of an 8-bit KV cache; see ``ltd_kv_compact_q8``.
+    With a leading dimension of layers, caches ``[layers][pages][Hkv][rows][d]``
+    and scales alike, the strides default to the tensors' own."""
+    lead = k_cache.dim() - 4
+    if lead not in (0, 1):
+        raise ValueError(f"k_cache has {k_cache.dim()} dimensions, not 4 or 5")
+    pages, Hkv, kv_rows, d, max_blocks = _q8_cache(k_cache, v_cache, k_scale, v_scale, block_table,
+                                                   num_blocks, scale_rows, lead)
+    if lead:
+        if num_layers > k_cache.shape[0]:
+            raise ValueError(f"num_layers is {num_layers}, the cache holds {k_cache.shape[0]}")
+        layer_stride_elems = layer_stride_elems or k_cache.stride(0)
+        scale_stride_elems = scale_stride_elems or k_scale.stride(0)
+    B, Nmax = accepted_nodes.shape
+    _batch_pages(B, pages, block_table)
+    _int32((B, Nmax), accepted_nodes=accepted_nodes)
+    _int32((B,), prefix_len=prefix_len, new_prefix_len=new_prefix_len, n_accepted=n_accepted)
+    _run("ltd_kv_compact_q8",
+         (_p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale), _p(block_table), _p(prefix_len),
+          _p(new_prefix_len), _p(accepted_nodes), _p(n_accepted), B, Nmax, Hkv, d, kv_rows,
+          max_blocks, int(num_blocks), int(scale_rows), int(num_layers), int(layer_stride_elems),
+          int(scale_stride_elems), int(validate), _p(status)),
+         (k_cache, v_cache, k_scale, v_scale, block_table, prefix_len, new_prefix_len,
+          accepted_nodes, n_accepted, status), stream)
+
+
+def token_counts(tokens, n_tokens, counts, *, prompt: bool = False, reset: bool = False,
+                 stream=None):
+    """Adds tokens ``[B][T]`` (the first n_tokens[b] of each row) to the table of
+    occurrences counts ``[B][Voc]`` int32; see ``ltd_token_counts``."""
+    _int32((None, None), tokens=tokens)
+    B, T = tokens.shape
+    _int32((B,), n_tokens=n_tokens)
+    _int32((B, None), counts=counts)
+    _run("ltd_token_counts",
+         (_p(tokens), _p(n_tokens), B, T, counts.shape[1], int(bool(prompt)), int(bool(reset)),
+          _p(counts)), (counts, tokens, n_tokens), stream)
+
+
+def _rules(logits, draft_tokens, parents, n_nodes, counts, penalties, bias_tokens, bias_values,
+           n_bias, mask):
+    """The checked arguments of a call with sampling rules, and its tensors."""
+    import torch
+    _want("logits", logits, (torch.float32,), (None, None, None))
+    B, Nmax, Voc = logits.shape
+    _int32((B, Nmax), draft_tokens=draft_tokens, parents=parents)
+    _int32((B,), n_nodes=n_nodes, n_bias=n_bias)
+    _int32((B, Voc), counts=counts)
+    _int32((B, Nmax, -(-Voc // 32)), mask=mask)
+    if penalties is not None:
+        _want("penalties", penalties, (torch.float32,), (B, 3))
+    max_bias = 0
+    if bias_tokens is not None:
+        if bias_values is None or n_bias is None:
+            raise ValueError("bias_tokens needs bias_values and n_bias")
+        _int32((B, None), bias_tokens=bias_tokens)
+        max_bias = bias_tokens.shape[1]
+        _want("bias_values", bias_values, (torch.float32,), (B, max_bias))
+    elif bias_values is not None or n_bias is not None:
+        raise ValueError("bias_values and n_bias need bias_tokens")
+    tensors = (logits, draft_tokens, parents, n_nodes, counts, penalties, bias_tokens, bias_values,
+               n_bias, mask)
+    return tuple(_p(t) for t in tensors) + (B, Nmax, Voc, max_bias), tensors
+
+
+def tree_process_logits(logits, draft_tokens, parents, n_nodes, out, *, counts=None, penalties=None,
+                        bias_tokens=None, bias_values=None, n_bias=None, mask=None,
+                        validate: bool = False, status=None, stream=None):
+    """Penalties, biases and masks on the logits ``[B][Nmax][Voc]`` of every tree
+    node, written to out (which may be logits itself); see
+    ``ltd_tree_process_logits``.  mask ``[B][Nmax][ceil(Voc / 32)]`` int32."""
+    import torch
+    args, tensors = _rules(logits, draft_tokens, parents, n_nodes, counts, penalties, bias_tokens,
+                           bias_values, n_bias, mask)
+    _want("out", out, (torch.float32,), tuple(logits.shape))
+    _run("ltd_tree_process_logits", args + (_p(out), int(validate), _p(status)),
+         tensors + (out, status), stream)
+    return out
+
+
+def tree_accept_processed(logits, draft_tokens, parents, n_nodes, pred, accepted_nodes, out_tokens,
+                          n_accepted, *, counts=None, penalties=None, bias_tokens=None,
+                          bias_values=None, n_bias=None, mask=None, workspace=None,
+                          validate: bool = False, status=None, stream=None):
+    """Greedy acceptance on processed logits, which are not written; see
+    ``ltd_tree_accept_processed``."""
+    args, tensors = _rules(logits, draft_tokens, parents, n_nodes, counts, penalties, bias_tokens,
+                           bias_values, n_bias, mask)
+    B, Nmax, Voc = logits.shape
+    _int32((B, Nmax), pred=pred, accepted_nodes=accepted_nodes, out_tokens=out_tokens)
+    _int32((B,), n_accepted=n_accepted)
+    if workspace is None:
+        workspace = _alloc_workspace(accept_workspace_size(B, Nmax, Voc), logits.device)
+    _run("ltd_tree_accept_processed",
+         args + (_p(pred), _p(accepted_nodes), _p(out_tokens), _p(n_accepted), _p(workspace),
+                 workspace.numel() * workspace.element_size(), int(validate), _p(status)),
+         tensors + (pred, accepted_nodes, out_tokens, n_accepted, workspace, status), stream)

@@ -258,6 +258,17 @@ size_t accept_workspace_bytes(int B, int Nmax, int Voc) {
   return static_cast<size_t>(B) * Nmax * chunks * sizeof(uint64_t);
 }
 
+hipError_t launch_accept_scan(const void* partial, const int32_t* draft_tokens,
+                              const int32_t* parents, const int32_t* n_nodes, int B, int Nmax,
+                              int Voc, int32_t* pred, int32_t* accepted_nodes, int32_t* out_tokens,
+                              int32_t* n_accepted, const int32_t* status, hipStream_t stream) {
+  const int chunks = (Voc + kChunk - 1) / kChunk;
+  hipLaunchKernelGGL(accept_scan_kernel, dim3(B), dim3(kScanThreads), 0, stream,
+                     static_cast<const uint64_t*>(partial), chunks, draft_tokens, parents, n_nodes,
+                     Nmax, pred, accepted_nodes, out_tokens, n_accepted, status);
+  return hipGetLastError();
+}
+
 hipError_t launch_accept(const float* logits, const int32_t* draft_tokens, const int32_t* parents,
                          const int32_t* n_nodes, int B, int Nmax, int Voc, int32_t* pred,
                          int32_t* accepted_nodes, int32_t* out_tokens, int32_t* n_accepted,
@@ -274,10 +285,8 @@ hipError_t launch_accept(const float* logits, const int32_t* draft_tokens, const
                        logits, n_nodes, Nmax, Voc, chunks, partial, status);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(accept_scan_kernel, dim3(B), dim3(kScanThreads), 0, stream, partial, chunks,
-                     draft_tokens, parents, n_nodes, Nmax, pred, accepted_nodes, out_tokens,
-                     n_accepted, status);
-  return hipGetLastError();
+  return launch_accept_scan(partial, draft_tokens, parents, n_nodes, B, Nmax, Voc, pred,
+                            accepted_nodes, out_tokens, n_accepted, status, stream);
 }
 
 }  // namespace ltd

@@ -41,7 +41,23 @@ bool attn_supported(int d, int dtype) {
 
 ltd::AttnShape make_shape(int B, int Nmax, int Hq, int Hkv, int d, int max_prefix, int kv_rows,
                           int max_blocks, int dtype) {
-  return ltd::AttnShape{B, Nmax, Hq, Hkv, d, max_prefix, kv_rows, max_blocks, dtype};
+  return ltd::AttnShape{B, Nmax, Hq, Hkv, d, max_prefix, kv_rows, max_blocks, dtype, 0};
+}
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// An 8-bit cache's geometry: what the kernels implement.
+bool q8_supported(int d, int kv_rows, int scale_rows, bool paged) {
+  return (d == 64 || d == 128) &&
+         (scale_rows == 16 || scale_rows == 32 || scale_rows == 64 || scale_rows == 128) &&
+         (!paged || kv_rows % scale_rows == 0);
+}
+
+ltd::AttnShape make_q8_shape(int B, int Nmax, int Hq, int Hkv, int d, int max_prefix, int kv_rows,
+                             int max_blocks, int dtype, int scale_rows) {
+  ltd::AttnShape s = make_shape(B, Nmax, Hq, Hkv, d, max_prefix, kv_rows, max_blocks, dtype);
+  s.scale_rows = scale_rows;
+  return s;
 }
 
 }  // namespace
@@ -98,8 +114,8 @@ int ltd_tree_verify_attn(const void* q, const void* k_cache, const void* v_cache
       return LTD_EHIP;
   }
   if (ltd::launch_attention(s, plan, q, k_cache, v_cache, block_table, prefix_len, parents,
-                            n_nodes, out, scale, workspace, validate ? status : nullptr,
-                            st) != hipSuccess)
+                            n_nodes, out, scale, workspace, ltd::KvScales{},
+                            validate ? status : nullptr, st) != hipSuccess)
     return LTD_EHIP;
   return LTD_OK;
 }
@@ -318,6 +334,210 @@ int ltd_policy_forward(int layout, const float* scores, const int32_t* pool_size
   if (ltd::launch_policy(layout, scores, pool_size, Vpool, depth, ctx_len, pad, B, in_dim, w1, b1,
                          h1, w2, b2, h2, wo, bo, n_out, action_offset, action_scale, logits, action,
                          workspace, static_cast<hipStream_t>(stream)) != hipSuccess)
+    return LTD_EHIP;
+  return LTD_OK;
+}
+
+int ltd_kv_append_q8(const void* k_new, const void* v_new, int64_t new_row_stride, void* k_cache,
+                     void* v_cache, uint8_t* k_scale, uint8_t* v_scale, const int32_t* block_table,
+                     const int32_t* prefix_len, const int32_t* n_rows, int B, int Nmax, int Hkv,
+                     int d, int kv_rows, int max_blocks, int num_blocks, int scale_rows, int dtype,
+                     int validate, int32_t* status, void* stream) {
+  if (B < 0 || Nmax < 1 || Hkv < 1 || d < 1 || kv_rows < 1) return LTD_EINVAL;
+  if (dtype != LTD_DTYPE_F32 && dtype != LTD_DTYPE_BF16) return LTD_EUNSUPPORTED;
+  if (!q8_supported(d, kv_rows, scale_rows, block_table != nullptr)) return LTD_EUNSUPPORTED;
+  if (block_table && (max_blocks < 1 || num_blocks < 1)) return LTD_EINVAL;
+  if (new_row_stride < static_cast<int64_t>(Hkv) * d) return LTD_EINVAL;
+  if (validate && !status) return LTD_EINVAL;
+  if (B == 0) return LTD_OK;
+  if (!k_new || !v_new || !k_cache || !v_cache || !k_scale || !v_scale || !prefix_len || !n_rows)
+    return LTD_EINVAL;
+  const int64_t row_bytes = new_row_stride * (dtype == LTD_DTYPE_F32 ? 4 : 2);
+  if (!aligned16(k_new) || !aligned16(v_new) || row_bytes % 16 != 0 || !aligned16(k_cache) ||
+      !aligned16(v_cache))
+    return LTD_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (validate) {
+    if (ltd::launch_validate_append(block_table, prefix_len, n_rows, B, Nmax, kv_rows, max_blocks,
+                                    num_blocks, status, st) != hipSuccess)
+      return LTD_EHIP;
+  }
+  if (ltd::launch_append_q8(k_new, v_new, new_row_stride, k_cache, v_cache, k_scale, v_scale,
+                            block_table, prefix_len, n_rows, B, Nmax, Hkv, d, kv_rows, max_blocks,
+                            scale_rows, dtype, validate ? status : nullptr, st) != hipSuccess)
+    return LTD_EHIP;
+  return LTD_OK;
+}
+
+size_t ltd_tree_verify_attn_q8_workspace_size(int B, int Nmax, int Hq, int Hkv, int d,
+                                              int max_prefix, int dtype) {
+  if (!attn_args_ok(B, Nmax, Hq, Hkv, d, max_prefix, dtype) || !attn_supported(d, dtype)) return 0;
+  // The largest need over the layouts, as for a 16-bit cache; an 8-bit one's
+  // smallest blocks hold 16 rows.
+  const int cus = device_cu_count();
+  const ltd::AttnShape contiguous =
+      make_q8_shape(B, Nmax, Hq, Hkv, d, max_prefix, max_prefix + Nmax, 0, dtype, 16);
+  const ltd::AttnShape small_blocks =
+      make_q8_shape(B, Nmax, Hq, Hkv, d, max_prefix, 16, 1, dtype, 16);
+  return std::max(ltd::plan_attention(contiguous, cus).workspace_bytes,
+                  ltd::plan_attention(small_blocks, cus).workspace_bytes);
+}
+
+int ltd_tree_verify_attn_q8(const void* q, const void* k_cache, const void* v_cache,
+                            const uint8_t* k_scale, const uint8_t* v_scale,
+                            const int32_t* block_table, const int32_t* prefix_len,
+                            const int32_t* parents, const int32_t* n_nodes, void* out, int B,
+                            int Nmax, int Hq, int Hkv, int d, int max_prefix, int kv_rows,
+                            int max_blocks, int num_blocks, int scale_rows, float scale, int dtype,
+                            void* workspace, size_t workspace_bytes, int validate, int32_t* status,
+                            void* stream) {
+  if (!attn_args_ok(B, Nmax, Hq, Hkv, d, max_prefix, dtype) || kv_rows < 1) return LTD_EINVAL;
+  if (!(scale > 0.f) || !std::isfinite(scale)) return LTD_EINVAL;
+  if (!attn_supported(d, dtype) || !q8_supported(d, kv_rows, scale_rows, block_table != nullptr))
+    return LTD_EUNSUPPORTED;
+  if (block_table && (max_blocks < 1 || num_blocks < 1)) return LTD_EINVAL;
+  if (validate && !status) return LTD_EINVAL;
+  if (B == 0) return LTD_OK;
+  if (!q || !k_cache || !v_cache || !k_scale || !v_scale || !prefix_len || !parents || !n_nodes ||
+      !out)
+    return LTD_EINVAL;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out))
+    return LTD_EINVAL;
+  const ltd::AttnShape s = make_q8_shape(B, Nmax, Hq, Hkv, d, max_prefix, kv_rows,
+                                         block_table ? max_blocks : 0, dtype, scale_rows);
+  const ltd::AttnPlan plan = ltd::plan_attention(s, device_cu_count());
+  if (plan.workspace_bytes > 0 &&
+      (!workspace || !aligned16(workspace) || workspace_bytes < plan.workspace_bytes))
+    return LTD_EWORKSPACE;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (validate) {
+    if (ltd::launch_validate_tree(block_table, prefix_len, parents, n_nodes, B, Nmax, max_prefix,
+                                  kv_rows, max_blocks, num_blocks, true, status, st) != hipSuccess)
+      return LTD_EHIP;
+  }
+  if (ltd::launch_attention(s, plan, q, k_cache, v_cache, block_table, prefix_len, parents,
+                            n_nodes, out, scale, workspace, ltd::KvScales{k_scale, v_scale},
+                            validate ? status : nullptr, st) != hipSuccess)
+    return LTD_EHIP;
+  return LTD_OK;
+}
+
+int ltd_kv_compact_q8(void* k_cache, void* v_cache, uint8_t* k_scale, uint8_t* v_scale,
+                      const int32_t* block_table, const int32_t* prefix_len,
+                      int32_t* new_prefix_len, const int32_t* accepted_nodes,
+                      const int32_t* n_accepted, int B, int Nmax, int Hkv, int d, int kv_rows,
+                      int max_blocks, int num_blocks, int scale_rows, int num_layers,
+                      int64_t layer_stride_elems, int64_t scale_stride_elems, int validate,
+                      int32_t* status, void* stream) {
+  if (B < 0 || Nmax < 1 || Nmax > LTD_MAX_NODES || Hkv < 1 || d < 1 || kv_rows < 1 ||
+      num_layers < 1 || layer_stride_elems < 0 || scale_stride_elems < 0)
+    return LTD_EINVAL;
+  if (!q8_supported(d, kv_rows, scale_rows, block_table != nullptr)) return LTD_EUNSUPPORTED;
+  if (block_table && (max_blocks < 1 || num_blocks < 1)) return LTD_EINVAL;
+  if (validate && !status) return LTD_EINVAL;
+  if (B == 0) return LTD_OK;
+  if (!k_cache || !v_cache || !k_scale || !v_scale || !prefix_len || !new_prefix_len ||
+      !accepted_nodes || !n_accepted)
+    return LTD_EINVAL;
+  if (new_prefix_len == prefix_len) return LTD_EINVAL;
+  if (num_layers > 1 && (layer_stride_elems == 0 || scale_stride_elems == 0)) return LTD_EINVAL;
+  if (!aligned16(k_cache) || !aligned16(v_cache) ||
+      (num_layers > 1 && layer_stride_elems % 16 != 0))
+    return LTD_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (validate) {
+    if (ltd::launch_validate_path(block_table, prefix_len, accepted_nodes, n_accepted, B, Nmax,
+                                  kv_rows, max_blocks, num_blocks, status, st) != hipSuccess)
+      return LTD_EHIP;
+  }
+  if (ltd::launch_compact_q8(k_cache, v_cache, k_scale, v_scale, block_table, prefix_len,
+                             new_prefix_len, accepted_nodes, n_accepted, B, Nmax, Hkv, d, kv_rows,
+                             max_blocks, scale_rows, num_layers, layer_stride_elems,
+                             scale_stride_elems, validate ? status : nullptr, st) != hipSuccess)
+    return LTD_EHIP;
+  return LTD_OK;
+}
+
+int ltd_token_counts(const int32_t* tokens, const int32_t* n_tokens, int B, int T, int Voc,
+                     int prompt, int reset, int32_t* counts, void* stream) {
+  if (B < 0 || T < 0 || Voc < 1) return LTD_EINVAL;
+  if (B == 0) return LTD_OK;
+  if (!counts || (T > 0 && (!tokens || !n_tokens))) return LTD_EINVAL;
+  if (ltd::launch_token_counts(tokens, n_tokens, B, T, Voc, prompt != 0, reset != 0, counts,
+                               static_cast<hipStream_t>(stream)) != hipSuccess)
+    return LTD_EHIP;
+  return LTD_OK;
+}
+
+namespace {
+// The scalar and pointer checks of a call with sampling rules (LTD_OK, or the
+// code to return); the caller has dealt with an empty batch.
+int rules_ok(const ltd::LogitRules& r) {
+  if (!r.logits || !r.tokens || !r.parents || !r.n_nodes) return LTD_EINVAL;
+  if (r.max_bias > 0 && (!r.bias_tokens || !r.bias_values || !r.n_bias)) return LTD_EINVAL;
+  return LTD_OK;
+}
+}  // namespace
+
+int ltd_tree_process_logits(const float* logits, const int32_t* draft_tokens,
+                            const int32_t* parents, const int32_t* n_nodes, const int32_t* counts,
+                            const float* penalties, const int32_t* bias_tokens,
+                            const float* bias_values, const int32_t* n_bias, const uint32_t* mask,
+                            int B, int Nmax, int Voc, int max_bias, float* out, int validate,
+                            int32_t* status, void* stream) {
+  if (B < 0 || Nmax < 1 || Nmax > LTD_MAX_NODES || Voc < 1 || max_bias < 0 ||
+      max_bias > LTD_MAX_BIAS)
+    return LTD_EINVAL;
+  if (validate && !status) return LTD_EINVAL;
+  if (B == 0) return LTD_OK;
+  const ltd::LogitRules r{logits,      draft_tokens, parents, n_nodes, counts, penalties,
+                          bias_tokens, bias_values,  n_bias,  mask,    max_bias};
+  const int rc = rules_ok(r);
+  if (rc != LTD_OK) return rc;
+  if (!out) return LTD_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (validate) {
+    if (ltd::launch_validate_rules(parents, n_nodes, penalties, n_bias, B, Nmax, max_bias, status,
+                                   st) != hipSuccess)
+      return LTD_EHIP;
+  }
+  if (ltd::launch_rules(r, B, Nmax, Voc, out, nullptr, validate ? status : nullptr, st) !=
+      hipSuccess)
+    return LTD_EHIP;
+  return LTD_OK;
+}
+
+int ltd_tree_accept_processed(const float* logits, const int32_t* draft_tokens,
+                              const int32_t* parents, const int32_t* n_nodes,
+                              const int32_t* counts, const float* penalties,
+                              const int32_t* bias_tokens, const float* bias_values,
+                              const int32_t* n_bias, const uint32_t* mask, int B, int Nmax,
+                              int Voc, int max_bias, int32_t* pred, int32_t* accepted_nodes,
+                              int32_t* out_tokens, int32_t* n_accepted, void* workspace,
+                              size_t workspace_bytes, int validate, int32_t* status, void* stream) {
+  if (B < 0 || Nmax < 1 || Nmax > LTD_MAX_NODES || Voc < 1 || max_bias < 0 ||
+      max_bias > LTD_MAX_BIAS)
+    return LTD_EINVAL;
+  if (validate && !status) return LTD_EINVAL;
+  if (B == 0) return LTD_OK;
+  const ltd::LogitRules r{logits,      draft_tokens, parents, n_nodes, counts, penalties,
+                          bias_tokens, bias_values,  n_bias,  mask,    max_bias};
+  const int rc = rules_ok(r);
+  if (rc != LTD_OK) return rc;
+  if (!pred || !accepted_nodes || !out_tokens || !n_accepted) return LTD_EINVAL;
+  if (!workspace || workspace_bytes < ltd::accept_workspace_bytes(B, Nmax, Voc))
+    return LTD_EWORKSPACE;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (validate) {
+    if (ltd::launch_validate_rules(parents, n_nodes, penalties, n_bias, B, Nmax, max_bias, status,
+                                   st) != hipSuccess)
+      return LTD_EHIP;
+  }
+  const int32_t* halt = validate ? status : nullptr;
+  if (ltd::launch_rules(r, B, Nmax, Voc, nullptr, workspace, halt, st) != hipSuccess)
+    return LTD_EHIP;
+  if (ltd::launch_accept_scan(workspace, draft_tokens, parents, n_nodes, B, Nmax, Voc, pred,
+                              accepted_nodes, out_tokens, n_accepted, halt, st) != hipSuccess)
     return LTD_EHIP;
   return LTD_OK;
 }

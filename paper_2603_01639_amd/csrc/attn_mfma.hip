@@ -1636,7 +1636,7 @@ void plan_split(const AttnShape& s, int num_cus, AttnPlan* p) {
 // The split plan needs splits of at least two key tiles whose block ids fit
 // the LDS table even with one-row blocks, and at most kMaxMergeSplits of them.
 bool mfma_supported(const AttnShape& s) {
-  if (s.dtype != LTD_DTYPE_BF16 || (s.d != 128 && s.d != 64)) return false;
+  if (s.dtype != LTD_DTYPE_BF16 || (s.d != 128 && s.d != 64) || s.scale_rows != 0) return false;
   if (use_stream(s)) return true;
   const int64_t cap = worst_split_key_cap(s);
   return cap >= 2 * kKT && s.max_prefix <= cap * kMaxMergeSplits;

@@ -1,4 +1,4 @@
-// Tree attention on the vector ALUs, the fp32 path: one workgroup of four
+// Tree attention on the vector ALUs, the fp32 path (caches in fp32 or in 8 bits): one workgroup of four
 // waves per (sequence, node, kv head) handles the G query heads of that kv
 // head, four at a time (one a wave).  Keys are visited in tiles of 64, each
 // tile's K and V rows staged in LDS by the whole workgroup with coalesced
@@ -15,8 +15,11 @@
 // The visible key set of node i is the prefix [0, P_b) plus the tree rows of
 // the node's root path (arXiv 2603.01639, section 3.2: the tree attention
 // mask shows each candidate its ancestors only).
+#include <type_traits>
+
 #include "ltd_device.hpp"
 #include "ltd_launch.hpp"
+#include "q8.hpp"
 #include "tree_walk.hpp"
 
 namespace ltd {
@@ -42,12 +45,32 @@ __device__ __forceinline__ void load4(const T* p, int64_t i, float (&x)[4]) {
   }
 }
 
-template <typename T, bool kVec, int HD>
+// Scale bytes of an 8-bit cache and their layout: row r of a page is covered by
+// byte r >> shift of the page's per_page.
+struct VecScales {
+  const uint8_t* k;
+  const uint8_t* v;
+  int per_page, shift;
+};
+
+// Four consecutive codes under a scale byte.
+__device__ __forceinline__ void load4_q8(const unsigned char* p, int64_t i, float s, float (&x)[4]) {
+  const uint32_t c = *reinterpret_cast<const uint32_t*>(p + i);
+  const q8_f32x2 lo = q8_decode2<false>(c), hi = q8_decode2<true>(c);
+  x[0] = lo.x * s;
+  x[1] = lo.y * s;
+  x[2] = hi.x * s;
+  x[3] = hi.y * s;
+}
+
+// C: the caches' element, T or (8-bit codes with scale bytes) unsigned char.
+template <typename T, typename C, bool kVec, int HD>
 __global__ void __launch_bounds__(kVecThreads) attn_vector_kernel(
-    const T* __restrict__ q, const T* __restrict__ k_cache, const T* __restrict__ v_cache,
+    const T* __restrict__ q, const C* __restrict__ k_cache, const C* __restrict__ v_cache,
     const int32_t* __restrict__ block_table, const int32_t* __restrict__ prefix_len,
     const int32_t* __restrict__ parents, const int32_t* __restrict__ n_nodes, T* __restrict__ out,
-    int Nmax, int Hq, int Hkv, int kv_rows, int max_blocks, float scale, const int32_t* status) {
+    int Nmax, int Hq, int Hkv, int kv_rows, int max_blocks, float scale, VecScales sc,
+    const int32_t* status) {
   constexpr int d = HD;
   constexpr int kPieces = kTileKeys * HD / 4 / kVecThreads;  // 16-byte pieces a thread loads
   // K transposed by groups of 4 dims (lane = key reads 16 consecutive bytes,
@@ -95,9 +118,18 @@ __global__ void __launch_bounds__(kVecThreads) attn_vector_kernel(
         if (r < cnt) {
           const int kt = base + r;
           const int row = kt < P ? kt : P + path_s[kt - P];
-          const int64_t off = cache_row(block_table, b, g, row, Hkv, d, kv_rows, max_blocks) + c;
-          load4<T, kVec>(k_cache, off, kr4[j]);
-          load4<T, kVec>(v_cache, off, vr4[j]);
+          if constexpr (std::is_same<C, unsigned char>::value) {
+            const Q8Row at = q8_row(block_table, b, row, kv_rows, max_blocks);
+            const int64_t head = at.page * Hkv + g;
+            const int64_t off = (head * kv_rows + at.row) * d + c;
+            const int64_t so = head * sc.per_page + (at.row >> sc.shift);
+            load4_q8(k_cache, off, q8_scale(sc.k[so]), kr4[j]);
+            load4_q8(v_cache, off, q8_scale(sc.v[so]), vr4[j]);
+          } else {
+            const int64_t off = cache_row(block_table, b, g, row, Hkv, d, kv_rows, max_blocks) + c;
+            load4<T, kVec>(k_cache, off, kr4[j]);
+            load4<T, kVec>(v_cache, off, vr4[j]);
+          }
         }
       }
     };
@@ -182,26 +214,42 @@ hipError_t launch_attn_rowwise(const AttnShape& s, const void* q, const void* k_
                                const void* v_cache, const int32_t* block_table,
                                const int32_t* prefix_len, const int32_t* parents,
                                const int32_t* n_nodes, void* out, float scale,
-                               const int32_t* status, hipStream_t stream) {
+                               const KvScales& scales, const int32_t* status, hipStream_t stream) {
   const dim3 grid(s.Nmax, s.Hkv, s.B);
-  const auto launch = [&](auto kern, auto elem) {
+  VecScales sc{scales.k, scales.v, 0, 0};
+  const auto launch_as = [&](auto kern, auto elem, auto code) {
     using T = decltype(elem);
+    using C = decltype(code);
     hipLaunchKernelGGL(kern, grid, dim3(kVecThreads), 0, stream, static_cast<const T*>(q),
-                       static_cast<const T*>(k_cache), static_cast<const T*>(v_cache), block_table,
+                       static_cast<const C*>(k_cache), static_cast<const C*>(v_cache), block_table,
                        prefix_len, parents, n_nodes, static_cast<T*>(out), s.Nmax, s.Hq, s.Hkv,
-                       s.kv_rows, s.max_blocks, scale, status);
+                       s.kv_rows, s.max_blocks, scale, sc, status);
   };
+  const auto launch = [&](auto kern, auto elem) { launch_as(kern, elem, elem); };
+  if (s.scale_rows > 0) {
+    using C = unsigned char;
+    while ((1 << sc.shift) < s.scale_rows) ++sc.shift;
+    sc.per_page = (s.kv_rows + s.scale_rows - 1) / s.scale_rows;
+    if (s.dtype == LTD_DTYPE_F32)
+      launch_as(s.d == 64 ? attn_vector_kernel<float, C, true, 64> : attn_vector_kernel<float, C, true, 128>,
+                float{}, C{});
+    else
+      launch_as(s.d == 64 ? attn_vector_kernel<uint16_t, C, true, 64> : attn_vector_kernel<uint16_t, C, true, 128>,
+                uint16_t{}, C{});
+    return hipGetLastError();
+  }
   if (s.dtype == LTD_DTYPE_F32) {
     // 16-byte loads when both caches are 16-byte aligned (every row and piece
     // offset is a multiple of 4 elements)
     const bool vec = (reinterpret_cast<uintptr_t>(k_cache) % 16) == 0 &&
                      (reinterpret_cast<uintptr_t>(v_cache) % 16) == 0;
     if (s.d == 64)
-      launch(vec ? attn_vector_kernel<float, true, 64> : attn_vector_kernel<float, false, 64>, float{});
+      launch(vec ? attn_vector_kernel<float, float, true, 64> : attn_vector_kernel<float, float, false, 64>, float{});
     else
-      launch(vec ? attn_vector_kernel<float, true, 128> : attn_vector_kernel<float, false, 128>, float{});
+      launch(vec ? attn_vector_kernel<float, float, true, 128> : attn_vector_kernel<float, float, false, 128>, float{});
   } else {
-    launch(s.d == 64 ? attn_vector_kernel<uint16_t, false, 64> : attn_vector_kernel<uint16_t, false, 128>,
+    launch(s.d == 64 ? attn_vector_kernel<uint16_t, uint16_t, false, 64>
+                     : attn_vector_kernel<uint16_t, uint16_t, false, 128>,
            uint16_t{});
   }
   return hipGetLastError();

@@ -20,6 +20,12 @@ hipError_t launch_validate_path(const int32_t* block_table, const int32_t* prefi
 // attn.hip
 struct AttnShape {
   int B, Nmax, Hq, Hkv, d, max_prefix, kv_rows, max_blocks, dtype;
+  int scale_rows;  // rows that share a scale byte of an 8-bit cache, 0: a cache of `dtype`
+};
+// The scale bytes of an 8-bit cache.
+struct KvScales {
+  const uint8_t* k;
+  const uint8_t* v;
 };
 struct AttnPlan {
   int grid;          // workgroups of the MFMA attention grid (0 on the row-wise path)
@@ -39,7 +45,7 @@ hipError_t launch_attention(const AttnShape& s, const AttnPlan& plan, const void
                             const void* k_cache, const void* v_cache, const int32_t* block_table,
                             const int32_t* prefix_len, const int32_t* parents,
                             const int32_t* n_nodes, void* out, float scale, void* workspace,
-                            const int32_t* status, hipStream_t stream);
+                            const KvScales& scales, const int32_t* status, hipStream_t stream);
 
 // accept.hip
 size_t accept_workspace_bytes(int B, int Nmax, int Voc);
@@ -51,6 +57,13 @@ hipError_t launch_accept(const float* logits, const int32_t* draft_tokens, const
                          const int32_t* n_nodes, int B, int Nmax, int Voc, int32_t* pred,
                          int32_t* accepted_nodes, int32_t* out_tokens, int32_t* n_accepted,
                          void* workspace, const int32_t* status, hipStream_t stream);
+
+// The second half of acceptance, from the argmax keys of every node's chunks
+// (as many as accept_workspace_bytes has room for).
+hipError_t launch_accept_scan(const void* partial, const int32_t* draft_tokens,
+                              const int32_t* parents, const int32_t* n_nodes, int B, int Nmax,
+                              int Voc, int32_t* pred, int32_t* accepted_nodes, int32_t* out_tokens,
+                              int32_t* n_accepted, const int32_t* status, hipStream_t stream);
 
 // compact.hip
 hipError_t launch_compact(void* k_cache, void* v_cache, const int32_t* block_table,
@@ -98,5 +111,49 @@ hipError_t launch_policy(int layout, const float* scores, const int32_t* pool_si
                          const float* b2, int h2, const float* wo, const float* bo, int n_out,
                          int action_offset, int action_scale, float* logits, int32_t* action,
                          void* workspace, hipStream_t stream);
+
+// q8_cache.hip
+hipError_t launch_validate_append(const int32_t* block_table, const int32_t* prefix_len,
+                                  const int32_t* n_rows, int B, int Nmax, int kv_rows,
+                                  int max_blocks, int num_blocks, int32_t* status,
+                                  hipStream_t stream);
+hipError_t launch_append_q8(const void* k_new, const void* v_new, int64_t row_stride,
+                            void* k_cache, void* v_cache, uint8_t* k_scale, uint8_t* v_scale,
+                            const int32_t* block_table, const int32_t* prefix_len,
+                            const int32_t* n_rows, int B, int Nmax, int Hkv, int d, int kv_rows,
+                            int max_blocks, int scale_rows, int dtype, const int32_t* status,
+                            hipStream_t stream);
+hipError_t launch_compact_q8(void* k_cache, void* v_cache, uint8_t* k_scale, uint8_t* v_scale,
+                             const int32_t* block_table, const int32_t* prefix_len,
+                             int32_t* new_prefix_len, const int32_t* accepted_nodes,
+                             const int32_t* n_accepted, int B, int Nmax, int Hkv, int d,
+                             int kv_rows, int max_blocks, int scale_rows, int num_layers,
+                             int64_t layer_stride, int64_t scale_stride, const int32_t* status,
+                             hipStream_t stream);
+
+// logits.hip
+struct LogitRules {
+  const float* logits;
+  const int32_t* tokens;
+  const int32_t* parents;
+  const int32_t* n_nodes;
+  const int32_t* counts;
+  const float* penalties;
+  const int32_t* bias_tokens;
+  const float* bias_values;
+  const int32_t* n_bias;
+  const uint32_t* mask;
+  int max_bias;
+};
+hipError_t launch_validate_rules(const int32_t* parents, const int32_t* n_nodes,
+                                 const float* penalties, const int32_t* n_bias, int B, int Nmax,
+                                 int max_bias, int32_t* status, hipStream_t stream);
+hipError_t launch_token_counts(const int32_t* tokens, const int32_t* n_tokens, int B, int T,
+                               int Voc, bool prompt, bool reset, int32_t* counts,
+                               hipStream_t stream);
+// Writes the processed rows to `out`, or (partial non-null) every chunk's
+// argmax key to `partial`.
+hipError_t launch_rules(const LogitRules& rules, int B, int Nmax, int Voc, float* out,
+                        void* partial, const int32_t* status, hipStream_t stream);
 
 }  // namespace ltd
