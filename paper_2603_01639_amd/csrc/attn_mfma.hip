@@ -52,6 +52,7 @@
 
 #include "ltd_device.hpp"
 #include "ltd_launch.hpp"
+#include "q8.hpp"
 #include "stream_plan.hpp"
 
 namespace ltd {
@@ -118,6 +119,10 @@ struct MfmaArgs {
   // the tree may take a split of its own, row tiles per (sequence, kv head)
   int split_keys, max_splits, tree_alone, row_tiles;
   int tile_rows;  // stacked rows per unit
+  // 8-bit cache: scale bytes, scale bytes per page and kv head, log2(scale_rows)
+  const uint8_t* ks;
+  const uint8_t* vs;
+  int scale_per_page, scale_shift;
   float scale_log2;
   float lazy_gap;  // kLazyMax / scale_log2: the raw-score margin of the lazy max
 };
@@ -245,6 +250,7 @@ struct Smem {
   uint32_t anc[kAncWords][LTD_MAX_NODES];  // word w of every node's ancestor set
   int32_t par[kWaves][LTD_MAX_NODES];  // each wave's parent links, then its jump pointers (mask build)
   int32_t blk[kMaxSplitBlocks];  // physical block ids of this split's rows (paged)
+  uint32_t nan_rows[kAncWords];  // 8-bit cache: tree rows whose V holds a NaN code
 };
 // The Q rows are loaded into ring slots 2 and 3 (8 KiB per wave) before the
 // first two tiles; the loop first writes those slots after its first barrier.
@@ -273,6 +279,40 @@ __device__ __forceinline__ LoadPlan make_load_plan(int wave, int lane) {
   return lp;
 }
 
+// An 8-bit cache's tile in flight: 16 codes of K and of V and the row's scale
+// bytes (with 64 dims a thread takes 16 codes of one of the two).
+struct Q8Piece {
+  u32x4 k, v;
+  uint32_t ks, vs;
+};
+
+// 16 codes under a scale byte as bf16 (exact: 4 significant bits and a power
+// of two well inside the type's range).
+__device__ __forceinline__ void q8_to_bf16(const u32x4& codes, uint32_t byte, u32x4 (&out)[2]) {
+  const float s = q8_scale(static_cast<int>(byte));
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[j], s, false);
+    const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[j], s, true);
+    out[j >> 1][2 * (j & 1)] = __builtin_bit_cast(uint32_t, lo);
+    out[j >> 1][2 * (j & 1) + 1] = __builtin_bit_cast(uint32_t, hi);
+  }
+}
+
+// The codes with NaN ones replaced by zero; whether there were any.
+__device__ __forceinline__ bool q8_clear_nan(u32x4& codes) {
+  bool any = false;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (((codes[j] >> (8 * e)) & 0x7Fu) == 0x7Fu) {
+        codes[j] &= ~(0xFFu << (8 * e));
+        any = true;
+      }
+  return any;
+}
+
 // The attention of one workgroup over its share of one unit: the prefix keys
 // [key_begin, key_begin + n_pre) and, with kTree, also the tree's keys
 // [P, P + n) under the ancestor mask.  Tiles t < tA cover the first range, the
@@ -289,7 +329,18 @@ __device__ __forceinline__ LoadPlan make_load_plan(int wave, int lane) {
 // LDS at the end: twice the waves then work on each tile (32/8 heads, prefix
 // 1196, 12 nodes, ten layers and acceptance 118.1 -> 115.7 us; 64/8 heads,
 // prefix 4096, 8 nodes 12.8 -> 12.0; 11 sequences of 56 rows 43.0 -> 42.0).
-template <bool kTree, int HD, bool kPaged, int kKG>
+//
+// kQ8: the cache holds 8-bit codes with a scale byte per block of rows.  A tile
+// then goes through registers: thread i loads 16 codes of key i / 8 (K and V,
+// 8 KiB each a tile instead of 16) with the block's scale bytes, two tiles
+// ahead, widens them to bf16 (v_cvt_scalef32_pk_bf16_fp8, 16 a thread and tile)
+// and writes them to the ring's slot, where everything downstream finds the
+// 16-bit kernel's layouts.  Widening in the staging threads costs each
+// element once per workgroup; every wave would repeat it on its fragments.
+// (The fp8 matrix instructions would take K's codes as they are, with Q in two
+// codes an element, but their sums keep too few bits: 1.3e-4 of the sum of
+// magnitudes off, measured over the codes' whole range.)
+template <bool kTree, int HD, bool kPaged, int kKG, bool kQ8>
 __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g, int row0,
                                        int valid_rows, int key_begin, int n_pre, int P, int n,
                                        bool final_out, int slot) {
@@ -374,6 +425,8 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
   const unsigned char* kbase = reinterpret_cast<const unsigned char*>(a.k);
   const unsigned char* vbase = reinterpret_cast<const unsigned char*>(a.v);
   constexpr bool paged = kPaged;  // a paged cache (block table) or one contiguous range per (b, g)
+  if (kQ8 && kTree && tid < kAncWords) sm.nan_rows[tid] = 0;
+  if (kQ8 && kTree && !paged) __syncthreads();
   if (paged) {
     // (stored as the block's row group of head g, blk * Hkv + g: its first
     // row is that times kv_rows)
@@ -381,6 +434,70 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
     for (int j = tid + kThreads; j < n_blk; j += kThreads) sm.blk[j] = bt[j] * a.Hkv + g;
     __syncthreads();
   }
+  // 8-bit cache: this thread's tile key and its 16 codes' first dim.  With 64
+  // dims the upper half of the threads takes V, the lower half K.
+  constexpr int kQLanes = HD / 16;
+  const bool q8_k = HD == 128 || tid < kThreads / 2, q8_v = HD == 128 || tid >= kThreads / 2;
+  const int q8_key = (tid / kQLanes) & (kKT - 1);
+  const int q8_dim = tid % kQLanes * 16;
+  auto load_piece = [&](int t, Q8Piece& x) {
+    const TileRef tr = tile_ref(t);
+    const int row = tr.row + min(q8_key, tr.left - 1);
+    int64_t rg;
+    int in;
+    if (!paged) {
+      rg = static_cast<int64_t>(b) * a.Hkv + g;
+      in = row;
+    } else if (a.kv_shift >= 0) {
+      rg = sm.blk[(row >> a.kv_shift) - first_blk];
+      in = row & (a.kv_rows - 1);
+    } else {
+      const int blk = row / a.kv_rows;
+      rg = sm.blk[blk - first_blk];
+      in = row - blk * a.kv_rows;
+    }
+    const int64_t at = (rg * a.kv_rows + in) * HD + q8_dim;
+    const int64_t st = rg * a.scale_per_page + (in >> a.scale_shift);
+    if (HD == 128) {
+      x.k = *reinterpret_cast<const u32x4*>(kbase + at);
+      x.v = *reinterpret_cast<const u32x4*>(vbase + at);
+      x.ks = a.ks[st];
+      x.vs = a.vs[st];
+    } else {
+      x.k = *reinterpret_cast<const u32x4*>((q8_k ? kbase : vbase) + at);
+      x.ks = (q8_k ? a.ks : a.vs)[st];
+    }
+  };
+  // Widens a piece into its tile's slot: K at the row that holds its key, both
+  // swizzled.  The upper dims write their second chunk first, so that the eight
+  // lanes of a row never meet in an LDS bank.
+  auto store_piece = [&](int t, Q8Piece& x) {
+    unsigned char* slot = sm.kv[t % kStages];
+    const int c0 = q8_dim / 8;
+    const int flip = (tid % kQLanes) >= kQLanes / 2 ? 1 : 0;
+    u32x4 w[2];
+    if (q8_k) {
+      const int k5 = q8_key & 31;
+      const int i = (q8_key & 32) | (k5 & 3) | ((k5 >> 4) << 2) | (((k5 >> 2) & 3) << 3);  // sigma(i) = k5
+      q8_to_bf16(x.k, x.ks, w);
+      unsigned char* row = slot + i * (kD * 2);
+      *reinterpret_cast<u32x4*>(row + (((c0 + flip) ^ (i & 15)) << 4)) = flip ? w[1] : w[0];
+      *reinterpret_cast<u32x4*>(row + (((c0 + 1 - flip) ^ (i & 15)) << 4)) = flip ? w[0] : w[1];
+    }
+    if (q8_v) {
+      u32x4& v = HD == 128 ? x.v : x.k;
+      if (kTree) {
+        const TileRef tr = tile_ref(t);
+        if (tr.tree && q8_clear_nan(v) && q8_key < tr.left)
+          atomicOr(&sm.nan_rows[(tr.rel + q8_key) >> 5], 1u << ((tr.rel + q8_key) & 31));
+      }
+      q8_to_bf16(v, HD == 128 ? x.vs : x.ks, w);
+      unsigned char* row = slot + kKBytes + q8_key * (kD * 2);
+      *reinterpret_cast<u32x4*>(row + (((c0 + flip) ^ swz_v(q8_key)) << 4)) = flip ? w[1] : w[0];
+      *reinterpret_cast<u32x4*>(row + (((c0 + 1 - flip) ^ swz_v(q8_key)) << 4)) = flip ? w[0] : w[1];
+    }
+  };
+  Q8Piece piece[2];  // tiles of even and of odd index
   auto row_byte = [&](int row) -> int64_t {  // byte offset of logical cache row `row`
     if (!paged) return ((static_cast<int64_t>(b) * a.Hkv + g) * a.kv_rows + row) * (HD * 2);
     if (a.kv_shift >= 0) {  // power-of-two blocks: shifts and masks, no division
@@ -476,11 +593,18 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
   };
 
   // The first tiles, behind Q.
+  if constexpr (kQ8) {
+    if (n_tiles > 0) load_piece(0, piece[0]);
+    if (n_tiles > 1) load_piece(1, piece[1]);
+  } else {
 #pragma unroll 1
-  for (int t = 0; t < min(kStages - 2, n_tiles); ++t) issue_tile(t);
+    for (int t = 0; t < min(kStages - 2, n_tiles); ++t) issue_tile(t);
+  }
   // This wave's Q rows and parent links have landed once no more than the
-  // tiles' loads are outstanding.
-  if (n_tiles >= 2)
+  // tiles' loads are outstanding.  (The compiler counts an 8-bit cache's loads.)
+  if (kQ8)
+    wait_vmcnt<0>();
+  else if (n_tiles >= 2)
     wait_vmcnt<2 * kLoadsPerTile>();
   else if (n_tiles == 1)
     wait_vmcnt<kLoadsPerTile>();
@@ -717,6 +841,14 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
   // barrier that publishes tile t+1 comes after the last read of tile t-1.
   constexpr int kAhead = kStages - 2;
   static_assert(kAhead == 2, "the vmcnt waits below assume two tiles of look-ahead");
+  // (8-bit cache: tile t + 1's codes are widened into its slot, whose last
+  // reader was iteration t - 2, and its registers take tile t + 3.)
+  auto publish_q8 = [&](int t, Q8Piece& next) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this thread's part of tile t is in LDS
+    barrier_only();
+    if (t + 1 < n_tiles) store_piece(t + 1, next);
+    if (t + 3 < n_tiles) load_piece(t + 3, next);
+  };
   auto publish = [&](int t) {  // wait for tile t, publish it, start loading tile t + kAhead
     if (t + 1 < n_tiles) wait_vmcnt<kLoadsPerTile>();  // tile t+1 may stay in flight
     else wait_vmcnt<0>();
@@ -727,8 +859,9 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
   // unrolled by two), so tile t-1's are never copied.
   f32x16 s_acc[kKB];
   bf16x8 pfa[kKB][2], pfb[kKB][2];
-  auto body = [&](int t, const bf16x8(&pf_prev)[kKB][2], bf16x8(&pf)[kKB][2]) {
-    publish(t);
+  auto body = [&](int t, const bf16x8(&pf_prev)[kKB][2], bf16x8(&pf)[kKB][2], Q8Piece& next) {
+    if constexpr (kQ8) publish_q8(t, next);
+    else publish(t);
     if (active) {
       load_k(t);
       scores(s_acc);
@@ -743,7 +876,13 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
     }
   };
   if (n_tiles > 0) {
-    publish(0);
+    if constexpr (kQ8) {
+      store_piece(0, piece[0]);
+      if (n_tiles > 2) load_piece(2, piece[0]);
+      publish_q8(0, piece[1]);
+    } else {
+      publish(0);
+    }
     if (active) {
       load_k(0);
       scores(s_acc);
@@ -753,12 +892,12 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
     }
   }
   int t = 1;
-  for (; t + 1 < n_tiles; t += 2) {
-    body(t, pfa, pfb);
-    body(t + 1, pfb, pfa);
+  for (; t + 1 < n_tiles; t += 2) {  // (odd t: the next tile's piece is the even one)
+    body(t, pfa, pfb, piece[0]);
+    body(t + 1, pfb, pfa, piece[1]);
   }
   if (t < n_tiles) {
-    body(t, pfa, pfb);
+    body(t, pfa, pfb, piece[0]);
     if (active) accumulate(n_tiles - 1, pfb);
   } else if (n_tiles > 0 && active) {
     accumulate(n_tiles - 1, pfa);
@@ -819,7 +958,14 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
       f32x2 ml = {lsum > 0.f ? m_run * c : -INFINITY, lsum};
       __builtin_nontemporal_store(ml, reinterpret_cast<f32x2*>(a.ws_ml + (part + qrow_idx) * 2));
     }
-    const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+    float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+    if constexpr (kQ8 && kTree) {
+      // A node that sees a tree row with a NaN in V (zero in the product, so
+      // that the nodes that do not see it are spared) gets NaN.
+      uint32_t hit = 0;
+      for (int w = 0; w < (n + 31) / 32; ++w) hit |= sm.nan_rows[w] & sm.anc[w][qnode];
+      if (hit != 0) inv = __builtin_nanf("");
+    }
     unsigned char* srow = stage + l32 * kRowPitch;
 #pragma unroll
     for (int db = 0; db < HD / 32; ++db) {
@@ -872,14 +1018,14 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
   }
 }
 
-template <int HD, bool kPaged, int kKG>
+template <int HD, bool kPaged, int kKG, bool kQ8>
 __device__ __forceinline__ void run_share(bool tree, const MfmaArgs& a, Smem& sm, int b, int g, int row0,
                                           int valid_rows, int key_begin, int n_pre, int P, int n,
                                           bool final_out, int slot) {
   if (tree)
-    attend<true, HD, kPaged, kKG>(a, sm, b, g, row0, valid_rows, key_begin, n_pre, P, n, final_out, slot);
+    attend<true, HD, kPaged, kKG, kQ8>(a, sm, b, g, row0, valid_rows, key_begin, n_pre, P, n, final_out, slot);
   else
-    attend<false, HD, kPaged, kKG>(a, sm, b, g, row0, valid_rows, key_begin, n_pre, P, n, final_out, slot);
+    attend<false, HD, kPaged, kKG, kQ8>(a, sm, b, g, row0, valid_rows, key_begin, n_pre, P, n, final_out, slot);
 }
 
 // ---- the call's work axis (stream_plan.hpp), computed by each wave on its
@@ -1044,7 +1190,7 @@ __device__ __forceinline__ int stream_index(int w, int W) { return (w % 8) * (W 
 // share one XCD (its L2 holds their common Q rows and K/V).  A unit with one
 // split writes its output directly; otherwise split sp leaves its partial in
 // slot (bg * max_splits + sp) * row_tiles + row tile.
-template <int HD, bool kPaged, int kKG>
+template <int HD, bool kPaged, int kKG, bool kQ8>
 __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(MfmaArgs a) {
   __shared__ __attribute__((aligned(16))) Smem sm;
   const int bg = blockIdx.x;
@@ -1065,7 +1211,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_split_kernel(MfmaArgs a) {
   const int key_begin = min(split * a.split_keys, P);
   const int n_pre = min(a.split_keys, P - key_begin);
   const int slot = (bg * a.max_splits + split) * a.row_tiles + rtile;
-  run_share<HD, kPaged, kKG>(split == nsp - 1, a, sm, b, g, row0, valid_rows, key_begin, n_pre, P, n,
+  run_share<HD, kPaged, kKG, kQ8>(split == nsp - 1, a, sm, b, g, row0, valid_rows, key_begin, n_pre, P, n,
                              nsp == 1, slot);
 }
 
@@ -1270,7 +1416,7 @@ __global__ void __launch_bounds__(256) attn_split_merge_few_kernel(MfmaArgs a) {
 // into LDS, then run one by one by the whole workgroup: the partition's state
 // (the sequence table, positions) is dead while the tile loop runs, which
 // keeps it out of the loop's registers.
-template <int HD, bool kPaged, int kKG>
+template <int HD, bool kPaged, int kKG, bool kQ8>
 __global__ void __launch_bounds__(kThreads, 1) attn_stream_kernel(MfmaArgs a) {
   __shared__ __attribute__((aligned(16))) Smem sm;
   if (halted(a.status)) return;
@@ -1328,7 +1474,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_stream_kernel(MfmaArgs a) {
       started = true;
       const ShareDesc d = sm.share[i];
       const int row0 = d.rt * kTileRows;
-      run_share<HD, kPaged, kKG>(d.tree != 0, a, sm, d.b, d.g, row0, a.G * d.n, d.key_begin, d.n_pre, d.P,
+      run_share<HD, kPaged, kKG, kQ8>(d.tree != 0, a, sm, d.b, d.g, row0, a.G * d.n, d.key_begin, d.n_pre, d.P,
                                  d.n, d.whole != 0, d.slot);
     }
     if (next_pos < 0) break;
@@ -1636,7 +1782,7 @@ void plan_split(const AttnShape& s, int num_cus, AttnPlan* p) {
 // The split plan needs splits of at least two key tiles whose block ids fit
 // the LDS table even with one-row blocks, and at most kMaxMergeSplits of them.
 bool mfma_supported(const AttnShape& s) {
-  if (s.dtype != LTD_DTYPE_BF16 || (s.d != 128 && s.d != 64) || s.scale_rows != 0) return false;
+  if (s.dtype != LTD_DTYPE_BF16 || (s.d != 128 && s.d != 64)) return false;
   if (use_stream(s)) return true;
   const int64_t cap = worst_split_key_cap(s);
   return cap >= 2 * kKT && s.max_prefix <= cap * kMaxMergeSplits;
@@ -1660,12 +1806,16 @@ void plan_mfma(const AttnShape& s, int num_cus, AttnPlan* p) {
     plan_split(s, num_cus, p);
 }
 
-// launch(head size, paged, key groups), as compile-time constants.
+// launch(head size, paged, key groups, 8-bit cache), as compile-time constants.
 template <class Launch>
 void pick_kernel(const AttnShape& s, bool paged, Launch launch) {
+  const auto with_cache = [&](auto d, auto pg, auto kg) {
+    if (s.scale_rows > 0) launch(d, pg, kg, std::true_type{});
+    else launch(d, pg, kg, std::false_type{});
+  };
   const auto with_groups = [&](auto d, auto pg) {
-    if (two_key_groups(s)) launch(d, pg, std::integral_constant<int, 2>{});
-    else launch(d, pg, std::integral_constant<int, 1>{});
+    if (two_key_groups(s)) with_cache(d, pg, std::integral_constant<int, 2>{});
+    else with_cache(d, pg, std::integral_constant<int, 1>{});
   };
   const auto with_layout = [&](auto d) {
     if (paged) with_groups(d, std::true_type{});
@@ -1679,8 +1829,14 @@ hipError_t launch_attn_mfma(const AttnShape& s, const AttnPlan& p, const void* q
                             const void* k_cache, const void* v_cache, const int32_t* block_table,
                             const int32_t* prefix_len, const int32_t* parents,
                             const int32_t* n_nodes, void* out, float scale, void* workspace,
-                            const int32_t* status, hipStream_t stream) {
+                            const KvScales& scales, const int32_t* status, hipStream_t stream) {
   MfmaArgs a{};
+  a.ks = scales.k;
+  a.vs = scales.v;
+  if (s.scale_rows > 0) {
+    a.scale_per_page = (s.kv_rows + s.scale_rows - 1) / s.scale_rows;
+    while ((1 << a.scale_shift) < s.scale_rows) ++a.scale_shift;
+  }
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k_cache);
   a.v = static_cast<const uint16_t*>(v_cache);
@@ -1716,8 +1872,8 @@ hipError_t launch_attn_mfma(const AttnShape& s, const AttnPlan& p, const void* q
     const size_t slots = static_cast<size_t>(s.B) * s.Hkv * p.max_splits * p.row_tiles * p.tile_rows;
     a.ws_ml = reinterpret_cast<float*>(ws + slots * kD * 2);
     const dim3 grid(s.B * s.Hkv, p.row_tiles, p.max_splits);
-    pick_kernel(s, a.block_table != nullptr, [&](auto d, auto paged, auto kg) {
-      hipLaunchKernelGGL((attn_split_kernel<d(), paged(), kg()>), grid, dim3(kThreads), 0, stream, a);
+    pick_kernel(s, a.block_table != nullptr, [&](auto d, auto paged, auto kg, auto q8) {
+      hipLaunchKernelGGL((attn_split_kernel<d(), paged(), kg(), q8()>), grid, dim3(kThreads), 0, stream, a);
     });
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.max_splits == 1) return e;  // one split: the output is final
@@ -1748,8 +1904,8 @@ hipError_t launch_attn_mfma(const AttnShape& s, const AttnPlan& p, const void* q
   a.W = p.grid;
   a.tile_rows = kTileRows;
   a.max_units = static_cast<int>(max_units(s));
-  pick_kernel(s, a.block_table != nullptr, [&](auto d, auto paged, auto kg) {
-    hipLaunchKernelGGL((attn_stream_kernel<d(), paged(), kg()>), dim3(p.grid), dim3(kThreads), 0, stream, a);
+  pick_kernel(s, a.block_table != nullptr, [&](auto d, auto paged, auto kg, auto q8) {
+    hipLaunchKernelGGL((attn_stream_kernel<d(), paged(), kg(), q8()>), dim3(p.grid), dim3(kThreads), 0, stream, a);
   });
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -16,7 +16,7 @@ hipError_t launch_attn_mfma(const AttnShape& s, const AttnPlan& p, const void* q
                             const void* k_cache, const void* v_cache, const int32_t* block_table,
                             const int32_t* prefix_len, const int32_t* parents,
                             const int32_t* n_nodes, void* out, float scale, void* workspace,
-                            const int32_t* status, hipStream_t stream);
+                            const KvScales& scales, const int32_t* status, hipStream_t stream);
 
 AttnPlan plan_attention(const AttnShape& s, int num_cus) {
   AttnPlan p{};
@@ -37,7 +37,7 @@ hipError_t launch_attention(const AttnShape& s, const AttnPlan& plan, const void
                             const KvScales& scales, const int32_t* status, hipStream_t stream) {
   if (plan.mfma)
     return launch_attn_mfma(s, plan, q, k_cache, v_cache, block_table, prefix_len, parents,
-                            n_nodes, out, scale, workspace, status, stream);
+                            n_nodes, out, scale, workspace, scales, status, stream);
   return launch_attn_rowwise(s, q, k_cache, v_cache, block_table, prefix_len, parents, n_nodes,
                              out, scale, scales, status, stream);
 }

@@ -60,7 +60,9 @@ def test_append(kw, code):
     (dict(B=-1), BAD), (dict(N=257), BAD), (dict(Hq=6), BAD), (dict(mp=-1), BAD), (dict(rows=0), BAD), (dict(scale=0.0), BAD),
     (dict(scale=float("nan")), BAD), (dict(d=96), NO), (dict(sr=256), NO), (dict(dtype=7), NO),
     (dict(table=X, mb=1, nb=1, rows=24), NO), (dict(table=X, mb=1, nb=0), BAD), (dict(ks=None), BAD), (dict(q=X + 4), BAD),
-    (dict(out=X + 2), BAD), (dict(validate=1), BAD), (dict(B=0, q=None), 0)])
+    (dict(out=X + 2), BAD), (dict(validate=1), BAD), (dict(dtype=1, N=60, mp=4096, rows=8192), WS),
+    (dict(dtype=1, N=60, mp=4096, rows=8192, ws=X, wsb=64), WS), (dict(dtype=1, N=60, mp=4096, rows=8192, ws=X + 8, wsb=1 << 30), WS),
+    (dict(B=0, q=None), 0)])
 def test_attention(kw, code):
     assert attn(**kw) == code
 
