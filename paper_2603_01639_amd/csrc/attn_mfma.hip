@@ -64,6 +64,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) void lds_void;
@@ -104,8 +105,8 @@ struct MfmaArgs {
   const int32_t* prefix_len;
   const int32_t* parents;
   const int32_t* n_nodes;
-  uint16_t* ws_o;  // [2W][256][128] bf16: a piece's O / l (slot 2s or 2s + 1)
-  float* ws_ml;    // [2W][256][2]: max (log2 units), sum l
+  uint16_t* ws_o;  // [2W][256][128] bf16: a piece's O / l (slot 2s or 2s + 1); 8-bit cache: see PartRow
+  float* ws_ml;    // [2W][256][2 or 4]: max (log2 units), sum l[, the row's scale]
   MergeDesc* ws_desc;  // [units]: each unit's merge (after a 64-byte header: the unit count)
   int max_units;       // units the launch can have at most (table entries)
   uint16_t* out;
@@ -297,6 +298,36 @@ __device__ __forceinline__ void q8_to_bf16(const u32x4& codes, uint32_t byte, u3
     out[j >> 1][2 * (j & 1)] = __builtin_bit_cast(uint32_t, lo);
     out[j >> 1][2 * (j & 1) + 1] = __builtin_bit_cast(uint32_t, hi);
   }
+}
+
+// How a piece's rows are stored until they are merged: O / l in bf16 or, for an
+// 8-bit cache, in fp16 under a power of two that brings the row's largest
+// value to [2^14, 2^15), beside max and sum.  Same bytes but for that factor,
+// and an error of 2^-11 of a value instead of 2^-8 (2-norm of the output's
+// error, 16 sequences over 1024 to 8192 keys: 2.5e-3 with bf16 pieces, 1.7e-3
+// with these, 1.6e-3 from the output's own rounding).  V's scales span 2^187,
+// hence a factor for each row.
+template <bool kQ8>
+struct PartRow;
+template <>
+struct PartRow<false> {
+  static constexpr int kMl = 2;  // floats beside a row
+  typedef f32x2 Ml;
+  static __device__ __forceinline__ float factor(const Ml&) { return 1.f; }
+  static __device__ __forceinline__ float low(uint32_t w) { return bf16_to_f32(static_cast<uint16_t>(w & 0xFFFFu)); }
+  static __device__ __forceinline__ float high(uint32_t w) { return bf16_to_f32(static_cast<uint16_t>(w >> 16)); }
+};
+template <>
+struct PartRow<true> {
+  static constexpr int kMl = 4;
+  typedef f32x4 Ml;
+  static __device__ __forceinline__ float factor(const Ml& ml) { return ml.z; }
+  static __device__ __forceinline__ float low(uint32_t w) { return static_cast<float>(__builtin_bit_cast(f16x2, w).x); }
+  static __device__ __forceinline__ float high(uint32_t w) { return static_cast<float>(__builtin_bit_cast(f16x2, w).y); }
+};
+constexpr int ml_floats(bool q8) { return q8 ? PartRow<true>::kMl : PartRow<false>::kMl; }
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, (f16x2){static_cast<_Float16>(lo), static_cast<_Float16>(hi)});
 }
 
 // The codes with NaN ones replaced by zero; whether there were any.
@@ -954,7 +985,7 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
   if (!active) return;
   unsigned char* stage = &sm.kv[0][0] + rb * (32 * kRowPitch);  // spans ring slots
   {
-    if (!final_out && qvalid && h == 0) {
+    if (!kQ8 && !final_out && qvalid && h == 0) {
       f32x2 ml = {lsum > 0.f ? m_run * c : -INFINITY, lsum};
       __builtin_nontemporal_store(ml, reinterpret_cast<f32x2*>(a.ws_ml + (part + qrow_idx) * 2));
     }
@@ -967,8 +998,36 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
       if (hit != 0) inv = __builtin_nanf("");
     }
     unsigned char* srow = stage + l32 * kRowPitch;
+    bool half = false;  // an fp16 piece (PartRow) rather than bf16
+    if constexpr (kQ8) {
+      if (!final_out) {
+        half = true;
+        float top = 0.f;
 #pragma unroll
-    for (int db = 0; db < HD / 32; ++db) {
+        for (int db = 0; db < HD / 32; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(o_acc[db][r]));  // (NaN is passed over)
+        top = fmaxf(top, xor32(top)) * (lsum > 0.f ? 1.f / lsum : 0.f);
+        const int e = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 14, 1), 253);  // byte of the factor
+        if (qvalid && h == 0) {
+          const f32x4 ml = {lsum > 0.f ? m_run * c : -INFINITY, lsum, q8_scale(e), 0.f};
+          __builtin_nontemporal_store(ml, reinterpret_cast<f32x4*>(a.ws_ml + (part + qrow_idx) * 4));
+        }
+        inv *= q8_scale(254 - e);
+#pragma unroll
+        for (int db = 0; db < HD / 32; ++db) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint2 v;
+            v.x = pack_f16x2(o_acc[db][4 * j] * inv, o_acc[db][4 * j + 1] * inv);
+            v.y = pack_f16x2(o_acc[db][4 * j + 2] * inv, o_acc[db][4 * j + 3] * inv);
+            *reinterpret_cast<uint2*>(srow + (db * 32 + 8 * j + 4 * h) * 2) = v;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int db = 0; db < HD / 32 && !half; ++db) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         uint2 v;
@@ -1238,8 +1297,11 @@ __device__ __forceinline__ int merge_splits(const MfmaArgs& a, int b, int row) {
 // every split index below max_splits inside its splits.  (A second round for the
 // splits past 16 and reductions through the LDS crossbar made it 5.0 us instead
 // of 4.1 for 240 rows of 17 splits on 8 kv heads.)
-template <int HD, bool kEarly>
+template <int HD, bool kEarly, bool kQ8>
 __global__ void __launch_bounds__(256) attn_split_merge_kernel(MfmaArgs a) {
+  using Part = PartRow<kQ8>;
+  using Ml = typename Part::Ml;
+  constexpr int kMl = Part::kMl;
   __shared__ float w_s[4][kMaxMergeSplits];
   constexpr int kFirst = 32;  // splits whose rows are requested up front
   const int bg = blockIdx.x;
@@ -1259,8 +1321,8 @@ __global__ void __launch_bounds__(256) attn_split_merge_kernel(MfmaArgs a) {
     live = merge_splits(a, b, row);
     if (live <= 1) return;
   }
-  f32x2 ml0 = {-INFINITY, 0.f};
-  if (lane < live) ml0 = *reinterpret_cast<const f32x2*>(a.ws_ml + (part0 + lane * Mpad) * 2);
+  Ml ml0 = {-INFINITY, 0.f};
+  if (lane < live) ml0 = *reinterpret_cast<const Ml*>(a.ws_ml + (part0 + lane * Mpad) * kMl);
   u32x4 o0[kFirst / 4];
 #pragma unroll
   for (int u = 0; u < kFirst / 4; ++u) {
@@ -1271,13 +1333,13 @@ __global__ void __launch_bounds__(256) attn_split_merge_kernel(MfmaArgs a) {
   const int n_splits = kEarly ? merge_splits(a, b, row) : live;
   if (n_splits <= 1) return;
   float M = lane < n_splits ? ml0.x : -INFINITY;
-  for (int s = lane + kWave; s < n_splits; s += kWave) M = fmaxf(M, a.ws_ml[(part0 + s * Mpad) * 2]);
+  for (int s = lane + kWave; s < n_splits; s += kWave) M = fmaxf(M, a.ws_ml[(part0 + s * Mpad) * kMl]);
   M = wave_max_dpp(M);
   float wsum = 0.f;
   for (int s = lane; s < n_splits; s += kWave) {
-    const f32x2 ml = s == lane ? ml0 : *reinterpret_cast<const f32x2*>(a.ws_ml + (part0 + s * Mpad) * 2);
+    const Ml ml = s == lane ? ml0 : *reinterpret_cast<const Ml*>(a.ws_ml + (part0 + s * Mpad) * kMl);
     const float w = exp2_fast(ml.x - M) * ml.y;
-    w_s[wv][s] = w;
+    w_s[wv][s] = w * Part::factor(ml);
     wsum += w;
   }
   wsum = wave_sum_dpp(wsum);
@@ -1288,8 +1350,8 @@ __global__ void __launch_bounds__(256) attn_split_merge_kernel(MfmaArgs a) {
   auto fold = [&](const u32x4& o, float w) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      acc[2 * e] += w * bf16_to_f32(static_cast<uint16_t>(o[e] & 0xFFFFu));
-      acc[2 * e + 1] += w * bf16_to_f32(static_cast<uint16_t>(o[e] >> 16));
+      acc[2 * e] += w * Part::low(o[e]);
+      acc[2 * e + 1] += w * Part::high(o[e]);
     }
   };
 #pragma unroll
@@ -1353,8 +1415,10 @@ constexpr int kFewSplits = 8;
 // launched: 64/8 heads of 64 dims, prefix 10050, 11 nodes, 88 rows of 256: 14.4 us
 // with them, 12.9 without.)
 constexpr size_t kEarlyMergeBytes = size_t{16} << 20;
-template <int HD, bool kEarly>
+template <int HD, bool kEarly, bool kQ8>
 __global__ void __launch_bounds__(256) attn_split_merge_few_kernel(MfmaArgs a) {
+  using Part = PartRow<kQ8>;
+  using Ml = typename Part::Ml;
   const int bg = blockIdx.x;
   const int b = bg / a.Hkv;
   const int g = bg % a.Hkv;
@@ -1368,15 +1432,15 @@ __global__ void __launch_bounds__(256) attn_split_merge_few_kernel(MfmaArgs a) {
     live = merge_splits(a, b, row);
     if (live <= 1) return;
   }
-  f32x2 ml[kFewSplits];
+  Ml ml[kFewSplits];
   u32x4 o[kFewSplits];
 #pragma unroll
   for (int s = 0; s < kFewSplits; ++s) {
-    ml[s] = (f32x2){-INFINITY, 0.f};
+    ml[s] = (Ml){-INFINITY, 0.f};
     o[s] = (u32x4){0u, 0u, 0u, 0u};
     if (s < live) {
       const int64_t r = part0 + static_cast<int64_t>(s) * Mpad;
-      ml[s] = *reinterpret_cast<const f32x2*>(a.ws_ml + r * 2);
+      ml[s] = *reinterpret_cast<const Ml*>(a.ws_ml + r * Part::kMl);
       o[s] = *reinterpret_cast<const u32x4*>(a.ws_o + r * kD + col * 8);
     }
   }
@@ -1393,10 +1457,14 @@ __global__ void __launch_bounds__(256) attn_split_merge_few_kernel(MfmaArgs a) {
     if (s < n_splits) {
       const float w = exp2_fast(ml[s].x - M) * ml[s].y;
       wsum += w;
+      const float wo = w * Part::factor(ml[s]);
+      // (holds the fp16 values back until their weight is known: converted ahead
+      // of it they took 240 registers)
+      if constexpr (kQ8) asm volatile("" : "+v"(o[s]));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        acc[2 * e] += w * bf16_to_f32(static_cast<uint16_t>(o[s][e] & 0xFFFFu));
-        acc[2 * e + 1] += w * bf16_to_f32(static_cast<uint16_t>(o[s][e] >> 16));
+        acc[2 * e] += wo * Part::low(o[s][e]);
+        acc[2 * e + 1] += wo * Part::high(o[s][e]);
       }
     }
   }
@@ -1497,8 +1565,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_stream_kernel(MfmaArgs a) {
 // sequences of 64/8 heads, 15 and 26 nodes over prefixes of 240 and 469, a call
 // 18.6 us instead of 16.7; 32 of 8/2 heads, 12-31 nodes over 545-1909, 22.6
 // instead of 20.7.)
-template <int HD, int kMergeRows>
+template <int HD, int kMergeRows, bool kQ8>
 __global__ void __launch_bounds__(256) attn_stream_merge_kernel(MfmaArgs a) {
+  using Part = PartRow<kQ8>;
+  using Ml = typename Part::Ml;
   constexpr int kBatch = 4;
   __shared__ int16_t slot_s[256 / kWave][kMaxGrid];  // a sparse unit's piece slots, or -1
   constexpr int kRowLanes = HD / 8;             // lanes of a row
@@ -1545,18 +1615,18 @@ __global__ void __launch_bounds__(256) attn_stream_merge_kernel(MfmaArgs a) {
   }
   auto fold_pieces = [&](auto slot_of) {
     for (int k0 = 0; k0 < npieces; k0 += kBatch) {
-      f32x2 ml[kRowSteps][kBatch];
+      Ml ml[kRowSteps][kBatch];
       u32x4 o[kRowSteps][kBatch];
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
         const int slot = k0 + j < npieces ? slot_of(k0 + j) : -1;
 #pragma unroll
         for (int i = 0; i < kRowSteps; ++i) {
-          ml[i][j] = (f32x2){-INFINITY, 0.f};
+          ml[i][j] = (Ml){-INFINITY, 0.f};
           o[i][j] = (u32x4){0u, 0u, 0u, 0u};
           if (slot >= 0) {
             const int64_t row = static_cast<int64_t>(slot) * kTileRows + r[i];
-            ml[i][j] = *reinterpret_cast<const f32x2*>(a.ws_ml + row * 2);
+            ml[i][j] = *reinterpret_cast<const Ml*>(a.ws_ml + row * Part::kMl);
             o[i][j] = *reinterpret_cast<const u32x4*>(a.ws_o + row * kD + col * 8);
           }
         }
@@ -1578,10 +1648,11 @@ __global__ void __launch_bounds__(256) attn_stream_merge_kernel(MfmaArgs a) {
         for (int j = 0; j < kBatch; ++j) {
           const float w = ml[i][j].y > 0.f ? exp2_fast(ml[i][j].x - M[i]) * ml[i][j].y : 0.f;
           wsum[i] += w;
+          const float wo = w * Part::factor(ml[i][j]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            acc[i][2 * e] += w * bf16_to_f32(static_cast<uint16_t>(o[i][j][e] & 0xFFFFu));
-            acc[i][2 * e + 1] += w * bf16_to_f32(static_cast<uint16_t>(o[i][j][e] >> 16));
+            acc[i][2 * e] += wo * Part::low(o[i][j][e]);
+            acc[i][2 * e + 1] += wo * Part::high(o[i][j][e]);
           }
         }
       }
@@ -1648,7 +1719,10 @@ int choose_grid(const AttnShape& s, int num_cus) {
   return W;
 }
 
-constexpr size_t kSlotBytes = static_cast<size_t>(kTileRows) * (kD * sizeof(uint16_t) + 2 * sizeof(float));
+// A partial row in the workspace: 128 dims in 16 bits, max, sum (and factor).
+size_t part_row_bytes(const AttnShape& s) {
+  return kD * sizeof(uint16_t) + ml_floats(s.scale_rows > 0) * sizeof(float);
+}
 constexpr size_t kDescBytes = 64;  // sizeof(MergeDesc)
 
 }  // namespace
@@ -1773,7 +1847,7 @@ void plan_split(const AttnShape& s, int num_cus, AttnPlan* p) {
   const int64_t bound = pre0 <= 1 ? 1 : std::min<int64_t>(pre0 + 1, kMaxMergeSplits);
   const int64_t slots = units * bound * p->tile_rows;
   p->workspace_bytes =
-      bound > 1 ? static_cast<size_t>(slots) * (kD * sizeof(uint16_t) + 2 * sizeof(float)) : 0;
+      bound > 1 ? static_cast<size_t>(slots) * part_row_bytes(s) : 0;
   p->mfma = true;
   p->stream = false;
   p->grid = s.B * s.Hkv * p->row_tiles * p->max_splits;
@@ -1796,7 +1870,8 @@ void plan_stream(const AttnShape& s, int num_cus, AttnPlan* p) {
   p->mfma = true;
   p->stream = true;
   p->grid = choose_grid(s, num_cus);
-  p->workspace_bytes = 2 * static_cast<size_t>(p->grid) * kSlotBytes + (1 + max_units(s)) * kDescBytes;
+  p->workspace_bytes =
+      2 * static_cast<size_t>(p->grid) * kTileRows * part_row_bytes(s) + (1 + max_units(s)) * kDescBytes;
 }
 
 void plan_mfma(const AttnShape& s, int num_cus, AttnPlan* p) {
@@ -1881,13 +1956,17 @@ hipError_t launch_attn_mfma(const AttnShape& s, const AttnPlan& p, const void* q
     // runs on the XCD whose workgroups wrote its partials.
     // (The call's rows, rounded up to a workgroup's below: still within Mpad.)
     const unsigned mrows = static_cast<unsigned>(a.G * s.Nmax);
-    const auto launch_merge = [&](auto d, auto early) {
+    const auto launch_cache = [&](auto d, auto early, auto q8) {
       if (p.max_splits <= kFewSplits)
-        hipLaunchKernelGGL((attn_split_merge_few_kernel<d(), early()>), dim3(s.B * s.Hkv, (mrows + 15) / 16), dim3(256),
-                           0, stream, a);
+        hipLaunchKernelGGL((attn_split_merge_few_kernel<d(), early(), q8()>), dim3(s.B * s.Hkv, (mrows + 15) / 16),
+                           dim3(256), 0, stream, a);
       else
-        hipLaunchKernelGGL((attn_split_merge_kernel<d(), early()>), dim3(s.B * s.Hkv, (mrows + 3) / 4), dim3(256), 0,
-                           stream, a);
+        hipLaunchKernelGGL((attn_split_merge_kernel<d(), early(), q8()>), dim3(s.B * s.Hkv, (mrows + 3) / 4), dim3(256),
+                           0, stream, a);
+    };
+    const auto launch_merge = [&](auto d, auto early) {
+      if (s.scale_rows > 0) launch_cache(d, early, std::true_type{});
+      else launch_cache(d, early, std::false_type{});
     };
     const auto with_early = [&](auto d) {
       const size_t bytes = static_cast<size_t>(s.B) * s.Hkv * p.max_splits * mrows * kD * 2;
@@ -1900,7 +1979,7 @@ hipError_t launch_attn_mfma(const AttnShape& s, const AttnPlan& p, const void* q
   }
   const size_t slots = static_cast<size_t>(2) * p.grid * kTileRows;
   a.ws_ml = reinterpret_cast<float*>(ws + slots * kD * 2);
-  a.ws_desc = reinterpret_cast<MergeDesc*>(ws + slots * (kD * 2 + 2 * sizeof(float)));
+  a.ws_desc = reinterpret_cast<MergeDesc*>(ws + slots * part_row_bytes(s));
   a.W = p.grid;
   a.tile_rows = kTileRows;
   a.max_units = static_cast<int>(max_units(s));
@@ -1917,9 +1996,13 @@ hipError_t launch_attn_mfma(const AttnShape& s, const AttnPlan& p, const void* q
   // 40.9 / 41.4, 2048 units 42.6 / 41.5, 4096 units 88.0 / 81.2, 8192 units 68.1 /
   // 63.4.  Head size 64: 4 units 42.1 / 51.3 (many pieces: one row a lane keeps
   // a batch's chain short), 128 units 18.7 / 20.8, 512 units 180.6 / 180.6.
-  const auto launch_merge = [&](auto d, auto rows) {
-    hipLaunchKernelGGL((attn_stream_merge_kernel<d(), rows()>), dim3(a.max_units, kTileRows / (4 * rows())),
+  const auto launch_cache = [&](auto d, auto rows, auto q8) {
+    hipLaunchKernelGGL((attn_stream_merge_kernel<d(), rows(), q8()>), dim3(a.max_units, kTileRows / (4 * rows())),
                        dim3(256), 0, stream, a);
+  };
+  const auto launch_merge = [&](auto d, auto rows) {
+    if (s.scale_rows > 0) launch_cache(d, rows, std::true_type{});
+    else launch_cache(d, rows, std::false_type{});
   };
   const auto with_rows = [&](auto d) {
     if (a.max_units >= kWideMerge) launch_merge(d, std::integral_constant<int, 16>{});
