@@ -49,6 +49,7 @@
 // 128-dim row pitch in the workspace.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "ltd_device.hpp"
 #include "ltd_launch.hpp"
@@ -322,12 +323,28 @@ struct PartRow<true> {
   static constexpr int kMl = 4;
   typedef f32x4 Ml;
   static __device__ __forceinline__ float factor(const Ml& ml) { return ml.z; }
-  static __device__ __forceinline__ float low(uint32_t w) { return static_cast<float>(__builtin_bit_cast(f16x2, w).x); }
-  static __device__ __forceinline__ float high(uint32_t w) { return static_cast<float>(__builtin_bit_cast(f16x2, w).y); }
+  static __device__ __forceinline__ float low(uint32_t w) {
+    return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(w & 0xFFFFu)));
+  }
+  static __device__ __forceinline__ float high(uint32_t w) {
+    return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(w >> 16)));
+  }
 };
 constexpr int ml_floats(bool q8) { return q8 ? PartRow<true>::kMl : PartRow<false>::kMl; }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, (f16x2){static_cast<_Float16>(lo), static_cast<_Float16>(hi)});
+}
+
+// f(0), ..., f(N - 1) with the indices as compile-time constants: arrays indexed
+// by them stay in registers of their own (a loop that hipcc unrolls late leaves
+// them one wide vector, copied whole at every branch).
+template <int... I, class F>
+__device__ __forceinline__ void for_each_of(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void for_each_index(F f) {
+  for_each_of(std::make_integer_sequence<int, N>{}, f);
 }
 
 // The codes with NaN ones replaced by zero; whether there were any.
@@ -466,16 +483,17 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
     __syncthreads();
   }
   // 8-bit cache: this thread's tile key and its 16 codes' first dim.  With 64
-  // dims the upper half of the threads takes V, the lower half K.
+  // dims the upper half of the threads takes V, the lower half K.  A wave's
+  // codes are those of 8 (or 16) consecutive keys, which lie in one page and one
+  // scale block wherever the tile's first row is a multiple of 16 (every prefix
+  // tile's is): such a tile is loaded from a base in scalar registers.
   constexpr int kQLanes = HD / 16;
-  const bool q8_k = HD == 128 || tid < kThreads / 2, q8_v = HD == 128 || tid >= kThreads / 2;
+  const bool q8_k = HD == 128 || wave < kWaves / 2, q8_v = HD == 128 || wave >= kWaves / 2;
   const int q8_key = (tid / kQLanes) & (kKT - 1);
+  const int q8_wave_key = __builtin_amdgcn_readfirstlane(q8_key);
   const int q8_dim = tid % kQLanes * 16;
-  auto load_piece = [&](int t, Q8Piece& x) {
-    const TileRef tr = tile_ref(t);
-    const int row = tr.row + min(q8_key, tr.left - 1);
-    int64_t rg;
-    int in;
+  // Row group (page and kv head) and row in the page of a logical cache row.
+  auto q8_place = [&](int row, int64_t& rg, int& in) {
     if (!paged) {
       rg = static_cast<int64_t>(b) * a.Hkv + g;
       in = row;
@@ -487,33 +505,60 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
       rg = sm.blk[blk - first_blk];
       in = row - blk * a.kv_rows;
     }
-    const int64_t at = (rg * a.kv_rows + in) * HD + q8_dim;
-    const int64_t st = rg * a.scale_per_page + (in >> a.scale_shift);
-    if (HD == 128) {
-      x.k = *reinterpret_cast<const u32x4*>(kbase + at);
-      x.v = *reinterpret_cast<const u32x4*>(vbase + at);
-      x.ks = a.ks[st];
-      x.vs = a.vs[st];
+  };
+  auto load_piece = [&](int t, Q8Piece& x) {
+    const TileRef tr = tile_ref(t);
+    const unsigned char *kp, *vp;
+    const uint8_t *ksp, *vsp;
+    if (!tr.tree && tr.left >= kKT) {
+      int64_t rg;
+      int in;
+      q8_place(tr.row + q8_wave_key, rg, in);
+      const int64_t rgs = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(rg)));
+      const int ins = __builtin_amdgcn_readfirstlane(in);
+      const int64_t at = (rgs * a.kv_rows + ins) * HD;
+      const int64_t st = rgs * a.scale_per_page + (ins >> a.scale_shift);
+      kp = kbase + at + lane * 16;
+      vp = vbase + at + lane * 16;
+      ksp = a.ks + st;
+      vsp = a.vs + st;
     } else {
-      x.k = *reinterpret_cast<const u32x4*>((q8_k ? kbase : vbase) + at);
-      x.ks = (q8_k ? a.ks : a.vs)[st];
+      int64_t rg;
+      int in;
+      q8_place(tr.row + min(q8_key, tr.left - 1), rg, in);
+      const int64_t at = (rg * a.kv_rows + in) * HD + q8_dim;
+      const int64_t st = rg * a.scale_per_page + (in >> a.scale_shift);
+      kp = kbase + at;
+      vp = vbase + at;
+      ksp = a.ks + st;
+      vsp = a.vs + st;
+    }
+    if (HD == 128) {
+      x.k = *reinterpret_cast<const u32x4*>(kp);
+      x.v = *reinterpret_cast<const u32x4*>(vp);
+      x.ks = *ksp;
+      x.vs = *vsp;
+    } else {
+      x.k = *reinterpret_cast<const u32x4*>(q8_k ? kp : vp);
+      x.ks = *(q8_k ? ksp : vsp);
     }
   };
   // Widens a piece into its tile's slot: K at the row that holds its key, both
-  // swizzled.  The upper dims write their second chunk first, so that the eight
-  // lanes of a row never meet in an LDS bank.
+  // swizzled (sigma(q8_row) is the key).
+  const int q8_row = (q8_key & 32) | (q8_key & 3) | (((q8_key >> 4) & 1) << 2) | (((q8_key >> 2) & 3) << 3);
+  int q8_kw[2], q8_vw[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    q8_kw[j] = q8_row * (kD * 2) + (((q8_dim / 8 + j) ^ (q8_row & 15)) << 4);
+    q8_vw[j] = kKBytes + q8_key * (kD * 2) + (((q8_dim / 8 + j) ^ swz_v(q8_key)) << 4);
+  }
   auto store_piece = [&](int t, Q8Piece& x) {
     unsigned char* slot = sm.kv[t % kStages];
-    const int c0 = q8_dim / 8;
-    const int flip = (tid % kQLanes) >= kQLanes / 2 ? 1 : 0;
     u32x4 w[2];
     if (q8_k) {
-      const int k5 = q8_key & 31;
-      const int i = (q8_key & 32) | (k5 & 3) | ((k5 >> 4) << 2) | (((k5 >> 2) & 3) << 3);  // sigma(i) = k5
       q8_to_bf16(x.k, x.ks, w);
-      unsigned char* row = slot + i * (kD * 2);
-      *reinterpret_cast<u32x4*>(row + (((c0 + flip) ^ (i & 15)) << 4)) = flip ? w[1] : w[0];
-      *reinterpret_cast<u32x4*>(row + (((c0 + 1 - flip) ^ (i & 15)) << 4)) = flip ? w[0] : w[1];
+      *reinterpret_cast<u32x4*>(slot + q8_kw[0]) = w[0];
+      *reinterpret_cast<u32x4*>(slot + q8_kw[1]) = w[1];
     }
     if (q8_v) {
       u32x4& v = HD == 128 ? x.v : x.k;
@@ -523,9 +568,8 @@ __device__ __forceinline__ void attend(const MfmaArgs& a, Smem& sm, int b, int g
           atomicOr(&sm.nan_rows[(tr.rel + q8_key) >> 5], 1u << ((tr.rel + q8_key) & 31));
       }
       q8_to_bf16(v, HD == 128 ? x.vs : x.ks, w);
-      unsigned char* row = slot + kKBytes + q8_key * (kD * 2);
-      *reinterpret_cast<u32x4*>(row + (((c0 + flip) ^ swz_v(q8_key)) << 4)) = flip ? w[1] : w[0];
-      *reinterpret_cast<u32x4*>(row + (((c0 + 1 - flip) ^ swz_v(q8_key)) << 4)) = flip ? w[0] : w[1];
+      *reinterpret_cast<u32x4*>(slot + q8_vw[0]) = w[0];
+      *reinterpret_cast<u32x4*>(slot + q8_vw[1]) = w[1];
     }
   };
   Q8Piece piece[2];  // tiles of even and of odd index
@@ -1418,7 +1462,6 @@ constexpr size_t kEarlyMergeBytes = size_t{16} << 20;
 template <int HD, bool kEarly, bool kQ8>
 __global__ void __launch_bounds__(256) attn_split_merge_few_kernel(MfmaArgs a) {
   using Part = PartRow<kQ8>;
-  using Ml = typename Part::Ml;
   const int bg = blockIdx.x;
   const int b = bg / a.Hkv;
   const int g = bg % a.Hkv;
@@ -1432,42 +1475,42 @@ __global__ void __launch_bounds__(256) attn_split_merge_few_kernel(MfmaArgs a) {
     live = merge_splits(a, b, row);
     if (live <= 1) return;
   }
-  Ml ml[kFewSplits];
+  f32x2 ml[kFewSplits];
+  float fc[kFewSplits];  // (8-bit cache: the rows' factors)
   u32x4 o[kFewSplits];
-#pragma unroll
-  for (int s = 0; s < kFewSplits; ++s) {
-    ml[s] = (Ml){-INFINITY, 0.f};
+  for_each_index<kFewSplits>([&](auto i) {
+    constexpr int s = i();
+    ml[s] = (f32x2){-INFINITY, 0.f};
+    fc[s] = 1.f;
     o[s] = (u32x4){0u, 0u, 0u, 0u};
     if (s < live) {
       const int64_t r = part0 + static_cast<int64_t>(s) * Mpad;
-      ml[s] = *reinterpret_cast<const Ml*>(a.ws_ml + r * Part::kMl);
+      ml[s] = *reinterpret_cast<const f32x2*>(a.ws_ml + r * Part::kMl);
+      if constexpr (kQ8) fc[s] = a.ws_ml[r * Part::kMl + 2];
       o[s] = *reinterpret_cast<const u32x4*>(a.ws_o + r * kD + col * 8);
     }
-  }
+  });
   const int n_splits = kEarly ? merge_splits(a, b, row) : live;
   if (n_splits <= 1) return;
   float M = -INFINITY;
-#pragma unroll
-  for (int s = 0; s < kFewSplits; ++s)
-    if (s < n_splits) M = fmaxf(M, ml[s].x);
+  for_each_index<kFewSplits>([&](auto i) {
+    if (i() < n_splits) M = fmaxf(M, ml[i()].x);
+  });
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   float wsum = 0.f;
-#pragma unroll
-  for (int s = 0; s < kFewSplits; ++s) {
+  for_each_index<kFewSplits>([&](auto i) {
+    constexpr int s = i();
     if (s < n_splits) {
       const float w = exp2_fast(ml[s].x - M) * ml[s].y;
       wsum += w;
-      const float wo = w * Part::factor(ml[s]);
-      // (holds the fp16 values back until their weight is known: converted ahead
-      // of it they took 240 registers)
-      if constexpr (kQ8) asm volatile("" : "+v"(o[s]));
+      const float wo = kQ8 ? w * fc[s] : w;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         acc[2 * e] += wo * Part::low(o[s][e]);
         acc[2 * e + 1] += wo * Part::high(o[s][e]);
       }
     }
-  }
+  });
   if (col < HD / 8) {  // (lanes past the head's dims summed unused workspace)
     const float inv = 1.f / wsum;
     const int node = node_of(a, row);
