@@ -48,6 +48,7 @@
 // 2 dim blocks for O^T, half the MFMAs of a tile.  Partial results keep the
 // 128-dim row pitch in the workspace.
 #include <algorithm>
+#include <cstddef>
 #include <type_traits>
 #include <utility>
 
@@ -67,7 +68,9 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_cvoid;
 
@@ -224,6 +227,11 @@ __device__ __forceinline__ void dma16(uint32_t lds, const void* uniform_base, ui
 }
 __device__ __forceinline__ void dma16(uint32_t lds, const void* lane_ptr) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(lane_ptr)
+               : "memory");
+}
+// Direct global->LDS load of a byte per lane (lane i's byte lands as a word at M0 + 4*i).
+__device__ __forceinline__ void dma1(uint32_t lds, const void* lane_ptr) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_ubyte %1, off" ::"s"(lds), "v"(lane_ptr)
                : "memory");
 }
 // Direct global->LDS load of 4 bytes per lane (lane i's word lands at M0 + 4*i).
@@ -1285,6 +1293,485 @@ static_assert(sizeof(MergeDesc) == 64, "descriptor layout");
 // (sequence, kv head), which read the same keys, run side by side on one L2.
 __device__ __forceinline__ int stream_index(int w, int W) { return (w % 8) * (W / 8) + w / 8; }
 
+// ---- units of at most 32 stacked rows over an 8-bit cache (decoding, short
+// trees).  Such calls are bound by the cache's bytes.  A (sequence, kv head) is
+// cut into splits of one length, the tree's keys joining the last, one for a
+// workgroup of four waves; two workgroups share a compute unit.  The length is
+// worked out on the GPU from the call's own lengths (few_find): the shortest for
+// which the splits fit the grid, so that all run at once and the longest
+// holds no more than its share, whatever max_prefix is.  Every wave takes all of the unit's rows and its own
+// 32-key blocks (block i: wave i mod 4), from loads to P.V, with no barrier until
+// the waves' results are joined.  Its blocks move straight into two slots of
+// LDS of its own, refilled as soon as they are read: 8 to 16 KiB requested per
+// wave, 64 to 128 per compute unit (with the next block in registers, which
+// are free only part of a block's time, 16 sequences of 1024 to 8192 keys took
+// 44.6 us instead of 42.2).
+//
+// K lies in LDS as the S^T operand takes it: lane l finds the codes of key
+// sigma(l & 31), 16 dims in every 32, where its own load put them (Q's fragments
+// have their dims in the same order), and widens them.  V's rows lie as in the
+// cache, 16-byte chunks swizzled; ds_read_b64_tr_b8 hands each lane 8 keys of one
+// dim, widened next.  A fragment of 8 keys lies in one scale block in every
+// full block; in a range's last partial block and the tree's (32 nodes at most,
+// one block) each key's V scale multiplies its weights instead, an exact power
+// of two.
+constexpr int kFewWaves = 4;
+constexpr int kFewThreads = kFewWaves * kWave;
+constexpr int kFewRows = 32;     // stacked rows of a unit at most
+constexpr int kFewBlocks = 512;  // paged block ids a split may span
+constexpr int kFewSlots = 2;     // blocks a wave has in LDS or on the way
+
+// A wave's slot: K's codes by lane, V's rows, the scale bytes (a word each) of
+// every lane's K row and of V (full block: keys 16 (l / 32) .., else key l & 31).
+template <int HD>
+struct FewSlot {
+  unsigned char k[32 * HD];
+  unsigned char v[32 * HD];
+  uint32_t ks[kWave];
+  uint32_t vs[kWave];
+};
+template <int HD>
+struct FewSmem {
+  union {
+    FewSlot<HD> slot[kFewWaves][kFewSlots];
+    float o[kFewWaves][kFewRows][HD];  // the waves' results
+  };
+  uint16_t q[kFewRows][HD];  // 16-byte chunk c of row r at c ^ (r & 7)
+  float ml[kFewWaves][kFewRows][2];
+  int32_t blk[kFewBlocks];  // row groups (id * Hkv + g) of the split's pages
+};
+
+// What a workgroup of the grid works on: split `split` of `n_splits` of
+// sequence b and kv head g; w is its place among the call's splits (b major,
+// then g, then split), and the unit's first split's place is w - split.  b < 0:
+// the call has fewer splits.
+struct FewWork {
+  int b, g, split, n_splits, P, split_keys;
+};
+
+// The split length is ceil(T Hkv / (W - B Hkv)) for T prefix keys in all and a
+// grid of W > B Hkv workgroups, rounded up to a key tile, at least a block a
+// wave: the splits then number at most T Hkv / length + B Hkv <= W.  Every
+// wave works it out on its own (lane l holds sequence c * 64 + l of chunk c).
+__device__ __forceinline__ FewWork few_find(const MfmaArgs& a, int w) {
+  const int lane = __lane_id();
+  FewWork r{-1, 0, 0, 0, 0, 0};
+  if (a.B == 1) {  // a scalar load and no scans
+    r.P = min(max(a.prefix_len[0], 0), a.max_prefix);
+    r.split_keys = max(static_cast<int>(static_cast<int64_t>(r.P) * a.Hkv / (a.W - a.Hkv) / kKT + 1) * kKT, a.split_keys);
+    r.n_splits = max((r.P + r.split_keys - 1) / r.split_keys, 1);
+    r.g = w / r.n_splits;
+    r.split = w - r.g * r.n_splits;
+    r.b = r.g < a.Hkv ? 0 : -1;
+    return r;
+  }
+  auto length = [&](int b) { return b < a.B ? min(max(a.prefix_len[b], 0), a.max_prefix) : 0; };
+  const int P0 = length(lane);
+  int64_t T = readlane_i64(wave_scan_i64(P0), kWave - 1);
+  for (int c0 = kWave; c0 < a.B; c0 += kWave) T += readlane_i64(wave_scan_i64(length(c0 + lane)), kWave - 1);
+  // (a float estimate, raised so that it is never short of the quotient)
+  const float want = static_cast<float>(T) * static_cast<float>(a.Hkv) / static_cast<float>(a.W - a.B * a.Hkv);
+  const int sk = max((static_cast<int>(want * 1.00001f) / kKT + 1) * kKT, a.split_keys);
+  r.split_keys = sk;
+  int before = 0;  // splits of the sequences before this chunk
+  for (int c0 = 0; c0 < a.B; c0 += kWave) {
+    const int P = c0 == 0 ? P0 : length(c0 + lane);
+    const int n = c0 + lane < a.B ? max((P + sk - 1) / sk, 1) : 0;  // splits per head
+    const int upto = static_cast<int>(wave_scan_i64(n * a.Hkv)) + before;
+    const int start = upto - n * a.Hkv;
+    const uint64_t hit = __ballot(start <= w && w < upto);
+    if (hit != 0) {
+      const int l = __ffsll(static_cast<long long>(hit)) - 1;
+      r.b = c0 + l;
+      r.P = __builtin_amdgcn_readlane(P, l);
+      r.n_splits = __builtin_amdgcn_readlane(n, l);
+      const int at = w - __builtin_amdgcn_readlane(start, l);
+      r.g = at / r.n_splits;
+      r.split = at - r.g * r.n_splits;
+      return r;
+    }
+    before = __builtin_amdgcn_readlane(upto, kWave - 1);
+  }
+  return r;
+}
+
+// The merge's entry of unit b * Hkv + g: its first split's slot, its splits.
+struct FewDesc {
+  int32_t first, n_splits;
+};
+
+template <int HD, bool kPaged>
+__global__ void __launch_bounds__(kFewThreads, 2) attn_few_kernel(MfmaArgs a) {
+  __shared__ __attribute__((aligned(16))) FewSmem<HD> sm;
+  if (halted(a.status)) return;
+  const int slot_id = blockIdx.x;
+  const FewWork fw = few_find(a, slot_id);
+  if (fw.b < 0) return;
+  const int b = fw.b, g = fw.g, P = fw.P;
+  const int n = min(max(a.n_nodes[b], 1), a.Nmax);
+  const bool has_tree = fw.split == fw.n_splits - 1;
+  const bool final_out = fw.n_splits == 1;
+  const int valid_rows = a.G * n;
+  const int key_begin = fw.split * fw.split_keys;
+  const int n_pre = min(fw.split_keys, P - key_begin);
+  if (fw.split == 0 && threadIdx.x == 0)
+    reinterpret_cast<FewDesc*>(a.ws_desc)[b * a.Hkv + g] = FewDesc{slot_id, fw.n_splits};
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int lane = tid % kWave;
+  const int h = lane >> 5, l32 = lane & 31;
+  constexpr int kKC = HD / 32;                // 16-code chunks of a lane's K
+  constexpr int kVRow = HD / 16;              // lanes of a V row
+  constexpr int kVKeys = kWave / kVRow;       // keys of a V load
+  constexpr int kVC = 32 / kVKeys;            // V loads of a block
+  constexpr int kLoads = kKC + kVC + 2;       // loads of a block
+  constexpr int kRowBytes = HD;               // a V row in LDS
+  const int n_full = n_pre / 32;              // full prefix blocks
+  const int n_blocks = (n_pre + 31) / 32;     // ... and a partial one
+  const int n_all = n_blocks + (has_tree ? 1 : 0);
+
+  // ---- Q's rows (rows past the unit's repeat its last) and, for a paged cache,
+  // the split's row groups
+  constexpr int kQRowChunks = HD / 8;
+  constexpr int kQLoads = kFewRows * kQRowChunks / kFewThreads;  // 16-byte chunks a thread: 2 or 1
+#pragma unroll
+  for (int j = 0; j < kQLoads; ++j) {
+    const int x = j * kFewThreads + tid;
+    const int r = x / kQRowChunks, qr = min(r, valid_rows - 1);
+    const int node = node_of(a, qr);
+    const uint16_t* src = a.q +
+        ((static_cast<int64_t>(b) * a.Nmax + node) * a.Hq + g * a.G + (qr - node * a.G)) * HD +
+        ((x % kQRowChunks) ^ (r & 7)) * 8;
+    dma16(lds_addr(&sm.q[0][0]) + (j * kFewThreads + wave * kWave) * 16, src);
+  }
+  const int first_blk = kPaged ? key_begin / a.kv_rows : 0;
+  if constexpr (kPaged) {
+    const int n_blk = (key_begin + n_pre + (has_tree ? n : 0) - 1) / a.kv_rows - first_blk + 1;
+    const int32_t* bt = a.block_table + static_cast<int64_t>(b) * a.max_blocks + first_blk;
+    for (int j = tid; j < n_blk; j += kFewThreads) sm.blk[j] = bt[j] * a.Hkv + g;
+    __syncthreads();
+  }
+  auto place = [&](int row, int64_t& rg, int& in) {
+    if (!kPaged) {
+      rg = static_cast<int64_t>(b) * a.Hkv + g;
+      in = row;
+    } else if (a.kv_shift >= 0) {
+      rg = sm.blk[(row >> a.kv_shift) - first_blk];
+      in = row & (a.kv_rows - 1);
+    } else {
+      const int blk = row / a.kv_rows;
+      rg = sm.blk[blk - first_blk];
+      in = row - blk * a.kv_rows;
+    }
+  };
+  // Byte offsets of a row's codes and of its scale byte; `uniform` rows go
+  // through scalar registers.
+  auto offsets = [&](int row, bool uniform, int64_t& at, int64_t& st) {
+    int64_t rg;
+    int in;
+    place(row, rg, in);
+    if (uniform) {
+      rg = __builtin_amdgcn_readfirstlane(static_cast<int>(rg));
+      in = __builtin_amdgcn_readfirstlane(in);
+    }
+    at = (rg * a.kv_rows + in) * HD;
+    st = rg * a.scale_per_page + (in >> a.scale_shift);
+  };
+  // V in LDS: chunk c of key k at c ^ f(k), so that the 8 keys x 16 dims of a
+  // transposed read spread over the banks.
+  const auto v_swz = [](int key) { return HD == 128 ? (key >> 1) & 3 : (key >> 2) & 3; };
+  const unsigned char* kbase = reinterpret_cast<const unsigned char*>(a.k);
+  const unsigned char* vbase = reinterpret_cast<const unsigned char*>(a.v);
+  const int k_key = sigma(l32);
+  const uint32_t slot0_lds = lds_addr(&sm.slot[wave][0]);
+  int v_off[kVC];  // the lane's chunk of each V load, within its row
+#pragma unroll
+  for (int j = 0; j < kVC; ++j) v_off[j] = ((lane % kVRow) ^ v_swz(j * kVKeys + lane / kVRow)) * 16;
+  // Requests block i (wave-uniform) into slot s.
+  auto load = [&](int i, int s) {
+    const uint32_t k_lds = slot0_lds + s * sizeof(FewSlot<HD>);
+    const uint32_t v_lds = k_lds + offsetof(FewSlot<HD>, v);
+    const uint32_t s_lds = k_lds + offsetof(FewSlot<HD>, ks);
+    if (i < n_full) {
+      // 32 keys from a multiple of 32: each half lies in one page and one scale block
+      const int row = key_begin + 32 * i;
+      int64_t at0, at1, st0, st1;
+      offsets(row, true, at0, st0);
+      offsets(row + 16, true, at1, st1);
+      const int up = k_key >> 4;
+      const unsigned char* kp = kbase + (up ? at1 : at0) + (k_key & 15) * HD + h * 16;
+#pragma unroll
+      for (int j = 0; j < kKC; ++j) dma16(k_lds + j * 1024, kp + 32 * j);
+#pragma unroll
+      for (int j = 0; j < kVC; ++j) {
+        const int first = j * kVKeys;  // (its keys share a half)
+        dma16(v_lds + j * 1024, vbase + (first >= 16 ? at1 : at0) + ((first & 15) + lane / kVRow) * HD + v_off[j]);
+      }
+      dma1(s_lds, a.ks + (up ? st1 : st0));
+      dma1(s_lds + sizeof(uint32_t) * kWave, a.vs + (h ? st1 : st0));
+      return;
+    }
+    const bool tree = i == n_blocks;
+    const int row = tree ? P : key_begin + 32 * i;
+    const int last = (tree ? n : n_pre - 32 * i) - 1;  // keys past the range read its last row, masked out
+    int64_t at, st;
+    offsets(row + min(k_key, last), false, at, st);
+#pragma unroll
+    for (int j = 0; j < kKC; ++j) dma16(k_lds + j * 1024, kbase + at + h * 16 + 32 * j);
+    dma1(s_lds, a.ks + st);
+#pragma unroll
+    for (int j = 0; j < kVC; ++j) {
+      offsets(row + min(j * kVKeys + lane / kVRow, last), false, at, st);
+      dma16(v_lds + j * 1024, vbase + at + v_off[j]);
+    }
+    offsets(row + min(l32, last), false, at, st);
+    dma1(s_lds + sizeof(uint32_t) * kWave, a.vs + st);
+  };
+  const int mine = wave < n_all ? (n_all - wave + kFewWaves - 1) / kFewWaves : 0;  // this wave's blocks
+#pragma unroll
+  for (int s = 0; s < kFewSlots; ++s)
+    if (s < mine) load(wave + s * kFewWaves, s);
+  // (Q has landed once no more than those loads are outstanding)
+  if (mine >= 2) wait_vmcnt<2 * kLoads>();
+  else if (mine == 1) wait_vmcnt<kLoads>();
+  else wait_vmcnt<0>();
+  barrier_only();
+
+  // ---- Q: lane holds row l32, chunk j's 16 dims 32 j + 16 h .. as two k-steps
+  const bool qvalid = l32 < valid_rows;
+  const int qnode = node_of(a, min(l32, valid_rows - 1));
+  bf16x8 qf[kKC][2];
+#pragma unroll
+  for (int j = 0; j < kKC; ++j)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      qf[j][e] = *reinterpret_cast<const bf16x8*>(&sm.q[l32][((4 * j + 2 * h + e) ^ (l32 & 7)) * 8]);
+
+  // ---- the ancestors of row l32's node, by doubling over the links (lane =
+  // node; at most 32 of them), in the wave that takes the tree's block
+  uint32_t anc = 0;
+  if (has_tree && wave == n_blocks % kFewWaves) {
+    int jump = lane > 0 && lane < n ? a.parents[static_cast<int64_t>(b) * a.Nmax + lane] : -1;
+    uint32_t set = lane < n ? 1u << (lane & 31) : 0u;
+    for (int r = 0; r < 5; ++r) {
+      const int j = min(max(jump, 0), kWave - 1);  // (a malformed link stays in the wave)
+      const uint32_t other = __shfl(set, j, kWave);
+      const int next = __shfl(jump, j, kWave);
+      if (jump >= 0) {
+        set |= other;
+        jump = next;
+      }
+    }
+    anc = __shfl(set, qnode, kWave);
+  }
+
+  float m_run = kNoMax, l_run = 0.f;
+  f32x16 o_acc[HD / 32];
+#pragma unroll
+  for (int db = 0; db < HD / 32; ++db) o_acc[db] = f32x16{};
+  const float c = a.scale_log2;
+  uint32_t nan_keys = 0;  // tree rows with a NaN code in V
+  // transposed read: 16-lane group q, lane s of it: key 16 (q / 2) + 8 kk + s / 2, dims 32 db + 16 (q % 2) + 8 (s % 2)
+  const int tq = lane >> 4, ts = lane & 15;
+  int v_rd[2][HD / 32];
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+    for (int db = 0; db < HD / 32; ++db) {
+      const int key = 16 * (tq >> 1) + 8 * kk + (ts >> 1);
+      v_rd[kk][db] = key * kRowBytes + (((2 * db + (tq & 1)) ^ v_swz(key)) << 4) + 8 * (ts & 1);
+    }
+
+#pragma unroll 1
+  for (int it = 0; it < mine; ++it) {
+    const int i = wave + it * kFewWaves;
+    const bool full = i < n_full;
+    const bool tree = has_tree && i == n_blocks;
+    FewSlot<HD>& sl = sm.slot[wave][it % kFewSlots];
+    if (it + 1 < mine) wait_vmcnt<kLoads>();
+    else wait_vmcnt<0>();
+    if (tree) {  // NaN codes in V leave the product (see attend)
+#pragma unroll
+      for (int j = 0; j < kVC; ++j) {
+        u32x4* at = reinterpret_cast<u32x4*>(sl.v + j * 1024) + lane;
+        u32x4 codes = *at;
+        const bool bad = q8_clear_nan(codes);
+        const uint64_t hit = __ballot(bad);
+        if (bad) *at = codes;
+        for (int k = 0; k < kVKeys && hit != 0; ++k)
+          if ((hit >> (k * kVRow)) & ((1u << kVRow) - 1)) nan_keys |= 1u << (j * kVKeys + k);
+      }
+    }
+    const uint32_t ks = sl.ks[lane];
+    const float v_scale = full ? q8_scale(static_cast<int>(sl.vs[lane])) : 1.f;
+    f32x16 s = {};
+#pragma unroll
+    for (int j = 0; j < kKC; ++j) {
+      u32x4 w[2];
+      q8_to_bf16(reinterpret_cast<const u32x4*>(sl.k)[j * kWave + lane], ks, w);
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[e]), qf[j][e], s, 0, 0, 0);
+    }
+    if (!full) {
+      const int left = tree ? n : n_pre - 32 * i;
+      uint32_t vis = left >= 32 ? 0xFFFFFFFFu : (1u << left) - 1u;
+      if (tree) vis &= anc;
+      vis >>= 16 * h;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (!((vis >> r) & 1u)) s[r] = -INFINITY;
+    }
+    // softmax, as in attend
+    float tmax = __builtin_elementwise_maximum(s[0], s[1]);
+#pragma unroll
+    for (int r = 2; r < 16; r += 2)
+      tmax = __builtin_elementwise_maximum(__builtin_elementwise_maximum(tmax, s[r]), s[r + 1]);
+    tmax = max_xor32(tmax);
+    const float m_new = tmax > m_run + a.lazy_gap ? tmax : m_run;
+    const float neg = fminf(-m_new * c, __FLT_MAX__);  // (no visible key yet: see attend)
+    const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
+    float ps = 0.f;
+    float p[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r] = exp2_fast(__builtin_fmaf(s[r], c, neg));
+    bf16x8 pf[2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      u32x4 pk;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf16x2 w = __builtin_convertvector((f32x2){p[8 * kk + 2 * j], p[8 * kk + 2 * j + 1]}, bf16x2);
+        ps = __builtin_amdgcn_fdot2_f32_bf16(w, ones, ps, false);
+        pk[j] = __builtin_bit_cast(uint32_t, w);
+      }
+      pf[kk] = __builtin_bit_cast(bf16x8, pk);
+    }
+    if (!full) {
+      // each key's scale onto its rounded weight (the sum has the weight itself)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        u32x4 pk = __builtin_bit_cast(u32x4, pf[kk]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t* sc = sl.vs + 16 * h + 8 * kk + 2 * j;
+          pk[j] = pack_bf16x2(bf16_to_f32(static_cast<uint16_t>(pk[j] & 0xFFFFu)) * q8_scale(static_cast<int>(sc[0])),
+                              bf16_to_f32(static_cast<uint16_t>(pk[j] >> 16)) * q8_scale(static_cast<int>(sc[1])));
+        }
+        pf[kk] = __builtin_bit_cast(bf16x8, pk);
+      }
+    }
+    if (__builtin_amdgcn_ballot_w64(m_new != m_run) != 0) {
+      const float alpha = exp2_fast((m_run - m_new) * c);
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < HD / 32; ++db) o_acc[db] *= alpha;
+    }
+    l_run += ps;
+    m_run = m_new;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int db = 0; db < HD / 32; ++db) {
+        const i32x2 codes = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)as_lds(sl.v + v_rd[kk][db]));
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t cw = static_cast<uint32_t>(codes[j]);
+          w[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(cw, v_scale, false));
+          w[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(cw, v_scale, true));
+        }
+        o_acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf[kk], o_acc[db], 0, 0, 0);
+      }
+    if (it + kFewSlots < mine) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this block's LDS reads are done
+      load(i + kFewSlots * kFewWaves, it % kFewSlots);
+    }
+  }
+  if ((anc & nan_keys) != 0) {
+#pragma unroll
+    for (int db = 0; db < HD / 32; ++db) o_acc[db] = f32x16{} + __builtin_nanf("");
+  }
+
+  // ---- the waves' results joined through LDS: O as [wave][row][HD] float,
+  // 16-byte chunk c of row r at c ^ r (and the row's chunks are a multiple of
+  // 16), max and sum beside.
+  const float lsum = l_run + xor32(l_run);
+  constexpr int kChunks = HD / 4;
+  __syncthreads();  // every wave is done with its V
+  if (qvalid) {
+    float* o_lds = sm.o[wave][l32];
+#pragma unroll
+    for (int db = 0; db < HD / 32; ++db)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 v = {o_acc[db][4 * j], o_acc[db][4 * j + 1], o_acc[db][4 * j + 2], o_acc[db][4 * j + 3]};
+        *reinterpret_cast<f32x4*>(o_lds + 4 * ((db * 8 + 2 * j + h) ^ (l32 & (kChunks - 1)))) = v;
+      }
+    if (h == 0) {
+      sm.ml[wave][l32][0] = m_run;
+      sm.ml[wave][l32][1] = lsum;
+    }
+  }
+  __syncthreads();
+  // 16 lanes take a row, 8 (or 4) of its dims each: 16 rows at a time.
+  constexpr int kPer = HD / 16;
+  const int col = lane % 16;
+  for (int r = wave * 4 + lane / 16; r < valid_rows; r += kFewWaves * 4) {
+    float mw[kFewWaves], lw[kFewWaves], M = kNoMax;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+      mw[w] = sm.ml[w][r][0];
+      lw[w] = sm.ml[w][r][1];
+      M = fmaxf(M, mw[w]);
+    }
+    float sum = 0.f, o[kPer] = {};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+      const float f = lw[w] > 0.f ? exp2_fast((mw[w] - M) * c) : 0.f;
+      sum += f * lw[w];
+#pragma unroll
+      for (int e = 0; e < kPer / 4; ++e) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(
+            &sm.o[w][r][4 * ((col * (kPer / 4) + e) ^ (r & (kChunks - 1)))]);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[4 * e + x] += f * v[x];
+      }
+    }
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    uint32_t out[kPer / 2];
+    uint16_t* dst;
+    if (final_out) {
+#pragma unroll
+      for (int e = 0; e < kPer / 2; ++e) out[e] = pack_bf16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
+      const int node = node_of(a, r);
+      dst = a.out + ((static_cast<int64_t>(b) * a.Nmax + node) * a.Hq + g * a.G + (r - node * a.G)) * HD;
+    } else {
+      float top = 0.f;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) top = fmaxf(top, fabsf(o[e]));
+      top = fmaxf(top, dpp<0xB1>(top));  // (over the row's 16 lanes, as in wave_reduce)
+      top = fmaxf(top, dpp<0x4E>(top));
+      top = fmaxf(top, dpp<0x141>(top));
+      top = fmaxf(top, dpp<0x140>(top)) * inv;
+      const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 14, 1), 253);  // (PartRow's factor)
+      const float down = inv * q8_scale(254 - ex);
+#pragma unroll
+      for (int e = 0; e < kPer / 2; ++e) out[e] = pack_f16x2(o[2 * e] * down, o[2 * e + 1] * down);
+      const int64_t row = static_cast<int64_t>(slot_id) * kFewRows + r;
+      dst = a.ws_o + row * kD;
+      if (col == 0) {
+        const f32x4 ml = {sum > 0.f ? M * c : -INFINITY, sum, q8_scale(ex), 0.f};
+        *reinterpret_cast<f32x4*>(a.ws_ml + row * 4) = ml;
+      }
+    }
+    if constexpr (kPer == 8)
+      *reinterpret_cast<u32x4*>(dst + col * 8) = (u32x4){out[0], out[1], out[2], out[3]};
+    else
+      *reinterpret_cast<uint2*>(dst + col * 4) = make_uint2(out[0], out[1]);
+  }
+}
+
 // ---- split plan (one sequence): grid = (b * Hkv + g, row tile, KV split).
 // Each (sequence, kv head, row tile) unit is cut into KV splits of
 // split_keys prefix keys; the tree's keys join the last split or take one of
@@ -1341,7 +1828,8 @@ __device__ __forceinline__ int merge_splits(const MfmaArgs& a, int b, int row) {
 // every split index below max_splits inside its splits.  (A second round for the
 // splits past 16 and reductions through the LDS crossbar made it 5.0 us instead
 // of 4.1 for 240 rows of 17 splits on 8 kv heads.)
-template <int HD, bool kEarly, bool kQ8>
+// kFew: the units and slots of attn_few_kernel.
+template <int HD, bool kEarly, bool kQ8, bool kFew = false>
 __global__ void __launch_bounds__(256) attn_split_merge_kernel(MfmaArgs a) {
   using Part = PartRow<kQ8>;
   using Ml = typename Part::Ml;
@@ -1357,12 +1845,18 @@ __global__ void __launch_bounds__(256) attn_split_merge_kernel(MfmaArgs a) {
   const int lane = threadIdx.x % kWave;
   const int grp = lane >> 4, col = lane & 15;  // split offset, 8-dim chunk
   const int Mpad = a.row_tiles * a.tile_rows;  // rows of a (sequence, kv head) unit set
-  const int64_t part0 = static_cast<int64_t>(bg) * a.max_splits * Mpad + row;
+  FewDesc few{0, 0};
+  if constexpr (kFew) {
+    few = reinterpret_cast<const FewDesc*>(a.ws_desc)[bg];
+    if (row >= a.G * a.n_nodes[b]) few.n_splits = 0;
+  }
+  const int64_t part0 =
+      (kFew ? static_cast<int64_t>(few.first) : static_cast<int64_t>(bg) * a.max_splits) * Mpad + row;
   const unsigned char* op = reinterpret_cast<const unsigned char*>(a.ws_o + part0 * kD) + col * 16;
   const int64_t stride = static_cast<int64_t>(Mpad) * kD * 2;  // bytes between splits
   int live = a.max_splits;  // splits whose partials are read
   if constexpr (!kEarly) {
-    live = merge_splits(a, b, row);
+    live = kFew ? few.n_splits : merge_splits(a, b, row);
     if (live <= 1) return;
   }
   Ml ml0 = {-INFINITY, 0.f};
@@ -1722,6 +2216,7 @@ __global__ void __launch_bounds__(256) attn_stream_merge_kernel(MfmaArgs a) {
 
 namespace {
 
+constexpr int kFewPerCu = 2;        // attn_few_kernel: workgroups per compute unit
 constexpr int kMinTilesPerWg = 2;   // a share shorter than this is mostly fixed cost
 constexpr int kWideMerge = 2048;    // stream merge: units from which a wave takes 16 rows
 
@@ -1812,6 +2307,50 @@ int64_t worst_split_key_cap(const AttnShape& s) {
 // batches of 32- to 220-row units.)
 bool two_key_groups(const AttnShape& s) { return s.Hq / s.Hkv * s.Nmax <= kTileRows / 4; }
 
+// Whether every unit of a call over an 8-bit cache has at most 32 rows
+// (attend_few).
+bool few_rows(const AttnShape& s) { return s.scale_rows > 0 && s.Hq / s.Hkv * s.Nmax <= kFewRows; }
+
+// Longest split few_find may come to: its block ids (16 rows a page at least)
+// and the tree's fit the LDS table, with room for the rounding to key tiles.
+constexpr int kFewCap = 7680;
+static_assert((kFewCap + 2 * kKT + kFewRows) / 16 + 2 <= kFewBlocks, "a split's block ids fit");
+
+// Shortest split: a block a wave, and few enough of them for the merge's table.
+int64_t few_min_keys(int64_t max_prefix) {
+  const int64_t keys = (max_prefix + kMaxMergeSplits - 25) / (kMaxMergeSplits - 24);
+  return std::max<int64_t>((keys + kKT - 1) / kKT * kKT, 32 * kFewWaves);
+}
+
+// The grid.  Up to a quarter as many units as workgroups that fit the card at
+// once: that many, so that all splits run side by side (16 sequences of 64/8
+// heads, 1024 to 8192 keys: 41.0 us, 43.3 in shorter ones).  With more units the
+// remainders of so few splits would leave compute units idle, and the splits
+// are cut into 4 a compute unit beyond the units, which the hardware deals out as
+// they end (in us, for a grid of 2, 3, 4 and 6 times the units: 256 units of 500
+// to 6000 keys 67 / 64 / 57 / 57, 384 of 2000 52 / 50 / 52 / 56, 512 of 200 to
+// 3000 62 / 57 / 58 / 65, 1024 of 100 to 1500 65 / 69 / 73 / 85).  More again
+// where a split would be longer than kFewCap.
+void plan_few(const AttnShape& s, int num_cus, AttnPlan* p) {
+  const int64_t units = static_cast<int64_t>(s.B) * s.Hkv;
+  const int64_t min_keys = few_min_keys(s.max_prefix);
+  const int64_t resident = static_cast<int64_t>(kFewPerCu) * num_cus;
+  const int64_t W = std::max(4 * units <= resident ? resident : units + 4 * num_cus,
+                             units * ((s.max_prefix + kFewCap - 1) / kFewCap + 1));
+  const int64_t most = units * std::max<int64_t>(1, (s.max_prefix + min_keys - 1) / min_keys);
+  p->mfma = true;
+  p->few = true;
+  p->stream = false;
+  p->split_keys = static_cast<int>(min_keys);
+  p->tile_rows = kFewRows;
+  p->row_tiles = 1;
+  p->max_splits = s.max_prefix > p->split_keys ? 2 : 1;  // (whether a unit can be cut at all)
+  p->few_width = static_cast<int>(W);
+  p->grid = static_cast<int>(std::min(W, most));
+  p->workspace_bytes =
+      static_cast<size_t>(p->grid) * kFewRows * part_row_bytes(s) + static_cast<size_t>(units) * sizeof(FewDesc);
+}
+
 // Estimated time of a split plan, in key tiles of a 256-row unit (about 2 us).
 // `tile` is the cost of one key tile for the plan's units (less with two key
 // groups).
@@ -1900,6 +2439,7 @@ void plan_split(const AttnShape& s, int num_cus, AttnPlan* p) {
 // the LDS table even with one-row blocks, and at most kMaxMergeSplits of them.
 bool mfma_supported(const AttnShape& s) {
   if (s.dtype != LTD_DTYPE_BF16 || (s.d != 128 && s.d != 64)) return false;
+  if (few_rows(s)) return few_min_keys(s.max_prefix) <= kFewCap;
   if (use_stream(s)) return true;
   const int64_t cap = worst_split_key_cap(s);
   return cap >= 2 * kKT && s.max_prefix <= cap * kMaxMergeSplits;
@@ -1918,7 +2458,9 @@ void plan_stream(const AttnShape& s, int num_cus, AttnPlan* p) {
 }
 
 void plan_mfma(const AttnShape& s, int num_cus, AttnPlan* p) {
-  if (use_stream(s))
+  if (few_rows(s))
+    plan_few(s, num_cus, p);
+  else if (use_stream(s))
     plan_stream(s, num_cus, p);
   else
     plan_split(s, num_cus, p);
@@ -1981,6 +2523,27 @@ hipError_t launch_attn_mfma(const AttnShape& s, const AttnPlan& p, const void* q
   a.lazy_gap = kLazyMax / a.scale_log2;
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   a.ws_o = static_cast<uint16_t*>(workspace);
+  if (p.few) {
+    a.split_keys = p.split_keys;
+    a.row_tiles = 1;
+    a.tile_rows = kFewRows;
+    a.W = p.few_width;
+    const size_t slots = static_cast<size_t>(p.grid) * kFewRows;
+    a.ws_ml = reinterpret_cast<float*>(ws + slots * kD * 2);
+    a.ws_desc = reinterpret_cast<MergeDesc*>(ws + slots * part_row_bytes(s));
+    const auto launch_few = [&](auto d) {
+      if (a.block_table)
+        hipLaunchKernelGGL((attn_few_kernel<d(), true>), dim3(p.grid), dim3(kFewThreads), 0, stream, a);
+      else
+        hipLaunchKernelGGL((attn_few_kernel<d(), false>), dim3(p.grid), dim3(kFewThreads), 0, stream, a);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess || p.max_splits == 1) return e;  // one split a unit: the output is final
+      hipLaunchKernelGGL((attn_split_merge_kernel<d(), false, true, true>),
+                         dim3(s.B * s.Hkv, (a.G * s.Nmax + 3) / 4), dim3(256), 0, stream, a);
+      return hipGetLastError();
+    };
+    return s.d == 64 ? launch_few(std::integral_constant<int, 64>{}) : launch_few(std::integral_constant<int, 128>{});
+  }
   if (!p.stream) {
     a.split_keys = p.split_keys;
     a.max_splits = p.max_splits;

@@ -235,3 +235,17 @@ def test_validation_reports_bad_data_and_writes_nothing():
     out = run(m, validate=True, status=status)
     assert int(status.cpu()[0]) == ltd.STATUS_BAD_PARENT
     assert (out == 7.0).all()
+
+
+@pytest.mark.parametrize("B, prefix, sizes, Hq, Hkv, d", [
+    (1, [5000], [4], 8, 1, 128), (70, None, None, 8, 8, 64), (130, None, None, 4, 4, 128), (3, [0, 0, 0], [1, 2, 3], 8, 1, 128),
+    (2, [9000, 1], [1, 4], 8, 1, 128), (5, [128, 129, 127, 64, 4000], [8, 1, 8, 3, 2], 4, 1, 64)])
+def test_short_units(B, prefix, sizes, Hq, Hkv, d):
+    """At most 32 stacked rows a unit, cut into splits of one length on the GPU: one sequence, more than 64 of them,
+    empty and very different prefixes, lengths around a split's."""
+    rng = np.random.default_rng(B)
+    prefix = prefix or [int(x) for x in rng.integers(0, 400, B)]
+    sizes = sizes or [int(x) for x in rng.integers(1, 9, B)]
+    m = make(B + d, B, Hq, Hkv, d, 16, prefix, sizes, 16)
+    check(m, run(m), label="short units")
+    check(m, run(m, max_prefix=40000), label="short units, loose bound")
