@@ -5,14 +5,18 @@
 // penalties read (ltd_token_counts).
 //
 // A workgroup takes a chunk of the vocabulary (16 tokens a thread) and a few
-// nodes of one sequence.  What the nodes share is set up once: which of a
-// thread's tokens have a count or a bias, and, per node, which draft tokens of
-// its root path lie in the chunk (a short list in LDS).  Then it streams the
-// nodes' rows, with the next node's logits in flight.  Most tokens are touched
-// by no rule and pass through.
+// nodes of one sequence, and sets up once what the nodes share: the tokens that a
+// count or a bias touches, and, per node, the draft tokens of its root path that
+// lie in the chunk.  Then it streams the nodes' rows in 16-byte groups, read
+// only where the mask allows one of their tokens, with the next node's on the
+// way.  Bound: HBM, 4 bytes read per logit and, when written, 4 more.
 //
-// Bound: HBM, 4 bytes read per logit (none for a group of 4 tokens that the
-// mask forbids) and, when written, 4 more.
+// Written rows: each thread applies the rules to its own tokens (single tokens
+// stored by the threads of a list left lines half written: 16 trees of 16 to 96
+// nodes, 128256 tokens, 620 us instead of DENSEUS).  Argmax: touched tokens
+// go into a list in LDS that all threads share out, so that the rules' arithmetic
+// (a division among it) runs for them alone, and the rest is one maximum.
+#include <algorithm>
 #include <type_traits>
 
 #include "ltd_device.hpp"
@@ -26,11 +30,14 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 // (a row starts at any multiple of 4 bytes; the hardware takes 16-byte accesses there)
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef i32x4 i32x4_any __attribute__((aligned(4)));
 
-constexpr int kVec = 4;           // 16-byte groups of a thread
-constexpr int kNodesMax = 8;      // nodes of a workgroup at most
+constexpr int kVec = 4;              // 16-byte groups of a thread
+constexpr int kNodesMax = 8;         // nodes of a workgroup at most
 constexpr int kAcceptChunk = 16384;  // the acceptance workspace's chunk
 constexpr uint32_t kPrompt = 0x80000000u;
+constexpr uint16_t kBiased = 0x8000;  // a list entry's bias flag, beside its offset in the chunk
 
 struct RuleArgs {
   const float* logits;
@@ -46,7 +53,7 @@ struct RuleArgs {
   float* out;                // written rows, or nullptr
   uint64_t* partial;         // argmax keys [B][Nmax][chunks], or nullptr
   const int32_t* status;
-  int Nmax, Voc, max_bias, chunks, nodes, groups;  // nodes a workgroup, node groups a sequence
+  int B, Nmax, Voc, max_bias, chunks, nodes, groups;  // nodes a workgroup, node groups a sequence
 };
 
 struct Penalty {
@@ -74,20 +81,26 @@ __device__ __forceinline__ uint64_t pack_key(float v, int idx) {
 // kArgmax: reduce to the chunk's argmax key; else write the row.  kInPlace: out
 // is logits, and groups of 4 that no rule touches are neither read nor written.
 template <int kThreads, bool kArgmax, bool kInPlace>
-__global__ void __launch_bounds__(kThreads) rules_kernel(RuleArgs a) {
+__global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleArgs a) {
   constexpr int kChunk = kThreads * 4 * kVec;
+  constexpr int kItems = 2;                 // list entries a thread
+  constexpr int kList = kArgmax ? kItems * kThreads : 1;  // tokens beyond stay with the thread that owns them
+  static_assert(kChunk <= kBiased, "offsets leave the flag's bit free");
   __shared__ int32_t par_s[LTD_MAX_NODES], tok_s[LTD_MAX_NODES];
-  __shared__ uint16_t path_s[kNodesMax][LTD_MAX_NODES];  // chunk offsets of the path's tokens
+  __shared__ uint16_t path_s[kNodesMax][LTD_MAX_NODES];  // chunk offsets of the root path's draft tokens
   __shared__ int path_len_s[kNodesMax];
   __shared__ int32_t bias_tok_s[LTD_MAX_BIAS];
   __shared__ float bias_val_s[LTD_MAX_BIAS];
-  __shared__ float bias_sum_s[LTD_MAX_BIAS];
-  __shared__ int bias_here_s;
+  __shared__ uint32_t biased_s[kChunk / 32];
+  __shared__ uint16_t list_off_s[kList];
+  __shared__ uint32_t list_cnt_s[kList];
+  __shared__ float bias_s[kChunk];  // a biased token's bias
+  __shared__ int list_n_s, twice_s;
   __shared__ unsigned long long best_s[kNodesMax];
-  const int chunk = blockIdx.x % a.chunks;
-  const int group = blockIdx.x / a.chunks;
-  const int b = group / a.groups;
-  const int i0 = group % a.groups * a.nodes;
+  const int chunk = static_cast<int>(blockIdx.x) % a.chunks;
+  const int group_id = static_cast<int>(blockIdx.x) / a.chunks;
+  const int b = group_id / a.groups;
+  const int i0 = group_id % a.groups * a.nodes;
   if (halted(a.status)) return;
   const int tid = threadIdx.x;
   const int n = min(a.n_nodes[b], a.Nmax);
@@ -97,167 +110,303 @@ __global__ void __launch_bounds__(kThreads) rules_kernel(RuleArgs a) {
   const int hi = min(a.Voc, lo + kChunk);
   const int64_t seq = static_cast<int64_t>(b) * a.Nmax;
   const int words = (a.Voc + 31) / 32;
+  const bool counted = a.penalties != nullptr;  // penalties act (and counts are read)
+  const int32_t* counts = counted && a.counts != nullptr ? a.counts + static_cast<int64_t>(b) * a.Voc : nullptr;
 
-  for (int j = tid; j < n; j += kThreads) {
-    par_s[j] = a.parents[seq + j];
-    tok_s[j] = a.tokens[seq + j];
+  // The tokens of group u that exist, and those of them that node i's mask allows.
+  auto group = [&](int u) { return lo + (u * kThreads + tid) * 4; };
+  auto inside = [&](int u) -> uint32_t {
+    const int v = group(u);
+    return v + 4 <= hi ? 0xFu : v < hi ? (1u << (hi - v)) - 1u : 0u;
+  };
+  auto load_mask = [&](int i, uint32_t(&ok)[kVec]) {
+#pragma unroll
+    for (int u = 0; u < kVec; ++u) {
+      const int v = group(u);
+      ok[u] = inside(u);
+      if (a.mask != nullptr && v < hi) ok[u] &= a.mask[(seq + i) * words + (v >> 5)] >> (v & 31);
+    }
+  };
+  // Node i's logits in the groups of which `want` has a token (-infinity elsewhere).
+  auto load_row = [&](int i, const uint32_t(&want)[kVec], f32x4(&x)[kVec]) {
+    const float* row = a.logits + (seq + i) * a.Voc;
+#pragma unroll
+    for (int u = 0; u < kVec; ++u) {
+      const int v = group(u);
+      x[u] = (f32x4){-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      if (want[u] == 0) continue;
+      if (v + 4 <= hi) {
+        x[u] = *reinterpret_cast<const f32x4_any*>(row + v);
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (v + c < hi) x[u][c] = row[v + c];
+      }
+    }
+  };
+  // ---- set up, with the first node's logits on the way
+  uint32_t ok[kVec];
+  f32x4 x[kVec];
+  load_mask(i0, ok);
+  if constexpr (!kInPlace) load_row(i0, ok, x);
+  int32_t cnt[kVec][4] = {};
+  if (counts != nullptr) {
+#pragma unroll
+    for (int u = 0; u < kVec; ++u) {
+      const int v = lo + (u * kThreads + tid) * 4;
+      if (v + 4 <= hi) {
+        const i32x4 x = *reinterpret_cast<const i32x4_any*>(counts + v);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) cnt[u][c] = x[c];
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (v + c < hi) cnt[u][c] = counts[v + c];
+      }
+    }
+  }
+  if (counted) {
+    for (int j = tid; j < n; j += kThreads) {
+      par_s[j] = a.parents[seq + j];
+      tok_s[j] = a.tokens[seq + j];
+    }
   }
   const int nb = a.max_bias > 0 ? min(max(a.n_bias[b], 0), a.max_bias) : 0;
   for (int j = tid; j < nb; j += kThreads) {
     bias_tok_s[j] = a.bias_tokens[static_cast<int64_t>(b) * a.max_bias + j];
     bias_val_s[j] = a.bias_values[static_cast<int64_t>(b) * a.max_bias + j];
   }
-  if (tid == 0) bias_here_s = 0;
+  for (int j = tid; j < kChunk / 32; j += kThreads) biased_s[j] = 0;
+  if (tid == 0) list_n_s = twice_s = 0;
   if (tid < kNodesMax) {
     path_len_s[tid] = 0;
     best_s[tid] = 0;
   }
   Penalty pen{1.f, 0.f, 0.f};
-  uint32_t cnt[kVec][4] = {};
-  if (a.penalties != nullptr) {
-    pen = Penalty{a.penalties[3 * b], a.penalties[3 * b + 1], a.penalties[3 * b + 2]};
-    if (a.counts != nullptr) {
-      const int32_t* row = a.counts + static_cast<int64_t>(b) * a.Voc;
-#pragma unroll
-      for (int u = 0; u < kVec; ++u)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int v = lo + (u * kThreads + tid) * 4 + c;
-          if (v < hi) cnt[u][c] = static_cast<uint32_t>(row[v]);
-        }
-    }
-  }
+  if (counted) pen = Penalty{a.penalties[3 * b], a.penalties[3 * b + 1], a.penalties[3 * b + 2]};
   __syncthreads();
-  // The first entry of each biased token in this chunk gets the sum of its
-  // entries, in list order.
   for (int j = tid; j < nb; j += kThreads) {
     const int t = bias_tok_s[j];
     if (t < lo || t >= hi) continue;
-    float sum = bias_val_s[j];
-    bool first = true;
-    for (int k = 0; k < nb; ++k)
-      if (bias_tok_s[k] == t && k != j) {
-        if (k < j) first = false;
-        else sum = sum + bias_val_s[k];
-      }
-    bias_sum_s[j] = sum;
-    if (first) bias_here_s = 1;
+    const int o = t - lo;
+    const uint32_t bit = 1u << (o & 31);
+    if (atomicOr(&biased_s[o >> 5], bit) & bit) twice_s = 1;
+    else bias_s[o] = bias_val_s[j];
   }
   // Root paths: one wave a node lists the draft tokens that lie in the chunk
   // (parents clamped below their child, so the walk ends whatever they hold).
-  if (a.penalties != nullptr) {
+  if (counted && tid % kWave == 0) {
     for (int k = tid / kWave; k < i1 - i0; k += kThreads / kWave) {
-      if (tid % kWave == 0) {
-        int len = 0;
-        for (int j = i0 + k; j > 0;) {
-          const int t = tok_s[j];
-          if (t >= lo && t < hi) path_s[k][len++] = static_cast<uint16_t>(t - lo);
-          j = min(max(par_s[j], 0), j - 1);
+      int len = 0;
+      for (int j = i0 + k; j > 0;) {
+        const int t = tok_s[j];
+        if (t >= lo && t < hi) path_s[k][len++] = static_cast<uint16_t>(t - lo);
+        j = min(max(par_s[j], 0), j - 1);
+      }
+      path_len_s[k] = len;
+    }
+  }
+  __syncthreads();
+  // A token listed more than once gets the sum of its entries, in list order,
+  // from the thread of its first.
+  if (twice_s) {
+    for (int j = tid; j < nb; j += kThreads) {
+      const int t = bias_tok_s[j];
+      if (t < lo || t >= hi) continue;
+      float sum = bias_val_s[j];
+      bool first = true;
+      for (int k = 0; k < nb; ++k) {
+        if (bias_tok_s[k] != t || k == j) continue;
+        if (k < j) first = false;
+        else sum = sum + bias_val_s[k];
+      }
+      if (first) bias_s[t - lo] = sum;
+    }
+  }
+  uint32_t touched = 0, kept = 0;  // of this thread's tokens (bit 4u + c): touched, and not in the list
+#pragma unroll
+  for (int u = 0; u < kVec; ++u) {
+    const int o = (u * kThreads + tid) * 4;
+    const uint32_t bits = (biased_s[o >> 5] >> (o & 31)) & 0xFu;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const bool biased = (bits >> c) & 1u;
+      if (cnt[u][c] == 0 && !biased) continue;
+      touched |= 1u << (4 * u + c);
+      if constexpr (kArgmax) {
+        const int at = atomicAdd(&list_n_s, 1);
+        if (at < kList) {
+          list_off_s[at] = static_cast<uint16_t>((o + c) | (biased ? kBiased : 0));
+          list_cnt_s[at] = static_cast<uint32_t>(cnt[u][c]);
+        } else {
+          kept |= 1u << (4 * u + c);
         }
-        path_len_s[k] = len;
+      }
+    }
+  }
+  // The root path's draft tokens among this thread's (bits as touched).
+  auto path_bits = [&](int i) {
+    uint32_t on_path = 0;
+    for (int k = 0; k < path_len_s[i - i0]; ++k) {
+      const int o = path_s[i - i0][k];
+      if ((o >> 2) % kThreads == tid) on_path |= 1u << ((o >> 2) / kThreads * 4 + (o & 3));
+    }
+    return on_path;
+  };
+  auto path_count = [&](int i, int o) {
+    uint32_t count = 0;
+    for (int k = 0; k < path_len_s[i - i0]; ++k) count += path_s[i - i0][k] == o ? 1u : 0u;
+    return count;
+  };
+
+  __syncthreads();
+  if constexpr (!kArgmax) {
+    for (int i = i0; i < i1; ++i) {
+      const uint32_t act = touched | path_bits(i);
+      uint32_t want[kVec];
+      if (kInPlace || i > i0) {
+        load_mask(i, ok);
+#pragma unroll
+        for (int u = 0; u < kVec; ++u)  // (in place: nothing to do where all is allowed and nothing touched)
+          want[u] = kInPlace && ok[u] == inside(u) && ((act >> (4 * u)) & 0xFu) == 0 ? 0u : ok[u];
+        load_row(i, want, x);
+      }
+      float* orow = a.out + (seq + i) * a.Voc;
+#pragma unroll
+      for (int u = 0; u < kVec; ++u) {
+        const int v = group(u);
+        const uint32_t in = inside(u);
+        if (in == 0 || (kInPlace && ok[u] == in && want[u] == 0)) continue;
+        const uint32_t mine = (act >> (4 * u)) & 0xFu;
+        if (mine != 0) {
+          const uint32_t bits = (biased_s[(v - lo) >> 5] >> ((v - lo) & 31)) & 0xFu;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            if (!((mine >> c) & 1u)) continue;
+            uint32_t count = static_cast<uint32_t>(cnt[u][c]);
+            if (path_len_s[i - i0] > 0) count += path_count(i, v - lo + c);
+            const bool biased = (bits >> c) & 1u;
+            x[u][c] = apply_rule(x[u][c], count, pen, biased, bias_s[v - lo + c]);
+          }
+        }
+        if (ok[u] != 0xFu) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (!((ok[u] >> c) & 1u)) x[u][c] = -INFINITY;
+        }
+        if (in == 0xFu) {
+          *reinterpret_cast<f32x4_any*>(orow + v) = x[u];
+        } else {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if ((in >> c) & 1u) orow[v + c] = x[u][c];
+        }
+      }
+    }
+    return;
+  }
+
+  const int n_list = min(list_n_s, kList);
+  // This thread's list entries, and their logits (and mask words) at a node.
+  auto load_items = [&](int i, float(&y)[kItems], uint32_t(&m)[kItems]) {
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      y[k] = 0.f;
+      m[k] = 0u;
+      const int at = k * kThreads + tid;
+      if (at < n_list) {
+        const int v = lo + (list_off_s[at] & (kBiased - 1));
+        y[k] = a.logits[(seq + i) * a.Voc + v];
+        m[k] = a.mask != nullptr ? a.mask[(seq + i) * words + (v >> 5)] >> (v & 31) : 1u;
+      }
+    }
+  };
+  uint32_t ok_next[kVec], want[kVec];
+  f32x4 x_next[kVec];
+  float y[kItems], y_next[kItems];
+  uint32_t m[kItems], m_next[kItems];
+  auto wanted = [&](const uint32_t(&allowed)[kVec]) {
+#pragma unroll
+    for (int u = 0; u < kVec; ++u) want[u] = allowed[u] & ~(touched >> (4 * u));
+  };
+  load_mask(min(i0 + 1, i1 - 1), ok_next);
+  load_items(i0, y, m);
+  for (int i = i0; i < i1; ++i) {
+    uint32_t ok_after[kVec];
+    if (i + 1 < i1) {  // the next node's logits, by its mask, and the mask of the one after it
+      wanted(ok_next);
+      load_row(i + 1, want, x_next);
+      load_items(i + 1, y_next, m_next);
+      load_mask(min(i + 2, i1 - 1), ok_after);
+    }
+    uint64_t best = 0;  // this thread's largest key, -infinity aside
+    auto take = [&](float r, int v) {
+      if (r > -INFINITY) {
+        const uint64_t key = pack_key(r, v);
+        best = key > best ? key : best;
+      }
+    };
+    const int len = path_len_s[i - i0];
+    const uint32_t on_path = len > 0 ? path_bits(i) : 0u;
+    const uint32_t sparse = touched | on_path;
+    float vm = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kVec; ++u) {
+      const uint32_t plain = ok[u] & ~(sparse >> (4 * u));
+      if (plain != 0xFu) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (!((plain >> c) & 1u)) x[u][c] = -INFINITY;
+      }
+      vm = fmaxf(vm, fmaxf(fmaxf(x[u].x, x[u].y), fmaxf(x[u].z, x[u].w)));
+    }
+    if (vm > -INFINITY) {  // the lowest index that holds the maximum
+      int bi = 0;
+#pragma unroll
+      for (int u = kVec - 1; u >= 0; --u)
+#pragma unroll
+        for (int c = 3; c >= 0; --c) bi = x[u][c] == vm ? group(u) + c : bi;
+      best = pack_key(vm, bi);
+    }
+    // the list's tokens, but for those of the path ...
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int at = k * kThreads + tid;
+      if (at >= n_list || !(m[k] & 1u)) continue;
+      const int o = list_off_s[at] & (kBiased - 1);
+      if (len > 0 && path_count(i, o) != 0) continue;
+      take(apply_rule(y[k], list_cnt_s[at], pen, (list_off_s[at] & kBiased) != 0, bias_s[o]), lo + o);
+    }
+    // ... which their owners take, with what the list has no room for
+    for (uint32_t left = kept | on_path; left != 0; left &= left - 1) {
+      const int s = __builtin_ctz(left);
+      const int o = ((s >> 2) * kThreads + tid) * 4 + (s & 3);
+      const int v = lo + o;
+      if (a.mask != nullptr && !((a.mask[(seq + i) * words + (v >> 5)] >> (v & 31)) & 1u)) continue;
+      const uint32_t count = (counts != nullptr ? static_cast<uint32_t>(counts[v]) : 0u) + path_count(i, o);
+      const bool biased = (biased_s[o >> 5] >> (o & 31)) & 1u;
+      take(apply_rule(a.logits[(seq + i) * a.Voc + v], count, pen, biased, bias_s[o]), v);
+    }
+    best = wave_max_u64(best, tid % kWave);
+    if (tid % kWave == 0) atomicMax(&best_s[i - i0], static_cast<unsigned long long>(best));
+    if (i + 1 < i1) {
+#pragma unroll
+      for (int u = 0; u < kVec; ++u) {
+        ok[u] = ok_next[u];
+        ok_next[u] = ok_after[u];
+        x[u] = x_next[u];
+      }
+#pragma unroll
+      for (int k = 0; k < kItems; ++k) {
+        y[k] = y_next[k];
+        m[k] = m_next[k];
       }
     }
   }
   __syncthreads();
-  float bias[kVec][4] = {};
-  uint32_t biased = 0;  // bit 4u + c
-  if (bias_here_s > 0) {
-    for (int j = 0; j < nb; ++j) {
-      const int o = bias_tok_s[j] - lo;
-      if (o < 0 || o >= hi - lo || ((o >> 2) % kThreads) != tid) continue;
-      const int slot = (o >> 2) / kThreads * 4 + (o & 3);
-      if ((biased >> slot) & 1u) continue;  // (its first entry holds the sum)
-      biased |= 1u << slot;
-      const float s = bias_sum_s[j];
-#pragma unroll
-      for (int u = 0; u < kVec; ++u)
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (slot == 4 * u + c) bias[u][c] = s;
-    }
-  }
-  uint32_t touched = biased;
-#pragma unroll
-  for (int u = 0; u < kVec; ++u)
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if (cnt[u][c] != 0) touched |= 1u << (4 * u + c);
-
-  for (int i = i0; i < i1; ++i) {
-    const float* row = a.logits + (seq + i) * a.Voc;
-    float* orow = kArgmax ? nullptr : a.out + (seq + i) * a.Voc;
-    // Draft tokens of the root path: extra counts, 8 bits a token (a path has
-    // at most 255 tokens below the root).
-    uint32_t extra[kVec] = {};
-    const int len = path_len_s[i - i0];
-    for (int k = 0; k < len; ++k) {
-      const int o = path_s[i - i0][k];
-      if (((o >> 2) % kThreads) == tid) {
-        const int u = (o >> 2) / kThreads;
-#pragma unroll
-        for (int w = 0; w < kVec; ++w)
-          if (w == u) extra[w] += 1u << (8 * (o & 3));
-      }
-    }
-    float vm = -INFINITY;
-    int bi = 0x7FFFFFFF;
-#pragma unroll
-    for (int u = 0; u < kVec; ++u) {
-      const int v = lo + (u * kThreads + tid) * 4;
-      if (v >= hi) continue;
-      uint32_t ok = 0xFu;
-      if (a.mask != nullptr) ok = (a.mask[(seq + i) * words + (v >> 5)] >> (v & 31)) & 0xFu;
-      const bool acts = ((touched >> (4 * u)) & 0xFu) != 0 || extra[u] != 0;
-      const bool full = v + 4 <= hi;
-      if (kInPlace && ok == 0xFu && !acts) continue;
-      float x[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) x[c] = -INFINITY;
-      if (ok != 0) {
-        if (full) {
-          const f32x4 y = *reinterpret_cast<const f32x4_any*>(row + v);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) x[c] = y[c];
-        } else {
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (v + c < hi) x[c] = row[v + c];
-        }
-        if (acts) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            x[c] = apply_rule(x[c], cnt[u][c] + ((extra[u] >> (8 * c)) & 0xFFu), pen,
-                              (biased >> (4 * u + c)) & 1u, bias[u][c]);
-        }
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (!((ok >> c) & 1u)) x[c] = -INFINITY;
-      }
-      if constexpr (kArgmax) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (v + c < hi && (x[c] > vm || bi == 0x7FFFFFFF)) {
-            vm = x[c];
-            bi = v + c;
-          }
-      } else if (full) {
-        *reinterpret_cast<f32x4_any*>(orow + v) = (f32x4){x[0], x[1], x[2], x[3]};
-      } else {
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (v + c < hi) orow[v + c] = x[c];
-      }
-    }
-    if constexpr (kArgmax) {
-      uint64_t best = bi == 0x7FFFFFFF ? 0 : pack_key(vm, bi);
-      best = wave_max_u64(best, tid % kWave);
-      if (tid % kWave == 0) atomicMax(&best_s[i - i0], static_cast<unsigned long long>(best));
-    }
-  }
-  if constexpr (kArgmax) {
-    __syncthreads();
-    if (tid < i1 - i0) a.partial[(seq + i0 + tid) * a.chunks + chunk] = best_s[tid];
-  }
+  // (no key: every token of the chunk is at -infinity, and its first one stands for it)
+  if (tid < i1 - i0)
+    a.partial[(seq + i0 + tid) * a.chunks + chunk] = best_s[tid] != 0 ? best_s[tid] : pack_key(-INFINITY, lo);
 }
 
 // ---- the table of occurrences
@@ -360,13 +509,18 @@ hipError_t launch_rules(const LogitRules& r, int B, int Nmax, int Voc, float* ou
   a.Nmax = Nmax;
   a.Voc = Voc;
   a.max_bias = r.max_bias;
-  a.nodes = 4;
-  a.groups = (Nmax + a.nodes - 1) / a.nodes;
+  a.B = B;
   const auto launch = [&](auto threads, auto argmax, auto in_place) {
     constexpr int kChunk = threads() * 4 * kVec;
     a.chunks = (Voc + kChunk - 1) / kChunk;
+    // As many nodes a workgroup as leave no more of them than fit the card at once.
+    const int64_t rows = static_cast<int64_t>(B) * Nmax * a.chunks;
+    const int64_t card = int64_t{256} * (1024 / threads());
+    a.nodes = static_cast<int>(std::min<int64_t>((rows + card - 1) / card, kNodesMax));
+    a.groups = (Nmax + a.nodes - 1) / a.nodes;
     hipLaunchKernelGGL((rules_kernel<threads(), argmax(), in_place()>),
-                       dim3(static_cast<unsigned>(a.chunks) * a.groups * B), dim3(threads()), 0, stream, a);
+                       dim3(static_cast<unsigned>(a.chunks) * a.groups * B),
+                       dim3(threads()), 0, stream, a);
   };
   using Large = std::integral_constant<int, 1024>;
   using Small = std::integral_constant<int, 256>;
