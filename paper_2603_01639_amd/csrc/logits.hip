@@ -113,42 +113,61 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
   const bool counted = a.penalties != nullptr;  // penalties act (and counts are read)
   const int32_t* counts = counted && a.counts != nullptr ? a.counts + static_cast<int64_t>(b) * a.Voc : nullptr;
 
-  // The tokens of group u that exist, and those of them that node i's mask allows.
+  // Bits 4u + c of a 16-bit set stand for token c of the thread's group u.  The
+  // tokens that exist; node i's mask words; and the tokens those allow.
   auto group = [&](int u) { return lo + (u * kThreads + tid) * 4; };
-  auto inside = [&](int u) -> uint32_t {
+  uint32_t exist = 0;
+#pragma unroll
+  for (int u = 0; u < kVec; ++u) {
     const int v = group(u);
-    return v + 4 <= hi ? 0xFu : v < hi ? (1u << (hi - v)) - 1u : 0u;
-  };
-  auto load_mask = [&](int i, uint32_t(&ok)[kVec]) {
+    exist |= (v + 4 <= hi ? 0xFu : v < hi ? (1u << (hi - v)) - 1u : 0u) << (4 * u);
+  }
+  auto load_mask = [&](int i, uint32_t(&w)[kVec]) {
 #pragma unroll
     for (int u = 0; u < kVec; ++u) {
-      const int v = group(u);
-      ok[u] = inside(u);
-      if (a.mask != nullptr && v < hi) ok[u] &= a.mask[(seq + i) * words + (v >> 5)] >> (v & 31);
+      w[u] = 0xFFFFFFFFu;
+      if (a.mask != nullptr && group(u) < hi) w[u] = a.mask[(seq + i) * words + (group(u) >> 5)];
     }
   };
-  // Node i's logits in the groups of which `want` has a token (-infinity elsewhere).
-  auto load_row = [&](int i, const uint32_t(&want)[kVec], f32x4(&x)[kVec]) {
+  auto allowed = [&](const uint32_t(&w)[kVec]) {
+    uint32_t ok = 0;
+#pragma unroll
+    for (int u = 0; u < kVec; ++u) ok |= ((w[u] >> (group(u) & 31)) & 0xFu) << (4 * u);
+    return ok & exist;
+  };
+  // A node on its way: its logits in the groups with a token in `want` (-infinity
+  // elsewhere), what its mask allows and, for the argmax, the logits and mask
+  // words of this thread's list entries.
+  struct Node {
+    f32x4 x[kVec];
+    uint32_t ok;
+    float y[kItems];
+    uint32_t m[kItems];
+  };
+  auto load_row = [&](int i, uint32_t want, Node& nd) {
     const float* row = a.logits + (seq + i) * a.Voc;
 #pragma unroll
     for (int u = 0; u < kVec; ++u) {
       const int v = group(u);
-      x[u] = (f32x4){-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-      if (want[u] == 0) continue;
+      nd.x[u] = (f32x4){-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      if (((want >> (4 * u)) & 0xFu) == 0) continue;
       if (v + 4 <= hi) {
-        x[u] = *reinterpret_cast<const f32x4_any*>(row + v);
+        nd.x[u] = *reinterpret_cast<const f32x4_any*>(row + v);
       } else {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-          if (v + c < hi) x[u][c] = row[v + c];
+          if (v + c < hi) nd.x[u][c] = row[v + c];
       }
     }
   };
+
   // ---- set up, with the first node's logits on the way
-  uint32_t ok[kVec];
-  f32x4 x[kVec];
-  load_mask(i0, ok);
-  if constexpr (!kInPlace) load_row(i0, ok, x);
+  Node na, nx;
+  uint32_t mw[kVec];
+  load_mask(i0, mw);
+  na.ok = allowed(mw);
+  if constexpr (!kInPlace) load_row(i0, na.ok, na);
+  load_mask(min(i0 + 1, i1 - 1), mw);
   int32_t cnt[kVec][4] = {};
   if (counts != nullptr) {
 #pragma unroll
@@ -260,85 +279,78 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
   };
 
   __syncthreads();
-  if constexpr (!kArgmax) {
-    for (int i = i0; i < i1; ++i) {
-      const uint32_t act = touched | path_bits(i);
-      uint32_t want[kVec];
-      if (kInPlace || i > i0) {
-        load_mask(i, ok);
-#pragma unroll
-        for (int u = 0; u < kVec; ++u)  // (in place: nothing to do where all is allowed and nothing touched)
-          want[u] = kInPlace && ok[u] == inside(u) && ((act >> (4 * u)) & 0xFu) == 0 ? 0u : ok[u];
-        load_row(i, want, x);
-      }
-      float* orow = a.out + (seq + i) * a.Voc;
-#pragma unroll
-      for (int u = 0; u < kVec; ++u) {
-        const int v = group(u);
-        const uint32_t in = inside(u);
-        if (in == 0 || (kInPlace && ok[u] == in && want[u] == 0)) continue;
-        const uint32_t mine = (act >> (4 * u)) & 0xFu;
-        if (mine != 0) {
-          const uint32_t bits = (biased_s[(v - lo) >> 5] >> ((v - lo) & 31)) & 0xFu;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (!((mine >> c) & 1u)) continue;
-            uint32_t count = static_cast<uint32_t>(cnt[u][c]);
-            if (path_len_s[i - i0] > 0) count += path_count(i, v - lo + c);
-            const bool biased = (bits >> c) & 1u;
-            x[u][c] = apply_rule(x[u][c], count, pen, biased, bias_s[v - lo + c]);
-          }
-        }
-        if (ok[u] != 0xFu) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (!((ok[u] >> c) & 1u)) x[u][c] = -INFINITY;
-        }
-        if (in == 0xFu) {
-          *reinterpret_cast<f32x4_any*>(orow + v) = x[u];
-        } else {
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if ((in >> c) & 1u) orow[v + c] = x[u][c];
-        }
-      }
-    }
-    return;
-  }
-
   const int n_list = min(list_n_s, kList);
-  // This thread's list entries, and their logits (and mask words) at a node.
-  auto load_items = [&](int i, float(&y)[kItems], uint32_t(&m)[kItems]) {
+  auto load_items = [&](int i, Node& nd) {
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
-      y[k] = 0.f;
-      m[k] = 0u;
+      nd.y[k] = 0.f;
+      nd.m[k] = 0u;
       const int at = k * kThreads + tid;
       if (at < n_list) {
         const int v = lo + (list_off_s[at] & (kBiased - 1));
-        y[k] = a.logits[(seq + i) * a.Voc + v];
-        m[k] = a.mask != nullptr ? a.mask[(seq + i) * words + (v >> 5)] >> (v & 31) : 1u;
+        nd.y[k] = a.logits[(seq + i) * a.Voc + v];
+        nd.m[k] = a.mask != nullptr ? a.mask[(seq + i) * words + (v >> 5)] >> (v & 31) : 1u;
       }
     }
   };
-  uint32_t ok_next[kVec], want[kVec];
-  f32x4 x_next[kVec];
-  float y[kItems], y_next[kItems];
-  uint32_t m[kItems], m_next[kItems];
-  auto wanted = [&](const uint32_t(&allowed)[kVec]) {
+  // The tokens whose logits node i needs, of those its mask allows: in place,
+  // groups with all tokens allowed and none touched need nothing; for the argmax
+  // touched tokens come by the list.
+  auto wanted = [&](int i, uint32_t ok) {
+    if constexpr (kArgmax) return ok & ~touched;
+    if constexpr (!kInPlace) return ok;
+    const uint32_t act = touched | path_bits(i);
+    uint32_t want = 0;
 #pragma unroll
-    for (int u = 0; u < kVec; ++u) want[u] = allowed[u] & ~(touched >> (4 * u));
-  };
-  load_mask(min(i0 + 1, i1 - 1), ok_next);
-  load_items(i0, y, m);
-  for (int i = i0; i < i1; ++i) {
-    uint32_t ok_after[kVec];
-    if (i + 1 < i1) {  // the next node's logits, by its mask, and the mask of the one after it
-      wanted(ok_next);
-      load_row(i + 1, want, x_next);
-      load_items(i + 1, y_next, m_next);
-      load_mask(min(i + 2, i1 - 1), ok_after);
+    for (int u = 0; u < kVec; ++u) {
+      const uint32_t g4 = 0xFu << (4 * u);
+      if ((ok & g4) != (exist & g4) || (act & g4) != 0) want |= ok & g4;
     }
+    return want;
+  };
+  auto fetch = [&](int i, Node& nd) {
+    load_row(i, wanted(i, nd.ok), nd);
+    if constexpr (kArgmax) load_items(i, nd);
+  };
+
+  auto write = [&](int i, Node& nd) {
+    const int len = path_len_s[i - i0];
+    const uint32_t act = touched | (len > 0 ? path_bits(i) : 0u);
+    float* orow = a.out + (seq + i) * a.Voc;
+#pragma unroll
+    for (int u = 0; u < kVec; ++u) {
+      const int v = group(u);
+      const uint32_t in = (exist >> (4 * u)) & 0xFu, ok = (nd.ok >> (4 * u)) & 0xFu, mine = (act >> (4 * u)) & 0xFu;
+      if (in == 0 || (kInPlace && ok == in && mine == 0)) continue;
+      if (mine != 0) {
+        const uint32_t bits = (biased_s[(v - lo) >> 5] >> ((v - lo) & 31)) & 0xFu;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          if (!((mine >> c) & 1u)) continue;
+          uint32_t count = static_cast<uint32_t>(cnt[u][c]);
+          if (len > 0) count += path_count(i, v - lo + c);
+          nd.x[u][c] = apply_rule(nd.x[u][c], count, pen, (bits >> c) & 1u, bias_s[v - lo + c]);
+        }
+      }
+      if (ok != 0xFu) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (!((ok >> c) & 1u)) nd.x[u][c] = -INFINITY;
+      }
+      if (in == 0xFu) {
+        *reinterpret_cast<f32x4_any*>(orow + v) = nd.x[u];
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if ((in >> c) & 1u) orow[v + c] = nd.x[u][c];
+      }
+    }
+  };
+
+  auto reduce = [&](int i, Node& nd) {
+    const int len = path_len_s[i - i0];
+    const uint32_t on_path = len > 0 ? path_bits(i) : 0u;
+    const uint32_t plain = nd.ok & ~(touched | on_path);
     uint64_t best = 0;  // this thread's largest key, -infinity aside
     auto take = [&](float r, int v) {
       if (r > -INFINITY) {
@@ -346,67 +358,72 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
         best = key > best ? key : best;
       }
     };
-    const int len = path_len_s[i - i0];
-    const uint32_t on_path = len > 0 ? path_bits(i) : 0u;
-    const uint32_t sparse = touched | on_path;
     float vm = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kVec; ++u) {
-      const uint32_t plain = ok[u] & ~(sparse >> (4 * u));
-      if (plain != 0xFu) {
+      if (((plain >> (4 * u)) & 0xFu) != 0xFu) {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-          if (!((plain >> c) & 1u)) x[u][c] = -INFINITY;
+          if (!((plain >> (4 * u + c)) & 1u)) nd.x[u][c] = -INFINITY;
       }
-      vm = fmaxf(vm, fmaxf(fmaxf(x[u].x, x[u].y), fmaxf(x[u].z, x[u].w)));
+      vm = fmaxf(vm, fmaxf(fmaxf(nd.x[u].x, nd.x[u].y), fmaxf(nd.x[u].z, nd.x[u].w)));
     }
     if (vm > -INFINITY) {  // the lowest index that holds the maximum
       int bi = 0;
 #pragma unroll
       for (int u = kVec - 1; u >= 0; --u)
 #pragma unroll
-        for (int c = 3; c >= 0; --c) bi = x[u][c] == vm ? group(u) + c : bi;
+        for (int c = 3; c >= 0; --c) bi = nd.x[u][c] == vm ? group(u) + c : bi;
       best = pack_key(vm, bi);
     }
     // the list's tokens, but for those of the path ...
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
       const int at = k * kThreads + tid;
-      if (at >= n_list || !(m[k] & 1u)) continue;
+      if (at >= n_list || !(nd.m[k] & 1u)) continue;
       const int o = list_off_s[at] & (kBiased - 1);
       if (len > 0 && path_count(i, o) != 0) continue;
-      take(apply_rule(y[k], list_cnt_s[at], pen, (list_off_s[at] & kBiased) != 0, bias_s[o]), lo + o);
+      take(apply_rule(nd.y[k], list_cnt_s[at], pen, (list_off_s[at] & kBiased) != 0, bias_s[o]), lo + o);
     }
     // ... which their owners take, with what the list has no room for
     for (uint32_t left = kept | on_path; left != 0; left &= left - 1) {
       const int s = __builtin_ctz(left);
       const int o = ((s >> 2) * kThreads + tid) * 4 + (s & 3);
       const int v = lo + o;
-      if (a.mask != nullptr && !((a.mask[(seq + i) * words + (v >> 5)] >> (v & 31)) & 1u)) continue;
+      if (!((nd.ok >> s) & 1u)) continue;
       const uint32_t count = (counts != nullptr ? static_cast<uint32_t>(counts[v]) : 0u) + path_count(i, o);
       const bool biased = (biased_s[o >> 5] >> (o & 31)) & 1u;
       take(apply_rule(a.logits[(seq + i) * a.Voc + v], count, pen, biased, bias_s[o]), v);
     }
-    best = wave_max_u64(best, tid % kWave);
-    if (tid % kWave == 0) atomicMax(&best_s[i - i0], static_cast<unsigned long long>(best));
+    uint32_t top;
+    const uint32_t at = wave_argmax(static_cast<uint32_t>(best >> 32), ~static_cast<uint32_t>(best), tid % kWave, &top);
+    if (tid % kWave == 0 && top != 0)
+      atomicMax(&best_s[i - i0], (static_cast<unsigned long long>(top) << 32) | static_cast<uint32_t>(~at));
+  };
+
+  // ---- the nodes, two sets of registers in turn: while one node is worked on,
+  // the next one's logits and the mask of the one after it are on the way
+  auto step = [&](int i, Node& cur, Node& next) {
     if (i + 1 < i1) {
-#pragma unroll
-      for (int u = 0; u < kVec; ++u) {
-        ok[u] = ok_next[u];
-        ok_next[u] = ok_after[u];
-        x[u] = x_next[u];
-      }
-#pragma unroll
-      for (int k = 0; k < kItems; ++k) {
-        y[k] = y_next[k];
-        m[k] = m_next[k];
-      }
+      next.ok = allowed(mw);
+      fetch(i + 1, next);
+      if (i + 2 < i1) load_mask(i + 2, mw);
     }
+    if constexpr (kArgmax) reduce(i, cur);
+    else write(i, cur);
+  };
+  if constexpr (kInPlace) fetch(i0, na);
+  if constexpr (kArgmax) load_items(i0, na);
+  for (int i = i0; i < i1; i += 2) {
+    step(i, na, nx);
+    if (i + 1 < i1) step(i + 1, nx, na);
   }
-  __syncthreads();
-  // (no key: every token of the chunk is at -infinity, and its first one stands for it)
-  if (tid < i1 - i0)
-    a.partial[(seq + i0 + tid) * a.chunks + chunk] = best_s[tid] != 0 ? best_s[tid] : pack_key(-INFINITY, lo);
+  if constexpr (kArgmax) {
+    __syncthreads();
+    // (no key: every token of the chunk is at -infinity, and its first one stands for it)
+    if (tid < i1 - i0)
+      a.partial[(seq + i0 + tid) * a.chunks + chunk] = best_s[tid] != 0 ? best_s[tid] : pack_key(-INFINITY, lo);
+  }
 }
 
 // ---- the table of occurrences
