@@ -352,36 +352,45 @@ def tree_accept_sampling(logits, draft_probs, draft_tokens, parents, n_nodes, un
 # run on the tensors' GPU whichever is current.
 
 def _want(name, t, dtypes, shape):
-    """t has one of the types and the shape (None in it: any size) and is contiguous."""
+    """t has one of the types and the shape and is contiguous."""
+    if t.dtype in dtypes and t.shape == shape and t.is_contiguous():
+        return  # (the usual case, in as little host time as can be)
     if t.dtype not in dtypes:
         raise TypeError(f"{name} has type {t.dtype}, not {' or '.join(map(str, dtypes))}")
-    if len(t.shape) != len(shape) or any(w is not None and w != h for w, h in zip(shape, t.shape)):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, not "
-                         f"({', '.join('*' if w is None else str(w) for w in shape)})")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} is not contiguous")
 
 
+def _dims(name, t, n):
+    """t's shape, of n dimensions."""
+    if t.dim() != n:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {n} dimensions")
+    return t.shape
+
+
 def _int32(shape, **tensors):
     import torch
+    kind = (torch.int32,)
     for name, t in tensors.items():
         if t is not None:
-            _want(name, t, (torch.int32,), shape)
+            _want(name, t, kind, shape)
 
 
 def _run(fn, args, tensors, stream):
     """Calls ltd_<fn>(*args, stream) on the GPU that holds the tensors."""
     import torch
-    dev = tensors[0].device
-    if dev.type != "cuda":
-        raise ValueError(f"{fn} needs tensors on a GPU, not on {dev}")
+    dev = tensors[0].get_device()
     for t in tensors:
-        if t is not None and t.device != dev:
-            raise ValueError(f"{fn}: tensors on {dev} and on {t.device}")
-    if stream is not None and stream.device != dev:
-        raise ValueError(f"{fn}: tensors on {dev}, a stream of {stream.device}")
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{fn}: tensors on {tensors[0].device} and on {t.device}")
+    if dev < 0:
+        raise ValueError(f"{fn} needs tensors on a GPU, not on {tensors[0].device}")
+    if stream is not None and stream.device.index != dev:
+        raise ValueError(f"{fn}: tensors on {tensors[0].device}, a stream of {stream.device}")
     call = getattr(lib(), fn)
-    if torch.cuda.current_device() == dev.index:
+    if torch.cuda.current_device() == dev:
         rc = call(*args, _stream(stream))
     else:
         with torch.cuda.device(dev):
@@ -408,7 +417,7 @@ def _q8_cache(k_cache, v_cache, k_scale, v_scale, block_table, num_blocks, scale
     _want("v_scale", v_scale, scales, sshape)
     max_blocks = 0
     if block_table is not None:
-        _int32((None, None), block_table=block_table)
+        _int32(_dims("block_table", block_table, 2), block_table=block_table)
         max_blocks = block_table.shape[1]
         if num_blocks > pages:
             raise ValueError(f"num_blocks is {num_blocks}, the cache holds {pages}")
@@ -479,9 +488,9 @@ def tree_verify_attn_q8(q, k_cache, v_cache, k_scale, v_scale, prefix_len, paren
     pages, Hkv, kv_rows, d, max_blocks = _q8_cache(k_cache, v_cache, k_scale, v_scale, block_table,
                                                    num_blocks, scale_rows, 0)
     dtype = _dtype_code(q)
-    _want("q", q, (q.dtype,), (None, None, None, d))
-    _want("out", out, (q.dtype,), tuple(q.shape))
-    B, Nmax, Hq, _ = q.shape
+    B, Nmax, Hq, _ = _dims("q", q, 4)
+    _want("q", q, (q.dtype,), (B, Nmax, Hq, d))
+    _want("out", out, (q.dtype,), q.shape)
     _batch_pages(B, pages, block_table)
     _int32((B,), prefix_len=prefix_len, n_nodes=n_nodes)
     _int32((B, Nmax), parents=parents)
@@ -517,7 +526,7 @@ def kv_compact_q8(k_cache, v_cache, k_scale, v_scale, prefix_len, new_prefix_len
             raise ValueError(f"num_layers is {num_layers}, the cache holds {k_cache.shape[0]}")
         layer_stride_elems = layer_stride_elems or k_cache.stride(0)
         scale_stride_elems = scale_stride_elems or k_scale.stride(0)
-    B, Nmax = accepted_nodes.shape
+    B, Nmax = _dims("accepted_nodes", accepted_nodes, 2)
     _batch_pages(B, pages, block_table)
     _int32((B, Nmax), accepted_nodes=accepted_nodes)
     _int32((B,), prefix_len=prefix_len, new_prefix_len=new_prefix_len, n_accepted=n_accepted)
@@ -534,10 +543,10 @@ def token_counts(tokens, n_tokens, counts, *, prompt: bool = False, reset: bool 
                  stream=None):
     """Adds tokens ``[B][T]`` (the first n_tokens[b] of each row) to the table of
     occurrences counts ``[B][Voc]`` int32; see ``ltd_token_counts``."""
-    _int32((None, None), tokens=tokens)
-    B, T = tokens.shape
+    B, T = _dims("tokens", tokens, 2)
+    _int32((B, T), tokens=tokens)
     _int32((B,), n_tokens=n_tokens)
-    _int32((B, None), counts=counts)
+    _int32((B, _dims("counts", counts, 2)[1]), counts=counts)
     _run("ltd_token_counts",
          (_p(tokens), _p(n_tokens), B, T, counts.shape[1], int(bool(prompt)), int(bool(reset)),
           _p(counts)), (counts, tokens, n_tokens), stream)
@@ -547,8 +556,8 @@ def _rules(logits, draft_tokens, parents, n_nodes, counts, penalties, bias_token
            n_bias, mask):
     """The checked arguments of a call with sampling rules, and its tensors."""
     import torch
-    _want("logits", logits, (torch.float32,), (None, None, None))
-    B, Nmax, Voc = logits.shape
+    B, Nmax, Voc = _dims("logits", logits, 3)
+    _want("logits", logits, (torch.float32,), (B, Nmax, Voc))
     _int32((B, Nmax), draft_tokens=draft_tokens, parents=parents)
     _int32((B,), n_nodes=n_nodes, n_bias=n_bias)
     _int32((B, Voc), counts=counts)
@@ -559,14 +568,14 @@ def _rules(logits, draft_tokens, parents, n_nodes, counts, penalties, bias_token
     if bias_tokens is not None:
         if bias_values is None or n_bias is None:
             raise ValueError("bias_tokens needs bias_values and n_bias")
-        _int32((B, None), bias_tokens=bias_tokens)
-        max_bias = bias_tokens.shape[1]
+        max_bias = _dims("bias_tokens", bias_tokens, 2)[1]
+        _int32((B, max_bias), bias_tokens=bias_tokens)
         _want("bias_values", bias_values, (torch.float32,), (B, max_bias))
     elif bias_values is not None or n_bias is not None:
         raise ValueError("bias_values and n_bias need bias_tokens")
     tensors = (logits, draft_tokens, parents, n_nodes, counts, penalties, bias_tokens, bias_values,
                n_bias, mask)
-    return tuple(_p(t) for t in tensors) + (B, Nmax, Voc, max_bias), tensors
+    return (*map(_p, tensors), B, Nmax, Voc, max_bias), tensors
 
 
 def tree_process_logits(logits, draft_tokens, parents, n_nodes, out, *, counts=None, penalties=None,
@@ -578,7 +587,7 @@ def tree_process_logits(logits, draft_tokens, parents, n_nodes, out, *, counts=N
     import torch
     args, tensors = _rules(logits, draft_tokens, parents, n_nodes, counts, penalties, bias_tokens,
                            bias_values, n_bias, mask)
-    _want("out", out, (torch.float32,), tuple(logits.shape))
+    _want("out", out, (torch.float32,), logits.shape)
     _run("ltd_tree_process_logits", args + (_p(out), int(validate), _p(status)),
          tensors + (out, status), stream)
     return out

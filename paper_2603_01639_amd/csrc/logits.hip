@@ -429,10 +429,41 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
 // ---- the table of occurrences
 
 constexpr int kCountThreads = 256;
+constexpr int kFreshChunk = 4096;  // tokens of a workgroup of the fresh table
 
-__global__ void __launch_bounds__(kCountThreads) counts_reset_kernel(int32_t* __restrict__ counts, int64_t total) {
-  const int64_t v = static_cast<int64_t>(blockIdx.x) * kCountThreads + threadIdx.x;
-  if (v < total) counts[v] = 0;
+// A table that starts anew: each workgroup counts the tokens of its chunk of the
+// vocabulary in LDS, from all of the sequence's, and writes the chunk once (one
+// launch instead of a clearing one and an adding one; 16 sequences of 4096
+// tokens and 128256 entries, with the counting of their outputs: FRESHUS).
+__global__ void __launch_bounds__(kCountThreads) counts_fresh_kernel(
+    const int32_t* __restrict__ tokens, const int32_t* __restrict__ n_tokens, int T, int Voc, int prompt,
+    int32_t* __restrict__ counts) {
+  __shared__ uint32_t count_s[kFreshChunk];
+  const int b = blockIdx.y;
+  const int lo = blockIdx.x * kFreshChunk;
+  const int size = min(kFreshChunk, Voc - lo);
+  for (int j = threadIdx.x; j < kFreshChunk; j += kCountThreads) count_s[j] = 0;
+  __syncthreads();
+  const int n = T > 0 ? min(n_tokens[b], T) : 0;
+  const int32_t* row = tokens + static_cast<int64_t>(b) * T;
+  constexpr int kAhead = 8;  // loads in flight a thread
+  for (int j0 = threadIdx.x; j0 < n; j0 += kAhead * kCountThreads) {
+    int t[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int j = j0 + u * kCountThreads;
+      t[u] = j < n ? row[j] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (t[u] < lo || t[u] >= lo + size) continue;
+      if (prompt) count_s[t[u] - lo] = kPrompt;  // (the same word from every thread)
+      else atomicAdd(&count_s[t[u] - lo], 1u);
+    }
+  }
+  __syncthreads();
+  int32_t* out = counts + static_cast<int64_t>(b) * Voc + lo;
+  for (int j = threadIdx.x; j < size; j += kCountThreads) out[j] = static_cast<int32_t>(count_s[j]);
 }
 
 // Integer atomics: the result does not depend on their order.
@@ -495,11 +526,9 @@ hipError_t launch_validate_rules(const int32_t* parents, const int32_t* n_nodes,
 hipError_t launch_token_counts(const int32_t* tokens, const int32_t* n_tokens, int B, int T, int Voc, bool prompt,
                                bool reset, int32_t* counts, hipStream_t stream) {
   if (reset) {
-    const int64_t total = static_cast<int64_t>(B) * Voc;
-    hipLaunchKernelGGL(counts_reset_kernel, dim3(static_cast<unsigned>((total + kCountThreads - 1) / kCountThreads)),
-                       dim3(kCountThreads), 0, stream, counts, total);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(counts_fresh_kernel, dim3((Voc + kFreshChunk - 1) / kFreshChunk, B), dim3(kCountThreads), 0,
+                       stream, tokens, n_tokens, T, Voc, prompt ? 1 : 0, counts);
+    return hipGetLastError();
   }
   if (T > 0)
     hipLaunchKernelGGL(counts_add_kernel, dim3((T + kCountThreads - 1) / kCountThreads, B), dim3(kCountThreads), 0,
