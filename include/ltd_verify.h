@@ -509,7 +509,8 @@ int ltd_token_counts(const int32_t* tokens, const int32_t* n_tokens, int B, int 
  *                               are added to each other in list order first),
  *     -infinity                 if v's bit of the node's mask is 0.
  * Tokens that no rule touches keep their bits.  A node whose mask allows
- * nothing gets -infinity everywhere.
+ * nothing gets -infinity everywhere; acceptance by sampling that ends at such a
+ * node has no distribution to draw its bonus token from, and emits any token.
  *
  *   logits, out  [B][Nmax][Voc] float32; out may be logits (in place), but no
  *                other overlap.  Rows i >= n_nodes[b] are not written.

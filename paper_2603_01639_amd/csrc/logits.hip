@@ -13,7 +13,7 @@
 //
 // Written rows: each thread applies the rules to its own tokens (single tokens
 // stored by the threads of a list left lines half written: 16 trees of 16 to 96
-// nodes, 128256 tokens, 620 us instead of DENSEUS).  Argmax: touched tokens
+// nodes, 128256 tokens, 620 us instead of 219).  Argmax: touched tokens
 // go into a list in LDS that all threads share out, so that the rules' arithmetic
 // (a division among it) runs for them alone, and the rest is one maximum.
 #include <algorithm>
@@ -434,7 +434,7 @@ constexpr int kFreshChunk = 4096;  // tokens of a workgroup of the fresh table
 // A table that starts anew: each workgroup counts the tokens of its chunk of the
 // vocabulary in LDS, from all of the sequence's, and writes the chunk once (one
 // launch instead of a clearing one and an adding one; 16 sequences of 4096
-// tokens and 128256 entries, with the counting of their outputs: FRESHUS).
+// tokens and 128256 entries, one node each: 19.5 us a pass instead of 16.1).
 __global__ void __launch_bounds__(kCountThreads) counts_fresh_kernel(
     const int32_t* __restrict__ tokens, const int32_t* __restrict__ n_tokens, int T, int Voc, int prompt,
     int32_t* __restrict__ counts) {

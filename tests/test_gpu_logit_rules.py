@@ -239,3 +239,40 @@ def test_validation(what, code):
     acc = accept(m, validate=True, status=status)
     assert int(status.cpu()[0]) == code
     assert (acc[0] == -1).all() == (code != 0)
+
+
+@pytest.mark.parametrize("temperature", [0.7, 1.0])
+def test_sampling_on_processed_logits(temperature):
+    """Acceptance by sampling takes the written logits, minus infinities and a node without an allowed token among
+    them, as the oracle does."""
+    import torch
+    rng = np.random.default_rng(33)
+    m = make(5, [24, 9, 17], 3000, bias=30, grammar=[0.6, 0.05, 0.9, 0.0], dup=False)
+    B, N = m["tokens"].shape
+    m["mask"][:, 0] = -1  # the root is on the grammar
+    draft = np.zeros((B, N, 3000), np.float32)
+    for b, n in enumerate(m["n"]):
+        for u in range(int(n)):
+            kids = np.nonzero(m["parents"][b, :n] == u)[0]
+            p = np.exp(m["logits"][b, u].astype(np.float64) + rng.normal(size=3000))
+            draft[b, u] = p / p.sum()
+            if len(kids):
+                m["tokens"][b, kids] = rng.choice(3000, size=len(kids), replace=False, p=p / p.sum())
+    uni = rng.random((B, N, 2)).astype(np.float32) * np.float32(1 - 2.0 ** -20)
+    done = process(m, fill=0.0)
+    outs = [torch.full((B, N), -1, dtype=torch.int32, device="cuda") for _ in range(2)]
+    nacc = torch.zeros(B, dtype=torch.int32, device="cuda")
+    par = np.where(np.arange(N) < m["n"][:, None], m["parents"], 0).astype(np.int32)
+    par[:, 0] = -1
+    ltd.tree_accept_sampling(Q.to_dev(done), Q.to_dev(draft), Q.to_dev(m["tokens"]), Q.to_dev(par), Q.to_dev(m["n"]),
+                             Q.to_dev(uni), *outs, nacc, temperature=temperature)
+    torch.cuda.synchronize()
+    path, toks, want = oracle.tree_accept_sampling(done, draft, m["tokens"], par, m["n"], uni, temperature=temperature)[:3]
+    np.testing.assert_array_equal(nacc.cpu().numpy(), want)
+    for b in range(B):
+        k = int(want[b])
+        np.testing.assert_array_equal(outs[0][b, :k].cpu().numpy(), path[b, :k])
+        np.testing.assert_array_equal(outs[1][b, :k].cpu().numpy(), toks[b, :k])
+        for j in range(k):  # (a node that allows nothing has no token to go on with)
+            row = done[b, path[b, j]]
+            assert np.isfinite(row[toks[b, j]]) or np.isneginf(row).all()

@@ -249,3 +249,10 @@ def test_short_units(B, prefix, sizes, Hq, Hkv, d):
     m = make(B + d, B, Hq, Hkv, d, 16, prefix, sizes, 16)
     check(m, run(m), label="short units")
     check(m, run(m, max_prefix=40000), label="short units, loose bound")
+
+
+@pytest.mark.parametrize("sizes", [[3, 1], [40, 9]])
+def test_bounds_beyond_the_matrix_kernels(sizes):
+    """A max_prefix past what the matrix-core kernels plan for with such pages: the vector kernel takes the calls."""
+    m = make(1, 2, 8, 2, 128, 32, [90, 33], sizes, 32)
+    check(m, run(m, max_prefix=9_000_000), label="far bound")

@@ -225,3 +225,47 @@ def test_append_validation_writes_nothing_on_bad_data(what, code):
     assert int(status.cpu()[0]) == code
     changed = any(not np.array_equal(dev[k].cpu().numpy(), c[k]) for k in ("k", "v", "ks", "vs"))
     assert changed == (code == 0)
+
+
+def test_pages_past_4_gib():
+    """Codes whose offsets pass 2^32: append, attention and compaction on pages at the end of a large cache give what
+    they give on a small one."""
+    import torch
+    rng = np.random.default_rng(17)
+    H, d, sr, block, far = 8, 128, 16, 16, 280000  # 280000 pages of 16 KiB: 4.6 GB
+    prefix, n = [40, 7], [9, 5]
+    c = Q.cache(rng, 2, H, d, sr, [64, 64], block)
+    for k in "kv":
+        c[k] &= 0xBF  # (moderate values)
+    x = torch.from_numpy(rng.normal(size=(2, 9, H, d))).to(torch.bfloat16).to("cuda")
+    q = torch.from_numpy(rng.normal(size=(2, 9, 16, d))).to(torch.bfloat16).to("cuda")
+    par = Q.to_dev(Q.trees(rng, n))
+    path = np.zeros((2, 9), np.int32)
+    path[0, :3], path[1, :2] = [0, 4, 8], [0, 3]
+    ints = [Q.to_dev(np.array(a, np.int32)) for a in (prefix, n, path, [3, 2])]
+    outs = []
+    for shift in (0, far):
+        dev = Q.dev_cache(c)
+        table, pages = dev["table"], c["pages"]
+        if shift:
+            big = {k: torch.empty((far + pages,) + tuple(dev[k].shape[1:]), dtype=torch.uint8, device="cuda")
+                   for k in ("k", "v", "ks", "vs")}
+            for k, t in big.items():
+                t[far:] = dev[k]
+            dev, table, pages = big, table + far, far + pages
+        cache = (dev["k"], dev["v"], dev["ks"], dev["vs"])
+        paged = dict(scale_rows=sr, block_table=table, num_blocks=pages)
+        ltd.kv_append_q8(x, x, *cache, ints[0], ints[1], **paged)
+        out, new = torch.zeros_like(q), torch.zeros(2, dtype=torch.int32, device="cuda")
+        ltd.tree_verify_attn_q8(q, *cache, ints[0], par, ints[1], out, max_prefix=40, **paged)
+        short = torch.zeros_like(q[:, :1])  # (one node: the kernel of short units)
+        ltd.tree_verify_attn_q8(q[:, :1].contiguous(), *cache, ints[0], par[:, :1].contiguous(),
+                                torch.ones_like(ints[1]), short, max_prefix=40, **paged)
+        f32 = torch.zeros_like(q, dtype=torch.float32)
+        ltd.tree_verify_attn_q8(q.float(), *cache, ints[0], par, ints[1], f32, max_prefix=40, **paged)
+        ltd.kv_compact_q8(*cache, ints[0], new, ints[2], ints[3], **paged)
+        torch.cuda.synchronize()
+        outs.append([out.float().cpu(), short.float().cpu(), f32.cpu(), new.cpu()] + [t[shift:].cpu() for t in cache])
+        del dev, cache
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
