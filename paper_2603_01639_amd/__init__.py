@@ -389,13 +389,15 @@ def _run(fn, args, tensors, stream):
         raise ValueError(f"{fn} needs tensors on a GPU, not on {tensors[0].device}")
     if stream is not None and stream.device.index != dev:
         raise ValueError(f"{fn}: tensors on {tensors[0].device}, a stream of {stream.device}")
+    handle = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
     call = getattr(lib(), fn)
     if torch.cuda.current_device() == dev:
-        rc = call(*args, _stream(stream))
+        rc = call(*args, handle)
     else:
         with torch.cuda.device(dev):
-            rc = call(*args, _stream(stream))
-    _check(fn, rc)
+            rc = call(*args, handle)
+    if rc != LTD_OK:
+        raise LtdError(fn, rc)
 
 
 def _q8_cache(k_cache, v_cache, k_scale, v_scale, block_table, num_blocks, scale_rows, lead):
@@ -464,7 +466,7 @@ def kv_append_q8(k_new, v_new, k_cache, v_cache, k_scale, v_scale, prefix_len, n
     if B == 0 or Nmax == 0:
         return
     stride = _row_stride("k_new", k_new)
-    if _row_stride("v_new", v_new) != stride:
+    if v_new.stride() != k_new.stride() and _row_stride("v_new", v_new) != stride:
         raise ValueError("k_new and v_new have rows of different strides")
     _run("ltd_kv_append_q8",
          (_p(k_new), _p(v_new), stride, _p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale),
