@@ -96,6 +96,7 @@ extern "C" {
 #define LTD_EXPAND_MAX_CHILDREN 256  /* F * W per round */
 
 #define LTD_MAX_BIAS 1024            /* biased tokens per sequence */
+#define LTD_MAX_LENGTH (1 << 30)     /* rows, tokens and vocabulary of the 8-bit cache's and the rules' calls */
 
 #define LTD_POLICY_SIZE 0          /* state [D, L, score of every pool candidate, pad ...] */
 #define LTD_POLICY_DEPTH 1         /* state [scores of the newest in_dim-2 candidates, D, L] */
@@ -402,8 +403,10 @@ int ltd_policy_forward(int layout, const float* scores, const int32_t* pool_size
  * code falls below the format's normal range.
  *   scale_rows  16, 32, 64 or 128; a paged cache's kv_rows is a multiple of it.
  *   d           64 or 128.
- * Anything else is LTD_EUNSUPPORTED.  Codes and rows passed to these calls are
- * 16-byte aligned (LTD_EINVAL otherwise).  Scale bytes of rows in use lie in
+ * Anything else is LTD_EUNSUPPORTED, as are more than LTD_MAX_LENGTH rows to
+ * append or max_prefix; logical rows end at LTD_MAX_LENGTH too, whatever the
+ * capacity.  Codes and rows passed to these calls are 16-byte aligned
+ * (LTD_EINVAL otherwise).  Scale bytes of rows in use lie in
  * [27, 214], as ltd_kv_append_q8 writes them: values of up to 2^96, so that
  * float32 sums of them under softmax weights stay finite.
  */
@@ -427,11 +430,11 @@ int ltd_policy_forward(int layout, const float* scores, const int32_t* pool_size
  *                 one row to the next (at least Hkv * d; rows may be views into
  *                 a fused projection's output); row i of sequence b starts at
  *                 (b * Nmax + i) * new_row_stride.  Each row is 16-byte aligned.
- *   n_rows        [B] int32 in [0, Nmax]; Nmax >= 1 has no upper limit here.
+ *   n_rows        [B] int32 in [0, Nmax]; Nmax may exceed LTD_MAX_NODES here.
  *   prefix_len    [B] int32 (read only).
  * No two sequences may append to the same block.  With validate != 0:
- * LTD_STATUS_BAD_NNODES (n_rows), LTD_STATUS_BAD_PREFIX (P_b < 0 or rows past
- * the capacity) and LTD_STATUS_BAD_BLOCK (ids of the blocks that are written).
+ * LTD_STATUS_BAD_NNODES (n_rows), LTD_STATUS_BAD_PREFIX (P_b < 0, or rows past
+ * the capacity or LTD_MAX_LENGTH) and LTD_STATUS_BAD_BLOCK (ids of the blocks that are written).
  */
 int ltd_kv_append_q8(const void* k_new, const void* v_new, int64_t new_row_stride, void* k_cache,
                      void* v_cache, uint8_t* k_scale, uint8_t* v_scale, const int32_t* block_table,
@@ -466,7 +469,8 @@ int ltd_tree_verify_attn_q8(const void* q, const void* k_cache, const void* v_ca
  * takes the largest of their scale bytes, and its own if it holds rows below
  * P_b; every row of it below P_b + n_accepted[b] whose scale byte was smaller is
  * encoded again (rounded to nearest even), others keep their codes.  Rows >=
- * P_b + n_accepted[b] stand for undefined values afterwards.
+ * P_b + n_accepted[b] stand for undefined values afterwards.  No two sequences
+ * may have the same block in rows >= P_b.
  *   layer_stride_elems  codes from one layer to the next (K and V);
  *   scale_stride_elems  scale bytes from one layer to the next; both > 0 with
  *                       more than one layer.
@@ -491,6 +495,7 @@ int ltd_kv_compact_q8(void* k_cache, void* v_cache, uint8_t* k_scale, uint8_t* v
  *             out_tokens and n_accepted of an acceptance call); prompt != 0: sets
  *             bit 31.
  *   reset     != 0: the table is zeroed first (a new request).
+ * T and Voc are at most LTD_MAX_LENGTH (LTD_EUNSUPPORTED).
  */
 int ltd_token_counts(const int32_t* tokens, const int32_t* n_tokens, int B, int T, int Voc,
                      int prompt, int reset, int32_t* counts, void* stream);
@@ -512,8 +517,9 @@ int ltd_token_counts(const int32_t* tokens, const int32_t* n_tokens, int B, int 
  * nothing gets -infinity everywhere; acceptance by sampling that ends at such a
  * node has no distribution to draw its bonus token from, and emits any token.
  *
- *   logits, out  [B][Nmax][Voc] float32; out may be logits (in place), but no
- *                other overlap.  Rows i >= n_nodes[b] are not written.
+ *   logits, out  [B][Nmax][Voc] float32; out may be logits (in place); any
+ *                other overlap is LTD_EINVAL, a Voc above
+ *                LTD_MAX_LENGTH LTD_EUNSUPPORTED.  Rows i >= n_nodes[b] are not written.
  *   draft_tokens [B][Nmax]; tokens outside [0, Voc) occur nowhere.
  *   counts       [B][Voc] as kept by ltd_token_counts, or NULL (all zero).
  *   penalties    [B][3] float32: repetition (> 0; 1 = none), frequency and

@@ -37,6 +37,7 @@ STATUS_BAD_RULE = 7
 
 MAX_NODES = 256
 MAX_BIAS = 1024
+MAX_LENGTH = 1 << 30
 MAX_POOL = 1024
 POLICY_SIZE = 0
 POLICY_DEPTH = 1
@@ -378,9 +379,30 @@ def _int32(shape, **tensors):
             _want(name, t, kind, shape)
 
 
-def _run(fn, args, tensors, stream):
-    """Calls ltd_<fn>(*args, stream) on the GPU that holds the tensors."""
+def _workspace_for(stream, nbytes, device):
+    """A workspace from the memory of the stream that will use it: of another
+    stream's, it could be handed out again while the call still runs."""
+    if stream is None:
+        return _alloc_workspace(nbytes, device)
     import torch
+    with torch.cuda.stream(stream):
+        return _alloc_workspace(nbytes, device)
+
+
+def _space(workspace):
+    """A workspace's pointer and bytes."""
+    if not workspace.is_contiguous():
+        raise ValueError("workspace is not contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _run(fn, args, tensors, stream):
+    """Calls fn(*args, stream) on the GPU that holds the tensors, the last of
+    which is the call's status."""
+    import torch
+    status = tensors[-1]
+    if status is not None and (status.dtype != torch.int32 or status.numel() < 1):
+        raise TypeError(f"status is {status.numel()} of {status.dtype}, not an int32")
     dev = tensors[0].get_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
@@ -499,13 +521,13 @@ def tree_verify_attn_q8(q, k_cache, v_cache, k_scale, v_scale, prefix_len, paren
     if scale is None:
         scale = d ** -0.5
     if workspace is None:
-        workspace = _alloc_workspace(attn_q8_workspace_size(B, Nmax, Hq, Hkv, d, max_prefix, dtype),
-                                     q.device)
+        workspace = _workspace_for(
+            stream, attn_q8_workspace_size(B, Nmax, Hq, Hkv, d, max_prefix, dtype), q.device)
     _run("ltd_tree_verify_attn_q8",
          (_p(q), _p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale), _p(block_table),
           _p(prefix_len), _p(parents), _p(n_nodes), _p(out), B, Nmax, Hq, Hkv, d, int(max_prefix),
           kv_rows, max_blocks, int(num_blocks), int(scale_rows), float(scale), dtype,
-          _p(workspace), workspace.numel() * workspace.element_size(), int(validate), _p(status)),
+          *_space(workspace), int(validate), _p(status)),
          (q, k_cache, v_cache, k_scale, v_scale, block_table, prefix_len, parents, n_nodes, out,
           workspace, status), stream)
     return out
@@ -513,21 +535,28 @@ def tree_verify_attn_q8(q, k_cache, v_cache, k_scale, v_scale, prefix_len, paren
 
 def kv_compact_q8(k_cache, v_cache, k_scale, v_scale, prefix_len, new_prefix_len, accepted_nodes,
                   n_accepted, *, scale_rows: int, block_table=None, num_blocks: int = 0,
-                  num_layers: int = 1, layer_stride_elems: int = 0, scale_stride_elems: int = 0,
+                  num_layers: Optional[int] = None, layer_stride_elems: int = 0, scale_stride_elems: int = 0,
                   validate: bool = False, status=None, stream=None):
     """In-place compaction of an 8-bit KV cache; see ``ltd_kv_compact_q8``.
     With a leading dimension of layers, caches ``[layers][pages][Hkv][rows][d]``
-    and scales alike, the strides default to the tensors' own."""
+    and scales alike, the strides default to the tensors' own and num_layers to
+    all of them."""
     lead = k_cache.dim() - 4
     if lead not in (0, 1):
         raise ValueError(f"k_cache has {k_cache.dim()} dimensions, not 4 or 5")
     pages, Hkv, kv_rows, d, max_blocks = _q8_cache(k_cache, v_cache, k_scale, v_scale, block_table,
                                                    num_blocks, scale_rows, lead)
+    if num_layers is None:
+        num_layers = k_cache.shape[0] if lead else 1
     if lead:
         if num_layers > k_cache.shape[0]:
             raise ValueError(f"num_layers is {num_layers}, the cache holds {k_cache.shape[0]}")
         layer_stride_elems = layer_stride_elems or k_cache.stride(0)
         scale_stride_elems = scale_stride_elems or k_scale.stride(0)
+        last = max(k_cache.shape[0] - 1, 0)
+        if ((num_layers - 1) * layer_stride_elems > last * k_cache.stride(0)
+                or (num_layers - 1) * scale_stride_elems > last * k_scale.stride(0)):
+            raise ValueError(f"{num_layers} layers at these strides pass the tensors' end")
     B, Nmax = _dims("accepted_nodes", accepted_nodes, 2)
     _batch_pages(B, pages, block_table)
     _int32((B, Nmax), accepted_nodes=accepted_nodes)
@@ -551,7 +580,7 @@ def token_counts(tokens, n_tokens, counts, *, prompt: bool = False, reset: bool 
     _int32((B, _dims("counts", counts, 2)[1]), counts=counts)
     _run("ltd_token_counts",
          (_p(tokens), _p(n_tokens), B, T, counts.shape[1], int(bool(prompt)), int(bool(reset)),
-          _p(counts)), (counts, tokens, n_tokens), stream)
+          _p(counts)), (counts, tokens, n_tokens, None), stream)
 
 
 def _rules(logits, draft_tokens, parents, n_nodes, counts, penalties, bias_tokens, bias_values,
@@ -607,8 +636,7 @@ def tree_accept_processed(logits, draft_tokens, parents, n_nodes, pred, accepted
     _int32((B, Nmax), pred=pred, accepted_nodes=accepted_nodes, out_tokens=out_tokens)
     _int32((B,), n_accepted=n_accepted)
     if workspace is None:
-        workspace = _alloc_workspace(accept_workspace_size(B, Nmax, Voc), logits.device)
+        workspace = _workspace_for(stream, accept_workspace_size(B, Nmax, Voc), logits.device)
     _run("ltd_tree_accept_processed",
-         args + (_p(pred), _p(accepted_nodes), _p(out_tokens), _p(n_accepted), _p(workspace),
-                 workspace.numel() * workspace.element_size(), int(validate), _p(status)),
+         args + (_p(pred), _p(accepted_nodes), _p(out_tokens), _p(n_accepted), *_space(workspace), int(validate), _p(status)),
          tensors + (pred, accepted_nodes, out_tokens, n_accepted, workspace, status), stream)

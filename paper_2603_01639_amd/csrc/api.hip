@@ -347,6 +347,7 @@ int ltd_kv_append_q8(const void* k_new, const void* v_new, int64_t new_row_strid
   if (dtype != LTD_DTYPE_F32 && dtype != LTD_DTYPE_BF16) return LTD_EUNSUPPORTED;
   if (!q8_supported(d, kv_rows, scale_rows, block_table != nullptr)) return LTD_EUNSUPPORTED;
   if (block_table && (max_blocks < 1 || num_blocks < 1)) return LTD_EINVAL;
+  if (Nmax > LTD_MAX_LENGTH) return LTD_EUNSUPPORTED;
   if (new_row_stride < static_cast<int64_t>(Hkv) * d) return LTD_EINVAL;
   if (validate && !status) return LTD_EINVAL;
   if (B == 0) return LTD_OK;
@@ -371,7 +372,9 @@ int ltd_kv_append_q8(const void* k_new, const void* v_new, int64_t new_row_strid
 
 size_t ltd_tree_verify_attn_q8_workspace_size(int B, int Nmax, int Hq, int Hkv, int d,
                                               int max_prefix, int dtype) {
-  if (!attn_args_ok(B, Nmax, Hq, Hkv, d, max_prefix, dtype) || !attn_supported(d, dtype)) return 0;
+  if (!attn_args_ok(B, Nmax, Hq, Hkv, d, max_prefix, dtype) || !attn_supported(d, dtype) ||
+      max_prefix > LTD_MAX_LENGTH)
+    return 0;
   // The largest need over the layouts, as for a 16-bit cache; an 8-bit one's
   // smallest blocks hold 16 rows.
   const int cus = device_cu_count();
@@ -393,7 +396,8 @@ int ltd_tree_verify_attn_q8(const void* q, const void* k_cache, const void* v_ca
                             void* stream) {
   if (!attn_args_ok(B, Nmax, Hq, Hkv, d, max_prefix, dtype) || kv_rows < 1) return LTD_EINVAL;
   if (!(scale > 0.f) || !std::isfinite(scale)) return LTD_EINVAL;
-  if (!attn_supported(d, dtype) || !q8_supported(d, kv_rows, scale_rows, block_table != nullptr))
+  if (!attn_supported(d, dtype) || !q8_supported(d, kv_rows, scale_rows, block_table != nullptr) ||
+      max_prefix > LTD_MAX_LENGTH)
     return LTD_EUNSUPPORTED;
   if (block_table && (max_blocks < 1 || num_blocks < 1)) return LTD_EINVAL;
   if (validate && !status) return LTD_EINVAL;
@@ -461,6 +465,7 @@ int ltd_kv_compact_q8(void* k_cache, void* v_cache, uint8_t* k_scale, uint8_t* v
 int ltd_token_counts(const int32_t* tokens, const int32_t* n_tokens, int B, int T, int Voc,
                      int prompt, int reset, int32_t* counts, void* stream) {
   if (B < 0 || T < 0 || Voc < 1) return LTD_EINVAL;
+  if (T > LTD_MAX_LENGTH || Voc > LTD_MAX_LENGTH) return LTD_EUNSUPPORTED;
   if (B == 0) return LTD_OK;
   if (!counts || (T > 0 && (!tokens || !n_tokens))) return LTD_EINVAL;
   if (ltd::launch_token_counts(tokens, n_tokens, B, T, Voc, prompt != 0, reset != 0, counts,
@@ -488,6 +493,7 @@ int ltd_tree_process_logits(const float* logits, const int32_t* draft_tokens,
   if (B < 0 || Nmax < 1 || Nmax > LTD_MAX_NODES || Voc < 1 || max_bias < 0 ||
       max_bias > LTD_MAX_BIAS)
     return LTD_EINVAL;
+  if (Voc > LTD_MAX_LENGTH) return LTD_EUNSUPPORTED;
   if (validate && !status) return LTD_EINVAL;
   if (B == 0) return LTD_OK;
   const ltd::LogitRules r{logits,      draft_tokens, parents, n_nodes, counts, penalties,
@@ -495,6 +501,10 @@ int ltd_tree_process_logits(const float* logits, const int32_t* draft_tokens,
   const int rc = rules_ok(r);
   if (rc != LTD_OK) return rc;
   if (!out) return LTD_EINVAL;
+  const uintptr_t in_at = reinterpret_cast<uintptr_t>(logits), out_at = reinterpret_cast<uintptr_t>(out);
+  if (in_at != out_at && (in_at < out_at ? out_at - in_at : in_at - out_at) / sizeof(float) <
+                             static_cast<uint64_t>(B) * Nmax * Voc)
+    return LTD_EINVAL;  // (a workgroup would read rows that another has written)
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (validate) {
     if (ltd::launch_validate_rules(parents, n_nodes, penalties, n_bias, B, Nmax, max_bias, status,
@@ -518,6 +528,7 @@ int ltd_tree_accept_processed(const float* logits, const int32_t* draft_tokens,
   if (B < 0 || Nmax < 1 || Nmax > LTD_MAX_NODES || Voc < 1 || max_bias < 0 ||
       max_bias > LTD_MAX_BIAS)
     return LTD_EINVAL;
+  if (Voc > LTD_MAX_LENGTH) return LTD_EUNSUPPORTED;
   if (validate && !status) return LTD_EINVAL;
   if (B == 0) return LTD_OK;
   const ltd::LogitRules r{logits,      draft_tokens, parents, n_nodes, counts, penalties,

@@ -259,8 +259,9 @@ __global__ void __launch_bounds__(kThreads) validate_append_kernel(
   __syncthreads();
   for (int b = threadIdx.x; b < B; b += kThreads) {
     const int n = n_rows[b], P = prefix_len[b];
-    const int64_t capacity =
-        block_table ? static_cast<int64_t>(kv_rows) * max_blocks : static_cast<int64_t>(kv_rows);
+    const int64_t capacity = min(
+        block_table ? static_cast<int64_t>(kv_rows) * max_blocks : static_cast<int64_t>(kv_rows),
+        static_cast<int64_t>(LTD_MAX_LENGTH));
     int code = 0;
     if (n < 0 || n > Nmax) {
       code = LTD_STATUS_BAD_NNODES;

@@ -160,3 +160,67 @@ def test_cycles(graph):
                     got = Q.values(dict(c, **{w: gk[x], w + "s": gs[x]}), w, c["table"], SR)(b, rows)
                     want = Q.values({w: ref[w][x], w + "s": ref[w + "s"][x]}, w, c["table"], SR)(b, rows)
                     np.testing.assert_array_equal(got, want)
+
+
+def test_two_streams_at_once(monkeypatch):
+    """Two cycles' reads side by side on streams of their own, given by argument, with workspaces the calls take: each comes
+    from its stream's memory, and the results are those of the calls one after the other."""
+    import torch
+    rng = np.random.default_rng(43)
+    P = [1500, 1024]
+    c = Q.cache(rng, B, Hkv, d, SR, [p + N for p in P], BLOCK)
+    dev = Q.dev_cache(c)
+    prefix, sizes = Q.to_dev(np.array(P, np.int32)), [N, 5]
+    n, par = Q.to_dev(np.array(sizes, np.int32)), Q.to_dev(Q.trees(rng, sizes))
+    tok = Q.to_dev(rng.integers(0, VOC, (B, N)).astype(np.int32))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    q = [torch.from_numpy(rng.normal(size=(B, N, Hq, d))).to(torch.bfloat16).to("cuda") for _ in streams]
+    lg = [torch.from_numpy(rng.normal(size=(B, N, VOC)).astype(np.float32)).to("cuda") for _ in streams]
+    took = []
+    alloc = ltd._alloc_workspace
+    monkeypatch.setattr(ltd, "_alloc_workspace", lambda *a: took.append(torch.cuda.current_stream()) or alloc(*a))
+
+    def read(k, stream):
+        out = torch.zeros_like(q[k])
+        got = [torch.zeros((B, N), **i32) for _ in range(3)] + [torch.zeros(B, **i32)]
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+        ltd.tree_verify_attn_q8(q[k], dev["k"], dev["v"], dev["ks"], dev["vs"], prefix, par, n, out, max_prefix=1500,
+                                scale_rows=SR, block_table=dev["table"], num_blocks=c["pages"], stream=stream)
+        ltd.tree_accept_processed(lg[k], tok, par, n, *got, stream=stream)
+        return [out] + got
+
+    want = [read(k, None) for k in range(2)]
+    torch.cuda.synchronize()
+    took.clear()
+    got = [read(k, streams[k]) for k in range(2)]
+    assert took == [streams[0], streams[0], streams[1], streams[1]]
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        for x, y in zip(a, b):
+            torch.testing.assert_close(x, y, rtol=0, atol=0)
+
+
+def test_compaction_of_all_layers_by_default():
+    """A cache with a leading dimension of layers, num_layers left out: every layer moves."""
+    import torch
+    rng = np.random.default_rng(44)
+    P, path, nacc = [30, 3], np.tile(np.arange(N, dtype=np.int32), (B, 1)), np.array([3, 2], np.int32)
+    path[0, :3], path[1, :2] = [0, 4, 9], [0, 7]
+    c = Q.cache(rng, B, Hkv, d, SR, [p + N for p in P], BLOCK, layers=3)
+    dev = Q.dev_cache(c)
+    prefix = np.array(P, np.int32)
+    new = torch.zeros(B, dtype=torch.int32, device="cuda")
+    ltd.kv_compact_q8(dev["k"], dev["v"], dev["ks"], dev["vs"], Q.to_dev(prefix), new, Q.to_dev(path), Q.to_dev(nacc),
+                      scale_rows=SR, block_table=dev["table"], num_blocks=c["pages"])
+    assert new.tolist() == [33, 5]
+    for w in "kv":
+        gk, gs = dev[w].cpu().numpy(), dev[w + "s"].cpu().numpy()
+        for x in range(3):
+            ref = {w: c[w][x].copy(), w + "s": c[w + "s"][x].copy()}
+            Q.compact(ref[w], ref[w + "s"], c["table"], prefix, path, nacc, SR)
+            for b in range(B):
+                rows = np.arange(prefix[b] + nacc[b])
+                np.testing.assert_array_equal(Q.values({w: gk[x], w + "s": gs[x]}, w, c["table"], SR)(b, rows),
+                                              Q.values(ref, w, c["table"], SR)(b, rows))

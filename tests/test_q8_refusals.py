@@ -202,6 +202,44 @@ def test_binding_rules():
         ltd.tree_accept_processed(lg, t, t, i, i, t, t, i)
 
 
+def test_lengths_past_the_limit():
+    """Rows, tokens and vocabularies whose last index, rounded up to a block or a chunk, would pass 32 bits."""
+    top = ltd.MAX_LENGTH
+    assert append(N=top + 1) == NO and append(N=2**31 - 1) == NO
+    assert attn(mp=top + 1, rows=2**31 - 1) == NO and attn(mp=2**31 - 1, rows=2**31 - 1) == NO
+    assert ltd.attn_q8_workspace_size(1, 60, 32, 8, 128, 2**31 - 1, ltd.DTYPE_BF16) == 0
+    for call in (process, accept):
+        assert call(V=top + 1) == NO and call(V=2**31 - 1) == NO
+    counts = FN().ltd_token_counts
+    assert counts(X, X, 1, top + 1, 100, 0, 0, X, None) == NO
+    assert counts(X, X, 1, 4, 2**31 - 1, 0, 1, X, None) == NO
+
+
+@pytest.mark.parametrize("off", [4, 100 * 4, 399 * 4, -4, -399 * 4])
+def test_overlapping_output(off):
+    """1 x 4 nodes of 100 tokens are 1600 bytes: an output that begins inside them, or reaches into them."""
+    assert process(lg=X, out=X + off) == BAD
+
+
+def test_binding_status_strides_and_workspace():
+    import torch
+    c = {k: torch.stack([v] * 3) for k, v in _cache(torch).items()}
+    i, path = torch.zeros(2, dtype=torch.int32), torch.zeros((2, 4), dtype=torch.int32)
+    move = lambda **kw: ltd.kv_compact_q8(c["k"], c["v"], c["ks"], c["vs"], i, i.clone(), path, i, scale_rows=16, **kw)  # noqa: E731
+    for kw in (dict(layer_stride_elems=8193), dict(scale_stride_elems=9), dict(num_layers=2, layer_stride_elems=16385)):
+        with pytest.raises(ValueError, match="pass the tensors' end"):
+            move(**kw)
+    for kw in ({}, dict(num_layers=2), dict(num_layers=2, layer_stride_elems=16384)):
+        with pytest.raises(ValueError, match="on a GPU"):
+            move(**kw)
+    for status in (torch.zeros(1), torch.zeros(1, dtype=torch.uint8), torch.zeros(0, dtype=torch.int32)):
+        with pytest.raises(TypeError, match="status"):
+            move(validate=True, status=status)
+    lg, t = torch.zeros((2, 3, 100)), torch.zeros((2, 3), dtype=torch.int32)
+    with pytest.raises(ValueError, match="workspace"):
+        ltd.tree_accept_processed(lg, t, t, i, t, t, t, i, workspace=torch.zeros(4096, dtype=torch.uint8)[::2])
+
+
 def test_the_reference_rounds_as_the_format_does():
     """The test's own encoder against torch's conversion, and its decoder against torch's values."""
     import numpy as np
