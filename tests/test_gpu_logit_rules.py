@@ -276,3 +276,22 @@ def test_sampling_on_processed_logits(temperature):
         for j in range(k):  # (a node that allows nothing has no token to go on with)
             row = done[b, path[b, j]]
             assert np.isfinite(row[toks[b, j]]) or np.isneginf(row).all()
+
+
+@pytest.mark.parametrize("voc", [100, 5003])
+def test_masked_logits_and_banned_tokens(voc):
+    """NaN and infinities where the mask forbids a token, rules or not, change nothing; a bias of -infinity bans its token."""
+    m = make(voc, [9, 20], voc, bias=30, grammar=[0.6, 0.02], nmax=24)
+    m["bias"][1][:, 1::7] = -np.inf
+    keep = np.unpackbits(m["mask"].view(np.uint8), axis=-1, bitorder="little").reshape(2, 24, -1)[..., :voc].astype(bool)
+    dirty = dict(m, logits=np.where(keep, m["logits"], np.resize(np.array([np.nan, np.inf, -np.inf], np.float32),
+                                                                 m["logits"].shape)))
+    for in_place in (False, True):
+        for b, n in enumerate(m["n"]):
+            np.testing.assert_array_equal(process(dirty, in_place)[b, :n], process(m, in_place)[b, :n])
+    got = process(dirty)
+    assert all((got[b, i][~keep[b, i]] == -np.inf).all() for b, n in enumerate(m["n"]) for i in range(n))
+    banned = [m["bias"][0][b, 1] for b in range(2)]
+    assert all((got[b, :n, banned[b]] == -np.inf).all() for b, n in enumerate(m["n"]) if m["bias"][2][b] > 1)
+    for x, y in zip(accept(dirty), accept(m)):
+        np.testing.assert_array_equal(x, y)
