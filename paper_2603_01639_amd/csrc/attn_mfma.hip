@@ -47,6 +47,16 @@
 // and the contractions run over the first 64 dims only: 4 k-steps for S^T and
 // 2 dim blocks for O^T, half the MFMAs of a tile.  Partial results keep the
 // 128-dim row pitch in the workspace.
+//
+// An 8-bit cache (kQ8; codes and scale bytes as in q8.hpp) goes through the same
+// tiles: each thread loads 16 codes of K and of V two tiles ahead into registers
+// and widens them to bf16 into the tile's slot, an exact step, so that what
+// follows is unchanged.  Long prefixes and full row tiles are bound by the tile
+// loop as before (16 sequences of 64/8 heads over 1024 to 8192 keys, 16 to 128
+// nodes: 225 us a call against 221 over a 16-bit cache; one of 32/8 heads over
+// 16384 keys, 60 nodes: 28.0 against 27.6).  Units of at most 32 rows, which the
+// bytes of the cache bound, take a kernel of their own (attn_few_kernel: the same
+// 16 sequences decoding one token 41.9 us against 63.5).
 #include <algorithm>
 #include <cstddef>
 #include <type_traits>
@@ -124,12 +134,12 @@ struct MfmaArgs {
   // the tree may take a split of its own, row tiles per (sequence, kv head)
   int split_keys, max_splits, tree_alone, row_tiles;
   int tile_rows;  // stacked rows per unit
+  float scale_log2;
+  float lazy_gap;  // kLazyMax / scale_log2: the raw-score margin of the lazy max
   // 8-bit cache: scale bytes, scale bytes per page and kv head, log2(scale_rows)
   const uint8_t* ks;
   const uint8_t* vs;
   int scale_per_page, scale_shift;
-  float scale_log2;
-  float lazy_gap;  // kLazyMax / scale_log2: the raw-score margin of the lazy max
 };
 
 // Node of stacked row r: r / G, by a multiplication.  With G <= 2^shift and
@@ -312,10 +322,10 @@ __device__ __forceinline__ void q8_to_bf16(const u32x4& codes, uint32_t byte, u3
 // How a piece's rows are stored until they are merged: O / l in bf16 or, for an
 // 8-bit cache, in fp16 under a power of two that brings the row's largest
 // value to [2^14, 2^15), beside max and sum.  Same bytes but for that factor,
-// and an error of 2^-11 of a value instead of 2^-8 (2-norm of the output's
-// error, 16 sequences over 1024 to 8192 keys: 2.5e-3 with bf16 pieces, 1.7e-3
-// with these, 1.6e-3 from the output's own rounding).  V's scales span 2^187,
-// hence a factor for each row.
+// and off by at most 2^-11 of a value instead of 2^-8 (2-norm of the output's
+// error, 16 sequences over 1024 to 8192 keys: 2.5e-3 of the output's with bf16
+// pieces, 1.8e-3 to 2.0e-3 with these, 1.6e-3 by the output's own rounding).
+// V's scales span 2^187, hence a factor for each row.
 template <bool kQ8>
 struct PartRow;
 template <>
@@ -1298,14 +1308,15 @@ __device__ __forceinline__ int stream_index(int w, int W) { return (w % 8) * (W 
 // cut into splits of one length, the tree's keys joining the last, one for a
 // workgroup of four waves; two workgroups share a compute unit.  The length is
 // worked out on the GPU from the call's own lengths (few_find): the shortest for
-// which the splits fit the grid, so that all run at once and the longest
-// holds no more than its share, whatever max_prefix is.  Every wave takes all of the unit's rows and its own
-// 32-key blocks (block i: wave i mod 4), from loads to P.V, with no barrier until
-// the waves' results are joined.  Its blocks move straight into two slots of
-// LDS of its own, refilled as soon as they are read: 8 to 16 KiB requested per
-// wave, 64 to 128 per compute unit (with the next block in registers, which
-// are free only part of a block's time, 16 sequences of 1024 to 8192 keys took
-// 44.6 us instead of 42.2).
+// which the splits fit the grid, so that all run at once and the longest holds
+// no more than its share, whatever max_prefix is.  Every wave takes all of the
+// unit's rows and its own 32-key blocks (block i: wave i mod 4), from loads to
+// P.V, with no barrier until the waves' results are joined.  Its blocks move
+// straight into two slots of LDS of its own, refilled as soon as they are read:
+// 8 to 16 KiB requested per wave, 64 to 128 per compute unit (with the next
+// block in registers, which are free only part of a block's time, 16 sequences
+// of 1024 to 8192 keys, 64/8 heads, one node: 44.6 us a call instead of 42.2; of
+// now 41.9 the kernel takes 35, 146 MB at 4.2 TB/s, and the merge 4).
 //
 // K lies in LDS as the S^T operand takes it: lane l finds the codes of key
 // sigma(l & 31), 16 dims in every 32, where its own load put them (Q's fragments
