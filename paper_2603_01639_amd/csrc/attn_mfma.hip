@@ -56,7 +56,7 @@
 // nodes: 225 us a call against 221 over a 16-bit cache; one of 32/8 heads over
 // 16384 keys, 60 nodes: 28.0 against 27.6).  Units of at most 32 rows, which the
 // bytes of the cache bound, take a kernel of their own (attn_few_kernel: the same
-// 16 sequences decoding one token 41.9 us against 63.5).
+// 16 sequences decoding one token 39.5 us against 64).
 #include <algorithm>
 #include <cstddef>
 #include <type_traits>
@@ -1316,7 +1316,7 @@ __device__ __forceinline__ int stream_index(int w, int W) { return (w % 8) * (W 
 // 8 to 16 KiB requested per wave, 64 to 128 per compute unit (with the next
 // block in registers, which are free only part of a block's time, 16 sequences
 // of 1024 to 8192 keys, 64/8 heads, one node: 44.6 us a call instead of 42.2; of
-// now 41.9 the kernel takes 35, 146 MB at 4.2 TB/s, and the merge 4).
+// now 39.5 the kernel takes 33, 146 MB at 4.4 TB/s, and the merge 4).
 //
 // K lies in LDS as the S^T operand takes it: lane l finds the codes of key
 // sigma(l & 31), 16 dims in every 32, where its own load put them (Q's fragments
@@ -1362,8 +1362,12 @@ struct FewWork {
 
 // The split length is ceil(T Hkv / (W - B Hkv)) for T prefix keys in all and a
 // grid of W > B Hkv workgroups, rounded up to a key tile, at least a block a
-// wave: the splits then number at most T Hkv / length + B Hkv <= W.  Every
-// wave works it out on its own (lane l holds sequence c * 64 + l of chunk c).
+// wave: the splits then number at most T Hkv / length + B Hkv <= W.  Where all
+// of them run at once, the longest split is what the call takes, and a binary
+// search finds the shortest length that fits (16 sequences of 1024 to 8192 keys,
+// 64/8 heads: 1280 to 1536 keys instead of 1472 to 1792, 39.5 us a call instead of
+// 42.0).  Every wave works it out on its own (lane l holds sequence c * 64 + l of
+// chunk c).
 __device__ __forceinline__ FewWork few_find(const MfmaArgs& a, int w) {
   const int lane = __lane_id();
   FewWork r{-1, 0, 0, 0, 0, 0};
@@ -1382,7 +1386,24 @@ __device__ __forceinline__ FewWork few_find(const MfmaArgs& a, int w) {
   for (int c0 = kWave; c0 < a.B; c0 += kWave) T += readlane_i64(wave_scan_i64(length(c0 + lane)), kWave - 1);
   // (a float estimate, raised so that it is never short of the quotient)
   const float want = static_cast<float>(T) * static_cast<float>(a.Hkv) / static_cast<float>(a.W - a.B * a.Hkv);
-  const int sk = max((static_cast<int>(want * 1.00001f) / kKT + 1) * kKT, a.split_keys);
+  int sk = max((static_cast<int>(want * 1.00001f) / kKT + 1) * kKT, a.split_keys);
+  if (4 * a.B * a.Hkv <= a.W) {  // (plan_few: the resident grid)
+    auto splits = [&](int len) {  // of the whole call (below 2^24: exact)
+      float n = 0.f;
+      for (int c0 = 0; c0 < a.B; c0 += kWave) {
+        const int P = c0 == 0 ? P0 : length(c0 + lane);
+        n += c0 + lane < a.B ? static_cast<float>(max((P + len - 1) / len, 1)) : 0.f;
+      }
+      return __builtin_amdgcn_readfirstlane(static_cast<int>(wave_sum_dpp(n))) * a.Hkv;
+    };
+    int lo = max(static_cast<int>(static_cast<float>(T) * static_cast<float>(a.Hkv) / static_cast<float>(a.W)) / kKT * kKT,
+                 a.split_keys);
+    while (lo < sk) {  // (both are multiples of kKT)
+      const int mid = (lo + sk) / (2 * kKT) * kKT;
+      if (splits(mid) <= a.W) sk = mid;
+      else lo = mid + kKT;
+    }
+  }
   r.split_keys = sk;
   int before = 0;  // splits of the sequences before this chunk
   for (int c0 = 0; c0 < a.B; c0 += kWave) {
