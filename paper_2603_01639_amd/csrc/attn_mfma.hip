@@ -2340,7 +2340,7 @@ int64_t worst_split_key_cap(const AttnShape& s) {
 bool two_key_groups(const AttnShape& s) { return s.Hq / s.Hkv * s.Nmax <= kTileRows / 4; }
 
 // Whether every unit of a call over an 8-bit cache has at most 32 rows
-// (attend_few).
+// (attn_few_kernel).
 bool few_rows(const AttnShape& s) { return s.scale_rows > 0 && s.Hq / s.Hkv * s.Nmax <= kFewRows; }
 
 // Longest split few_find may come to: its block ids (16 rows a page at least)
