@@ -1316,7 +1316,7 @@ __device__ __forceinline__ int stream_index(int w, int W) { return (w % 8) * (W 
 // 8 to 16 KiB requested per wave, 64 to 128 per compute unit (with the next
 // block in registers, which are free only part of a block's time, 16 sequences
 // of 1024 to 8192 keys, 64/8 heads, one node: 44.6 us a call instead of 42.2; of
-// now 39.5 the kernel takes 33, 146 MB at 4.4 TB/s, and the merge 4).
+// now 39.5 the kernel takes 33, 154 MB at 4.6 TB/s, and the merge 4).
 //
 // K lies in LDS as the S^T operand takes it: lane l finds the codes of key
 // sigma(l & 31), 16 dims in every 32, where its own load put them (Q's fragments
