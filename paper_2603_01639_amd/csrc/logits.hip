@@ -13,9 +13,12 @@
 //
 // Written rows: each thread applies the rules to its own tokens (single tokens
 // stored by the threads of a list left lines half written: 16 trees of 16 to 96
-// nodes, 128256 tokens, 620 us instead of 219).  Argmax: touched tokens
-// go into a list in LDS that all threads share out, so that the rules' arithmetic
-// (a division among it) runs for them alone, and the rest is one maximum.
+// nodes, 128256 tokens, 620 us instead of 219).  Argmax: biased tokens go into a
+// list in LDS that all threads share out.  Penalised ones stay with their owners,
+// which bound what the rules may make of them and work them out where the bound
+// reaches the largest logit so far, so that the rest is two maxima (a list of all
+// touched tokens read each row's lines twice, for that and for itself: 16 trees of
+// 16 to 128 nodes 167 us instead of 141).
 #include <algorithm>
 #include <type_traits>
 
@@ -37,7 +40,6 @@ constexpr int kVec = 4;              // 16-byte groups of a thread
 constexpr int kNodesMax = 8;         // nodes of a workgroup at most
 constexpr int kAcceptChunk = 16384;  // the acceptance workspace's chunk
 constexpr uint32_t kPrompt = 0x80000000u;
-constexpr uint16_t kBiased = 0x8000;  // a list entry's bias flag, beside its offset in the chunk
 
 struct RuleArgs {
   const float* logits;
@@ -78,14 +80,20 @@ __device__ __forceinline__ uint64_t pack_key(float v, int idx) {
   return (static_cast<uint64_t>(u) << 32) | static_cast<uint32_t>(0xFFFFFFFFu - idx);
 }
 
+// A logit's bits where bit s of `set` is 1, those of -infinity elsewhere.
+__device__ __forceinline__ uint32_t pick(uint32_t x, uint32_t set, int s) {
+  const uint32_t all = static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(set), s, 1));
+  return (x & all) | (0xFF800000u & ~all);
+}
+
 // kArgmax: reduce to the chunk's argmax key; else write the row.  kInPlace: out
 // is logits, and groups of 4 that no rule touches are neither read nor written.
 template <int kThreads, bool kArgmax, bool kInPlace>
 __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleArgs a) {
   constexpr int kChunk = kThreads * 4 * kVec;
-  constexpr int kItems = 2;                 // list entries a thread
-  constexpr int kList = kArgmax ? kItems * kThreads : 1;  // tokens beyond stay with the thread that owns them
-  static_assert(kChunk <= kBiased, "offsets leave the flag's bit free");
+  constexpr int kList = kArgmax ? kThreads : 1;  // biased tokens, an entry a thread
+  static_assert(!kArgmax || kList >= LTD_MAX_BIAS, "room for every bias");
+  static_assert(kChunk <= 65536, "offsets in a chunk fit 16 bits");
   __shared__ int32_t par_s[LTD_MAX_NODES], tok_s[LTD_MAX_NODES];
   __shared__ uint16_t path_s[kNodesMax][LTD_MAX_NODES];  // chunk offsets of the root path's draft tokens
   __shared__ int path_len_s[kNodesMax];
@@ -136,13 +144,13 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
     return ok & exist;
   };
   // A node on its way: its logits in the groups with a token in `want` (-infinity
-  // elsewhere), what its mask allows and, for the argmax, the logits and mask
-  // words of this thread's list entries.
+  // elsewhere), what its mask allows and, for the argmax, the logit and mask word
+  // of this thread's list entry.
   struct Node {
     f32x4 x[kVec];
     uint32_t ok;
-    float y[kItems];
-    uint32_t m[kItems];
+    float y;
+    uint32_t m;
   };
   auto load_row = [&](int i, uint32_t want, Node& nd) {
     const float* row = a.logits + (seq + i) * a.Voc;
@@ -152,7 +160,7 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
       nd.x[u] = (f32x4){-INFINITY, -INFINITY, -INFINITY, -INFINITY};
       if (((want >> (4 * u)) & 0xFu) == 0) continue;
       if (v + 4 <= hi) {
-        nd.x[u] = *reinterpret_cast<const f32x4_any*>(row + v);
+        nd.x[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_any*>(row + v));
       } else {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
@@ -242,7 +250,10 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
       if (first) bias_s[t - lo] = sum;
     }
   }
-  uint32_t touched = 0, kept = 0;  // of this thread's tokens (bit 4u + c): touched, and not in the list
+  // Of this thread's tokens (bit 4u + c): those a rule touches, and those of them
+  // that only penalties do; the largest emitted count among the latter.
+  uint32_t touched = 0, penal = 0;
+  int cnt_max = 1;
 #pragma unroll
   for (int u = 0; u < kVec; ++u) {
     const int o = (u * kThreads + tid) * 4;
@@ -253,12 +264,13 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
       if (cnt[u][c] == 0 && !biased) continue;
       touched |= 1u << (4 * u + c);
       if constexpr (kArgmax) {
-        const int at = atomicAdd(&list_n_s, 1);
-        if (at < kList) {
-          list_off_s[at] = static_cast<uint16_t>((o + c) | (biased ? kBiased : 0));
+        if (biased) {
+          const int at = atomicAdd(&list_n_s, 1);  // (at most LTD_MAX_BIAS)
+          list_off_s[at] = static_cast<uint16_t>(o + c);
           list_cnt_s[at] = static_cast<uint32_t>(cnt[u][c]);
         } else {
-          kept |= 1u << (4 * u + c);
+          penal |= 1u << (4 * u + c);
+          cnt_max = max(cnt_max, static_cast<int>(static_cast<uint32_t>(cnt[u][c]) & ~kPrompt));
         }
       }
     }
@@ -279,25 +291,20 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
   };
 
   __syncthreads();
-  const int n_list = min(list_n_s, kList);
-  auto load_items = [&](int i, Node& nd) {
-#pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-      nd.y[k] = 0.f;
-      nd.m[k] = 0u;
-      const int at = k * kThreads + tid;
-      if (at < n_list) {
-        const int v = lo + (list_off_s[at] & (kBiased - 1));
-        nd.y[k] = a.logits[(seq + i) * a.Voc + v];
-        nd.m[k] = a.mask != nullptr ? a.mask[(seq + i) * words + (v >> 5)] >> (v & 31) : 1u;
-      }
-    }
+  const bool listed = kArgmax && tid < list_n_s;  // (an entry's thread)
+  const int item = listed ? list_off_s[tid] : 0;
+  auto load_item = [&](int i, Node& nd) {
+    nd.m = 0u;
+    if (!listed) return;
+    const int v = lo + item;
+    nd.y = a.logits[(seq + i) * a.Voc + v];
+    nd.m = a.mask != nullptr ? a.mask[(seq + i) * words + (v >> 5)] >> (v & 31) : 1u;
   };
   // The tokens whose logits node i needs, of those its mask allows: in place,
   // groups with all tokens allowed and none touched need nothing; for the argmax
-  // touched tokens come by the list.
+  // biased tokens come by the list.
   auto wanted = [&](int i, uint32_t ok) {
-    if constexpr (kArgmax) return ok & ~touched;
+    if constexpr (kArgmax) return ok & (~touched | penal);
     if constexpr (!kInPlace) return ok;
     const uint32_t act = touched | path_bits(i);
     uint32_t want = 0;
@@ -310,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
   };
   auto fetch = [&](int i, Node& nd) {
     load_row(i, wanted(i, nd.ok), nd);
-    if constexpr (kArgmax) load_items(i, nd);
+    if constexpr (kArgmax) load_item(i, nd);
   };
 
   auto write = [&](int i, Node& nd) {
@@ -338,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
           if (!((ok >> c) & 1u)) nd.x[u][c] = -INFINITY;
       }
       if (in == 0xFu) {
-        *reinterpret_cast<f32x4_any*>(orow + v) = nd.x[u];
+        __builtin_nontemporal_store(static_cast<f32x4_any>(nd.x[u]), reinterpret_cast<f32x4_any*>(orow + v));
       } else {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
@@ -350,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
   auto reduce = [&](int i, Node& nd) {
     const int len = path_len_s[i - i0];
     const uint32_t on_path = len > 0 ? path_bits(i) : 0u;
-    const uint32_t plain = nd.ok & ~(touched | on_path);
+    const uint32_t plain = nd.ok & ~(touched | on_path), mild = nd.ok & penal & ~on_path;
     uint64_t best = 0;  // this thread's largest key, -infinity aside
     auto take = [&](float r, int v) {
       if (r > -INFINITY) {
@@ -358,13 +365,31 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
         best = key > best ? key : best;
       }
     };
-    float vm = -INFINITY;
+    // one of this thread's tokens (bit s), from memory
+    auto take_token = [&](int s) {
+      const int o = ((s >> 2) * kThreads + tid) * 4 + (s & 3);
+      const int v = lo + o;
+      const uint32_t count = (counts != nullptr ? static_cast<uint32_t>(counts[v]) : 0u) + path_count(i, o);
+      const bool biased = (biased_s[o >> 5] >> (o & 31)) & 1u;
+      take(apply_rule(a.logits[(seq + i) * a.Voc + v], count, pen, biased, bias_s[o]), v);
+    };
+    // the wave's largest key into the node's; its upper half
+    auto publish = [&]() {
+      uint32_t top;
+      const uint32_t at =
+          wave_argmax(static_cast<uint32_t>(best >> 32), ~static_cast<uint32_t>(best), tid % kWave, &top);
+      if (tid % kWave == 0 && top != 0)
+        atomicMax(&best_s[i - i0], (static_cast<unsigned long long>(top) << 32) | static_cast<uint32_t>(~at));
+      return top;
+    };
+    float vm = -INFINITY, pm = -INFINITY;  // the largest logit of those no rule touches, and of those penalties do
 #pragma unroll
     for (int u = 0; u < kVec; ++u) {
-      if (((plain >> (4 * u)) & 0xFu) != 0xFu) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (!((plain >> (4 * u + c)) & 1u)) nd.x[u][c] = -INFINITY;
+      for (int c = 0; c < 4; ++c) {  // (by bit masks: branches and conditions took 153 us where this takes 141)
+        const uint32_t x = __float_as_uint(nd.x[u][c]);
+        pm = fmaxf(pm, __uint_as_float(pick(x, mild, 4 * u + c)));
+        nd.x[u][c] = __uint_as_float(pick(x, plain, 4 * u + c));
       }
       vm = fmaxf(vm, fmaxf(fmaxf(nd.x[u].x, nd.x[u].y), fmaxf(nd.x[u].z, nd.x[u].w)));
     }
@@ -376,29 +401,27 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
         for (int c = 3; c >= 0; --c) bi = nd.x[u][c] == vm ? group(u) + c : bi;
       best = pack_key(vm, bi);
     }
-    // the list's tokens, but for those of the path ...
-#pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-      const int at = k * kThreads + tid;
-      if (at >= n_list || !(nd.m[k] & 1u)) continue;
-      const int o = list_off_s[at] & (kBiased - 1);
-      if (len > 0 && path_count(i, o) != 0) continue;
-      take(apply_rule(nd.y[k], list_cnt_s[at], pen, (list_off_s[at] & kBiased) != 0, bias_s[o]), lo + o);
+    // biased tokens, but for those of the path, which their owners take
+    if ((nd.m & 1u) && !(len > 0 && path_count(i, item) != 0))
+      take(apply_rule(nd.y, list_cnt_s[tid], pen, true, bias_s[item]), lo + item);
+    for (uint32_t left = on_path & nd.ok; left != 0; left &= left - 1) take_token(__builtin_ctz(left));
+    uint32_t bar = publish();
+    // Penalised tokens matter where one may reach what the wave or the workgroup has
+    // found (seldom: a token comes down, or up a little).  A rule's rounded steps
+    // never fall as the logit grows or, under a negative frequency, the count, so
+    // none exceeds the largest logit's result at the largest such count (at one,
+    // otherwise; at none, in the prompt alone).
+    if (counts != nullptr) {
+      bar = max(bar, reinterpret_cast<volatile uint32_t*>(&best_s[i - i0])[1]);
+      const float x = pm > 0.f ? pm / pen.rep : pm * pen.rep;
+      const float up = fmaxf(x, (x - pen.freq * static_cast<float>(pen.freq < 0.f ? cnt_max : 1)) - pen.pres);
+      const bool may = up > -INFINITY && static_cast<uint32_t>(pack_key(up, 0) >> 32) >= bar;
+      if (__ballot(may) != 0) {
+        best = 0;
+        for (uint32_t left = may ? mild : 0u; left != 0; left &= left - 1) take_token(__builtin_ctz(left));
+        publish();
+      }
     }
-    // ... which their owners take, with what the list has no room for
-    for (uint32_t left = kept | on_path; left != 0; left &= left - 1) {
-      const int s = __builtin_ctz(left);
-      const int o = ((s >> 2) * kThreads + tid) * 4 + (s & 3);
-      const int v = lo + o;
-      if (!((nd.ok >> s) & 1u)) continue;
-      const uint32_t count = (counts != nullptr ? static_cast<uint32_t>(counts[v]) : 0u) + path_count(i, o);
-      const bool biased = (biased_s[o >> 5] >> (o & 31)) & 1u;
-      take(apply_rule(a.logits[(seq + i) * a.Voc + v], count, pen, biased, bias_s[o]), v);
-    }
-    uint32_t top;
-    const uint32_t at = wave_argmax(static_cast<uint32_t>(best >> 32), ~static_cast<uint32_t>(best), tid % kWave, &top);
-    if (tid % kWave == 0 && top != 0)
-      atomicMax(&best_s[i - i0], (static_cast<unsigned long long>(top) << 32) | static_cast<uint32_t>(~at));
   };
 
   // ---- the nodes, two sets of registers in turn: while one node is worked on,
@@ -413,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleAr
     else write(i, cur);
   };
   if constexpr (kInPlace) fetch(i0, na);
-  if constexpr (kArgmax) load_items(i0, na);
+  if constexpr (kArgmax) load_item(i0, na);
   for (int i = i0; i < i1; i += 2) {
     step(i, na, nx);
     if (i + 1 < i1) step(i + 1, nx, na);
@@ -559,10 +582,17 @@ hipError_t launch_rules(const LogitRules& r, int B, int Nmax, int Voc, float* ou
   const auto launch = [&](auto threads, auto argmax, auto in_place) {
     constexpr int kChunk = threads() * 4 * kVec;
     a.chunks = (Voc + kChunk - 1) / kChunk;
-    // As many nodes a workgroup as leave no more of them than fit the card at once.
+    // As many nodes a workgroup as leave no more of them than fit the card at once,
+    // up to 8.  The argmax's come to an end at once then, one or two to a compute
+    // unit; in more rounds than two 7 nodes do better (in us, for 4, 6, 7 and 8: 16
+    // trees of 60, 32000 tokens 41 / 48 / 50 / 37; of 128256 tokens, 16 of 16 to 128
+    // nodes 148 / 136 / 137 / 141, 32 of 16 to 64 171 / 149 / 150 / 160, 64 of 1 to
+    // 16 113 / 80 / 80 / 94).
     const int64_t rows = static_cast<int64_t>(B) * Nmax * a.chunks;
     const int64_t card = int64_t{256} * (1024 / threads());
-    a.nodes = static_cast<int>(std::min<int64_t>((rows + card - 1) / card, kNodesMax));
+    const int64_t eights = static_cast<int64_t>(B) * ((Nmax + kNodesMax - 1) / kNodesMax) * a.chunks;
+    const int most = argmax() && eights > 2 * card ? kNodesMax - 1 : kNodesMax;
+    a.nodes = static_cast<int>(std::min<int64_t>((rows + card - 1) / card, most));
     a.groups = (Nmax + a.nodes - 1) / a.nodes;
     hipLaunchKernelGGL((rules_kernel<threads(), argmax(), in_place()>),
                        dim3(static_cast<unsigned>(a.chunks) * a.groups * B),

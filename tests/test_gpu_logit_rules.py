@@ -295,3 +295,21 @@ def test_masked_logits_and_banned_tokens(voc):
     assert all((got[b, :n, banned[b]] == -np.inf).all() for b, n in enumerate(m["n"]) if m["bias"][2][b] > 1)
     for x, y in zip(accept(dirty), accept(m)):
         np.testing.assert_array_equal(x, y)
+
+
+@pytest.mark.parametrize("rep, freq, pres", [(1.3, 0.4, 0.2), (0.6, 0.0, 0.0), (1.0, -0.7, 0.1), (1.2, -0.3, -0.5), (1.0, 0.0, 0.0),
+                                             (1.0, 2.0, 1.0)])
+def test_accept_where_penalised_tokens_compete(rep, freq, pres):
+    """Vocabularies of mostly counted tokens with logits close together, equal ones among them: the best token is now a
+    penalised one, now a plain one, and often tied."""
+    rng = np.random.default_rng(int(rep * 100 + freq * 10 + 50))
+    sizes, voc = [24, 7, 40], 20000
+    m = make(3, sizes, voc, prompt=9000, gen=12000, bias=12, std=0.0)
+    m["pen"] = np.tile(np.array([rep, freq, pres], np.float32), (3, 1))
+    m["logits"] = (rng.integers(-3, 4, m["logits"].shape) / 4).astype(np.float32)
+    m["logits"][0] += 2
+    m["logits"][1] -= 2
+    got = accept(m)
+    written = np.nan_to_num(process(m), neginf=-3.0e38)
+    for b, n in enumerate(m["n"]):
+        np.testing.assert_array_equal(got[0][b, :n], written[b, :n].argmax(-1))
