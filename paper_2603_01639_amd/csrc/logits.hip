@@ -13,7 +13,7 @@
 //
 // Written rows: each thread applies the rules to its own tokens (single tokens
 // stored by the threads of a list left lines half written: 16 trees of 16 to 96
-// nodes, 128256 tokens, 620 us instead of 219; now 202, 837 MB at 4.4 TB/s).  Argmax: biased tokens go into a
+// nodes, 128256 tokens, 620 us instead of 219; now 190, 837 MB at 4.7 TB/s).  Argmax: biased tokens go into a
 // list in LDS that all threads share out.  Penalised ones stay with their owners,
 // which bound what the rules may make of them and work them out where the bound
 // reaches the largest logit so far, so that the rest is two maxima (a list of all
@@ -37,7 +37,7 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef i32x4 i32x4_any __attribute__((aligned(4)));
 
 constexpr int kVec = 4;              // 16-byte groups of a thread
-constexpr int kNodesMax = 8;         // nodes of a workgroup at most
+constexpr int nodes_max(bool argmax) { return argmax ? 8 : 4; }  // nodes of a workgroup at most
 constexpr int kAcceptChunk = 16384;  // the acceptance workspace's chunk
 constexpr uint32_t kPrompt = 0x80000000u;
 
@@ -91,6 +91,7 @@ __device__ __forceinline__ uint32_t pick(uint32_t x, uint32_t set, int s) {
 template <int kThreads, bool kArgmax, bool kInPlace>
 __global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleArgs a) {
   constexpr int kChunk = kThreads * 4 * kVec;
+  constexpr int kNodesMax = nodes_max(kArgmax);
   constexpr int kList = kArgmax ? kThreads : 1;  // biased tokens, an entry a thread
   static_assert(!kArgmax || kList >= LTD_MAX_BIAS, "room for every bias");
   static_assert(kChunk <= 65536, "offsets in a chunk fit 16 bits");
@@ -583,15 +584,19 @@ hipError_t launch_rules(const LogitRules& r, int B, int Nmax, int Voc, float* ou
     constexpr int kChunk = threads() * 4 * kVec;
     a.chunks = (Voc + kChunk - 1) / kChunk;
     // As many nodes a workgroup as leave no more of them than fit the card at once,
-    // up to 8.  The argmax's come to an end at once then, one or two to a compute
+    // up to 4 where rows are written (in us, for 2, 3, 4, 6 and 8: 16 trees of 16 to 96
+    // nodes, 128256 tokens 200 / 198 / 196 / 206 / 211 without and 203 / 194 / 190 / 197
+    // / 201 with masks; 64 of 1 to 16 123 / 124 / 125 / 131 / 136) and up to 8 for the
+    // argmax.  Its workgroups come to an end at once then, one or two to a compute
     // unit; in more rounds than two 7 nodes do better (in us, for 4, 6, 7 and 8: 16
     // trees of 60, 32000 tokens 41 / 48 / 50 / 37; of 128256 tokens, 16 of 16 to 128
     // nodes 148 / 136 / 137 / 141, 32 of 16 to 64 171 / 149 / 150 / 160, 64 of 1 to
     // 16 113 / 80 / 80 / 94).
     const int64_t rows = static_cast<int64_t>(B) * Nmax * a.chunks;
     const int64_t card = int64_t{256} * (1024 / threads());
-    const int64_t eights = static_cast<int64_t>(B) * ((Nmax + kNodesMax - 1) / kNodesMax) * a.chunks;
-    const int most = argmax() && eights > 2 * card ? kNodesMax - 1 : kNodesMax;
+    constexpr int kMost = nodes_max(argmax());
+    const int64_t fullest = static_cast<int64_t>(B) * ((Nmax + kMost - 1) / kMost) * a.chunks;
+    const int most = argmax() && fullest > 2 * card ? kMost - 1 : kMost;
     a.nodes = static_cast<int>(std::min<int64_t>((rows + card - 1) / card, most));
     a.groups = (Nmax + a.nodes - 1) / a.nodes;
     hipLaunchKernelGGL((rules_kernel<threads(), argmax(), in_place()>),
