@@ -540,7 +540,8 @@ def kv_compact_q8(k_cache, v_cache, k_scale, v_scale, prefix_len, new_prefix_len
     """In-place compaction of an 8-bit KV cache; see ``ltd_kv_compact_q8``.
     With a leading dimension of layers, caches ``[layers][pages][Hkv][rows][d]``
     and scales alike, the strides default to the tensors' own and num_layers to
-    all of them."""
+    all of them; without one the tensors are the first layer's views of buffers
+    that hold num_layers at the strides."""
     lead = k_cache.dim() - 4
     if lead not in (0, 1):
         raise ValueError(f"k_cache has {k_cache.dim()} dimensions, not 4 or 5")
@@ -557,6 +558,12 @@ def kv_compact_q8(k_cache, v_cache, k_scale, v_scale, prefix_len, new_prefix_len
         if ((num_layers - 1) * layer_stride_elems > last * k_cache.stride(0)
                 or (num_layers - 1) * scale_stride_elems > last * k_scale.stride(0)):
             raise ValueError(f"{num_layers} layers at these strides pass the tensors' end")
+    elif num_layers > 1:  # one layer's view of a larger buffer: the others lie in the same one
+        for t, stride in ((k_cache, layer_stride_elems), (v_cache, layer_stride_elems),
+                          (k_scale, scale_stride_elems), (v_scale, scale_stride_elems)):
+            end = t.storage_offset() + (num_layers - 1) * stride + t.numel()  # (elements of a byte)
+            if end > t.untyped_storage().nbytes():
+                raise ValueError(f"{num_layers} layers at these strides pass the tensors' end")
     B, Nmax = _dims("accepted_nodes", accepted_nodes, 2)
     _batch_pages(B, pages, block_table)
     _int32((B, Nmax), accepted_nodes=accepted_nodes)
