@@ -15,6 +15,7 @@
 #include "ltd_device.hpp"
 #include "ltd_launch.hpp"
 #include "q8.hpp"
+#include "q8_rows.hpp"
 
 namespace ltd {
 namespace {
@@ -89,9 +90,9 @@ __global__ void __launch_bounds__(kThreads) kv_append_q8_kernel(AppendArgs a) {
   const int n = min(a.n_rows[b], a.Nmax);
   // The unit's rows [r0, r1) of the logical cache: blocks never cross a page
   // (a page holds whole blocks), so they follow one another.
-  const int r0 = (P / SR + unit) * SR;
+  const int r0 = append_block(P, n, unit, SR);
   const int64_t end = static_cast<int64_t>(P) + n;
-  const bool work = n > 0 && r0 < end;
+  const bool work = r0 >= 0;
   const int lane = t % kLanes;
   Raw16<T> x[kIter];
   float amax = 0.f;
@@ -329,7 +330,7 @@ hipError_t launch_append_q8(const void* k_new, const void* v_new, int64_t row_st
   a.kv_rows = kv_rows;
   a.max_blocks = max_blocks;
   a.scale_per_page = (kv_rows + scale_rows - 1) / scale_rows;
-  a.units = (Nmax + scale_rows - 2) / scale_rows + 1;  // blocks that Nmax rows can touch
+  a.units = append_units(Nmax, scale_rows);
   pick_block(d, scale_rows, [&](auto hd, auto sr) {
     constexpr int kUnits = kThreads / unit_threads(sr() * hd() / 16);
     const dim3 grid(static_cast<unsigned>(B) * ((a.units + kUnits - 1) / kUnits), Hkv * 2);
