@@ -62,6 +62,7 @@
 #include <type_traits>
 #include <utility>
 
+#include "few_plan.hpp"
 #include "ltd_device.hpp"
 #include "ltd_launch.hpp"
 #include "q8.hpp"
@@ -129,7 +130,7 @@ struct MfmaArgs {
   uint32_t g_magic;  // node_of's multiplier and shift
   int g_shift;
   int kv_shift;  // log2(kv_rows) when kv_rows is a power of two, else -1
-  int W;  // stream plan: workgroups of the grid (a power of two)
+  int W;  // stream plan: workgroups of the grid (a power of two); few_plan.hpp's target
   // split plan: prefix keys per split, splits of the longest sequence, whether
   // the tree may take a split of its own, row tiles per (sequence, kv head)
   int split_keys, max_splits, tree_alone, row_tiles;
@@ -1307,10 +1308,8 @@ __device__ __forceinline__ int stream_index(int w, int W) { return (w % 8) * (W 
 // trees).  Such calls are bound by the cache's bytes.  A (sequence, kv head) is
 // cut into splits of one length, the tree's keys joining the last, one for a
 // workgroup of four waves; two workgroups share a compute unit.  The length is
-// worked out on the GPU from the call's own lengths (few_find): the shortest for
-// which the splits fit the grid, so that all run at once and the longest holds
-// no more than its share, whatever max_prefix is.  Every wave takes all of the
-// unit's rows and its own 32-key blocks (block i: wave i mod 4), from loads to
+// worked out on the GPU from the call's own lengths (few_plan.hpp).  Every wave
+// takes all of the unit's rows and its own 32-key blocks (block i: wave i mod 4), from loads to
 // P.V, with no barrier until the waves' results are joined.  Its blocks move
 // straight into two slots of LDS of its own, refilled as soon as they are read:
 // 8 to 16 KiB requested per wave, 64 to 128 per compute unit (with the next
@@ -1355,25 +1354,22 @@ struct FewSmem {
 // What a workgroup of the grid works on: split `split` of `n_splits` of
 // sequence b and kv head g; w is its place among the call's splits (b major,
 // then g, then split), and the unit's first split's place is w - split.  b < 0:
-// the call has fewer splits.
+// the call has fewer splits.  more: it may have more than workgroups.
 struct FewWork {
   int b, g, split, n_splits, P, split_keys;
+  bool more;
 };
 
-// The split length is ceil(T Hkv / (W - B Hkv)) for T prefix keys in all and a
-// grid of W > B Hkv workgroups, rounded up to a key tile, at least a block a
-// wave: the splits then number at most T Hkv / length + B Hkv <= W.  Where all
-// of them run at once, the longest split is what the call takes, and a binary
-// search finds the shortest length that fits (16 sequences of 1024 to 8192 keys,
-// 64/8 heads: 1280 to 1536 keys instead of 1472 to 1792, 39.5 us a call instead of
-// 42.0).  Every wave works it out on its own (lane l holds sequence c * 64 + l of
-// chunk c).
+// Every wave works it out on its own (lane l holds sequence c * 64 + l of chunk
+// c; one sequence takes a scalar load and no scans).
 __device__ __forceinline__ FewWork few_find(const MfmaArgs& a, int w) {
   const int lane = __lane_id();
-  FewWork r{-1, 0, 0, 0, 0, 0};
-  if (a.B == 1) {  // a scalar load and no scans
+  FewWork r{-1, 0, 0, 0, 0, 0, false};
+  if (a.B == 1) {
     r.P = min(max(a.prefix_len[0], 0), a.max_prefix);
-    r.split_keys = max(static_cast<int>(static_cast<int64_t>(r.P) * a.Hkv / (a.W - a.Hkv) / kKT + 1) * kKT, a.split_keys);
+    const few::Length len = few::one_length(r.P, a.Hkv, a.W, a.max_prefix);
+    r.split_keys = len.keys;
+    r.more = len.rounds > 1;
     r.n_splits = max((r.P + r.split_keys - 1) / r.split_keys, 1);
     r.g = w / r.n_splits;
     r.split = w - r.g * r.n_splits;
@@ -1384,27 +1380,17 @@ __device__ __forceinline__ FewWork few_find(const MfmaArgs& a, int w) {
   const int P0 = length(lane);
   int64_t T = readlane_i64(wave_scan_i64(P0), kWave - 1);
   for (int c0 = kWave; c0 < a.B; c0 += kWave) T += readlane_i64(wave_scan_i64(length(c0 + lane)), kWave - 1);
-  // (a float estimate, raised so that it is never short of the quotient)
-  const float want = static_cast<float>(T) * static_cast<float>(a.Hkv) / static_cast<float>(a.W - a.B * a.Hkv);
-  int sk = max((static_cast<int>(want * 1.00001f) / kKT + 1) * kKT, a.split_keys);
-  if (4 * a.B * a.Hkv <= a.W) {  // (plan_few: the resident grid)
-    auto splits = [&](int len) {  // of the whole call (below 2^24: exact)
-      float n = 0.f;
-      for (int c0 = 0; c0 < a.B; c0 += kWave) {
-        const int P = c0 == 0 ? P0 : length(c0 + lane);
-        n += c0 + lane < a.B ? static_cast<float>(max((P + len - 1) / len, 1)) : 0.f;
-      }
-      return __builtin_amdgcn_readfirstlane(static_cast<int>(wave_sum_dpp(n))) * a.Hkv;
-    };
-    int lo = max(static_cast<int>(static_cast<float>(T) * static_cast<float>(a.Hkv) / static_cast<float>(a.W)) / kKT * kKT,
-                 a.split_keys);
-    while (lo < sk) {  // (both are multiples of kKT)
-      const int mid = (lo + sk) / (2 * kKT) * kKT;
-      if (splits(mid) <= a.W) sk = mid;
-      else lo = mid + kKT;
+  const few::Length len = few::batch_length(T, a.Hkv, a.B * a.Hkv, a.W, a.max_prefix, [&](int keys) {
+    float n = 0.f;  // (below 2^24: exact)
+    for (int c0 = 0; c0 < a.B; c0 += kWave) {
+      const int P = c0 == 0 ? P0 : length(c0 + lane);
+      n += c0 + lane < a.B ? static_cast<float>(max((P + keys - 1) / keys, 1)) : 0.f;
     }
-  }
+    return __builtin_amdgcn_readfirstlane(static_cast<int>(wave_sum_dpp(n))) * a.Hkv;
+  });
+  const int sk = len.keys;
   r.split_keys = sk;
+  r.more = len.rounds > 1;
   int before = 0;  // splits of the sequences before this chunk
   for (int c0 = 0; c0 < a.B; c0 += kWave) {
     const int P = c0 == 0 ? P0 : length(c0 + lane);
@@ -1432,13 +1418,11 @@ struct FewDesc {
   int32_t first, n_splits;
 };
 
-template <int HD, bool kPaged>
-__global__ void __launch_bounds__(kFewThreads, 2) attn_few_kernel(MfmaArgs a) {
-  __shared__ __attribute__((aligned(16))) FewSmem<HD> sm;
-  if (halted(a.status)) return;
-  const int slot_id = blockIdx.x;
+// The split at place slot_id; whether the call may have more than workgroups.
+template <int HD, bool kPaged, bool kLoop>
+__device__ __forceinline__ bool attend_few(const MfmaArgs& a, FewSmem<HD>& sm, int slot_id) {
   const FewWork fw = few_find(a, slot_id);
-  if (fw.b < 0) return;
+  if (fw.b < 0) return false;
   const int b = fw.b, g = fw.g, P = fw.P;
   const int n = min(max(a.n_nodes[b], 1), a.Nmax);
   const bool has_tree = fw.split == fw.n_splits - 1;
@@ -1448,7 +1432,10 @@ __global__ void __launch_bounds__(kFewThreads, 2) attn_few_kernel(MfmaArgs a) {
   const int n_pre = min(fw.split_keys, P - key_begin);
   if (fw.split == 0 && threadIdx.x == 0)
     reinterpret_cast<FewDesc*>(a.ws_desc)[b * a.Hkv + g] = FewDesc{slot_id, fw.n_splits};
-  const int tid = threadIdx.x;
+  // (an opaque copy of the thread's index: otherwise the compiler keeps what
+  // follows from it alone in registers from one split to the next)
+  int tid = threadIdx.x;
+  if constexpr (kLoop) asm volatile("" : "+v"(tid));
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int lane = tid % kWave;
   const int h = lane >> 5, l32 = lane & 31;
@@ -1801,6 +1788,33 @@ __global__ void __launch_bounds__(kFewThreads, 2) attn_few_kernel(MfmaArgs a) {
       *reinterpret_cast<u32x4*>(dst + col * 8) = (u32x4){out[0], out[1], out[2], out[3]};
     else
       *reinterpret_cast<uint2*>(dst + col * 4) = make_uint2(out[0], out[1]);
+  }
+  return fw.more;
+}
+
+// kLoop: the launch's bounds allow more splits than workgroups, which come back
+// for more where the call's own lengths make so many.  (One sequence of 128 keys:
+// 7.1 us a call without the loop, 7.25 with it; of 16384 keys 16.8 and 17.0.)
+template <int HD, bool kPaged, bool kLoop>
+__global__ void __launch_bounds__(kFewThreads, 2) attn_few_kernel(MfmaArgs a) {
+  __shared__ __attribute__((aligned(16))) FewSmem<HD> sm;
+  if (halted(a.status)) return;
+  if constexpr (!kLoop) {
+    attend_few<HD, kPaged, false>(a, sm, blockIdx.x);
+  } else {
+#if defined(__HIP_DEVICE_COMPILE__)  // (the host's pass copies no structure out of an address space)
+    // (The arguments are read anew for each split: kept from one to the next, they
+    // and what follows from them take more scalar registers than there are, 40.4 us
+    // a call where this takes 38.7.)
+    typedef const __attribute__((address_space(4))) MfmaArgs KernArgs;
+    KernArgs* args = (KernArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    for (int slot_id = blockIdx.x;; slot_id += gridDim.x) {
+      asm volatile("" : "+s"(args));
+      const MfmaArgs now = *args;
+      if (!attend_few<HD, kPaged, true>(now, sm, slot_id)) return;
+      __syncthreads();  // every wave is done with the results in LDS
+    }
+#endif
   }
 }
 
@@ -2343,44 +2357,24 @@ bool two_key_groups(const AttnShape& s) { return s.Hq / s.Hkv * s.Nmax <= kTileR
 // (attn_few_kernel).
 bool few_rows(const AttnShape& s) { return s.scale_rows > 0 && s.Hq / s.Hkv * s.Nmax <= kFewRows; }
 
-// Longest split few_find may come to: its block ids (16 rows a page at least)
-// and the tree's fit the LDS table, with room for the rounding to key tiles.
-constexpr int kFewCap = 7680;
-static_assert((kFewCap + 2 * kKT + kFewRows) / 16 + 2 <= kFewBlocks, "a split's block ids fit");
+static_assert((few::kMaxKeys + 2 * kKT + kFewRows) / 16 + 2 <= kFewBlocks, "a split's block ids fit");
+static_assert(few::kKeyTile == kKT && few::kMinKeys == 32 * kFewWaves && few::kMostSplits == kMaxMergeSplits,
+              "the plan's constants");
 
-// Shortest split: a block a wave, and few enough of them for the merge's table.
-int64_t few_min_keys(int64_t max_prefix) {
-  const int64_t keys = (max_prefix + kMaxMergeSplits - 25) / (kMaxMergeSplits - 24);
-  return std::max<int64_t>((keys + kKT - 1) / kKT * kKT, 32 * kFewWaves);
-}
-
-// The grid.  Up to a quarter as many units as workgroups that fit the card at
-// once: that many, so that all splits run side by side (16 sequences of 64/8
-// heads, 1024 to 8192 keys: 41.0 us, 43.3 in shorter ones).  With more units the
-// remainders of so few splits would leave compute units idle, and the splits
-// are cut into 4 a compute unit beyond the units, which the hardware deals out as
-// they end (in us, for a grid of 2, 3, 4 and 6 times the units: 256 units of 500
-// to 6000 keys 67 / 64 / 57 / 57, 384 of 2000 52 / 50 / 52 / 56, 512 of 200 to
-// 3000 62 / 57 / 58 / 65, 1024 of 100 to 1500 65 / 69 / 73 / 85).  More again
-// where a split would be longer than kFewCap.
 void plan_few(const AttnShape& s, int num_cus, AttnPlan* p) {
   const int64_t units = static_cast<int64_t>(s.B) * s.Hkv;
-  const int64_t min_keys = few_min_keys(s.max_prefix);
-  const int64_t resident = static_cast<int64_t>(kFewPerCu) * num_cus;
-  const int64_t W = std::max(4 * units <= resident ? resident : units + 4 * num_cus,
-                             units * ((s.max_prefix + kFewCap - 1) / kFewCap + 1));
-  const int64_t most = units * std::max<int64_t>(1, (s.max_prefix + min_keys - 1) / min_keys);
+  const int64_t target = few::target(units, kFewPerCu, num_cus);
   p->mfma = true;
   p->few = true;
   p->stream = false;
-  p->split_keys = static_cast<int>(min_keys);
   p->tile_rows = kFewRows;
   p->row_tiles = 1;
-  p->max_splits = s.max_prefix > p->split_keys ? 2 : 1;  // (whether a unit can be cut at all)
-  p->few_width = static_cast<int>(W);
-  p->grid = static_cast<int>(std::min(W, most));
-  p->workspace_bytes =
-      static_cast<size_t>(p->grid) * kFewRows * part_row_bytes(s) + static_cast<size_t>(units) * sizeof(FewDesc);
+  p->max_splits = s.max_prefix > few::kMinKeys ? 2 : 1;  // (whether a unit can be cut at all)
+  p->few_target = static_cast<int>(target);
+  p->few_slots = few::most_splits(units, s.max_prefix, target);
+  p->grid = static_cast<int>(few::workgroups(units, s.max_prefix, target));
+  p->workspace_bytes = static_cast<size_t>(p->few_slots) * kFewRows * part_row_bytes(s) +
+                       static_cast<size_t>(units) * sizeof(FewDesc);
 }
 
 // Estimated time of a split plan, in key tiles of a 256-row unit (about 2 us).
@@ -2471,7 +2465,7 @@ void plan_split(const AttnShape& s, int num_cus, AttnPlan* p) {
 // the LDS table even with one-row blocks, and at most kMaxMergeSplits of them.
 bool mfma_supported(const AttnShape& s) {
   if (s.dtype != LTD_DTYPE_BF16 || (s.d != 128 && s.d != 64)) return false;
-  if (few_rows(s)) return few_min_keys(s.max_prefix) <= kFewCap;
+  if (few_rows(s)) return s.max_prefix <= static_cast<int64_t>(few::kMaxKeys) * few::kMostSplits;
   if (use_stream(s)) return true;
   const int64_t cap = worst_split_key_cap(s);
   return cap >= 2 * kKT && s.max_prefix <= cap * kMaxMergeSplits;
@@ -2556,18 +2550,21 @@ hipError_t launch_attn_mfma(const AttnShape& s, const AttnPlan& p, const void* q
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   a.ws_o = static_cast<uint16_t*>(workspace);
   if (p.few) {
-    a.split_keys = p.split_keys;
     a.row_tiles = 1;
     a.tile_rows = kFewRows;
-    a.W = p.few_width;
-    const size_t slots = static_cast<size_t>(p.grid) * kFewRows;
+    a.W = p.few_target;
+    const size_t slots = static_cast<size_t>(p.few_slots) * kFewRows;
     a.ws_ml = reinterpret_cast<float*>(ws + slots * kD * 2);
     a.ws_desc = reinterpret_cast<MergeDesc*>(ws + slots * part_row_bytes(s));
-    const auto launch_few = [&](auto d) {
-      if (a.block_table)
-        hipLaunchKernelGGL((attn_few_kernel<d(), true>), dim3(p.grid), dim3(kFewThreads), 0, stream, a);
+    const auto launch_paged = [&](auto d, auto paged) {
+      if (p.few_slots > p.grid)
+        hipLaunchKernelGGL((attn_few_kernel<d(), paged(), true>), dim3(p.grid), dim3(kFewThreads), 0, stream, a);
       else
-        hipLaunchKernelGGL((attn_few_kernel<d(), false>), dim3(p.grid), dim3(kFewThreads), 0, stream, a);
+        hipLaunchKernelGGL((attn_few_kernel<d(), paged(), false>), dim3(p.grid), dim3(kFewThreads), 0, stream, a);
+    };
+    const auto launch_few = [&](auto d) {
+      if (a.block_table) launch_paged(d, std::true_type{});
+      else launch_paged(d, std::false_type{});
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess || p.max_splits == 1) return e;  // one split a unit: the output is final
       hipLaunchKernelGGL((attn_split_merge_kernel<d(), false, true, true>),
