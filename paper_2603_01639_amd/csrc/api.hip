@@ -511,8 +511,8 @@ int ltd_tree_process_logits(const float* logits, const int32_t* draft_tokens,
                                    st) != hipSuccess)
       return LTD_EHIP;
   }
-  if (ltd::launch_rules(r, B, Nmax, Voc, out, nullptr, validate ? status : nullptr, st) !=
-      hipSuccess)
+  if (ltd::launch_rules(r, B, Nmax, Voc, out, nullptr, device_cu_count(),
+                        validate ? status : nullptr, st) != hipSuccess)
     return LTD_EHIP;
   return LTD_OK;
 }
@@ -545,7 +545,8 @@ int ltd_tree_accept_processed(const float* logits, const int32_t* draft_tokens,
       return LTD_EHIP;
   }
   const int32_t* halt = validate ? status : nullptr;
-  if (ltd::launch_rules(r, B, Nmax, Voc, nullptr, workspace, halt, st) != hipSuccess)
+  if (ltd::launch_rules(r, B, Nmax, Voc, nullptr, workspace, device_cu_count(), halt, st) !=
+      hipSuccess)
     return LTD_EHIP;
   if (ltd::launch_accept_scan(workspace, draft_tokens, parents, n_nodes, B, Nmax, Voc, pred,
                               accepted_nodes, out_tokens, n_accepted, halt, st) != hipSuccess)

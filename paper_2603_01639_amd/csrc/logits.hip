@@ -24,6 +24,7 @@
 
 #include "ltd_device.hpp"
 #include "ltd_launch.hpp"
+#include "rules_plan.hpp"
 
 #pragma clang fp contract(off)  // every step of a rule is rounded, as documented
 
@@ -37,7 +38,6 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef i32x4 i32x4_any __attribute__((aligned(4)));
 
 constexpr int kVec = 4;              // 16-byte groups of a thread
-constexpr int nodes_max(bool argmax) { return argmax ? 8 : 4; }  // nodes of a workgroup at most
 constexpr int kAcceptChunk = 16384;  // the acceptance workspace's chunk
 constexpr uint32_t kPrompt = 0x80000000u;
 
@@ -89,9 +89,9 @@ __device__ __forceinline__ uint32_t pick(uint32_t x, uint32_t set, int s) {
 // kArgmax: reduce to the chunk's argmax key; else write the row.  kInPlace: out
 // is logits, and groups of 4 that no rule touches are neither read nor written.
 template <int kThreads, bool kArgmax, bool kInPlace>
-__global__ void __launch_bounds__(kThreads, kArgmax ? 4 : 4) rules_kernel(RuleArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) rules_kernel(RuleArgs a) {
   constexpr int kChunk = kThreads * 4 * kVec;
-  constexpr int kNodesMax = nodes_max(kArgmax);
+  constexpr int kNodesMax = rules::nodes_max(kArgmax);
   constexpr int kList = kArgmax ? kThreads : 1;  // biased tokens, an entry a thread
   static_assert(!kArgmax || kList >= LTD_MAX_BIAS, "room for every bias");
   static_assert(kChunk <= 65536, "offsets in a chunk fit 16 bits");
@@ -560,7 +560,7 @@ hipError_t launch_token_counts(const int32_t* tokens, const int32_t* n_tokens, i
   return hipGetLastError();
 }
 
-hipError_t launch_rules(const LogitRules& r, int B, int Nmax, int Voc, float* out, void* partial,
+hipError_t launch_rules(const LogitRules& r, int B, int Nmax, int Voc, float* out, void* partial, int cus,
                         const int32_t* status, hipStream_t stream) {
   RuleArgs a{};
   a.logits = r.logits;
@@ -583,21 +583,7 @@ hipError_t launch_rules(const LogitRules& r, int B, int Nmax, int Voc, float* ou
   const auto launch = [&](auto threads, auto argmax, auto in_place) {
     constexpr int kChunk = threads() * 4 * kVec;
     a.chunks = (Voc + kChunk - 1) / kChunk;
-    // As many nodes a workgroup as leave no more of them than fit the card at once,
-    // up to 4 where rows are written (in us, for 2, 3, 4, 6 and 8: 16 trees of 16 to 96
-    // nodes, 128256 tokens 200 / 198 / 196 / 206 / 211 without and 203 / 194 / 190 / 197
-    // / 201 with masks; 64 of 1 to 16 123 / 124 / 125 / 131 / 136) and up to 8 for the
-    // argmax.  Its workgroups come to an end at once then, one or two to a compute
-    // unit; in more rounds than two 7 nodes do better (in us, for 4, 6, 7 and 8: 16
-    // trees of 60, 32000 tokens 41 / 48 / 50 / 37; of 128256 tokens, 16 of 16 to 128
-    // nodes 148 / 136 / 137 / 141, 32 of 16 to 64 171 / 149 / 150 / 160, 64 of 1 to
-    // 16 113 / 80 / 80 / 94).
-    const int64_t rows = static_cast<int64_t>(B) * Nmax * a.chunks;
-    const int64_t card = int64_t{256} * (1024 / threads());
-    constexpr int kMost = nodes_max(argmax());
-    const int64_t fullest = static_cast<int64_t>(B) * ((Nmax + kMost - 1) / kMost) * a.chunks;
-    const int most = argmax() && fullest > 2 * card ? kMost - 1 : kMost;
-    a.nodes = static_cast<int>(std::min<int64_t>((rows + card - 1) / card, most));
+    a.nodes = rules::nodes(B, Nmax, a.chunks, argmax(), threads(), cus);
     a.groups = (Nmax + a.nodes - 1) / a.nodes;
     hipLaunchKernelGGL((rules_kernel<threads(), argmax(), in_place()>),
                        dim3(static_cast<unsigned>(a.chunks) * a.groups * B),

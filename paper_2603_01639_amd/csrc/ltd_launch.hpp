@@ -155,8 +155,8 @@ hipError_t launch_token_counts(const int32_t* tokens, const int32_t* n_tokens, i
                                int Voc, bool prompt, bool reset, int32_t* counts,
                                hipStream_t stream);
 // Writes the processed rows to `out`, or (partial non-null) every chunk's
-// argmax key to `partial`.
+// argmax key to `partial`; `cus`: the device's compute units.
 hipError_t launch_rules(const LogitRules& rules, int B, int Nmax, int Voc, float* out,
-                        void* partial, const int32_t* status, hipStream_t stream);
+                        void* partial, int cus, const int32_t* status, hipStream_t stream);
 
 }  // namespace ltd
