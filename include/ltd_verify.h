@@ -449,6 +449,8 @@ int ltd_kv_append_q8(const void* k_new, const void* v_new, int64_t new_row_strid
  * ltd_tree_verify_attn_q8_workspace_size().  A NaN code in a tree row reaches
  * the outputs of the nodes that see the row, and no others: a NaN in a visible
  * row's V may make every dimension of those outputs NaN.
+ * With bfloat16, values below 2^-29 of the largest of an output row's dimensions
+ * may be off by 2^-39 of that largest.
  */
 size_t ltd_tree_verify_attn_q8_workspace_size(int B, int Nmax, int Hq, int Hkv, int d,
                                               int max_prefix, int dtype);

@@ -52,11 +52,14 @@
 // tiles: each thread loads 16 codes of K and of V two tiles ahead into registers
 // and widens them to bf16 into the tile's slot, an exact step, so that what
 // follows is unchanged.  Long prefixes and full row tiles are bound by the tile
-// loop as before (16 sequences of 64/8 heads over 1024 to 8192 keys, 16 to 128
-// nodes: 225 us a call against 221 over a 16-bit cache; one of 32/8 heads over
-// 16384 keys, 60 nodes: 28.0 against 27.6).  Units of at most 32 rows, which the
-// bytes of the cache bound, take a kernel of their own (attn_few_kernel: the same
-// 16 sequences decoding one token 39.5 us against 64).
+// loop, to which the widening adds 2 to 14% (us a call over an 8-bit and over a
+// 16-bit cache: 16 sequences of 64/8 heads over 1024 to 8192 keys, 16 to 128 nodes
+// 231.6 / 227.4, with 8/1 heads 46.9 / 43.4; one of 32/8 heads over 16384 keys, 60
+// nodes 29.6 / 28.7; one of 64/8 heads over 4096 keys, 256 nodes 51.6 / 45.4).
+// Batches of small trees gain, less than their bytes fall (the 16 sequences with
+// 8 nodes each 59.4 / 70.3).  Units of at most 32 rows, which the bytes of the cache
+// bound, take a kernel of their own (attn_mfma_q8.hip: the same 16 sequences
+// decoding one token 39.5 / 63.9).
 #pragma once
 
 #include <algorithm>
@@ -323,9 +326,10 @@ __device__ __forceinline__ void q8_to_bf16(const u32x4& codes, uint32_t byte, u3
 // How a piece's rows are stored until they are merged: O / l in bf16 or, for an
 // 8-bit cache, in fp16 under a power of two that brings the row's largest
 // value to [2^14, 2^15), beside max and sum.  Same bytes but for that factor,
-// and off by at most 2^-11 of a value instead of 2^-8 (2-norm of the output's
-// error, 16 sequences over 1024 to 8192 keys: 2.5e-3 of the output's with bf16
-// pieces, 1.8e-3 to 2.0e-3 with these, 1.6e-3 by the output's own rounding).
+// and off by at most 2^-11 of a value instead of 2^-8 (values below 2^-29 of the
+// row's largest: by at most 2^-39 of that) (2-norm of the output's error, 16
+// sequences over 1024 to 8192 keys: 2.5e-3 of the output's with bf16 pieces,
+// 1.8e-3 to 2.0e-3 with these, 1.6e-3 by the output's own rounding).
 // V's scales span 2^187, hence a factor for each row.
 template <bool kQ8>
 struct PartRow;

@@ -13,13 +13,13 @@ namespace {
 // cut into splits of one length, the tree's keys joining the last, one for a
 // workgroup of four waves; two workgroups share a compute unit.  The length is
 // worked out on the GPU from the call's own lengths (few_plan.hpp).  Every wave
-// takes all of the unit's rows and its own 32-key blocks (block i: wave i mod 4), from loads to
-// P.V, with no barrier until the waves' results are joined.  Its blocks move
-// straight into two slots of LDS of its own, refilled as soon as they are read:
-// 8 to 16 KiB requested per wave, 64 to 128 per compute unit (with the next
-// block in registers, which are free only part of a block's time, 16 sequences
-// of 1024 to 8192 keys, 64/8 heads, one node: 44.6 us a call instead of 42.2; of
-// now 39.5 the kernel takes 33, 154 MB at 4.6 TB/s, and the merge 4).
+// takes all of the unit's rows and its own 32-key blocks (block i: wave i mod 4),
+// from loads to P.V, with no barrier until the waves' results are joined.  Its
+// blocks move straight into two slots of LDS of its own, refilled as soon as they
+// are read: 8 to 16 KiB requested per wave, 64 to 128 per compute unit (with the
+// next block in registers, which are free only part of a block's time, 16
+// sequences of 1024 to 8192 keys, 64/8 heads, one node: 44.6 us a call instead of
+// 42.2; of now 39.5 the kernel takes about 35, 154 MB at 4.4 TB/s, and the merge 4).
 //
 // K lies in LDS as the S^T operand takes it: lane l finds the codes of key
 // sigma(l & 31), 16 dims in every 32, where its own load put them (Q's fragments

@@ -13,12 +13,17 @@
 //
 // Written rows: each thread applies the rules to its own tokens (single tokens
 // stored by the threads of a list left lines half written: 16 trees of 16 to 96
-// nodes, 128256 tokens, 620 us instead of 219; now 190, 837 MB at 4.7 TB/s).  Argmax: biased tokens go into a
-// list in LDS that all threads share out.  Penalised ones stay with their owners,
-// which bound what the rules may make of them and work them out where the bound
-// reaches the largest logit so far, so that the rest is two maxima (a list of all
-// touched tokens read each row's lines twice, for that and for itself: 16 trees of
-// 16 to 128 nodes 167 us instead of 141; now 138, 602 MB at 4.5 TB/s).
+// nodes, 128256 tokens, 620 us instead of 219; now 190 with the table's two
+// launches, of which this kernel takes about 180, 833 MB at 4.6 TB/s; in place,
+// where groups that no rule touches stay as they are, 175).  Rows are read and
+// written past the caches: 181 us instead of 191 alone, 491 instead of 528 with
+// acceptance by sampling reading them next; one user's 60 rows 60 us either way.
+// Argmax: biased tokens go into a list in LDS that all threads share out.  Penalised
+// ones stay with their owners, which bound what the rules may make of them and work
+// them out where the bound reaches the largest logit so far, so that the rest is two
+// maxima (a list of all touched tokens read each row's lines twice, for that and for
+// itself: 16 trees of 16 to 128 nodes 167 us instead of 141; now 138.7 with the scan,
+// about 135 of them here, 597 MB at 4.4 TB/s).
 #include <algorithm>
 #include <type_traits>
 
