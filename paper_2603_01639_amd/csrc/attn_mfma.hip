@@ -95,16 +95,18 @@ bool few_rows(const AttnShape& s) { return s.scale_rows > 0 && s.Hq / s.Hkv * s.
 
 void plan_few(const AttnShape& s, int num_cus, AttnPlan* p) {
   const int64_t units = static_cast<int64_t>(s.B) * s.Hkv;
-  const int64_t target = few::target(units, kFewPerCu, num_cus);
+  const int resident = kFewPerCu * num_cus;
   p->mfma = true;
   p->few = true;
   p->stream = false;
   p->tile_rows = kFewRows;
   p->row_tiles = 1;
   p->max_splits = s.max_prefix > few::kMinKeys ? 2 : 1;  // (whether a unit can be cut at all)
-  p->few_target = static_cast<int>(target);
-  p->few_slots = few::most_splits(units, s.max_prefix, target);
-  p->grid = static_cast<int>(few::workgroups(units, s.max_prefix, target));
+  p->few_target = static_cast<int>(few::target(units, resident));
+  p->few_width = static_cast<int>(few::round_width(units, resident));
+  p->few_wide = few::may_widen(units, s.max_prefix, resident);
+  p->few_slots = few::most_splits(units, s.max_prefix, resident);
+  p->grid = static_cast<int>(few::workgroups(units, s.max_prefix, resident));
   p->workspace_bytes = static_cast<size_t>(p->few_slots) * kFewRows * part_row_bytes(s) +
                        static_cast<size_t>(units) * sizeof(FewDesc);
 }

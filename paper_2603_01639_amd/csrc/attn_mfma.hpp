@@ -144,6 +144,7 @@ struct MfmaArgs {
   const uint8_t* ks;
   const uint8_t* vs;
   int scale_per_page, scale_shift;
+  int few_width;  // short units: workgroups of the wider cut (few_plan.hpp)
 };
 
 // Node of stacked row r: r / G, by a multiplication.  With G <= 2^shift and

@@ -57,7 +57,7 @@ struct FewSmem {
 // What a workgroup of the grid works on: split `split` of `n_splits` of
 // sequence b and kv head g; w is its place among the call's splits (b major,
 // then g, then split), and the unit's first split's place is w - split.  b < 0:
-// the call has fewer splits.  more: it may have more than workgroups.
+// the call has fewer splits.  more: they come in rounds.
 struct FewWork {
   int b, g, split, n_splits, P, split_keys;
   bool more;
@@ -70,7 +70,7 @@ __device__ __forceinline__ FewWork few_find(const MfmaArgs& a, int w) {
   FewWork r{-1, 0, 0, 0, 0, 0, false};
   if (a.B == 1) {
     r.P = min(max(a.prefix_len[0], 0), a.max_prefix);
-    const few::Length len = few::one_length(r.P, a.Hkv, a.W, a.max_prefix);
+    const few::Length len = few::one_length(r.P, a.Hkv, a.W, a.few_width, a.max_prefix);
     r.split_keys = len.keys;
     r.more = len.rounds > 1;
     r.n_splits = max((r.P + r.split_keys - 1) / r.split_keys, 1);
@@ -83,7 +83,7 @@ __device__ __forceinline__ FewWork few_find(const MfmaArgs& a, int w) {
   const int P0 = length(lane);
   int64_t T = readlane_i64(wave_scan_i64(P0), kWave - 1);
   for (int c0 = kWave; c0 < a.B; c0 += kWave) T += readlane_i64(wave_scan_i64(length(c0 + lane)), kWave - 1);
-  const few::Length len = few::batch_length(T, a.Hkv, a.B * a.Hkv, a.W, a.max_prefix, [&](int keys) {
+  const few::Length len = few::batch_length(T, a.Hkv, a.B * a.Hkv, a.W, a.few_width, a.max_prefix, [&](int keys) {
     float n = 0.f;  // (below 2^24: exact)
     for (int c0 = 0; c0 < a.B; c0 += kWave) {
       const int P = c0 == 0 ? P0 : length(c0 + lane);
@@ -116,7 +116,7 @@ __device__ __forceinline__ FewWork few_find(const MfmaArgs& a, int w) {
   return r;
 }
 
-// The split at place slot_id; whether the call may have more than workgroups.
+// The split at place slot_id; whether the workgroup may have another, a grid on.
 template <int HD, bool kPaged, bool kLoop>
 __device__ __forceinline__ bool attend_few(const MfmaArgs& a, FewSmem<HD>& sm, int slot_id) {
   const FewWork fw = few_find(a, slot_id);
@@ -490,8 +490,8 @@ __device__ __forceinline__ bool attend_few(const MfmaArgs& a, FewSmem<HD>& sm, i
   return fw.more;
 }
 
-// kLoop: the launch's bounds allow more splits than workgroups, which come back
-// for more where the call's own lengths make so many.  (One sequence of 128 keys:
+// kLoop: the launch's bounds allow more splits than workgroups, which the call's own
+// lengths may or may not make.  (One sequence of 128 keys:
 // 7.1 us a call without the loop, 7.25 with it; of 16384 keys 16.8 and 17.0.)
 template <int HD, bool kPaged, bool kLoop>
 __global__ void __launch_bounds__(kFewThreads, 2) attn_few_kernel(MfmaArgs a) {
@@ -538,11 +538,12 @@ hipError_t launch_attn_mfma_q8(const AttnShape& s, const AttnPlan& p, const void
   a.row_tiles = 1;
   a.tile_rows = kFewRows;
   a.W = p.few_target;
+  a.few_width = p.few_width;
   const size_t slots = static_cast<size_t>(p.few_slots) * kFewRows;
   a.ws_ml = reinterpret_cast<float*>(ws + slots * kD * 2);
   a.ws_desc = reinterpret_cast<MergeDesc*>(ws + slots * part_row_bytes(s));
   const auto launch_paged = [&](auto d, auto paged) {
-    if (p.few_slots > p.grid)
+    if (p.few_wide)
       hipLaunchKernelGGL((attn_few_kernel<d(), paged(), true>), dim3(p.grid), dim3(kFewThreads), 0, stream, a);
     else
       hipLaunchKernelGGL((attn_few_kernel<d(), paged(), false>), dim3(p.grid), dim3(kFewThreads), 0, stream, a);

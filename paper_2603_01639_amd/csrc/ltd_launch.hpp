@@ -37,7 +37,9 @@ struct AttnPlan {
   int tile_rows;     // split plan: stacked rows of a row tile
   bool tree_alone;   // split plan: the tree's keys may take a split of their own
   bool few;          // 8-bit cache, units of at most 32 rows: splits planned on the GPU ...
-  int few_target;    // ... for this many workgroups (the grid may need fewer)
+  int few_target;    // ... for this many workgroups (the grid may need fewer), or
+  int few_width;     // for rounds of this many (few_plan.hpp)
+  bool few_wide;     // the bounds allow more splits than few_target
   int64_t few_slots;  // splits that the call can have
   size_t workspace_bytes;
 };

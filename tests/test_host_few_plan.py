@@ -17,7 +17,7 @@ DRIVER = r"""
 #include <vector>
 #include "few_plan.hpp"
 using namespace ltd::few;
-// stdin: "B Hkv cus max_prefix" and B prefixes; stdout: target, slots, workgroups, keys, rounds
+// stdin: "B Hkv cus max_prefix" and B prefixes; stdout: target, width, slots, workgroups, keys, rounds
 int main() {
   int B, H, cus, mp;
   while (std::scanf("%d %d %d %d", &B, &H, &cus, &mp) == 4) {
@@ -27,15 +27,16 @@ int main() {
       if (std::scanf("%d", &p) != 1) return 2;
       T += p;
     }
-    const int64_t units = int64_t(B) * H, t = target(units, 2, cus);
-    const Length len = B == 1 ? one_length(P[0], H, int(t), mp)
-                              : batch_length(T, H, int(units), int(t), mp, [&](int keys) {
+    const int resident = 2 * cus;
+    const int64_t units = int64_t(B) * H, t = target(units, resident), width = round_width(units, resident);
+    const Length len = B == 1 ? one_length(P[0], H, int(t), int(width), mp)
+                              : batch_length(T, H, int(units), int(t), int(width), mp, [&](int keys) {
                                   int n = 0;
                                   for (int p : P) n += p > 0 ? (p + keys - 1) / keys : 1;
                                   return n * H;
                                 });
-    std::printf("%lld %lld %lld %d %d\n", (long long)t, (long long)most_splits(units, mp, t),
-                (long long)workgroups(units, mp, t), len.keys, len.rounds);
+    std::printf("%lld %lld %lld %lld %d %d\n", (long long)t, (long long)width, (long long)most_splits(units, mp, resident),
+                (long long)workgroups(units, mp, resident), len.keys, len.rounds);
   }
   return 0;
 }
@@ -63,18 +64,17 @@ def _splits(P, H, keys):
 
 def _check(case, got):
     H, _, mp, P = case
-    target, slots, wgs, keys, rounds = got
-    units, n = len(P) * H, _splits(P, H, keys)
+    target, width, slots, wgs, keys, rounds = got
+    units, n, few = len(P) * H, _splits(P, H, keys), _splits(P, H, MAX)
+    top = MAX // 2 if width > target and len(P) > 1 else MAX
     assert keys % TILE == 0 and MIN <= keys <= MAX
     assert max(-(-p // keys) for p in P) <= MOST
-    assert n <= rounds * target and n <= slots
-    assert wgs == min(target, slots)
-    if rounds == 1:
-        assert n <= wgs  # (a workgroup each)
+    assert n <= rounds * wgs and n <= slots  # (every split has a workgroup and a slot)
+    assert units <= n and wgs <= max(target, width)
+    if _splits(P, H, top) <= target:  # the splits run side by side, or are dealt out once
+        assert rounds == 1 and n <= target and keys <= top
     else:
-        assert _splits(P, H, MAX) > target  # (no length in one round)
-        assert n > target and _splits(P, H, MAX) >= (rounds - 1) * target
-    return n, units
+        assert keys >= MAX // 2 and (rounds - 1) * width < few <= rounds * width
 
 
 def _random(rng):
@@ -110,16 +110,16 @@ def test_the_bound_on_the_prefixes_does_not_move_the_splits(plan):
         loose = [(H, cus, max(mp, m), P) for H, cus, m, P in cases]
         for a, b, got in zip(loose, tight, plan(loose)):
             _check(a, got)
-            assert got[3:] == b[3:], (a, b, got)
+            assert got[4:] == b[4:], (a, b, got)
 
 
 def test_the_shortest_length_that_fits_side_by_side(plan):
     rng = np.random.default_rng(7)
     cases = [c for c in (_random(rng) for _ in range(2000)) if 1 < len(c[3]) and 4 * len(c[3]) * c[0] <= 512 and c[1] == 256]
     assert len(cases) > 300
-    for (H, _, _, P), (target, _, _, keys, rounds) in zip(cases, plan(cases)):
-        least = MIN if rounds == 1 else MAX // 2
-        assert keys == least or _splits(P, H, keys - TILE) > rounds * target
+    for (H, _, _, P), (target, width, _, _, keys, rounds) in zip(cases, plan(cases)):
+        least, room = (MIN, target) if _splits(P, H, MAX) <= target else (MAX // 2, rounds * width)
+        assert keys == least or _splits(P, H, keys - TILE) > room
 
 
 @pytest.mark.parametrize("B, H", [(1, 1), (1, 8), (129, 1), (200, 1), (2, 1)])
