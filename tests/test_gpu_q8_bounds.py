@@ -61,3 +61,36 @@ def test_more_splits_than_workgroups(B, H, d, lengths, paged):
         assert (rows == rows[0]).all(), length
         check(dict(one, prefix=np.array([length], np.int32)), rows[0].view(torch.bfloat16).view(1, 1, 1, d),
               label=f"length {length}")
+
+
+@pytest.mark.parametrize("B, n", [(1, 1), (16, 1), (16, 4)])
+def test_a_captured_call_follows_its_lengths(B, n):
+    """A graph captured under a bound far above the lengths, whose prefixes then grow and shrink between replays: each
+    replay answers as an eager call with tight bounds."""
+    import torch
+    lengths = [[40] * B, [3000 - 100 * b for b in range(B)], [0] * B, [2500 if b == B // 2 else 7 for b in range(B)]]
+    top = [max(x[b] for x in lengths) for b in range(B)]
+    m = make(5, B, 8, 2, 128, 16, top, [n] * B, 16)
+    dev = Q.dev_cache(m["c"])
+    q, par, sizes = m["q"].to("cuda"), Q.to_dev(m["par"]), Q.to_dev(m["n"])
+    prefix, out = Q.to_dev(np.array(lengths[0], np.int32)), torch.full_like(q, 7.0)
+    ws = torch.empty(ltd.attn_q8_workspace_size(B, n, 8, 2, 128, 131072, ltd.DTYPE_BF16), dtype=torch.uint8, device="cuda")
+    call = lambda: ltd.tree_verify_attn_q8(q, dev["k"], dev["v"], dev["ks"], dev["vs"], prefix, par, sizes, out,  # noqa: E731
+                                           max_prefix=131072, scale_rows=16, block_table=dev["table"],
+                                           num_blocks=m["c"]["pages"], workspace=ws)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            call()
+    for x in lengths + lengths[:2]:
+        prefix.copy_(torch.tensor(x, dtype=torch.int32))
+        out.fill_(7.0)
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        now = dict(m, prefix=np.array(x, np.int32))
+        check(now, out, label=str(x[:3]))
+        assert torch.equal(out.view(torch.int16), run(now, dev=dev).view(torch.int16))
