@@ -37,6 +37,11 @@
  * the target's logits and acceptance (ltd_token_counts,
  * ltd_tree_process_logits, ltd_tree_accept_processed).
  *
+ * Queries and keys get their rotary positions from ltd_tree_rope.  A model with
+ * latent attention keeps one vector a token, which all heads share, and has the
+ * cycle's calls for that cache (ltd_latent_append, ltd_tree_verify_attn_latent,
+ * ltd_latent_compact).
+ *
  * Conventions for every call
  * --------------------------
  * - All array pointers are DEVICE pointers, owned by the caller.  The library
@@ -96,7 +101,10 @@ extern "C" {
 #define LTD_EXPAND_MAX_CHILDREN 256  /* F * W per round */
 
 #define LTD_MAX_BIAS 1024            /* biased tokens per sequence */
-#define LTD_MAX_LENGTH (1 << 30)     /* rows, tokens and vocabulary of the 8-bit cache's and the rules' calls */
+#define LTD_MAX_LENGTH (1 << 30)     /* rows, tokens and vocabulary of the 8-bit cache's and the rules' calls, positions */
+
+#define LTD_ROPE_MAX_DIM 4096 /* head size of ltd_tree_rope */
+#define LTD_LATENT_ROPE 64    /* rotated dims of a latent cache's rows */
 
 #define LTD_POLICY_SIZE 0          /* state [D, L, score of every pool candidate, pad ...] */
 #define LTD_POLICY_DEPTH 1         /* state [scores of the newest in_dim-2 candidates, D, L] */
@@ -556,6 +564,141 @@ int ltd_tree_accept_processed(const float* logits, const int32_t* draft_tokens,
                               int Voc, int max_bias, int32_t* pred, int32_t* accepted_nodes,
                               int32_t* out_tokens, int32_t* n_accepted, void* workspace,
                               size_t workspace_bytes, int validate, int32_t* status, void* stream);
+
+/*
+ * Rotary positions of queries and keys: a draft tree's, or consecutive tokens'.
+ *
+ * Row i of sequence b stands at position p = P_b + depth[b][i] (P_b =
+ * prefix_len[b]).  In every head the dims [rot_offset, rot_offset + rot_dim) turn:
+ * pair j < rot_dim / 2, with values (x0, x1) at dims (rot_offset + j, rot_offset +
+ * rot_dim / 2 + j), or (rot_offset + 2j, rot_offset + 2j + 1) when interleaved != 0,
+ * becomes
+ *     (mscale (x0 cos t - x1 sin t), mscale (x1 cos t + x0 sin t)),  t = p * inv_freq[j].
+ * The angle is formed and reduced in float64, so that a position a million tokens
+ * out is as exact as the first; the rest is float32, rounded once.  Other dims
+ * are copied.
+ *
+ *   q, q_out     [B][Nmax] rows of Hq heads of d elements (dtype): row (b, i) starts
+ *                at (b * Nmax + i) * q_row_stride, its head h q_head_stride elements
+ *                after head h - 1; a head's elements follow one another.  q_out has
+ *                strides of its own.  q_out may be q, with the same strides (in
+ *                place); other overlaps give undefined results.
+ *   k, k_out     the same with Hk heads, or Hk = 0 and NULL.
+ *   inv_freq     [rot_dim / 2] float64: radians a position.
+ *   depth        [B][Nmax] int32 >= 0 (as ltd_select_candidates writes it), or NULL
+ *                for consecutive tokens (depth[b][i] = i).
+ *   n_rows       [B] int32 in [0, Nmax]; rows i >= n_rows[b] are not written.
+ *   rot_dim even, 2 <= rot_dim, rot_offset >= 0, rot_offset + rot_dim <= d <=
+ *   LTD_ROPE_MAX_DIM, (Hq + Hk) * d <= 2^24, Nmax and positions up to
+ *   LTD_MAX_LENGTH; Nmax may exceed LTD_MAX_NODES.  mscale is finite.
+ * Any alignment is taken; 16-byte aligned rows and heads are faster.
+ * With validate != 0: LTD_STATUS_BAD_NNODES (n_rows) and LTD_STATUS_BAD_PREFIX
+ * (a position outside [0, LTD_MAX_LENGTH)).
+ */
+int ltd_tree_rope(const void* q, int64_t q_row_stride, int64_t q_head_stride, void* q_out,
+                  int64_t q_out_row_stride, int64_t q_out_head_stride, const void* k,
+                  int64_t k_row_stride, int64_t k_head_stride, void* k_out,
+                  int64_t k_out_row_stride, int64_t k_out_head_stride, const double* inv_freq,
+                  const int32_t* prefix_len, const int32_t* depth, const int32_t* n_rows, int B,
+                  int Nmax, int Hq, int Hk, int d, int rot_offset, int rot_dim, int interleaved,
+                  float mscale, int dtype, int validate, int32_t* status, void* stream);
+
+/*
+ * The latent cache.
+ *
+ * A model with latent attention keeps, for every token and layer, one row that all
+ * heads share: d_latent dims (the compressed key and value) followed by d_rope dims
+ * (the rotated key), in
+ *   contiguous [B][kv_rows][d_latent + d_rope], paged [num_blocks][kv_rows][d_latent
+ *   + d_rope] (dtype), logical row r of sequence b in block
+ *   block_table[b][r / kv_rows].
+ * d_latent is 256 or 512, d_rope is LTD_LATENT_ROPE; anything else is
+ * LTD_EUNSUPPORTED, as are more than LTD_MAX_LENGTH rows to append or max_prefix.
+ * Caches are 16-byte aligned (LTD_EINVAL otherwise).
+ */
+
+/*
+ * Appends rows to a latent cache: a prompt's, or a draft tree's before its
+ * verification.
+ *
+ * For every sequence b and i < n_rows[b], with (c, k) the first d_latent and the
+ * last d_rope elements of row i, logical row P_b + i of the cache becomes
+ *     [ c / sqrt(mean(c^2) + norm_eps) * norm_weight | k turned as in ltd_tree_rope ]
+ * at position P_b + depth[b][i] (float32 statistics, each element rounded once); with
+ * norm_weight NULL the latent part is copied.
+ *
+ *   kv_new       [B][Nmax][d_latent + d_rope] (dtype), row (b, i) at (b * Nmax + i) *
+ *                new_row_stride (at least d_latent + d_rope: rows may be views into
+ *                a fused projection's output); rows are 16-byte aligned.
+ *   norm_weight  [d_latent] (dtype), 16-byte aligned, or NULL; norm_eps finite, >= 0.
+ *   inv_freq     [d_rope / 2] float64; interleaved, mscale, depth and n_rows as for
+ *                ltd_tree_rope.
+ * Other rows keep their bytes.  No two sequences may append to the same row.  With
+ * validate != 0: LTD_STATUS_BAD_NNODES, LTD_STATUS_BAD_PREFIX (P_b < 0, rows past the
+ * capacity or LTD_MAX_LENGTH) and LTD_STATUS_BAD_BLOCK (ids of the blocks that are
+ * written); depth is not checked.
+ */
+int ltd_latent_append(const void* kv_new, int64_t new_row_stride, const void* norm_weight,
+                      float norm_eps, const double* inv_freq, int interleaved, float mscale,
+                      void* cache, const int32_t* block_table, const int32_t* prefix_len,
+                      const int32_t* depth, const int32_t* n_rows, int B, int Nmax, int d_latent,
+                      int d_rope, int kv_rows, int max_blocks, int num_blocks, int dtype,
+                      int validate, int32_t* status, void* stream);
+
+/*
+ * Tree attention over a latent cache, in the absorbed form: the queries have been
+ * multiplied into the latent space, and the output is in it.
+ *
+ * For every sequence b, node i < n_nodes[b] and head h, with x_t = [c_t | k_t] row t
+ * of the cache:
+ *     out[b][i][h] = softmax_t(scale * (<q_latent[b][i][h], c_t> + <q_rope[b][i][h], k_t>)) . c_t
+ * over the visible rows t = {0, ..., P_b - 1} u {P_b + j : j on the root path of
+ * node i, i included}.  Statistics and accumulation are float32; with bfloat16 the
+ * weights are rounded to bfloat16 before they multiply the values, and the sum that
+ * normalises them is that of the rounded ones.
+ *
+ *   q_latent     rows of Hq heads of d_latent elements, q_rope of d_rope elements
+ *                (dtype): row (b, i) at (b * Nmax + i) * row stride, head h at h * head
+ *                stride (any layout whose heads' elements follow one another, such as
+ *                [Hq][B][Nmax][d_latent], as a product per head leaves it).
+ *                With bfloat16 rows and heads are 16-byte aligned (LTD_EINVAL).
+ *   out          [B][Nmax][Hq][d_latent] (dtype), 16-byte aligned; rows i >=
+ *                n_nodes[b] are not written.
+ *   scale        finite and > 0 (that of the expanded heads, which the latent size
+ *                does not tell).
+ *   prefix_len, max_prefix, parents, n_nodes, block_table as for
+ *   ltd_tree_verify_attn; a single token a sequence is a tree of one node.
+ *   workspace    at least ltd_tree_verify_attn_latent_workspace_size() bytes for the
+ *                same (B, Nmax, Hq, d_latent, d_rope, max_prefix, dtype), 16-byte
+ *                aligned; needs no initialisation.
+ * A NaN or an infinity in a row's latent part, or a NaN score, reaches the outputs
+ * of the nodes that see the row (where it may make every dimension NaN), and no
+ * others.  B <= 65535 with float32.
+ */
+size_t ltd_tree_verify_attn_latent_workspace_size(int B, int Nmax, int Hq, int d_latent,
+                                                  int d_rope, int max_prefix, int dtype);
+
+int ltd_tree_verify_attn_latent(const void* q_latent, int64_t ql_row_stride,
+                                int64_t ql_head_stride, const void* q_rope, int64_t qr_row_stride,
+                                int64_t qr_head_stride, const void* cache,
+                                const int32_t* block_table, const int32_t* prefix_len,
+                                const int32_t* parents, const int32_t* n_nodes, void* out, int B,
+                                int Nmax, int Hq, int d_latent, int d_rope, int max_prefix,
+                                int kv_rows, int max_blocks, int num_blocks, float scale,
+                                int dtype, void* workspace, size_t workspace_bytes, int validate,
+                                int32_t* status, void* stream);
+
+/*
+ * Compaction of a latent cache: ltd_kv_compact for its one row a token.  Layer l
+ * starts layer_stride_elems elements after layer l - 1 (a multiple of 16 bytes).
+ * num_layers <= 65535.
+ */
+int ltd_latent_compact(void* cache, const int32_t* block_table, const int32_t* prefix_len,
+                       int32_t* new_prefix_len, const int32_t* accepted_nodes,
+                       const int32_t* n_accepted, int B, int Nmax, int d_latent, int d_rope,
+                       int kv_rows, int max_blocks, int num_blocks, int num_layers,
+                       int64_t layer_stride_elems, int dtype, int validate, int32_t* status,
+                       void* stream);
 
 /* Library version string. */
 const char* ltd_version(void);

@@ -39,6 +39,7 @@ MAX_NODES = 256
 MAX_BIAS = 1024
 MAX_LENGTH = 1 << 30
 MAX_POOL = 1024
+LATENT_ROPE = 64
 POLICY_SIZE = 0
 POLICY_DEPTH = 1
 
@@ -66,6 +67,11 @@ EXPORTED = (
     "ltd_token_counts",
     "ltd_tree_process_logits",
     "ltd_tree_accept_processed",
+    "ltd_tree_rope",
+    "ltd_latent_append",
+    "ltd_tree_verify_attn_latent_workspace_size",
+    "ltd_tree_verify_attn_latent",
+    "ltd_latent_compact",
 )
 
 
@@ -134,6 +140,17 @@ def lib() -> ctypes.CDLL:
         L.ltd_tree_process_logits.restype = i32
         L.ltd_tree_accept_processed.argtypes = [P] * 10 + [i32] * 4 + [P] * 5 + [sz, i32, P, P]
         L.ltd_tree_accept_processed.restype = i32
+        L.ltd_tree_rope.argtypes = [P, i64, i64] * 4 + [P] * 4 + [i32] * 8 + [f32, i32, i32, P, P]
+        L.ltd_tree_rope.restype = i32
+        L.ltd_latent_append.argtypes = [P, i64, P, f32, P, i32, f32] + [P] * 5 + [i32] * 9 + [P, P]
+        L.ltd_latent_append.restype = i32
+        L.ltd_tree_verify_attn_latent_workspace_size.argtypes = [i32] * 7
+        L.ltd_tree_verify_attn_latent_workspace_size.restype = sz
+        L.ltd_tree_verify_attn_latent.argtypes = ([P, i64, i64] * 2 + [P] * 6 + [i32] * 9
+                                                  + [f32, i32, P, sz, i32, P, P])
+        L.ltd_tree_verify_attn_latent.restype = i32
+        L.ltd_latent_compact.argtypes = [P] * 6 + [i32] * 8 + [i64, i32, i32, P, P]
+        L.ltd_latent_compact.restype = i32
         L.ltd_version.argtypes = []
         L.ltd_version.restype = ctypes.c_char_p
         _lib = L
@@ -647,3 +664,245 @@ def tree_accept_processed(logits, draft_tokens, parents, n_nodes, pred, accepted
     _run("ltd_tree_accept_processed",
          args + (_p(pred), _p(accepted_nodes), _p(out_tokens), _p(n_accepted), *_space(workspace), int(validate), _p(status)),
          tensors + (pred, accepted_nodes, out_tokens, n_accepted, workspace, status), stream)
+
+
+# ---- rotary positions and the latent cache
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, *, scaling: Optional[str] = None,
+                     factor: float = 1.0, trained_len: int = 0, beta_fast: float = 32.0,
+                     beta_slow: float = 1.0, low_factor: float = 1.0, high_factor: float = 4.0,
+                     device=None):
+    """Rotary frequencies for ``tree_rope`` and ``latent_append``: a float64 tensor
+    ``[rot_dim / 2]`` of radians a position, and the factor mscale.
+
+    Pair j turns by f_j = base^(-2j / rot_dim) a position.  ``scaling`` stretches
+    them for contexts ``factor`` times as long as ``trained_len``, the one the
+    model was trained on:
+
+    - ``"linear"``: f_j / factor, every position moved closer.
+    - ``"ntk"``: base becomes base * factor^(rot_dim / (rot_dim - 2)), so that the
+      fastest pair keeps its speed and the slowest is divided by factor.
+    - ``"yarn"``: a pair that turns more than beta_fast times within trained_len keeps
+      f_j, one that turns less than beta_slow times gets f_j / factor, with a
+      linear ramp over the pair's index between; mscale = 0.1 ln(factor) + 1.
+    - ``"bands"``: a pair whose wavelength is below trained_len / high_factor keeps
+      f_j, one above trained_len / low_factor gets f_j / factor, and between them
+      the two are blended by trained_len / wavelength.
+    """
+    import math
+
+    import torch
+    if rot_dim < 2 or rot_dim % 2 or not base > 1 or not factor > 0:
+        raise ValueError(f"rot_dim {rot_dim}, base {base}, factor {factor}")
+    half = rot_dim // 2
+    j = torch.arange(half, dtype=torch.float64)
+    mscale = 1.0
+    if scaling == "ntk":
+        if rot_dim < 4:
+            raise ValueError("ntk scaling needs two pairs")
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    f = base ** (-2 * j / rot_dim)
+    if scaling == "linear":
+        f = f / factor
+    elif scaling in ("yarn", "bands"):
+        if trained_len < 1:
+            raise ValueError(f"{scaling} scaling needs trained_len")
+        if scaling == "yarn":
+            def index(turns):  # of the pair that turns so often within trained_len
+                return rot_dim * math.log(trained_len / (turns * 2 * math.pi)) / (2 * math.log(base))
+            lo, hi = max(math.floor(index(beta_fast)), 0), min(math.ceil(index(beta_slow)), rot_dim - 1)
+            slow = ((j - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
+            mscale = 0.1 * math.log(factor) + 1.0 if factor > 1 else 1.0
+        else:
+            if not high_factor > low_factor > 0:
+                raise ValueError(f"low_factor {low_factor}, high_factor {high_factor}")
+            keep = (trained_len * f / (2 * math.pi) - low_factor) / (high_factor - low_factor)
+            slow = 1 - keep.clamp(0, 1)
+        f = f * (1 - slow) + f / factor * slow
+    elif scaling not in (None, "ntk"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    return f.to(device), mscale
+
+
+def _heads(name, t):
+    """Row and head strides, in elements, of t [B][Nmax][H][d]."""
+    B, N, H, d = t.shape
+    if d > 1 and t.stride(3) != 1:
+        raise ValueError(f"{name}: a head's dims are not contiguous")
+    row = t.stride(1) if N > 1 else t.stride(0) if B > 1 else H * d
+    if B > 1 and t.stride(0) != N * row:
+        raise ValueError(f"{name}: rows are not evenly spaced over the batch")
+    return row, t.stride(2) if H > 1 else d
+
+
+def _frequencies(inv_freq):
+    import torch
+    _want("inv_freq", inv_freq, (torch.float64,), (_dims("inv_freq", inv_freq, 1)[0],))
+    return 2 * inv_freq.shape[0]
+
+
+def _span(t):
+    """First and past-the-last byte of a non-empty tensor's elements."""
+    size = t.element_size()
+    return t.data_ptr(), t.data_ptr() + size * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+
+
+def _in_place_or_apart(name, t, out):
+    """out is t itself or overlaps it nowhere."""
+    if t.data_ptr() == out.data_ptr() and _heads(name, t) == _heads(name, out):
+        return
+    (a0, a1), (b0, b1) = _span(t), _span(out)
+    if a0 < b1 and b0 < a1:
+        raise ValueError(f"{name}_out overlaps {name}")
+
+
+def tree_rope(q, q_out, inv_freq, prefix_len, n_rows, *, k=None, k_out=None, depth=None,
+              rot_offset: int = 0, interleaved: bool = False, mscale: float = 1.0,
+              validate: bool = False, status=None, stream=None):
+    """Rotary positions of queries ``[B][Nmax][Hq][d]`` and, if given, keys
+    ``[B][Nmax][Hk][d]`` (bfloat16 or float32, views with evenly spaced rows
+    welcome; the outputs may be the inputs); see ``ltd_tree_rope``.  inv_freq
+    ``[rot_dim / 2]`` float64 from ``rope_frequencies``, depth ``[B][Nmax]`` int32 for
+    a draft tree's rows."""
+    dtype = _dtype_code(q)
+    B, Nmax, Hq, d = _dims("q", q, 4)
+    rot_dim = _frequencies(inv_freq)
+    pairs = [("q", q, q_out)]
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out come together")
+    Hk = 0
+    if k is not None:
+        Hk = _dims("k", k, 4)[2]
+        if tuple(k.shape) != (B, Nmax, Hk, d):
+            raise ValueError(f"k has shape {tuple(k.shape)}, q {tuple(q.shape)}")
+        pairs.append(("k", k, k_out))
+    args = []
+    for name, t, out in pairs:
+        if t.dtype != q.dtype or out.dtype != q.dtype:
+            raise TypeError(f"{name} and {name}_out have types {t.dtype} and {out.dtype}, not {q.dtype}")
+        if out.shape != t.shape:
+            raise ValueError(f"{name}_out has shape {tuple(out.shape)}, not {tuple(t.shape)}")
+        args += [t, *_heads(name, t), out, *_heads(name + "_out", out)]
+    if rot_offset < 0 or rot_offset + rot_dim > d:
+        raise ValueError(f"dims {rot_offset} to {rot_offset + rot_dim} of {d}")
+    _int32((B,), prefix_len=prefix_len, n_rows=n_rows)
+    _int32((B, Nmax), depth=depth)
+    if B == 0 or Nmax == 0 or Hq == 0:
+        return
+    for name, t, out in pairs:
+        if t.numel():
+            _in_place_or_apart(name, t, out)
+    if Hk == 0:
+        args = args[:6] + [None, 0, 0, None, 0, 0]
+    _run("ltd_tree_rope",
+         (*(a if a is None or isinstance(a, int) else _p(a) for a in args), _p(inv_freq), _p(prefix_len),
+          _p(depth), _p(n_rows), B, Nmax, Hq, Hk, d, int(rot_offset), rot_dim, int(bool(interleaved)),
+          float(mscale), dtype, int(validate), _p(status)),
+         (q, q_out, k, k_out, inv_freq, prefix_len, depth, n_rows, status), stream)
+
+
+def _latent_cache(cache, block_table, num_blocks, lead):
+    """The geometry of a latent cache of `lead` leading dimensions (layers):
+    pages, rows of a page, row size, blocks a sequence."""
+    if cache.dim() != lead + 3:
+        raise ValueError(f"cache has {cache.dim()} dimensions, not {lead + 3}")
+    pages, kv_rows, d = cache.shape[lead:]
+    if not cache.is_contiguous():
+        raise ValueError("cache is not contiguous")
+    max_blocks = 0
+    if block_table is not None:
+        _int32(_dims("block_table", block_table, 2), block_table=block_table)
+        max_blocks = block_table.shape[1]
+        if num_blocks > pages:
+            raise ValueError(f"num_blocks is {num_blocks}, the cache holds {pages}")
+    return pages, kv_rows, d, max_blocks
+
+
+def latent_append(kv_new, cache, inv_freq, prefix_len, n_rows, *, depth=None, norm_weight=None,
+                  norm_eps: float = 1e-6, interleaved: bool = False, mscale: float = 1.0,
+                  block_table=None, num_blocks: int = 0, validate: bool = False, status=None,
+                  stream=None):
+    """Rows of a prompt or a draft tree into a latent cache; see
+    ``ltd_latent_append``.  kv_new ``[B][Nmax][d_latent + d_rope]`` (bfloat16 or
+    float32, a view with evenly spaced rows), cache ``[pages][rows][d_latent +
+    d_rope]``, inv_freq ``[d_rope / 2]`` float64, norm_weight ``[d_latent]``."""
+    pages, kv_rows, D, max_blocks = _latent_cache(cache, block_table, num_blocks, 0)
+    dtype = _dtype_code(kv_new)
+    if cache.dtype != kv_new.dtype:
+        raise TypeError(f"kv_new has type {kv_new.dtype}, cache {cache.dtype}")
+    B, Nmax, d = _dims("kv_new", kv_new, 3)
+    d_rope = _frequencies(inv_freq)
+    if d != D or d_rope >= d:
+        raise ValueError(f"rows of {d} with {d_rope} rotated dims, the cache's have {D}")
+    if norm_weight is not None:
+        _want("norm_weight", norm_weight, (kv_new.dtype,), (d - d_rope,))
+    _batch_pages(B, pages, block_table)
+    _int32((B,), prefix_len=prefix_len, n_rows=n_rows)
+    _int32((B, Nmax), depth=depth)
+    if B == 0 or Nmax == 0:
+        return
+    row, _ = _heads("kv_new", kv_new.unsqueeze(2))
+    _run("ltd_latent_append",
+         (_p(kv_new), row, _p(norm_weight), float(norm_eps), _p(inv_freq), int(bool(interleaved)),
+          float(mscale), _p(cache), _p(block_table), _p(prefix_len), _p(depth), _p(n_rows), B, Nmax,
+          d - d_rope, d_rope, kv_rows, max_blocks, int(num_blocks), dtype, int(validate), _p(status)),
+         (kv_new, cache, inv_freq, prefix_len, n_rows, depth, norm_weight, block_table, status), stream)
+
+
+def attn_latent_workspace_size(B, Nmax, Hq, d_latent, d_rope, max_prefix, dtype) -> int:
+    return int(lib().ltd_tree_verify_attn_latent_workspace_size(B, Nmax, Hq, d_latent, d_rope, max_prefix,
+                                                                dtype))
+
+
+def tree_verify_attn_latent(q_latent, q_rope, cache, prefix_len, parents, n_nodes, out, *,
+                            max_prefix: int, scale: float, block_table=None, num_blocks: int = 0,
+                            workspace=None, validate: bool = False, status=None, stream=None):
+    """Tree attention over a latent cache; see ``ltd_tree_verify_attn_latent``.
+    q_latent ``[B][Nmax][Hq][d_latent]`` and q_rope ``[B][Nmax][Hq][d_rope]`` with any row
+    and head strides, out ``[B][Nmax][Hq][d_latent]``, the cache as for
+    ``latent_append``."""
+    pages, kv_rows, D, max_blocks = _latent_cache(cache, block_table, num_blocks, 0)
+    dtype = _dtype_code(q_latent)
+    B, Nmax, Hq, d_latent = _dims("q_latent", q_latent, 4)
+    d_rope = _dims("q_rope", q_rope, 4)[3]
+    if q_rope.dtype != q_latent.dtype or cache.dtype != q_latent.dtype:
+        raise TypeError(f"q_latent has type {q_latent.dtype}, q_rope {q_rope.dtype}, cache {cache.dtype}")
+    if tuple(q_rope.shape[:3]) != (B, Nmax, Hq) or d_latent + d_rope != D:
+        raise ValueError(f"q_latent {tuple(q_latent.shape)}, q_rope {tuple(q_rope.shape)}, cache rows of {D}")
+    _want("out", out, (q_latent.dtype,), (B, Nmax, Hq, d_latent))
+    _batch_pages(B, pages, block_table)
+    _int32((B,), prefix_len=prefix_len, n_nodes=n_nodes)
+    _int32((B, Nmax), parents=parents)
+    if workspace is None:
+        workspace = _workspace_for(
+            stream, attn_latent_workspace_size(B, Nmax, Hq, d_latent, d_rope, max_prefix, dtype),
+            q_latent.device)
+    _run("ltd_tree_verify_attn_latent",
+         (_p(q_latent), *_heads("q_latent", q_latent), _p(q_rope), *_heads("q_rope", q_rope), _p(cache),
+          _p(block_table), _p(prefix_len), _p(parents), _p(n_nodes), _p(out), B, Nmax, Hq, d_latent,
+          d_rope, int(max_prefix), kv_rows, max_blocks, int(num_blocks), float(scale), dtype,
+          *_space(workspace), int(validate), _p(status)),
+         (q_latent, q_rope, cache, block_table, prefix_len, parents, n_nodes, out, workspace, status),
+         stream)
+    return out
+
+
+def latent_compact(cache, prefix_len, new_prefix_len, accepted_nodes, n_accepted, *,
+                   d_rope: int = LATENT_ROPE, block_table=None, num_blocks: int = 0,
+                   validate: bool = False, status=None, stream=None):
+    """In-place compaction of a latent cache ``[pages][rows][d]`` or, for all layers at
+    once, ``[layers][pages][rows][d]``; see ``ltd_latent_compact``."""
+    lead = cache.dim() - 3
+    if lead not in (0, 1):
+        raise ValueError(f"cache has {cache.dim()} dimensions, not 3 or 4")
+    pages, kv_rows, D, max_blocks = _latent_cache(cache, block_table, num_blocks, lead)
+    layers = cache.shape[0] if lead else 1
+    B, Nmax = _dims("accepted_nodes", accepted_nodes, 2)
+    _batch_pages(B, pages, block_table)
+    _int32((B, Nmax), accepted_nodes=accepted_nodes)
+    _int32((B,), prefix_len=prefix_len, new_prefix_len=new_prefix_len, n_accepted=n_accepted)
+    _run("ltd_latent_compact",
+         (_p(cache), _p(block_table), _p(prefix_len), _p(new_prefix_len), _p(accepted_nodes),
+          _p(n_accepted), B, Nmax, D - d_rope, d_rope, kv_rows, max_blocks, int(num_blocks), layers,
+          cache.stride(0) if lead else 0, _dtype_code(cache), int(validate), _p(status)),
+         (cache, block_table, prefix_len, new_prefix_len, accepted_nodes, n_accepted, status), stream)

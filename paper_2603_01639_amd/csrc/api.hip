@@ -554,4 +554,190 @@ int ltd_tree_accept_processed(const float* logits, const int32_t* draft_tokens,
   return LTD_OK;
 }
 
+namespace {
+
+bool dtype_known(int dtype) { return dtype == LTD_DTYPE_F32 || dtype == LTD_DTYPE_BF16; }
+bool latent_supported(int d_latent, int d_rope) {
+  return (d_latent == 256 || d_latent == 512) && d_rope == LTD_LATENT_ROPE;
+}
+
+}  // namespace
+
+int ltd_tree_rope(const void* q, int64_t q_row_stride, int64_t q_head_stride, void* q_out,
+                  int64_t q_out_row_stride, int64_t q_out_head_stride, const void* k,
+                  int64_t k_row_stride, int64_t k_head_stride, void* k_out,
+                  int64_t k_out_row_stride, int64_t k_out_head_stride, const double* inv_freq,
+                  const int32_t* prefix_len, const int32_t* depth, const int32_t* n_rows, int B,
+                  int Nmax, int Hq, int Hk, int d, int rot_offset, int rot_dim, int interleaved,
+                  float mscale, int dtype, int validate, int32_t* status, void* stream) {
+  if (B < 0 || Nmax < 1 || Hq < 1 || Hk < 0 || d < 1 || rot_dim < 2 || rot_dim % 2 != 0 ||
+      rot_offset < 0 || static_cast<int64_t>(rot_offset) + rot_dim > d || !std::isfinite(mscale))
+    return LTD_EINVAL;
+  if (!dtype_known(dtype) || d > LTD_ROPE_MAX_DIM || Nmax > LTD_MAX_LENGTH ||
+      (static_cast<int64_t>(Hq) + Hk) * d > (1 << 24))
+    return LTD_EUNSUPPORTED;
+  if (validate && !status) return LTD_EINVAL;
+  if (B == 0) return LTD_OK;
+  if (!q || !q_out || (Hk > 0 && (!k || !k_out)) || !inv_freq || !prefix_len || !n_rows)
+    return LTD_EINVAL;
+  // (in place means the same places)
+  if (q == q_out && (q_row_stride != q_out_row_stride || q_head_stride != q_out_head_stride))
+    return LTD_EINVAL;
+  if (Hk > 0 && k == k_out && (k_row_stride != k_out_row_stride || k_head_stride != k_out_head_stride))
+    return LTD_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (validate) {
+    if (ltd::launch_validate_rows(prefix_len, depth, n_rows, B, Nmax, status, st) != hipSuccess)
+      return LTD_EHIP;
+  }
+  ltd::RopeArgs a{};
+  a.x[0] = q;
+  a.x[1] = k;
+  a.y[0] = q_out;
+  a.y[1] = k_out;
+  a.x_row[0] = q_row_stride;
+  a.x_row[1] = k_row_stride;
+  a.x_head[0] = q_head_stride;
+  a.x_head[1] = k_head_stride;
+  a.y_row[0] = q_out_row_stride;
+  a.y_row[1] = k_out_row_stride;
+  a.y_head[0] = q_out_head_stride;
+  a.y_head[1] = k_out_head_stride;
+  a.H[0] = Hq;
+  a.H[1] = Hk;
+  a.freq = inv_freq;
+  a.prefix_len = prefix_len;
+  a.depth = depth;
+  a.n_rows = n_rows;
+  a.status = validate ? status : nullptr;
+  a.B = B;
+  a.Nmax = Nmax;
+  a.d = d;
+  a.off = rot_offset;
+  a.rot = rot_dim;
+  a.interleaved = interleaved != 0;
+  a.m = mscale;
+  return ltd::launch_rope(a, dtype, st) == hipSuccess ? LTD_OK : LTD_EHIP;
+}
+
+int ltd_latent_append(const void* kv_new, int64_t new_row_stride, const void* norm_weight,
+                      float norm_eps, const double* inv_freq, int interleaved, float mscale,
+                      void* cache, const int32_t* block_table, const int32_t* prefix_len,
+                      const int32_t* depth, const int32_t* n_rows, int B, int Nmax, int d_latent,
+                      int d_rope, int kv_rows, int max_blocks, int num_blocks, int dtype,
+                      int validate, int32_t* status, void* stream) {
+  if (B < 0 || Nmax < 1 || kv_rows < 1 || !(norm_eps >= 0.f) || !std::isfinite(norm_eps) ||
+      !std::isfinite(mscale))
+    return LTD_EINVAL;
+  if (!dtype_known(dtype) || !latent_supported(d_latent, d_rope) || Nmax > LTD_MAX_LENGTH)
+    return LTD_EUNSUPPORTED;
+  if (block_table && (max_blocks < 1 || num_blocks < 1)) return LTD_EINVAL;
+  if (new_row_stride < d_latent + d_rope) return LTD_EINVAL;
+  if (validate && !status) return LTD_EINVAL;
+  if (B == 0) return LTD_OK;
+  if (!kv_new || !inv_freq || !cache || !prefix_len || !n_rows) return LTD_EINVAL;
+  if (!aligned16(kv_new) || new_row_stride * (dtype == LTD_DTYPE_F32 ? 4 : 2) % 16 != 0 ||
+      !aligned16(cache) || !aligned16(norm_weight))
+    return LTD_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (validate) {
+    if (ltd::launch_validate_append(block_table, prefix_len, n_rows, B, Nmax, kv_rows, max_blocks,
+                                    num_blocks, status, st) != hipSuccess)
+      return LTD_EHIP;
+  }
+  const ltd::LatentAppendArgs a{kv_new, new_row_stride, norm_weight, inv_freq, cache, block_table, prefix_len, depth,
+                                n_rows, validate ? status : nullptr, B, Nmax, kv_rows, max_blocks,
+                                interleaved != 0, mscale, norm_eps};
+  return ltd::launch_latent_append(a, d_latent, dtype, st) == hipSuccess ? LTD_OK : LTD_EHIP;
+}
+
+namespace {
+bool latent_attn_args_ok(int B, int Nmax, int Hq, int max_prefix) {
+  return B >= 0 && Nmax >= 1 && Nmax <= LTD_MAX_NODES && Hq >= 1 && max_prefix >= 0;
+}
+}  // namespace
+
+size_t ltd_tree_verify_attn_latent_workspace_size(int B, int Nmax, int Hq, int d_latent,
+                                                  int d_rope, int max_prefix, int dtype) {
+  if (!latent_attn_args_ok(B, Nmax, Hq, max_prefix) || !dtype_known(dtype) ||
+      !latent_supported(d_latent, d_rope) || max_prefix > LTD_MAX_LENGTH)
+    return 0;
+  ltd::LatentAttn s{};
+  s.B = B;
+  s.Nmax = Nmax;
+  s.Hq = Hq;
+  s.max_prefix = max_prefix;
+  return ltd::latent_attn_workspace_bytes(s, d_latent, dtype, device_cu_count());
+}
+
+int ltd_tree_verify_attn_latent(const void* q_latent, int64_t ql_row_stride,
+                                int64_t ql_head_stride, const void* q_rope, int64_t qr_row_stride,
+                                int64_t qr_head_stride, const void* cache,
+                                const int32_t* block_table, const int32_t* prefix_len,
+                                const int32_t* parents, const int32_t* n_nodes, void* out, int B,
+                                int Nmax, int Hq, int d_latent, int d_rope, int max_prefix,
+                                int kv_rows, int max_blocks, int num_blocks, float scale,
+                                int dtype, void* workspace, size_t workspace_bytes, int validate,
+                                int32_t* status, void* stream) {
+  if (!latent_attn_args_ok(B, Nmax, Hq, max_prefix) || kv_rows < 1) return LTD_EINVAL;
+  if (!(scale > 0.f) || !std::isfinite(scale)) return LTD_EINVAL;
+  if (!dtype_known(dtype) || !latent_supported(d_latent, d_rope) || max_prefix > LTD_MAX_LENGTH ||
+      (dtype == LTD_DTYPE_F32 && B > 65535))
+    return LTD_EUNSUPPORTED;
+  if (block_table && (max_blocks < 1 || num_blocks < 1)) return LTD_EINVAL;
+  if (validate && !status) return LTD_EINVAL;
+  if (B == 0) return LTD_OK;
+  if (!q_latent || !q_rope || !cache || !prefix_len || !parents || !n_nodes || !out)
+    return LTD_EINVAL;
+  if (!aligned16(cache) || !aligned16(out)) return LTD_EINVAL;
+  if (dtype == LTD_DTYPE_BF16 &&
+      (!aligned16(q_latent) || !aligned16(q_rope) || ql_row_stride % 8 != 0 ||
+       ql_head_stride % 8 != 0 || qr_row_stride % 8 != 0 || qr_head_stride % 8 != 0))
+    return LTD_EINVAL;
+  const ltd::LatentAttn s{q_latent, q_rope, ql_row_stride, ql_head_stride, qr_row_stride, qr_head_stride, cache,
+                          block_table, prefix_len, parents, n_nodes, out, validate ? status : nullptr, B, Nmax, Hq,
+                          max_prefix, kv_rows, max_blocks, scale};
+  const int cus = device_cu_count();
+  const size_t need = ltd::latent_attn_workspace_bytes(s, d_latent, dtype, cus);
+  if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return LTD_EWORKSPACE;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (validate) {
+    if (ltd::launch_validate_tree(block_table, prefix_len, parents, n_nodes, B, Nmax, max_prefix,
+                                  kv_rows, max_blocks, num_blocks, true, status, st) != hipSuccess)
+      return LTD_EHIP;
+  }
+  return ltd::launch_latent_attn(s, d_latent, dtype, workspace, cus, st) == hipSuccess ? LTD_OK : LTD_EHIP;
+}
+
+int ltd_latent_compact(void* cache, const int32_t* block_table, const int32_t* prefix_len,
+                       int32_t* new_prefix_len, const int32_t* accepted_nodes,
+                       const int32_t* n_accepted, int B, int Nmax, int d_latent, int d_rope,
+                       int kv_rows, int max_blocks, int num_blocks, int num_layers,
+                       int64_t layer_stride_elems, int dtype, int validate, int32_t* status,
+                       void* stream) {
+  if (B < 0 || Nmax < 1 || Nmax > LTD_MAX_NODES || kv_rows < 1 || num_layers < 1 ||
+      num_layers > 65535 || layer_stride_elems < 0)
+    return LTD_EINVAL;
+  if (!dtype_known(dtype) || !latent_supported(d_latent, d_rope)) return LTD_EUNSUPPORTED;
+  if (block_table && (max_blocks < 1 || num_blocks < 1)) return LTD_EINVAL;
+  if (validate && !status) return LTD_EINVAL;
+  if (B == 0) return LTD_OK;
+  if (!cache || !prefix_len || !new_prefix_len || !accepted_nodes || !n_accepted) return LTD_EINVAL;
+  if (new_prefix_len == prefix_len) return LTD_EINVAL;
+  const int elem = dtype == LTD_DTYPE_F32 ? 4 : 2;
+  if (!aligned16(cache) ||
+      (num_layers > 1 && (layer_stride_elems == 0 || layer_stride_elems * elem % 16 != 0)))
+    return LTD_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (validate) {
+    if (ltd::launch_validate_path(block_table, prefix_len, accepted_nodes, n_accepted, B, Nmax,
+                                  kv_rows, max_blocks, num_blocks, status, st) != hipSuccess)
+      return LTD_EHIP;
+  }
+  const ltd::LatentCompactArgs a{cache, block_table, prefix_len, new_prefix_len, accepted_nodes, n_accepted,
+                                 validate ? status : nullptr, layer_stride_elems * elem, Nmax,
+                                 (d_latent + d_rope) * elem, kv_rows, max_blocks};
+  return ltd::launch_latent_compact(a, B, num_layers, st) == hipSuccess ? LTD_OK : LTD_EHIP;
+}
+
 }  // extern "C"

@@ -1,0 +1,175 @@
+// The latent cache's writes: appending a prompt's or a draft tree's rows, and
+// moving the accepted rows next to the prefix (arXiv 2603.01639, section 3.2: the
+// candidates after the first mismatch are discarded).
+//
+// A cache row holds one token's latent part (d_latent dims, the key and value
+// of every head) and its rotated part (d_rope dims, key alone).
+//
+// Append: a wave a row.  The latent part's mean square is a wave reduction over
+// registers, the rotated part's angles are computed by the lanes (a pair each)
+// and handed over by lane exchanges, so a row is read and written once and
+// nothing goes through LDS.  Bound: HBM, or the launch for a tree's rows.
+#include "ltd_device.hpp"
+#include "ltd_launch.hpp"
+#include "rope.hpp"
+
+namespace ltd {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+constexpr int kRopeDims = 64;  // d_rope
+constexpr int kPairs = kRopeDims / 2;
+
+template <typename T>
+struct Piece {  // 16 bytes
+  static constexpr int N = 16 / sizeof(T);
+  typedef T V __attribute__((ext_vector_type(16 / sizeof(T))));
+  V v;
+  __device__ __forceinline__ void load(const T* p) { v = *reinterpret_cast<const V*>(p); }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<V*>(p) = v; }
+  __device__ __forceinline__ float get(int i) const { return static_cast<float>(v[i]); }
+};
+
+template <typename T, int DL>
+__global__ void __launch_bounds__(kThreads) latent_append_kernel(LatentAppendArgs a) {
+  constexpr int N = Piece<T>::N;
+  constexpr int D = DL + kRopeDims;
+  constexpr int kPieces = DL / N;                             // of the latent part
+  constexpr int kIter = (kPieces + kWave - 1) / kWave;        // a lane's
+  if (halted(a.status)) return;
+  const int lane = threadIdx.x % kWave;
+  const int64_t waves = static_cast<int64_t>(gridDim.x) * (kThreads / kWave);
+  const int64_t all = static_cast<int64_t>(a.B) * a.Nmax;
+  for (int64_t at = static_cast<int64_t>(blockIdx.x) * (kThreads / kWave) + threadIdx.x / kWave; at < all; at += waves) {
+    const int b = static_cast<int>(at / a.Nmax), i = static_cast<int>(at % a.Nmax);
+    if (i >= a.n_rows[b]) continue;
+    const T* src = static_cast<const T*>(a.x) + at * a.x_row;
+    Piece<T> c[kIter], w[kIter], r0, r1;
+#pragma unroll
+    for (int k = 0; k < kIter; ++k)
+      if (lane + k * kWave < kPieces) {
+        c[k].load(src + (lane + k * kWave) * N);
+        if (a.weight) w[k].load(static_cast<const T*>(a.weight) + (lane + k * kWave) * N);
+      }
+    // The rotated part: lanes below kRopeDims / N (neighbouring pairs) or half of
+    // that (halves: a lane has the first and the second values of its pairs).
+    const int turning = a.interleaved ? kRopeDims / N : kPairs / N;
+    if (lane < turning) {
+      r0.load(src + DL + lane * N);
+      if (!a.interleaved) r1.load(src + DL + kPairs + lane * N);
+    }
+    const int64_t P = a.prefix_len[b];
+    const int64_t pos = P + (a.depth ? a.depth[at] : i);
+    const float2 t = rope_turn(pos, a.freq[lane % kPairs], a.m);
+    const int row = static_cast<int>(P) + i;
+    T* dst = static_cast<T*>(a.cache) + cache_row(a.block_table, b, 0, row, 1, D, a.kv_rows, a.max_blocks);
+    if (a.weight) {
+      float ss = 0.f;
+#pragma unroll
+      for (int k = 0; k < kIter; ++k)
+        if (lane + k * kWave < kPieces)
+#pragma unroll
+          for (int e = 0; e < N; ++e) ss = __builtin_fmaf(c[k].get(e), c[k].get(e), ss);
+      ss = wave_sum_dpp(ss);
+      const float rs = 1.f / __builtin_sqrtf(ss * (1.f / DL) + a.eps);
+#pragma unroll
+      for (int k = 0; k < kIter; ++k)
+        if (lane + k * kWave < kPieces)
+#pragma unroll
+          for (int e = 0; e < N; ++e) c[k].v[e] = static_cast<T>(c[k].get(e) * rs * w[k].get(e));
+    }
+#pragma unroll
+    for (int k = 0; k < kIter; ++k)
+      if (lane + k * kWave < kPieces) c[k].store(dst + (lane + k * kWave) * N);
+    // (every lane takes part in the exchanges)
+    if (a.interleaved) {
+#pragma unroll
+      for (int e = 0; e < N / 2; ++e) {
+        const int from = (lane * (N / 2) + e) % kPairs;
+        const float cs = __shfl(t.x, from, kWave), sn = __shfl(t.y, from, kWave);
+        const float p0 = r0.get(2 * e), p1 = r0.get(2 * e + 1);
+        r0.v[2 * e] = static_cast<T>(p0 * cs - p1 * sn);
+        r0.v[2 * e + 1] = static_cast<T>(p1 * cs + p0 * sn);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const int from = (lane * N + e) % kPairs;
+        const float cs = __shfl(t.x, from, kWave), sn = __shfl(t.y, from, kWave);
+        const float p0 = r0.get(e), p1 = r1.get(e);
+        r0.v[e] = static_cast<T>(p0 * cs - p1 * sn);
+        r1.v[e] = static_cast<T>(p1 * cs + p0 * sn);
+      }
+    }
+    if (lane < turning) {
+      r0.store(dst + DL + lane * N);
+      if (!a.interleaved) r1.store(dst + DL + kPairs + lane * N);
+    }
+  }
+}
+
+// Compaction: one workgroup per (sequence, layer); rows move in ascending passes
+// that read all their sources before the first write.  Row j comes from P +
+// path[j], path[j] >= j, so a later pass's sources lie past every destination
+// already written.
+constexpr int kMoves = 4;  // 16-byte pieces of a pass that a thread holds
+
+__global__ void __launch_bounds__(kThreads) latent_compact_kernel(LatentCompactArgs a) {
+  if (halted(a.status)) return;
+  const int b = blockIdx.x, layer = blockIdx.y;
+  const int32_t* path = a.accepted_nodes + static_cast<int64_t>(b) * a.Nmax;
+  const int P = a.prefix_len[b];
+  const int n = a.n_accepted[b];
+  unsigned char* base = static_cast<unsigned char*>(a.cache) + layer * a.layer_stride_bytes;
+  const int per_row = a.row_bytes / 16;
+  const int rows = kThreads * kMoves / per_row;  // of a pass
+  for (int j0 = 0; j0 < n; j0 += rows) {
+    u32x4 v[kMoves];
+    int64_t to[kMoves];
+#pragma unroll
+    for (int k = 0; k < kMoves; ++k) {
+      const int e = threadIdx.x + k * kThreads;
+      const int j = j0 + e / per_row, col = e % per_row;
+      to[k] = -1;
+      if (e / per_row < rows && j < n) {
+        const int pj = path[j];
+        if (pj != j) {
+          const int64_t from = cache_row(a.block_table, b, 0, P + pj, 1, a.row_bytes, a.kv_rows, a.max_blocks);
+          to[k] = cache_row(a.block_table, b, 0, P + j, 1, a.row_bytes, a.kv_rows, a.max_blocks) + col * 16;
+          v[k] = *reinterpret_cast<const u32x4*>(base + from + col * 16);
+        }
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kMoves; ++k)
+      if (to[k] >= 0) *reinterpret_cast<u32x4*>(base + to[k]) = v[k];
+    __syncthreads();
+  }
+  if (layer == 0 && threadIdx.x == 0) a.new_prefix_len[b] = P + n;
+}
+
+}  // namespace
+
+hipError_t launch_latent_append(const LatentAppendArgs& a, int d_latent, int dtype, hipStream_t stream) {
+  const int64_t all = static_cast<int64_t>(a.B) * a.Nmax;
+  const int64_t groups = (all + kThreads / kWave - 1) / (kThreads / kWave);
+  const dim3 grid(static_cast<unsigned>(groups < (1 << 20) ? groups : (1 << 20)));
+  if (dtype == LTD_DTYPE_F32) {
+    if (d_latent == 512) hipLaunchKernelGGL((latent_append_kernel<float, 512>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((latent_append_kernel<float, 256>), grid, dim3(kThreads), 0, stream, a);
+  } else {
+    if (d_latent == 512) hipLaunchKernelGGL((latent_append_kernel<__bf16, 512>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((latent_append_kernel<__bf16, 256>), grid, dim3(kThreads), 0, stream, a);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_latent_compact(const LatentCompactArgs& a, int B, int num_layers, hipStream_t stream) {
+  hipLaunchKernelGGL(latent_compact_kernel, dim3(B, num_layers), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace ltd

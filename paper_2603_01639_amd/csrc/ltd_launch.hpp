@@ -161,4 +161,76 @@ hipError_t launch_token_counts(const int32_t* tokens, const int32_t* n_tokens, i
 hipError_t launch_rules(const LogitRules& rules, int B, int Nmax, int Voc, float* out,
                         void* partial, int cus, const int32_t* status, hipStream_t stream);
 
+// rope.hip
+struct RopeArgs {
+  const void* x[2];  // queries and keys ...
+  void* y[2];        // ... and where they go
+  int64_t x_row[2], x_head[2], y_row[2], y_head[2];  // elements from one row (head) to the next
+  int H[2];                                          // heads (0: none)
+  const double* freq;
+  const int32_t* prefix_len;
+  const int32_t* depth;
+  const int32_t* n_rows;
+  const int32_t* status;
+  int B, Nmax, d, off, rot;
+  int interleaved;
+  float m;
+  int rows, copies;  // set by the launcher: rows a workgroup, whether the other dims are copied
+};
+hipError_t launch_rope(RopeArgs a, int dtype, hipStream_t stream);
+hipError_t launch_validate_rows(const int32_t* prefix_len, const int32_t* depth,
+                                const int32_t* n_rows, int B, int Nmax, int32_t* status,
+                                hipStream_t stream);
+
+// latent_cache.hip
+struct LatentAppendArgs {
+  const void* x;
+  int64_t x_row;
+  const void* weight;  // null: the latent part as it is
+  const double* freq;
+  void* cache;
+  const int32_t* block_table;
+  const int32_t* prefix_len;
+  const int32_t* depth;
+  const int32_t* n_rows;
+  const int32_t* status;
+  int B, Nmax, kv_rows, max_blocks;
+  int interleaved;
+  float m, eps;
+};
+hipError_t launch_latent_append(const LatentAppendArgs& a, int d_latent, int dtype,
+                                hipStream_t stream);
+struct LatentCompactArgs {
+  void* cache;
+  const int32_t* block_table;
+  const int32_t* prefix_len;
+  int32_t* new_prefix_len;
+  const int32_t* accepted_nodes;
+  const int32_t* n_accepted;
+  const int32_t* status;
+  int64_t layer_stride_bytes;
+  int Nmax, row_bytes, kv_rows, max_blocks;
+};
+hipError_t launch_latent_compact(const LatentCompactArgs& a, int B, int num_layers,
+                                 hipStream_t stream);
+
+// latent_attn.hip
+struct LatentAttn {
+  const void* q_latent;
+  const void* q_rope;
+  int64_t ql_row, ql_head, qr_row, qr_head;  // elements from one row (head) to the next
+  const void* cache;
+  const int32_t* block_table;
+  const int32_t* prefix_len;
+  const int32_t* parents;
+  const int32_t* n_nodes;
+  void* out;
+  const int32_t* status;
+  int B, Nmax, Hq, max_prefix, kv_rows, max_blocks;
+  float scale;
+};
+size_t latent_attn_workspace_bytes(const LatentAttn& s, int d_latent, int dtype, int cus);
+hipError_t launch_latent_attn(const LatentAttn& s, int d_latent, int dtype, void* workspace,
+                              int cus, hipStream_t stream);
+
 }  // namespace ltd
