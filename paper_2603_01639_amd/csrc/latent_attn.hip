@@ -125,11 +125,14 @@ __device__ __forceinline__ int rare_thread() {
   return t;
 }
 
-// S^T's products, with the accumulators in vector registers: O's take all 256
-// accumulation registers, and the compiler, which keeps every product's there,
-// would move them out and in for S each tile.  A product may follow one that it
-// adds to at once; what else reads the sum waits for it (mfma_settle: 18 wait
-// states after a product of 8 passes).
+// The products by hand: O's accumulators take all 256 accumulation registers, and S's
+// go to vector registers (the compiler would keep both in the former, and move O out
+// and in for every tile).  A product may follow one that it adds to at once; what
+// else reads a sum waits for it, 18 wait states at most after a product of 8 passes
+// (mfma_settle), which nobody else sees to.
+__device__ __forceinline__ void mfma_acc(f32x16& o, bf16x8 a, bf16x8 b) {
+  asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o) : "v"(a), "v"(b));
+}
 __device__ __forceinline__ void mfma_first(f32x16& s, bf16x8 a, bf16x8 b) {
   asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
 }
@@ -137,6 +140,7 @@ __device__ __forceinline__ void mfma_next(f32x16& s, bf16x8 a, bf16x8 b) {
   asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void mfma_settle(f32x16& s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s)); }
+__device__ __forceinline__ void mfma_settle_acc(f32x16& o) { asm volatile("s_nop 15\n\ts_nop 7" : "+a"(o)); }
 
 // A direct load of 16 bytes a lane (lane i's land at lds + 16 i) from kOff bytes past
 // p.  (The instruction's offset moves its place in LDS as well, so that is taken back.)
@@ -299,7 +303,6 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
         }
       }
     }
-    if (threadIdx.x < 2 * kWaves) sm.moved[threadIdx.x / kWaves][threadIdx.x % kWaves] = 0;
     __syncthreads();
 
     float m_run = kNoMax, l_run = 0.f;
@@ -312,6 +315,12 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
         asm volatile("" : "+a"(o[db][g]));
       }
     const float c = a.scale_log2;
+    auto settle_all = [&] {
+#pragma unroll
+      for (int db = 0; db < kDB; ++db)
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) mfma_settle_acc(o[db][g]);
+    };
 
     // bits base .. base + 15 of a node's visible tree keys (earlier ones are the prefix)
     auto visible = [&](int base) -> uint32_t {
@@ -323,124 +332,213 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
       return static_cast<uint32_t>(two >> (base & 31)) & 0xFFFFu;
     };
 
+    // The weights of the tile whose scores are in s, in 16 pieces (each beside one of
+    // the other products): the maximum, which moves only when a score passes it by
+    // 2^kLazyMax, two weights a piece, and what follows from them.
+    float alpha = 1.f, top, neg, ps;
+    u32x4 pk[2];
+    auto weigh = [&](auto piece, const f32x16& s, int par) {
+      constexpr int i = piece();
+      if constexpr (i < 4) {
+        if constexpr (i == 0) top = s[0];
+        top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top, s[4 * i]), s[4 * i + 1]);
+        top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top, s[4 * i + 2]), s[4 * i + 3]);
+      } else if constexpr (i == 4) {
+        top = max_xor32(top);
+        const float m_new = top > m_run + a.lazy_gap ? top : m_run;
+        neg = fminf(-m_new * c, __FLT_MAX__);
+        alpha = exp2_fast((m_run - m_new) * c);  // (1 where it has not moved)
+        m_run = m_new;
+        ps = 0.f;
+      } else if constexpr (i < 13) {
+        constexpr int j = i - 5;
+        const float p0 = exp2_fast(__builtin_fmaf(s[2 * j], c, neg));
+        const float p1 = exp2_fast(__builtin_fmaf(s[2 * j + 1], c, neg));
+        // (the sum is that of the rounded weights, the very ones that multiply the values)
+        const bf16x2 w = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
+        ps = __builtin_amdgcn_fdot2_f32_bf16(w, __builtin_bit_cast(bf16x2, 0x3F803F80u), ps, false);
+        pk[j >> 2][j & 3] = __builtin_bit_cast(uint32_t, w);
+        if constexpr (j == 3) *reinterpret_cast<u32x4*>(sm.p[par][2 * h][32 * wave + l32]) = pk[0];
+      } else if constexpr (i == 13) {
+        *reinterpret_cast<u32x4*>(sm.p[par][2 * h + 1][32 * wave + l32]) = pk[1];
+        l_run = l_run * alpha + ps;
+      }
+    };
+    // Tells the other waves what the rows' sums so far are multiplied by.
+    auto tell = [&](int par) {
+      const uint64_t any = __ballot(alpha != 1.f);
+      if (any != 0) sm.alpha[par][32 * wave + l32] = alpha;
+      if (lane == 0) sm.moved[par][wave] = any != 0;
+    };
+    // Hides the keys that the lane's node does not see.  A tree key whose latent part
+    // holds a NaN or an infinity (bad) gives NaN to the nodes that see it.
+    auto mask = [&](f32x16& s, int t, uint32_t bad) {
+      const uint32_t vis = visible(t * kKeys - P + 16 * h);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if (!((vis >> r) & 1u)) s[r] = -INFINITY;
+        else if ((bad >> (16 * h + r)) & 1u) s[r] = NAN;
+      }
+    };
+    auto masked = [&](int t) { return (t + 1) * static_cast<int64_t>(kKeys) > P; };
+    // The keys of tile t (landed) whose latent part is not finite; the whole
+    // workgroup looks.
+    auto find_bad = [&](int t) -> uint32_t {
+      const unsigned char* kv = sm.kv[t % kStages];
+      if (threadIdx.x == 0) sm.bad[t & 1] = 0;
+      __syncthreads();
+#pragma unroll 1
+      for (int e = rare_thread(); e < kKeys * DL / 8; e += kThreads) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(kv + e * 16);
+        uint32_t any = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          any |= ((x[j] & 0x7F80u) == 0x7F80u) | ((x[j] & 0x7F800000u) == 0x7F800000u);
+        if (any) atomicOr(&sm.bad[t & 1], 1u << (e / 8 % kKeys));
+      }
+      __syncthreads();
+      return __builtin_amdgcn_readfirstlane(sm.bad[t & 1]);
+    };
+    // 0 times a NaN would be one in the rows that do not see it.
+    auto clear_bad = [&](int t, uint32_t bad) {
+      unsigned char* kv = sm.kv[t % kStages];
+#pragma unroll 1
+      for (int e = rare_thread(); e < kKeys * DL / 8; e += kThreads)
+        if ((bad >> (e / 8 % kKeys)) & 1u) *reinterpret_cast<u32x4*>(kv + e * 16) = u32x4{0, 0, 0, 0};
+      __syncthreads();
+    };
+
+    auto load_k = [&](const unsigned char* kv, int kk) {
+      return *reinterpret_cast<const bf16x8*>(kv + k_rd[kk & 3] + (kk >> 2) * kPlane);
+    };
+    auto load_v = [&](const unsigned char* kv, int db, int ks) {
+      const unsigned char* at = kv + v_rd[db & 1][ks] + (db >> 1) * kPlane;
+      const s16x4 lo = lds_read_tr(at), hi = lds_read_tr(at + 4 * 128);
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto load_p = [&](int par, int g, int ks) {
+      return *reinterpret_cast<const bf16x8*>(sm.p[par][2 * ks + h][32 * g + l32]);
+    };
+
+    // One step: the scores and weights of tile t (kS) with the product of tile
+    // t - 1's weights and values (kPV).  The score products and the first half
+    // of the other ones alternate, which spreads the key reads (all that LDS can
+    // give while scores alone run) over both; the weights are then worked out
+    // beside the second half.
+    constexpr int kPV1 = kDB * kGroups;  // products of 16 keys
+    auto step = [&](auto with_s, auto with_pv, int t, uint32_t bad) {
+      constexpr bool kS = with_s(), kPV = with_pv();
+      const unsigned char* kv = sm.kv[t % kStages];
+      const unsigned char* kv_old = sm.kv[(t + kStages - 1) % kStages];
+      const int par = t & 1;
+      f32x16 s;
+      bf16x8 kf[kAhead], vf[kDB], pf[2];
+      if constexpr (kS) {
+#pragma unroll
+        for (int kk = 0; kk < kAhead; ++kk) kf[kk] = load_k(kv, kk);
+      }
+      if constexpr (kPV) {
+#pragma unroll
+        for (int db = 0; db < kDB; ++db) vf[db] = load_v(kv_old, db, 0);
+        pf[0] = load_p(par ^ 1, 0, 0);
+      }
+      // product i of 16 keys ks: rows g, dims db
+      auto pv = [&](auto ix, auto half) {
+        constexpr int i = ix(), g = i / kDB, db = i % kDB, ks = half();
+        if constexpr (db == 0 && g + 1 < kGroups) pf[(g + 1) & 1] = load_p(par ^ 1, g + 1, ks);
+        mfma_acc(o[db][g], vf[db], pf[g & 1]);
+      };
+      using first = std::integral_constant<int, 0>;
+      using second = std::integral_constant<int, 1>;
+      if constexpr (kS) {
+        for_each_index<kSteps>([&](auto ix) {
+          constexpr int kk = ix();
+          if constexpr (kk == 0) mfma_first(s, kf[0], qf[0]);
+          else mfma_next(s, kf[kk % kAhead], qf[kk]);
+          if constexpr (kk + kAhead < kSteps) kf[kk % kAhead] = load_k(kv, kk + kAhead);
+          if constexpr (kPV) {
+            // (all but the last four: those stand between the scores and their readers)
+            constexpr int from = kk * (kPV1 - 4) / kSteps, to = (kk + 1) * (kPV1 - 4) / kSteps;
+            if constexpr (to > from) pv(std::integral_constant<int, from>{}, first{});
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        if constexpr (kPV)
+          for_each_index<4>([&](auto ix) { pv(std::integral_constant<int, kPV1 - 4 + ix()>{}, first{}); });
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+        for_each_index<kPV1>([&](auto ix) { pv(ix, first{}); });
+      }
+      if constexpr (kPV) {
+#pragma unroll
+        for (int db = 0; db < kDB; ++db) vf[db] = load_v(kv_old, db, 1);
+        pf[0] = load_p(par ^ 1, 0, 1);
+      }
+      if constexpr (kS) {
+        mfma_settle(s);
+        __builtin_amdgcn_sched_barrier(0);
+        if (masked(t)) mask(s, t, bad);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      for_each_index<16>([&](auto ix) {
+        constexpr int i = ix();
+        if constexpr (kPV) {
+          constexpr int from = i * kPV1 / 16, to = (i + 1) * kPV1 / 16;
+          if constexpr (to > from) pv(std::integral_constant<int, from>{}, second{});
+        }
+        if constexpr (kS) weigh(ix, s, par);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+
+    using yes = std::true_type;
+    using no = std::false_type;
     issue(t0, source(t0));
     if (t0 + 1 < t1) issue(t0 + 1, source(t0 + 1));
-    for (int t = t0; t < t1; ++t) {
+    if (t0 + 1 < t1) wait_vmcnt<kPlanes>();
+    else wait_vmcnt<0>();
+    barrier_only();
+    uint32_t bad = masked(t0) ? find_bad(t0) : 0;
+    step(yes{}, no{}, t0, bad);
+    // (nothing has been summed up yet that the first maximum could change)
+    // Tile t + 1 has landed, tile t's weights are in LDS, and everyone is done with
+    // tile t - 1.
+    auto turn = [&] {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      barrier_only();
+    };
+    auto catch_up = [&](int t) {
+      const int par = t & 1;
+      if (bad != 0) clear_bad(t, bad);
+      if (t > t0 && (sm.moved[par][0] | sm.moved[par][1] | sm.moved[par][2] | sm.moved[par][3]) != 0) {
+        settle_all();
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+          const float al = sm.moved[par][g] ? sm.alpha[par][32 * g + l32] : 1.f;
+#pragma unroll
+          for (int db = 0; db < kDB; ++db) rescale(o[db][g], al);
+        }
+        settle_all();
+      }
+    };
+#pragma unroll 1
+    for (int t = t0; t + 1 < t1; ++t) {
       // (opaque to the compiler, which would keep every address that follows from
       // these in registers of its own over the loop)
       asm volatile("" : "+v"(k_rd[0]), "+v"(k_rd[1]), "+v"(k_rd[2]), "+v"(k_rd[3]));
       asm volatile("" : "+v"(v_rd[0][0]), "+v"(v_rd[0][1]), "+v"(v_rd[1][0]), "+v"(v_rd[1][1]));
       asm volatile("" : "+v"(l32), "+v"(h));
-      const unsigned char* kv = sm.kv[t % kStages];
-      const int par = t & 1;
-      const bool masked = (t + 1) * static_cast<int64_t>(kKeys) > P;
-      if (t + 1 < t1) wait_vmcnt<kPlanes>();
-      else wait_vmcnt<0>();
-      __syncthreads();  // tile t has landed; everyone is done with tile t - 1
+      turn();
       if (t + 2 < t1) issue(t + 2, source(t + 2));
-      // A tree key whose latent part holds a NaN or an infinity: the nodes that
-      // see it get NaN, and for the others 0 times it must not become one.
-      uint32_t bad = 0;
-      if (masked) {
-        if (threadIdx.x == 0) sm.bad[par] = 0;
-        __syncthreads();
-#pragma unroll 1
-        for (int e = rare_thread(); e < kKeys * DL / 8; e += kThreads) {
-          const u32x4 x = *reinterpret_cast<const u32x4*>(kv + e * 16);
-          uint32_t any = 0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            any |= ((x[j] & 0x7F80u) == 0x7F80u) | ((x[j] & 0x7F800000u) == 0x7F800000u);
-          if (any) atomicOr(&sm.bad[par], 1u << (e / 8 % kKeys));
-        }
-        __syncthreads();
-        bad = sm.bad[par];
-      }
-      {
-        f32x16 s;
-        bf16x8 kf[kAhead];
-#pragma unroll
-        for (int kk = 0; kk < kAhead; ++kk) kf[kk] = *reinterpret_cast<const bf16x8*>(kv + k_rd[kk & 3] + (kk >> 2) * kPlane);
-#pragma unroll
-        for (int kk = 0; kk < kSteps; ++kk) {
-          if (kk == 0) mfma_first(s, kf[0], qf[0]);
-          else mfma_next(s, kf[kk % kAhead], qf[kk]);
-          if (kk + kAhead < kSteps)
-            kf[kk % kAhead] = *reinterpret_cast<const bf16x8*>(kv + k_rd[(kk + kAhead) & 3] + ((kk + kAhead) >> 2) * kPlane);
-        }
-        mfma_settle(s);
-        if (masked) {
-          const uint32_t vis = visible(t * kKeys - P + 16 * h);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            if (!((vis >> r) & 1u)) s[r] = -INFINITY;
-            else if ((bad >> (16 * h + r)) & 1u) s[r] = NAN;
-          }
-        }
-        float top = s[0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) top = __builtin_elementwise_maximum(top, s[r]);
-        top = max_xor32(top);
-        const float m_new = top > m_run + a.lazy_gap ? top : m_run;
-        const float neg = fminf(-m_new * c, __FLT_MAX__);
-        const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
-        float ps = 0.f;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          u32x4 pk;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float p0 = exp2_fast(__builtin_fmaf(s[8 * q + 2 * j], c, neg));
-            const float p1 = exp2_fast(__builtin_fmaf(s[8 * q + 2 * j + 1], c, neg));
-            const bf16x2 w = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
-            ps = __builtin_amdgcn_fdot2_f32_bf16(w, ones, ps, false);
-            pk[j] = __builtin_bit_cast(uint32_t, w);
-          }
-          *reinterpret_cast<u32x4*>(sm.p[par][2 * h + q][32 * wave + l32]) = pk;
-        }
-        const float alpha = exp2_fast((m_run - m_new) * c);
-        const bool any = __ballot(m_new != m_run) != 0;
-        sm.alpha[par][32 * wave + l32] = m_new != m_run ? alpha : 1.f;
-        if (lane == 0) sm.moved[par][wave] = any;
-        if (m_new != m_run) l_run *= alpha;
-        l_run += ps;
-        m_run = m_new;
-      }
-      __syncthreads();  // the weights are in LDS, and every score of the tile is taken
-      if (bad != 0) {
-#pragma unroll 1
-        for (int e = rare_thread(); e < kKeys * DL / 8; e += kThreads) {
-          if ((bad >> (e / 8 % kKeys)) & 1u) *reinterpret_cast<u32x4*>(const_cast<unsigned char*>(kv) + e * 16) = u32x4{0, 0, 0, 0};
-        }
-        __syncthreads();
-      }
-      if ((sm.moved[par][0] | sm.moved[par][1] | sm.moved[par][2] | sm.moved[par][3]) != 0) {
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          const float al = sm.alpha[par][32 * g + l32];
-#pragma unroll
-          for (int db = 0; db < kDB; ++db) {
-            rescale(o[db][g], al);
-          }
-        }
-      }
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        bf16x8 vf[kDB];
-#pragma unroll
-        for (int db = 0; db < kDB; ++db) {
-          const unsigned char* at = kv + v_rd[db & 1][ks] + (db >> 1) * kPlane;
-          const s16x4 lo = lds_read_tr(at), hi = lds_read_tr(at + 4 * 128);
-          vf[db] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        }
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          const bf16x8 pf = *reinterpret_cast<const bf16x8*>(sm.p[par][2 * ks + h][32 * g + l32]);
-#pragma unroll
-          for (int db = 0; db < kDB; ++db) o[db][g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[db], pf, o[db][g], 0, 0, 0);
-        }
-      }
+      catch_up(t);
+      bad = masked(t + 1) ? find_bad(t + 1) : 0;
+      step(yes{}, yes{}, t + 1, bad);
+      tell((t + 1) & 1);
     }
+    turn();
+    catch_up(t1 - 1);
+    step(no{}, yes{}, t1, 0);
+    settle_all();
 
     // ---- results
     {
