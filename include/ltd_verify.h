@@ -105,6 +105,7 @@ extern "C" {
 
 #define LTD_ROPE_MAX_DIM 4096 /* head size of ltd_tree_rope */
 #define LTD_LATENT_ROPE 64    /* rotated dims of a latent cache's rows */
+#define LTD_LATENT_MAX_HEADS 65536
 
 #define LTD_POLICY_SIZE 0          /* state [D, L, score of every pool candidate, pad ...] */
 #define LTD_POLICY_DEPTH 1         /* state [scores of the newest in_dim-2 candidates, D, L] */
@@ -673,7 +674,7 @@ int ltd_latent_append(const void* kv_new, int64_t new_row_stride, const void* no
  *                aligned; needs no initialisation.
  * A NaN or an infinity in a row's latent part, or a NaN score, reaches the outputs
  * of the nodes that see the row (where it may make every dimension NaN), and no
- * others.  B <= 65535 with float32.
+ * others.  Hq <= LTD_LATENT_MAX_HEADS; B <= 65535 with float32.
  */
 size_t ltd_tree_verify_attn_latent_workspace_size(int B, int Nmax, int Hq, int d_latent,
                                                   int d_rope, int max_prefix, int dtype);

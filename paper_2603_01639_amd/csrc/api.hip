@@ -660,7 +660,7 @@ bool latent_attn_args_ok(int B, int Nmax, int Hq, int max_prefix) {
 size_t ltd_tree_verify_attn_latent_workspace_size(int B, int Nmax, int Hq, int d_latent,
                                                   int d_rope, int max_prefix, int dtype) {
   if (!latent_attn_args_ok(B, Nmax, Hq, max_prefix) || !dtype_known(dtype) ||
-      !latent_supported(d_latent, d_rope) || max_prefix > LTD_MAX_LENGTH)
+      !latent_supported(d_latent, d_rope) || max_prefix > LTD_MAX_LENGTH || Hq > LTD_LATENT_MAX_HEADS)
     return 0;
   ltd::LatentAttn s{};
   s.B = B;
@@ -682,7 +682,7 @@ int ltd_tree_verify_attn_latent(const void* q_latent, int64_t ql_row_stride,
   if (!latent_attn_args_ok(B, Nmax, Hq, max_prefix) || kv_rows < 1) return LTD_EINVAL;
   if (!(scale > 0.f) || !std::isfinite(scale)) return LTD_EINVAL;
   if (!dtype_known(dtype) || !latent_supported(d_latent, d_rope) || max_prefix > LTD_MAX_LENGTH ||
-      (dtype == LTD_DTYPE_F32 && B > 65535))
+      Hq > LTD_LATENT_MAX_HEADS || (dtype == LTD_DTYPE_F32 && B > 65535))
     return LTD_EUNSUPPORTED;
   if (block_table && (max_blocks < 1 || num_blocks < 1)) return LTD_EINVAL;
   if (validate && !status) return LTD_EINVAL;

@@ -23,6 +23,8 @@
 namespace ltd {
 namespace {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kRows = latent::kUnitRows;
@@ -31,38 +33,69 @@ constexpr int kRopeDims = 64;
 constexpr int kStages = 3;                     // tiles in the LDS ring
 constexpr int kAncWords = LTD_MAX_NODES / 32;  // 256 bits a node
 constexpr int kPlane = kKeys * 128;             // bytes of a tile's plane in LDS
-constexpr float kLazyMax = 8.f;                // a running max moves when a score passes it by 2^8 (log2 units)
-constexpr int kAhead = 4;                      // key fragments in flight
+// A row's reference maximum moves when a score passes it by 2^16: weights up to that
+// and their sums have as many bits in float32 and bfloat16 as small ones, and
+// moving it costs 256 accumulators a lane.  (At 2^8 two tiles in ten moved some
+// row's, 1400 cycles a tile; 8 sequences of 128 heads 774 us.)
+constexpr float kLazyMax = 16.f;
+constexpr int kAhead = 6;                      // key fragments in flight
 constexpr float kNoMax = -__FLT_MAX__;
+
+// A piece's row beside its O / l: the maximum (log2 units), the sum, and for each wave's
+// dims the power of two that the stored values are to be multiplied by.
+struct PieceRow {
+  float m, l, factor[kWaves];
+};
+// A unit that was cut: its rows, and the workgroups that have the other pieces.
+struct CutUnit {
+  int b, r0, valid, last;
+};
 
 struct LatentArgs {
   LatentAttn in;
-  float* ws_o;   // [2 W][128][DL]: a piece's O / l
-  float* ws_ml;  // [2 W][128][2]: its rows' max (log2 units) and sum
+  _Float16* ws_o;    // [2 W][128][DL]: pieces' O / l
+  PieceRow* ws_row;  // [2 W][128]
+  CutUnit* ws_cut;   // [W]: the cut unit that begins in a workgroup's share (valid 0: none)
   int W;         // workgroups
   float scale_log2, lazy_gap;
+  uint32_t row_magic;  // block_of's multiplier and shift
+  int row_shift;
 };
 
-// Where a position of the laid-out tiles falls.
+// Where a place of the laid-out units falls.
 struct Place {
   int b;
-  int64_t before;  // tiles before sequence b
+  int64_t before;  // length before sequence b
 };
 
-// Tiles of sequence b (0 past the batch; counts out of range are clamped).
-__device__ __forceinline__ int64_t seq_tiles(const LatentAttn& a, int b) {
+// Length of sequence b's units (0 past the batch; counts out of range are clamped).
+__device__ __forceinline__ int64_t seq_length(const LatentAttn& a, int b) {
   if (b >= a.B) return 0;
   const int n = min(max(a.n_nodes[b], 0), a.Nmax), P = max(a.prefix_len[b], 0);
-  return latent::units_of(n, a.Hq) * latent::tiles_of(P, n);
+  return latent::length_of(P, n, a.Hq);
 }
 
-__device__ __forceinline__ int64_t wave_scan(int64_t v, int lane) {  // inclusive
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const int64_t o = __shfl_up(v, off, kWave);
-    if (lane >= off) v += o;
-  }
+// x moved between lanes by DPP (0 where there is none to take).
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ int64_t dpp64(int64_t x) {
+  const uint64_t u = static_cast<uint64_t>(x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), kCtrl, kRowMask, 0xF, kRowMask == 0xF);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), kCtrl, kRowMask, 0xF, kRowMask == 0xF);
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ int64_t wave_scan(int64_t v) {  // inclusive
+  v += dpp64<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8
+  v += dpp64<0x112, 0xF>(v);
+  v += dpp64<0x114, 0xF>(v);
+  v += dpp64<0x118, 0xF>(v);
+  v += dpp64<0x142, 0xA>(v);  // row_bcast 15 into rows 1 and 3
+  v += dpp64<0x143, 0xC>(v);  // row_bcast 31 into rows 2 and 3
   return v;
+}
+__device__ __forceinline__ int64_t read_lane(int64_t v, int l) {
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(v), l);
+  const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(static_cast<uint64_t>(v) >> 32), l);
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
 // A value that is the same in all lanes, in scalar registers.
@@ -72,58 +105,71 @@ __device__ __forceinline__ int64_t uniform(int64_t v) {
   return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
 }
 
-// All sequences' tiles, and the sequence that holds tile pos(total); every wave
-// computes it by itself.
+// The length of all sequences' units, and the sequence that place pos(length) falls
+// into (B past the end); every wave works it out by itself.
 template <class Pos>
 __device__ __forceinline__ Place find_place(const LatentAttn& a, int lane, int64_t* total_out, Pos pos) {
-  int64_t total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kWave) total += __shfl(wave_scan(seq_tiles(a, b0 + lane), lane), kWave - 1, kWave);
-  total = uniform(total);
+  const int64_t mine = seq_length(a, lane), upto = wave_scan(mine);
+  const int64_t first = read_lane(upto, kWave - 1);
+  int64_t total = first;
+  for (int b0 = kWave; b0 < a.B; b0 += kWave) total += read_lane(wave_scan(seq_length(a, b0 + lane)), kWave - 1);
   *total_out = total;
   const int64_t at = pos(total);
-  Place p{a.B, total};
-  int64_t before = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kWave) {
-    const int64_t mine = seq_tiles(a, b0 + lane);
-    const int64_t incl = wave_scan(mine, lane) + before;
-    const uint64_t hit = __ballot(at < incl);
+  if (at < first) {
+    const int l = __ffsll(static_cast<long long>(__ballot(at < upto))) - 1;
+    return Place{l, read_lane(upto - mine, l)};
+  }
+  int64_t before = first;
+  for (int b0 = kWave; b0 < a.B; b0 += kWave) {
+    const int64_t here = seq_length(a, b0 + lane), past = wave_scan(here) + before;
+    const uint64_t hit = __ballot(at < past);
     if (hit != 0) {
       const int l = __ffsll(static_cast<long long>(hit)) - 1;
-      p.b = b0 + l;
-      p.before = __shfl(incl - mine, l, kWave);
-      break;
+      return Place{b0 + l, read_lane(past - here, l)};
     }
-    before = __shfl(incl, kWave - 1, kWave);
+    before = read_lane(past, kWave - 1);
   }
-  p.b = __builtin_amdgcn_readfirstlane(p.b);
-  p.before = uniform(p.before);
-  return p;
+  return Place{a.B, total};
 }
 
 template <int DL>
 struct Smem {
-  unsigned char kv[kStages][(DL + kRopeDims) / 64 * kPlane];
-  unsigned char p[2][kKeys / 8][kRows][16];  // weights: 8 keys of a row
+  alignas(16) unsigned char kv[kStages][(DL + kRopeDims) / 64 * kPlane];
+  u32x4 p[2][kKeys / 8][kRows];              // weights: 8 keys of a row
   float alpha[2][kRows];                     // what a row's sums so far are multiplied by
-  int moved[2][kWaves];                      // whether a wave's rows have such factors
-  float row_l[kRows], row_m[kRows];
+  i32x4 moved[2];                            // whether a wave's rows have such factors
+  float row_l[kRows];                        // sums
   uint32_t anc[kAncWords][LTD_MAX_NODES];    // word w of every node's ancestor set
   int jump[LTD_MAX_NODES];
   uint32_t bad[2];                           // tree keys of a tile with a NaN or an infinity
 };
 
-// A tile in LDS: planes of 64 dims, each 128 bytes of every key.  A row's 16-byte
-// chunks within a plane trade places by its key, so that the eight keys of an S^T
-// operand's read, and the four of a transposed read, fall on different banks.
-__device__ __forceinline__ int swz(int key) { return ((key & 3) << 1) | ((key >> 4) & 1); }
-
-// The thread's index, computed anew: what a rare branch derives from it would be
-// hoisted out of the tile loop into registers that the loop does not have.
-__device__ __forceinline__ int rare_thread() {
-  int t = threadIdx.x;
-  asm volatile("" : "+v"(t));
-  return t;
+// The key in row i of an S^T operand.  Accumulator r of lane half h, row 8 (r / 4) +
+// 4 h + r % 4 of the product, then holds key acc_key(r) + 8 h: the registers of
+// (r / 4) % 2 = q are the eight keys of chunk 2 q + h, in order.
+__device__ __forceinline__ int operand_key(int i) {
+  return (i & 3) | ((i >> 4) & 1) << 2 | ((i >> 2) & 1) << 3 | ((i >> 3) & 1) << 4;
 }
+constexpr int acc_key(int r) { return (r & 3) | (r >> 3) << 2 | ((r >> 2) & 1) << 4; }
+
+// A tile in LDS: planes of 64 dims, each 128 bytes of every key.  A row's 16-byte
+// chunks within a plane trade places by its key, so that neither 16 lanes of an S^T
+// operand's read (keys that differ in bits 0, 1, 3 and 4; even and odd ones lie in
+// different halves of the banks) nor 32 lanes of a transposed read (64 bytes of four
+// neighbouring keys) meet on a bank.
+__device__ __forceinline__ int swz(int key) {
+  return ((key >> 1) & 1) << 2 | ((key >> 3) & 1) << 1 | ((key >> 4) & 1);
+}
+
+// x, made anew: constants of rare branches and what they derive from the thread's
+// index would be hoisted out of the tile loop into registers that the loop does
+// not have.
+template <typename T>
+__device__ __forceinline__ T rare(T x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+__device__ __forceinline__ int rare_thread() { return rare(static_cast<int>(threadIdx.x)); }
 
 // The products by hand: O's accumulators take all 256 accumulation registers, and S's
 // go to vector registers (the compiler would keep both in the former, and move O out
@@ -140,7 +186,7 @@ __device__ __forceinline__ void mfma_next(f32x16& s, bf16x8 a, bf16x8 b) {
   asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void mfma_settle(f32x16& s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s)); }
-__device__ __forceinline__ void mfma_settle_acc(f32x16& o) { asm volatile("s_nop 15\n\ts_nop 7" : "+a"(o)); }
+__device__ __forceinline__ void settled(f32x16& o) { asm volatile("" : "+a"(o)); }
 
 // A direct load of 16 bytes a lane (lane i's land at lds + 16 i) from kOff bytes past
 // p.  (The instruction's offset moves its place in LDS as well, so that is taken back.)
@@ -189,81 +235,94 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     share = latent::share_of(t, a.W);
     return rank * share;
   });
+  share = uniform(share);
   pos = rank * share;
   const int64_t end = min(pos + share, total);
+  if (threadIdx.x == 0) a.ws_cut[rank].valid = 0;
   if (pos >= end) return;
-  int b = place.b;
-  int64_t before = place.before;
-  int slot = 2 * rank;
+  int b = __builtin_amdgcn_readfirstlane(place.b);
+  int64_t before = uniform(place.before);
+  int tree_of = -1;  // the sequence whose ancestor sets are in LDS
 
   // ---- lane constants
   // direct loads: lane 8 k + c of wave w fetches chunk c of key 8 w + k in every group
-  const int load_key = 8 * wave + (lane >> 3);
-  const int load_off = ((lane & 7) ^ swz(load_key)) * 16;
-  // S^T operand: row l32 reads key sigma(l32), chunk 2 kk + h
-  const int s_key = sigma(l32);
-  int k_rd[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) k_rd[e] = s_key * 128 + (((2 * e + h) ^ swz(s_key)) << 4);
+  int load_key = 8 * wave + (lane >> 3);
+  // S^T operand: row l32, chunk 2 kk + h, which step kk moves by an exclusive or
+  int k_rd = operand_key(l32) * 128 + ((h ^ swz(operand_key(l32))) << 4);
   // C^T operand: 16-lane group g reads keys 16 ks + 8 (g / 2) + .. (two reads of
-  // 4), dims 32 db + 16 (g % 2) + ..
-  const int tg = lane >> 4, ts = lane & 15;
-  int v_rd[2][2];
-#pragma unroll
-  for (int e = 0; e < 2; ++e)
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const int key = 16 * ks + 8 * (tg >> 1) + (ts >> 2);
-      const int c = 4 * e + 2 * (tg & 1) + ((ts & 3) >> 1);
-      v_rd[e][ks] = wave * (kCols / 64) * kPlane + key * 128 + ((c ^ swz(key)) << 4) + (ts & 1) * 8;
-    }
+  // 4), dims 32 db + 16 (g % 2) + ..; the same way from ks = 0, db = 0
+  const int v_key = 8 * (lane >> 5) + ((lane >> 2) & 3);
+  int v_rd = wave * (kCols / 64) * kPlane + v_key * 128 +
+             (((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ swz(v_key)) << 4) + (lane & 1) * 8;
   const uint32_t kv_lds = lds_addr(sm.kv[0]);
+  // a row's block, by a multiplication (row_magic)
+  auto block_of = [&](int row) {
+    return static_cast<int>(__umulhi(2u * static_cast<uint32_t>(row), a.row_magic) >> a.row_shift);
+  };
 
   while (pos < end) {
     // ---- the unit's piece in this share
-    const int n = min(max(in.n_nodes[b], 0), in.Nmax), P = max(in.prefix_len[b], 0);
-    const int64_t units = latent::units_of(n, in.Hq), tiles = latent::tiles_of(P, n);
-    if (pos >= before + units * tiles) {
-      before += units * tiles;
+    const int n = min(max(__builtin_amdgcn_readfirstlane(in.n_nodes[b]), 0), in.Nmax);
+    const int P = max(__builtin_amdgcn_readfirstlane(in.prefix_len[b]), 0);
+    const int64_t length = latent::kUnitCost + latent::tiles_of(P, n);
+    const int64_t all = latent::units_of(n, in.Hq) * length;
+    if (pos >= before + all) {
+      before += all;
       ++b;
       continue;
     }
-    const int64_t unit = (pos - before) / tiles;
-    const int t0 = static_cast<int>(pos - before - unit * tiles);
-    const int t1 = static_cast<int>(min(tiles, t0 + (end - pos)));
-    const bool whole = t0 == 0 && t1 == tiles;
-    const int64_t R = static_cast<int64_t>(n) * in.Hq;
-    const int64_t r0 = unit * kRows;
-    const int valid = static_cast<int>(min(static_cast<int64_t>(kRows), R - r0));
+    const int unit = static_cast<int>(uniform((pos - before) / length));
+    const int64_t start = before + unit * length;
+    const int64_t stop = uniform(min(start + length, end));
+    const int t0 = __builtin_amdgcn_readfirstlane(static_cast<int>(latent::tile_at(pos - start)));
+    const int t1 = __builtin_amdgcn_readfirstlane(static_cast<int>(latent::tile_at(stop - start)));
+    if (t1 == t0) {  // (a share that ends within a unit's own cost)
+      pos = stop;
+      continue;
+    }
+    const bool whole = t0 == 0 && stop == start + length;
+    const int slot = 2 * rank + (t0 == 0);  // (one piece that goes on, one that begins)
+    const int r0 = unit * kRows;
+    const int valid = min(kRows, n * in.Hq - r0);
     const int last = P + n - 1;
-    const bool tree = static_cast<int64_t>(t1) * kKeys > P;
+    const bool tree = static_cast<int64_t>(t1) * kKeys > P && tree_of != b;
     __syncthreads();  // the last piece's LDS is free
 
-    // the lane's chunk of its key's first group in tile t (rows past the last are
-    // not read: the last one is, again, and never visible)
-    auto source = [&](int t) -> const unsigned char* {
+    // Direct loads.  at(t): where the lane's chunk of its key's first plane lies for
+    // tile t (rows past the last are not read: the last one is, again, and never
+    // visible).  A paged cache's block ids are read a tile ahead.
+    int32_t block = 0;
+    auto look_up = [&](int t) {
+      if constexpr (kPaged)
+        block = in.block_table[static_cast<int64_t>(b) * in.max_blocks + block_of(min(t * kKeys + load_key, last))];
+    };
+    auto at = [&](int t) -> const unsigned char* {
       const int row = min(t * kKeys + load_key, last);
-      int64_t at;
-      if constexpr (kPaged) {
-        const int64_t blk = in.block_table[static_cast<int64_t>(b) * in.max_blocks + row / in.kv_rows];
-        at = blk * in.kv_rows + row % in.kv_rows;
-      } else {
-        at = static_cast<int64_t>(b) * in.kv_rows + row;
-      }
-      return static_cast<const unsigned char*>(in.cache) + at * kRowBytes + load_off;
+      // (rows of a cache are counted in 32 bits: 2^31 of them pass any memory)
+      const uint32_t place = kPaged ? block * in.kv_rows + (row - block_of(row) * in.kv_rows) : b * in.kv_rows + row;
+      return static_cast<const unsigned char*>(in.cache) +
+             (static_cast<uint64_t>(place) * kRowBytes + ((lane & 7) ^ swz(load_key)) * 16);
     };
-    auto issue = [&](int t, const unsigned char* from) {
-      const uint32_t dst = kv_lds + (t % kStages) * kTileBytes + wave * 1024;
-      for_each_index<kPlanes>([&](auto g) { dma16_at<g() * 128>(dst + g() * kPlane, from); });
+    auto issue_plane = [&](int t, const unsigned char* from, auto plane) {
+      dma16_at<plane() * 128>(kv_lds + (t % kStages) * kTileBytes + wave * 1024 + plane() * kPlane, from);
     };
+    auto issue = [&](int t) {
+      const unsigned char* from = at(t);
+      for_each_index<kPlanes>([&](auto g) { issue_plane(t, from, g); });
+    };
+    look_up(t0);
+    issue(t0);
+    look_up(t0 + 1);
+    if (t0 + 1 < t1) issue(t0 + 1);
+    look_up(t0 + 2);
 
     // ---- queries: lane holds row l32 of the wave's 32, dims 16 kk + 8 h ..
     bf16x8 qf[kSteps];
     int node;
     {
-      const int64_t r = r0 + min(32 * wave + l32, valid - 1);
-      node = static_cast<int>(r / in.Hq);
-      const int head = static_cast<int>(r % in.Hq);
+      const uint32_t r = r0 + min(32 * wave + l32, valid - 1), heads = rare(in.Hq);
+      node = static_cast<int>(r / heads);
+      const int head = static_cast<int>(r % heads);
       const int64_t row = static_cast<int64_t>(b) * in.Nmax + node;
       const uint16_t* ql = static_cast<const uint16_t*>(in.q_latent) + row * in.ql_row + head * in.ql_head + 8 * h;
       const uint16_t* qr = static_cast<const uint16_t*>(in.q_rope) + row * in.qr_row + head * in.qr_head + 8 * h;
@@ -276,6 +335,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     // ---- ancestor sets (256 bits a node) by pointer doubling: anc(i) |= anc(jump(i)),
     // jump(i) = jump(jump(i)); thread i has node i
     if (tree) {
+      tree_of = b;
       const int i = rare_thread();
       uint32_t mine[kAncWords];
 #pragma unroll
@@ -305,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     }
     __syncthreads();
 
-    float m_run = kNoMax, l_run = 0.f;
+    float m_run = rare(kNoMax), l_run = 0.f;
     f32x16 o[kDB][kGroups];
 #pragma unroll
     for (int db = 0; db < kDB; ++db)
@@ -316,27 +376,32 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
       }
     const float c = a.scale_log2;
     auto settle_all = [&] {
+      asm volatile("s_nop 15\n\ts_nop 7");
 #pragma unroll
       for (int db = 0; db < kDB; ++db)
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) mfma_settle_acc(o[db][g]);
+        for (int g = 0; g < kGroups; ++g) settled(o[db][g]);
     };
 
-    // bits base .. base + 15 of a node's visible tree keys (earlier ones are the prefix)
+    // bits base .. base + 31 of a node's visible tree keys (earlier ones are the prefix)
     auto visible = [&](int base) -> uint32_t {
       const auto word = [&](int w) -> uint32_t {
-        return w < 0 ? 0xFFFFFFFFu : w >= kAncWords ? 0u : sm.anc[w][node];
+        uint32_t x = w < 0 ? 0xFFFFFFFFu : 0u;
+        if (static_cast<uint32_t>(w) < kAncWords) x = sm.anc[w][node];
+        return x;
       };
       const int w = base >> 5;
-      const uint64_t two = (static_cast<uint64_t>(word(w + 1)) << 32) | word(w);
-      return static_cast<uint32_t>(two >> (base & 31)) & 0xFFFFu;
+      return __builtin_amdgcn_alignbit(word(w + 1), word(w), base & 31);
     };
 
-    // The weights of the tile whose scores are in s, in 16 pieces (each beside one of
-    // the other products): the maximum, which moves only when a score passes it by
-    // 2^kLazyMax, two weights a piece, and what follows from them.
-    float alpha = 1.f, top, neg, ps;
+    // The weights of the tile whose scores are in s, in pieces of a few instructions that
+    // fit beside one of the other products: the maximum, which moves only when a
+    // score passes it by 2^kLazyMax, a weight a piece, and what follows from them.
+    // (With two products and two weights a piece the vector operations of a piece
+    // outlasted the second product: 1250 cycles a tile where the products take 670.)
+    float alpha = 1.f, top, neg, ps, p0;
     u32x4 pk[2];
+    constexpr int kPieces = 23;
     auto weigh = [&](auto piece, const f32x16& s, int par) {
       constexpr int i = piece();
       if constexpr (i < 4) {
@@ -345,22 +410,26 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
         top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top, s[4 * i + 2]), s[4 * i + 3]);
       } else if constexpr (i == 4) {
         top = max_xor32(top);
-        const float m_new = top > m_run + a.lazy_gap ? top : m_run;
-        neg = fminf(-m_new * c, __FLT_MAX__);
-        alpha = exp2_fast((m_run - m_new) * c);  // (1 where it has not moved)
-        m_run = m_new;
+        top = top > m_run + a.lazy_gap ? top : m_run;
+      } else if constexpr (i == 5) {
+        neg = fminf(-top * c, __FLT_MAX__);
+        alpha = exp2_fast((m_run - top) * c);  // (1 where it has not moved)
+        m_run = top;
         ps = 0.f;
-      } else if constexpr (i < 13) {
-        constexpr int j = i - 5;
-        const float p0 = exp2_fast(__builtin_fmaf(s[2 * j], c, neg));
-        const float p1 = exp2_fast(__builtin_fmaf(s[2 * j + 1], c, neg));
-        // (the sum is that of the rounded weights, the very ones that multiply the values)
-        const bf16x2 w = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
-        ps = __builtin_amdgcn_fdot2_f32_bf16(w, __builtin_bit_cast(bf16x2, 0x3F803F80u), ps, false);
-        pk[j >> 2][j & 3] = __builtin_bit_cast(uint32_t, w);
-        if constexpr (j == 3) *reinterpret_cast<u32x4*>(sm.p[par][2 * h][32 * wave + l32]) = pk[0];
-      } else if constexpr (i == 13) {
-        *reinterpret_cast<u32x4*>(sm.p[par][2 * h + 1][32 * wave + l32]) = pk[1];
+      } else if constexpr (i < 22) {
+        constexpr int j = (i - 6) / 2, q = j >> 2, r = 4 * q + 8 * ((j >> 1) & 1) + 2 * (j & 1);
+        if constexpr ((i - 6) % 2 == 0) {
+          p0 = exp2_fast(__builtin_fmaf(s[r], c, neg));
+          if constexpr (j == 4) sm.p[par][h][32 * wave + l32] = pk[0];
+        } else {
+          const float p1 = exp2_fast(__builtin_fmaf(s[r + 1], c, neg));
+          // (the sum is that of the rounded weights, the very ones that multiply the values)
+          const bf16x2 w = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
+          ps = __builtin_amdgcn_fdot2_f32_bf16(w, __builtin_bit_cast(bf16x2, 0x3F803F80u), ps, false);
+          pk[q][j & 3] = __builtin_bit_cast(uint32_t, w);
+        }
+      } else {
+        sm.p[par][2 + h][32 * wave + l32] = pk[1];
         l_run = l_run * alpha + ps;
       }
     };
@@ -368,17 +437,21 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     auto tell = [&](int par) {
       const uint64_t any = __ballot(alpha != 1.f);
       if (any != 0) sm.alpha[par][32 * wave + l32] = alpha;
-      if (lane == 0) sm.moved[par][wave] = any != 0;
+      if (lane == 0) reinterpret_cast<int*>(&sm.moved[par])[wave] = any != 0;
     };
     // Hides the keys that the lane's node does not see.  A tree key whose latent part
     // holds a NaN or an infinity (bad) gives NaN to the nodes that see it.
     auto mask = [&](f32x16& s, int t, uint32_t bad) {
-      const uint32_t vis = visible(t * kKeys - P + 16 * h);
+      const uint32_t vis = visible(t * kKeys - P) >> (8 * h);
+      const uint32_t nan = bad >> (8 * h);
+      if (bad != 0) {
+        const float none = rare(NAN);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (!((vis >> r) & 1u)) s[r] = -INFINITY;
-        else if ((bad >> (16 * h + r)) & 1u) s[r] = NAN;
+        for (int r = 0; r < 16; ++r) s[r] = (nan >> acc_key(r)) & 1u ? none : s[r];
       }
+      const float hidden = rare(-INFINITY);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = (vis >> acc_key(r)) & 1u ? s[r] : hidden;
     };
     auto masked = [&](int t) { return (t + 1) * static_cast<int64_t>(kKeys) > P; };
     // The keys of tile t (landed) whose latent part is not finite; the whole
@@ -404,117 +477,92 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
       unsigned char* kv = sm.kv[t % kStages];
 #pragma unroll 1
       for (int e = rare_thread(); e < kKeys * DL / 8; e += kThreads)
-        if ((bad >> (e / 8 % kKeys)) & 1u) *reinterpret_cast<u32x4*>(kv + e * 16) = u32x4{0, 0, 0, 0};
+        if ((bad >> (e / 8 % kKeys)) & 1u) {
+          const uint32_t zero = rare(0u);
+          *reinterpret_cast<u32x4*>(kv + e * 16) = u32x4{zero, zero, zero, zero};
+        }
       __syncthreads();
     };
 
     auto load_k = [&](const unsigned char* kv, int kk) {
-      return *reinterpret_cast<const bf16x8*>(kv + k_rd[kk & 3] + (kk >> 2) * kPlane);
+      return *reinterpret_cast<const bf16x8*>(kv + (k_rd ^ ((kk & 3) << 5)) + (kk >> 2) * kPlane);
     };
     auto load_v = [&](const unsigned char* kv, int db, int ks) {
-      const unsigned char* at = kv + v_rd[db & 1][ks] + (db >> 1) * kPlane;
+      const unsigned char* at = kv + (v_rd ^ ((db & 1) << 6 | ks << 4)) + ks * 16 * 128 + (db >> 1) * kPlane;
       const s16x4 lo = lds_read_tr(at), hi = lds_read_tr(at + 4 * 128);
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
     auto load_p = [&](int par, int g, int ks) {
-      return *reinterpret_cast<const bf16x8*>(sm.p[par][2 * ks + h][32 * g + l32]);
+      return __builtin_bit_cast(bf16x8, sm.p[par][2 * ks + h][32 * g + l32]);
     };
 
-    // One step: the scores and weights of tile t (kS) with the product of tile
-    // t - 1's weights and values (kPV).  The score products and the first half
-    // of the other ones alternate, which spreads the key reads (all that LDS can
-    // give while scores alone run) over both; the weights are then worked out
-    // beside the second half.
-    constexpr int kPV1 = kDB * kGroups;  // products of 16 keys
-    auto step = [&](auto with_s, auto with_pv, int t, uint32_t bad) {
-      constexpr bool kS = with_s(), kPV = with_pv();
-      const unsigned char* kv = sm.kv[t % kStages];
-      const unsigned char* kv_old = sm.kv[(t + kStages - 1) % kStages];
-      const int par = t & 1;
-      f32x16 s;
-      bf16x8 kf[kAhead], vf[kDB], pf[2];
-      if constexpr (kS) {
+    // The products of a tile's weights and values, in the order q = 4 ks + g of 16 keys
+    // (ks) and 32 rows (g): weights are read three q ahead, values a ks ahead.
+    bf16x8 va[kDB], vb[kDB], pf[3];
+    auto product = [&](auto ix, const bf16x8(&v)[kDB], int par) {  // of index q * kDB + db
+      constexpr int q = ix() / kDB, db = ix() % kDB;
+      mfma_acc(o[db][q & 3], v[db], pf[q % 3]);
+      if constexpr (db == kDB - 1 && q + 3 < 2 * kGroups) pf[q % 3] = load_p(par, (q + 3) & 3, (q + 3) >> 2);
+    };
+    constexpr int kHalf = 2 * kDB;  // products of two q
+    // The last quarter of a tile's products waits in registers for the next step: it
+    // fills the time that the step's first reads take.
+    auto last_products = [&] { for_each_index<kHalf>([&](auto i) { product(std::integral_constant<int, 3 * kHalf + i()>{}, vb, 0); }); };
+    auto load_values = [&](bf16x8(&v)[kDB], const unsigned char* kv, int ks) {
 #pragma unroll
-        for (int kk = 0; kk < kAhead; ++kk) kf[kk] = load_k(kv, kk);
-      }
-      if constexpr (kPV) {
+      for (int db = 0; db < kDB; ++db) v[db] = load_v(kv, db, ks);
+    };
+    // Scores of tile t from its first fragments in kf; beside(kk) runs beside product kk.
+    bf16x8 kf[kAhead];
+    auto first_keys = [&](const unsigned char* kv) {
 #pragma unroll
-        for (int db = 0; db < kDB; ++db) vf[db] = load_v(kv_old, db, 0);
-        pf[0] = load_p(par ^ 1, 0, 0);
-      }
-      // product i of 16 keys ks: rows g, dims db
-      auto pv = [&](auto ix, auto half) {
-        constexpr int i = ix(), g = i / kDB, db = i % kDB, ks = half();
-        if constexpr (db == 0 && g + 1 < kGroups) pf[(g + 1) & 1] = load_p(par ^ 1, g + 1, ks);
-        mfma_acc(o[db][g], vf[db], pf[g & 1]);
-      };
-      using first = std::integral_constant<int, 0>;
-      using second = std::integral_constant<int, 1>;
-      if constexpr (kS) {
-        for_each_index<kSteps>([&](auto ix) {
-          constexpr int kk = ix();
-          if constexpr (kk == 0) mfma_first(s, kf[0], qf[0]);
-          else mfma_next(s, kf[kk % kAhead], qf[kk]);
-          if constexpr (kk + kAhead < kSteps) kf[kk % kAhead] = load_k(kv, kk + kAhead);
-          if constexpr (kPV) {
-            // (all but the last four: those stand between the scores and their readers)
-            constexpr int from = kk * (kPV1 - 4) / kSteps, to = (kk + 1) * (kPV1 - 4) / kSteps;
-            if constexpr (to > from) pv(std::integral_constant<int, from>{}, first{});
-          }
-          __builtin_amdgcn_sched_barrier(0);
-        });
-        if constexpr (kPV)
-          for_each_index<4>([&](auto ix) { pv(std::integral_constant<int, kPV1 - 4 + ix()>{}, first{}); });
-        __builtin_amdgcn_sched_barrier(0);
-      } else {
-        for_each_index<kPV1>([&](auto ix) { pv(ix, first{}); });
-      }
-      if constexpr (kPV) {
-#pragma unroll
-        for (int db = 0; db < kDB; ++db) vf[db] = load_v(kv_old, db, 1);
-        pf[0] = load_p(par ^ 1, 0, 1);
-      }
-      if constexpr (kS) {
-        mfma_settle(s);
-        __builtin_amdgcn_sched_barrier(0);
-        if (masked(t)) mask(s, t, bad);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      for_each_index<16>([&](auto ix) {
-        constexpr int i = ix();
-        if constexpr (kPV) {
-          constexpr int from = i * kPV1 / 16, to = (i + 1) * kPV1 / 16;
-          if constexpr (to > from) pv(std::integral_constant<int, from>{}, second{});
-        }
-        if constexpr (kS) weigh(ix, s, par);
+      for (int kk = 0; kk < kAhead; ++kk) kf[kk] = load_k(kv, kk);
+    };
+    auto scores = [&](f32x16& s, const unsigned char* kv, auto beside) {
+      for_each_index<kSteps>([&](auto ix) {
+        constexpr int kk = ix();
+        if constexpr (kk == 0) mfma_first(s, kf[0], qf[0]);
+        else mfma_next(s, kf[kk % kAhead], qf[kk]);
+        if constexpr (kk + kAhead < kSteps) kf[kk % kAhead] = load_k(kv, kk + kAhead);
+        beside(ix);
         __builtin_amdgcn_sched_barrier(0);
       });
     };
 
-    using yes = std::true_type;
-    using no = std::false_type;
-    issue(t0, source(t0));
-    if (t0 + 1 < t1) issue(t0 + 1, source(t0 + 1));
-    if (t0 + 1 < t1) wait_vmcnt<kPlanes>();
-    else wait_vmcnt<0>();
+    // ---- the tile loop, software-pipelined by one tile: step t works out the scores and
+    // weights of tile t + 1 and multiplies tile t's weights and values.  A quarter of
+    // those products runs in front of the scores', and three beside the weights'
+    // vector operations.
+    wait_vmcnt<0>();
     barrier_only();
     uint32_t bad = masked(t0) ? find_bad(t0) : 0;
-    step(yes{}, no{}, t0, bad);
-    // (nothing has been summed up yet that the first maximum could change)
+    {
+      f32x16 s;
+      const unsigned char* kv = sm.kv[t0 % kStages];
+      first_keys(kv);
+      scores(s, kv, [](auto) {});
+      mfma_settle(s);
+      if (masked(t0)) mask(s, t0, bad);
+      for_each_index<kPieces>([&](auto i) { weigh(i, s, t0 & 1); });
+      // (nothing has been summed up yet that the first maximum could change)
+    }
+#pragma unroll
+    for (int db = 0; db < kDB; ++db) vb[db] = bf16x8{};
+    pf[0] = pf[1] = pf[2] = bf16x8{};
     // Tile t + 1 has landed, tile t's weights are in LDS, and everyone is done with
     // tile t - 1.
     auto turn = [&] {
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       barrier_only();
     };
-    auto catch_up = [&](int t) {
+    auto catch_up = [&](int t, const i32x4& moved) {
       const int par = t & 1;
       if (bad != 0) clear_bad(t, bad);
-      if (t > t0 && (sm.moved[par][0] | sm.moved[par][1] | sm.moved[par][2] | sm.moved[par][3]) != 0) {
+      if (t > t0 && __builtin_amdgcn_readfirstlane(moved[0] | moved[1] | moved[2] | moved[3]) != 0) {
         settle_all();
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
-          const float al = sm.moved[par][g] ? sm.alpha[par][32 * g + l32] : 1.f;
+          const float al = moved[g] ? sm.alpha[par][32 * g + l32] : 1.f;
 #pragma unroll
           for (int db = 0; db < kDB; ++db) rescale(o[db][g], al);
         }
@@ -525,125 +573,199 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     for (int t = t0; t + 1 < t1; ++t) {
       // (opaque to the compiler, which would keep every address that follows from
       // these in registers of its own over the loop)
-      asm volatile("" : "+v"(k_rd[0]), "+v"(k_rd[1]), "+v"(k_rd[2]), "+v"(k_rd[3]));
-      asm volatile("" : "+v"(v_rd[0][0]), "+v"(v_rd[0][1]), "+v"(v_rd[1][0]), "+v"(v_rd[1][1]));
-      asm volatile("" : "+v"(l32), "+v"(h));
+      asm volatile("" : "+v"(k_rd), "+v"(v_rd), "+v"(l32), "+v"(h), "+v"(load_key));
+      const unsigned char* kv = sm.kv[(t + 1) % kStages];
+      const unsigned char* kv_old = sm.kv[t % kStages];
+      const int par = t & 1;
       turn();
-      if (t + 2 < t1) issue(t + 2, source(t + 2));
-      catch_up(t);
+      first_keys(kv);
+      const i32x4 moved = sm.moved[par];
+      __builtin_amdgcn_sched_barrier(0);
+      last_products();
+      __builtin_amdgcn_sched_barrier(0);
+      catch_up(t, moved);
       bad = masked(t + 1) ? find_bad(t + 1) : 0;
-      step(yes{}, yes{}, t + 1, bad);
-      tell((t + 1) & 1);
+      const unsigned char* from;
+      f32x16 s;
+      scores(s, kv, [&](auto ix) {
+        constexpr int kk = ix();
+        if constexpr (kk == 0) from = at(t + 2);
+        if constexpr (kk == 4) look_up(t + 3);
+        // (tile t + 2's direct loads go out one by one; one tile past the piece's last
+        // is loaded and not used)
+        if constexpr (kk % 3 == 2 && kk / 3 < kPlanes) issue_plane(t + 2, from, std::integral_constant<int, kk / 3>{});
+        // (the first values and weights, ahead of their products)
+        constexpr int late = kk - (kSteps - kDB - 3);
+        if constexpr (late >= 0 && late < kDB) va[late] = load_v(kv_old, late, 0);
+        if constexpr (late >= kDB) pf[late - kDB] = load_p(par, late - kDB, 0);
+      });
+      // (what stands between the scores and their readers)
+      constexpr int kApart = 3;
+      for_each_index<kApart>([&](auto i) { product(i, va, par); });
+      load_values(vb, kv_old, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      mfma_settle(s);
+      __builtin_amdgcn_sched_barrier(0);
+      if (masked(t + 1)) mask(s, t + 1, bad);
+      __builtin_amdgcn_sched_barrier(0);
+      for_each_index<kPieces>([&](auto ix) {
+        constexpr int n = 3 * kHalf - kApart, a0 = kApart + ix() * n / kPieces, a1 = kApart + (ix() + 1) * n / kPieces;
+        for_each_index<a1 - a0>([&](auto i) {
+          constexpr int at = a0 + i();
+          if constexpr (at < 2 * kHalf) product(std::integral_constant<int, at>{}, va, par);
+          else product(std::integral_constant<int, at>{}, vb, par);
+        });
+        weigh(ix, s, par ^ 1);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      tell(par ^ 1);
     }
-    turn();
-    catch_up(t1 - 1);
-    step(no{}, yes{}, t1, 0);
-    settle_all();
-
-    // ---- results
     {
       const float l = l_run + xor32(l_run);
-      if (h == 0) {
-        sm.row_l[32 * wave + l32] = l;
-        sm.row_m[32 * wave + l32] = m_run * c;
+      if (h == 0) sm.row_l[32 * wave + l32] = l;
+      if (!whole && h == 0 && 32 * wave + l32 < valid) {
+        PieceRow& row = a.ws_row[static_cast<int64_t>(slot) * kRows + 32 * wave + l32];
+        row.m = m_run * c;
+        row.l = l;
       }
+      if (!whole && t0 == 0 && threadIdx.x == 0)
+        a.ws_cut[rank] = CutUnit{b, r0, valid, static_cast<int>((start + length - 1) / share)};
     }
-    __syncthreads();
-    if (!whole && threadIdx.x < kRows) {
-      float* ml = a.ws_ml + (static_cast<int64_t>(slot) * kRows + threadIdx.x) * 2;
-      if (threadIdx.x < valid) {
-        ml[0] = sm.row_m[threadIdx.x];
-        ml[1] = sm.row_l[threadIdx.x];
-      }
+    turn();
+    last_products();
+    catch_up(t1 - 1, sm.moved[(t1 - 1) & 1]);
+    {
+      const unsigned char* kv = sm.kv[(t1 - 1) % kStages];
+      const int par = (t1 - 1) & 1;
+      load_values(va, kv, 0);
+      load_values(vb, kv, 1);
+      for_each_index<3>([&](auto g) { pf[g()] = load_p(par, g(), 0); });
+      for_each_index<2 * kHalf>([&](auto i) { product(i, va, par); });
+      for_each_index<2 * kHalf>([&](auto i) { product(std::integral_constant<int, 2 * kHalf + i()>{}, vb, par); });
     }
+    settle_all();
+
+    // ---- results, 32 rows at a time: O / l, in bf16 where the unit is whole, or as a
+    // piece in fp16 under a power of two a wave's dims of a row (off by at most 2^-11 of
+    // the largest of them).  They pass through LDS (a part of the ring that no wave
+    // reads any more) so that a row's dims of a wave go out in one run.
+    constexpr int kPitch = kCols * 2 + 16;
+    unsigned char* stage = sm.kv[t1 % kStages] + wave * 32 * kPitch;
+    static_assert(kWaves * 32 * kPitch <= kTileBytes, "rows fit a tile");
+    {
+      for_each_index<kGroups>([&](auto gx) {
+        constexpr int g = gx();
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" : "+v"(l32), "+v"(h));
+        const int to_lane = rare(lane);
+        const float l = sm.row_l[32 * g + l32];
+        // (a piece without a visible key has weight 0 in the merge, and O = 0)
+        float mul = !whole && l == 0.f ? 0.f : 1.f / l;
+        if (!whole) {
+          float most = 0.f;
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      const int row = 32 * g + l32;
-      if (row >= valid) continue;
-      const float l = sm.row_l[row];
-      // (a piece without a visible key has weight 0 in the merge, and O = 0)
-      const float inv = !whole && l == 0.f ? 0.f : 1.f / l;
-      const int col = wave * kCols + 4 * h;
-      if (whole) {
-        uint16_t* out = static_cast<uint16_t*>(in.out) + (static_cast<int64_t>(b) * in.Nmax * in.Hq + r0 + row) * DL + col;
+          for (int db = 0; db < kDB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(o[db][g][i]));
+          most = max_xor32(most * mul);
+          // 2^14 to 2^15 for the largest
+          const int e = max(static_cast<int>(__float_as_uint(most) >> 23), 32);
+          if (h == 0 && 32 * g + l32 < valid)
+            a.ws_row[static_cast<int64_t>(slot) * kRows + 32 * g + l32].factor[wave] = __uint_as_float((e - 14) << 23);
+          mul *= __uint_as_float((268 - e) << 23);
+        }
+        unsigned char* to = stage + l32 * kPitch + 8 * h;
 #pragma unroll
         for (int db = 0; db < kDB; ++db)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
+            const float x0 = o[db][g][4 * q] * mul, x1 = o[db][g][4 * q + 1] * mul;
+            const float x2 = o[db][g][4 * q + 2] * mul, x3 = o[db][g][4 * q + 3] * mul;
             uint2 w;
-            w.x = pack_bf16x2(o[db][g][4 * q] * inv, o[db][g][4 * q + 1] * inv);
-            w.y = pack_bf16x2(o[db][g][4 * q + 2] * inv, o[db][g][4 * q + 3] * inv);
-            *reinterpret_cast<uint2*>(out + 32 * db + 8 * q) = w;
+            w.x = whole ? pack_bf16x2(x0, x1) : pack_f16x2(x0, x1);
+            w.y = whole ? pack_bf16x2(x2, x3) : pack_f16x2(x2, x3);
+            *reinterpret_cast<uint2*>(to + 64 * db + 16 * q) = w;
           }
-      } else {
-        float* out = a.ws_o + (static_cast<int64_t>(slot) * kRows + row) * DL + col;
+        constexpr int kLanes = kCols / 8;  // of a row
+        uint16_t* out = whole ? static_cast<uint16_t*>(in.out) + (static_cast<int64_t>(b) * in.Nmax * in.Hq + r0) * DL
+                              : reinterpret_cast<uint16_t*>(a.ws_o) + static_cast<int64_t>(slot) * kRows * DL;
 #pragma unroll
-        for (int db = 0; db < kDB; ++db)
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<f32x4*>(out + 32 * db + 8 * q) =
-                f32x4{o[db][g][4 * q] * inv, o[db][g][4 * q + 1] * inv, o[db][g][4 * q + 2] * inv, o[db][g][4 * q + 3] * inv};
-      }
+        for (int i = 0; i < 32 * kLanes / kWave; ++i) {
+          const int row = i * (kWave / kLanes) + to_lane / kLanes, col = to_lane % kLanes * 8;
+          const u32x4 x = *reinterpret_cast<const u32x4*>(stage + row * kPitch + col * 2);
+          if (32 * g + row < valid)
+            *reinterpret_cast<u32x4*>(out + static_cast<int64_t>(32 * g + row) * DL + wave * kCols + col) = x;
+        }
+      });
     }
-    pos += t1 - t0;
-    slot = 2 * rank + 1;
+    pos = stop;
   }
 }
 
-// Joins the pieces of cut units: workgroup x looks after the unit that the cut
-// after share x is the first to fall into, a wave a row.
+// Joins the pieces of the cut unit that begins in workgroup x's share, a wave a row:
+// lane p takes piece p's maximum and sum for the weights, then each lane its dims of
+// every piece.
 template <int DL>
 __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
   constexpr int kEach = DL / kWave;  // dims a lane
+  typedef _Float16 Dims __attribute__((ext_vector_type(DL / kWave)));
   const LatentAttn& in = a.in;
   if (halted(in.status)) return;
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  int64_t total, share;
-  const int x = blockIdx.x + 1;
-  const Place place = find_place(in, lane, &total, [&](int64_t t) {
-    share = latent::share_of(t, a.W);
-    return x * share;
-  });
-  const int64_t cut = x * share;
-  if (cut >= total) return;
-  const int b = place.b;
-  const int n = min(max(in.n_nodes[b], 0), in.Nmax), P = max(in.prefix_len[b], 0);
-  const int64_t tiles = latent::tiles_of(P, n);
-  const int64_t unit = (cut - place.before) / tiles;
-  const int64_t first = place.before + unit * tiles;
-  if (cut == first || cut - share > first) return;  // (not cut here, or an earlier cut's)
-  const int64_t r0 = unit * kRows;
-  const int valid = static_cast<int>(min(static_cast<int64_t>(kRows), static_cast<int64_t>(n) * in.Hq - r0));
-  const int64_t past = first + tiles;
-  const int slot0 = 2 * (x - 1) + (cut - share != first);
-  for (int row = blockIdx.y * kWaves + wave; row < valid; row += gridDim.y * kWaves) {
-    float M = kNoMax * __FLT_MAX__, L = 0.f;  // (-inf)
-    float acc[kEach];
+  const int lane = threadIdx.x % kWave;
+  const int x = blockIdx.x;
+  const CutUnit cut = a.ws_cut[x];
+  const int row = blockIdx.y * kWaves + threadIdx.x / kWave;
+  if (row >= cut.valid) return;
+  const int pieces = cut.last - x + 1;
+  // (the first piece begins in share x, the others go on in the next ones)
+  auto slot = [&](int p) { return static_cast<int64_t>(p == 0 ? 2 * x + 1 : 2 * (x + p)) * kRows + row; };
+  float M = kNoMax, L = 0.f;
+  float acc[kEach];
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
-    int slot = slot0;
-    for (int64_t at = cut;; at += share) {
-      const float2 ml = *reinterpret_cast<const float2*>(a.ws_ml + (static_cast<int64_t>(slot) * kRows + row) * 2);
-      const float* p = a.ws_o + (static_cast<int64_t>(slot) * kRows + row) * DL + lane * kEach;
-      if (ml.y != 0.f) {
-        const float m_new = fmaxf(M, ml.x);
-        const float old = exp2_fast(M - m_new), w = exp2_fast(ml.x - m_new) * ml.y;
-        L = L * old + w;
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) acc[e] = acc[e] * old + w * p[e];
-        M = m_new;
-      }
-      if (at >= past) break;
-      slot = 2 * static_cast<int>(at / share);
+  for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
+  for (int p0 = 0; p0 < pieces; p0 += kWave) {
+    const int count = min(kWave, pieces - p0);
+    float m = kNoMax, l = 0.f;
+    if (lane < count) {
+      const PieceRow& r = a.ws_row[slot(p0 + lane)];
+      l = r.l;
+      if (l != 0.f) m = r.m;
     }
-    const float inv = 1.f / L;
-    uint16_t* out = static_cast<uint16_t*>(in.out) + (static_cast<int64_t>(b) * in.Nmax * in.Hq + r0 + row) * DL + lane * kEach;
-    uint32_t w[kEach / 2];
+    const float m_new = fmaxf(M, wave_max_dpp(m));
+    const float old = exp2_fast(M - m_new), w = l != 0.f ? exp2_fast(m - m_new) * l : 0.f;
+    L = L * old + wave_sum_dpp(w);
+    M = m_new;
 #pragma unroll
-    for (int e = 0; e < kEach / 2; ++e) w[e] = pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+    for (int e = 0; e < kEach; ++e) acc[e] *= old;
+    constexpr int kUnroll = 8;
+    for (int p = 0; p < count; p += kUnroll) {
+      Dims d[kUnroll];
+      float f[kUnroll];
 #pragma unroll
-    for (int e = 0; e < kEach / 2; ++e) reinterpret_cast<uint32_t*>(out)[e] = w[e];
+      for (int u = 0; u < kUnroll; ++u) {
+        const int64_t s = slot(p0 + min(p + u, count - 1));
+        d[u] = *reinterpret_cast<const Dims*>(a.ws_o + s * DL + lane * kEach);
+        f[u] = a.ws_row[s].factor[lane / (kWave / kWaves)];
+      }
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const float wu = p + u < count ? __shfl(w, p + u, kWave) : 0.f;
+        // (a piece of weight 0 has no rows to be read: it may hold anything)
+        if (wu != 0.f) {
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) acc[e] = __builtin_fmaf(wu * f[u], static_cast<float>(d[u][e]), acc[e]);
+        }
+      }
+    }
   }
+  const float inv = 1.f / L;
+  uint16_t* out = static_cast<uint16_t*>(in.out) +
+                  (static_cast<int64_t>(cut.b) * in.Nmax * in.Hq + cut.r0 + row) * DL + lane * kEach;
+  uint32_t w[kEach / 2];
+#pragma unroll
+  for (int e = 0; e < kEach / 2; ++e) w[e] = pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+#pragma unroll
+  for (int e = 0; e < kEach / 2; ++e) reinterpret_cast<uint32_t*>(out)[e] = w[e];
 }
 
 // The float32 path, on the vector ALUs: a workgroup per (sequence, node, four
@@ -750,7 +872,7 @@ hipError_t launch_bf16(const LatentArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((latent_attn_kernel<DL, false>), dim3(a.W), dim3(kThreads), 0, stream, a);
   const hipError_t rc = hipGetLastError();
   if (rc != hipSuccess || a.W < 2) return rc;
-  hipLaunchKernelGGL((latent_merge_kernel<DL>), dim3(a.W - 1, 16), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL((latent_merge_kernel<DL>), dim3(a.W - 1, kRows / kWaves), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -758,8 +880,8 @@ hipError_t launch_bf16(const LatentArgs& a, hipStream_t stream) {
 
 size_t latent_attn_workspace_bytes(const LatentAttn& s, int d_latent, int dtype, int cus) {
   if (dtype == LTD_DTYPE_F32 || s.B == 0) return 0;
-  const int W = grid_of(s, cus);
-  return W < 2 ? 0 : static_cast<size_t>(2) * W * kRows * (d_latent + 2) * sizeof(float);
+  const size_t W = grid_of(s, cus);
+  return 2 * W * kRows * (d_latent * sizeof(_Float16) + sizeof(PieceRow)) + W * sizeof(CutUnit);
 }
 
 hipError_t launch_latent_attn(const LatentAttn& s, int d_latent, int dtype, void* workspace, int cus,
@@ -773,10 +895,15 @@ hipError_t launch_latent_attn(const LatentAttn& s, int d_latent, int dtype, void
   LatentArgs a{};
   a.in = s;
   a.W = grid_of(s, cus);
-  a.ws_o = static_cast<float*>(workspace);
-  a.ws_ml = a.ws_o + static_cast<int64_t>(2) * a.W * kRows * d_latent;
+  a.ws_o = static_cast<_Float16*>(workspace);
+  a.ws_cut = reinterpret_cast<CutUnit*>(a.ws_o + static_cast<int64_t>(2) * a.W * kRows * d_latent);
+  a.ws_row = reinterpret_cast<PieceRow*>(a.ws_cut + a.W);
   a.scale_log2 = s.scale * kLog2e;
   a.lazy_gap = kLazyMax / a.scale_log2;
+  // row / kv_rows = floor(2 row * magic / 2^(32 + shift)): with kv_rows <= 2^shift and magic =
+  // floor(2^(31 + shift) / kv_rows) + 1 it is exact for every row below 2^31.
+  while (a.row_shift < 31 && (1u << a.row_shift) < static_cast<uint32_t>(s.kv_rows)) ++a.row_shift;
+  a.row_magic = static_cast<uint32_t>((uint64_t{1} << (31 + a.row_shift)) / s.kv_rows + 1);
   return d_latent == 512 ? launch_bf16<512>(a, stream) : launch_bf16<256>(a, stream);
 }
 
