@@ -41,10 +41,9 @@ constexpr float kLazyMax = 16.f;
 constexpr int kAhead = 6;                      // key fragments in flight
 constexpr float kNoMax = -__FLT_MAX__;
 
-// A piece's row beside its O / l: the maximum (log2 units), the sum, and for each wave's
-// dims the power of two that the stored values are to be multiplied by.
+// A piece's row beside its O / l: the maximum (log2 units) and the sum.
 struct PieceRow {
-  float m, l, factor[kWaves];
+  float m, l;
 };
 // A unit that was cut: its rows, and the workgroups that have the other pieces.
 struct CutUnit {
@@ -53,7 +52,7 @@ struct CutUnit {
 
 struct LatentArgs {
   LatentAttn in;
-  _Float16* ws_o;    // [2 W][128][DL]: pieces' O / l
+  uint16_t* ws_o;    // [2 W][128][DL] bf16: pieces' O / l
   PieceRow* ws_row;  // [2 W][128]
   CutUnit* ws_cut;   // [W]: the cut unit that begins in a workgroup's share (valid 0: none)
   int W;         // workgroups
@@ -68,11 +67,16 @@ struct Place {
   int64_t before;  // length before sequence b
 };
 
-// Length of sequence b's units (0 past the batch; counts out of range are clamped).
-__device__ __forceinline__ int64_t seq_length(const LatentAttn& a, int b) {
-  if (b >= a.B) return 0;
-  const int n = min(max(a.n_nodes[b], 0), a.Nmax), P = max(a.prefix_len[b], 0);
-  return latent::length_of(P, n, a.Hq);
+// Nodes and prefix of sequence b (none past the batch; what is out of range is clamped).
+struct Seq {
+  int n, P;
+};
+__device__ __forceinline__ Seq seq_of(const LatentAttn& a, int b) {
+  if (b >= a.B) return Seq{0, 0};
+  return Seq{min(max(a.n_nodes[b], 0), a.Nmax), max(a.prefix_len[b], 0)};
+}
+__device__ __forceinline__ int64_t seq_length(const LatentAttn& a, const Seq& s) {
+  return s.n > 0 ? latent::length_of(s.P, s.n, a.Hq) : 0;
 }
 
 // x moved between lanes by DPP (0 where there is none to take).
@@ -106,13 +110,13 @@ __device__ __forceinline__ int64_t uniform(int64_t v) {
 }
 
 // The length of all sequences' units, and the sequence that place pos(length) falls
-// into (B past the end); every wave works it out by itself.
+// into (B past the end); every wave works it out by itself.  seq: sequence `lane`.
 template <class Pos>
-__device__ __forceinline__ Place find_place(const LatentAttn& a, int lane, int64_t* total_out, Pos pos) {
-  const int64_t mine = seq_length(a, lane), upto = wave_scan(mine);
+__device__ __forceinline__ Place find_place(const LatentAttn& a, int lane, const Seq& seq, int64_t* total_out, Pos pos) {
+  const int64_t mine = seq_length(a, seq), upto = wave_scan(mine);
   const int64_t first = read_lane(upto, kWave - 1);
   int64_t total = first;
-  for (int b0 = kWave; b0 < a.B; b0 += kWave) total += read_lane(wave_scan(seq_length(a, b0 + lane)), kWave - 1);
+  for (int b0 = kWave; b0 < a.B; b0 += kWave) total += read_lane(wave_scan(seq_length(a, seq_of(a, b0 + lane))), kWave - 1);
   *total_out = total;
   const int64_t at = pos(total);
   if (at < first) {
@@ -121,7 +125,7 @@ __device__ __forceinline__ Place find_place(const LatentAttn& a, int lane, int64
   }
   int64_t before = first;
   for (int b0 = kWave; b0 < a.B; b0 += kWave) {
-    const int64_t here = seq_length(a, b0 + lane), past = wave_scan(here) + before;
+    const int64_t here = seq_length(a, seq_of(a, b0 + lane)), past = wave_scan(here) + before;
     const uint64_t hit = __ballot(at < past);
     if (hit != 0) {
       const int l = __ffsll(static_cast<long long>(hit)) - 1;
@@ -231,7 +235,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
   int64_t total, share, pos;
   const int rank = a.W % 8 == 0 ? static_cast<int>(blockIdx.x % 8) * (a.W / 8) + static_cast<int>(blockIdx.x / 8)
                                 : static_cast<int>(blockIdx.x);
-  const Place place = find_place(in, lane, &total, [&](int64_t t) {
+  const Seq first_seqs = seq_of(in, lane);
+  const Place place = find_place(in, lane, first_seqs, &total, [&](int64_t t) {
     share = latent::share_of(t, a.W);
     return rank * share;
   });
@@ -262,8 +267,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
 
   while (pos < end) {
     // ---- the unit's piece in this share
-    const int n = min(max(__builtin_amdgcn_readfirstlane(in.n_nodes[b]), 0), in.Nmax);
-    const int P = max(__builtin_amdgcn_readfirstlane(in.prefix_len[b]), 0);
+    const Seq seq = b < kWave ? first_seqs : seq_of(in, b);
+    const int n = __builtin_amdgcn_readlane(seq.n, b % kWave), P = __builtin_amdgcn_readlane(seq.P, b % kWave);
     const int64_t length = latent::kUnitCost + latent::tiles_of(P, n);
     const int64_t all = latent::units_of(n, in.Hq) * length;
     if (pos >= before + all) {
@@ -271,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
       ++b;
       continue;
     }
-    const int unit = static_cast<int>(uniform((pos - before) / length));
+    const int unit = __builtin_amdgcn_readfirstlane(static_cast<int>(latent::quotient(pos - before, length)));
     const int64_t start = before + unit * length;
     const int64_t stop = uniform(min(start + length, end));
     const int t0 = __builtin_amdgcn_readfirstlane(static_cast<int>(latent::tile_at(pos - start)));
@@ -292,11 +297,11 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     // tile t (rows past the last are not read: the last one is, again, and never
     // visible).  A paged cache's block ids are read a tile ahead.
     int32_t block = 0;
-    auto look_up = [&](int t) {
+    auto look_up = [&](int t, int32_t& block) {
       if constexpr (kPaged)
         block = in.block_table[static_cast<int64_t>(b) * in.max_blocks + block_of(min(t * kKeys + load_key, last))];
     };
-    auto at = [&](int t) -> const unsigned char* {
+    auto at = [&](int t, int32_t block) -> const unsigned char* {
       const int row = min(t * kKeys + load_key, last);
       // (rows of a cache are counted in 32 bits: 2^31 of them pass any memory)
       const uint32_t place = kPaged ? block * in.kv_rows + (row - block_of(row) * in.kv_rows) : b * in.kv_rows + row;
@@ -306,16 +311,14 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     auto issue_plane = [&](int t, const unsigned char* from, auto plane) {
       dma16_at<plane() * 128>(kv_lds + (t % kStages) * kTileBytes + wave * 1024 + plane() * kPlane, from);
     };
-    auto issue = [&](int t) {
-      const unsigned char* from = at(t);
+    auto issue = [&](int t, int32_t block) {
+      const unsigned char* from = at(t, block);
       for_each_index<kPlanes>([&](auto g) { issue_plane(t, from, g); });
     };
-    look_up(t0);
-    issue(t0);
-    look_up(t0 + 1);
-    if (t0 + 1 < t1) issue(t0 + 1);
-    look_up(t0 + 2);
-
+    int32_t block0 = 0, block1 = 0;
+    look_up(t0, block0);
+    look_up(t0 + 1, block1);
+    look_up(t0 + 2, block);
     // ---- queries: lane holds row l32 of the wave's 32, dims 16 kk + 8 h ..
     bf16x8 qf[kSteps];
     int node;
@@ -331,6 +334,9 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
 #pragma unroll
       for (int kk = 0; kk < kRopeDims / 16; ++kk) qf[DL / 16 + kk] = *reinterpret_cast<const bf16x8*>(qr + 16 * kk);
     }
+
+    issue(t0, block0);
+    if (t0 + 1 < t1) issue(t0 + 1, block1);
 
     // ---- ancestor sets (256 bits a node) by pointer doubling: anc(i) |= anc(jump(i)),
     // jump(i) = jump(jump(i)); thread i has node i
@@ -589,8 +595,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
       f32x16 s;
       scores(s, kv, [&](auto ix) {
         constexpr int kk = ix();
-        if constexpr (kk == 0) from = at(t + 2);
-        if constexpr (kk == 4) look_up(t + 3);
+        if constexpr (kk == 0) from = at(t + 2, block);
+        if constexpr (kk == 4) look_up(t + 3, block);
         // (tile t + 2's direct loads go out one by one; one tile past the piece's last
         // is loaded and not used)
         if constexpr (kk % 3 == 2 && kk / 3 < kPlanes) issue_plane(t + 2, from, std::integral_constant<int, kk / 3>{});
@@ -629,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
         row.l = l;
       }
       if (!whole && t0 == 0 && threadIdx.x == 0)
-        a.ws_cut[rank] = CutUnit{b, r0, valid, static_cast<int>((start + length - 1) / share)};
+        a.ws_cut[rank] = CutUnit{b, r0, valid, static_cast<int>(latent::quotient(start + length - 1, share))};
     }
     turn();
     last_products();
@@ -645,50 +651,37 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     }
     settle_all();
 
-    // ---- results, 32 rows at a time: O / l, in bf16 where the unit is whole, or as a
-    // piece in fp16 under a power of two a wave's dims of a row (off by at most 2^-11 of
-    // the largest of them).  They pass through LDS (a part of the ring that no wave
-    // reads any more) so that a row's dims of a wave go out in one run.
+    // ---- results, 32 rows at a time: O / l in bf16, of a whole unit to `out`, as a piece
+    // to the workspace.  (Rounding a piece costs at most 2^-9 of its own weight; in fp16
+    // under a power of two a row they were a third of the kernel's code, read but once a
+    // unit: 15600 cycles each.)  They pass through LDS, a part of the ring that no wave
+    // reads any more, so that a row's dims of a wave go out in one run.
     constexpr int kPitch = kCols * 2 + 16;
     unsigned char* stage = sm.kv[t1 % kStages] + wave * 32 * kPitch;
     static_assert(kWaves * 32 * kPitch <= kTileBytes, "rows fit a tile");
     {
       for_each_index<kGroups>([&](auto gx) {
         constexpr int g = gx();
+        if (32 * g >= valid) return;
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("" : "+v"(l32), "+v"(h));
         const int to_lane = rare(lane);
         const float l = sm.row_l[32 * g + l32];
         // (a piece without a visible key has weight 0 in the merge, and O = 0)
-        float mul = !whole && l == 0.f ? 0.f : 1.f / l;
-        if (!whole) {
-          float most = 0.f;
-#pragma unroll
-          for (int db = 0; db < kDB; ++db)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(o[db][g][i]));
-          most = max_xor32(most * mul);
-          // 2^14 to 2^15 for the largest
-          const int e = max(static_cast<int>(__float_as_uint(most) >> 23), 32);
-          if (h == 0 && 32 * g + l32 < valid)
-            a.ws_row[static_cast<int64_t>(slot) * kRows + 32 * g + l32].factor[wave] = __uint_as_float((e - 14) << 23);
-          mul *= __uint_as_float((268 - e) << 23);
-        }
+        const float mul = !whole && l == 0.f ? 0.f : 1.f / l;
         unsigned char* to = stage + l32 * kPitch + 8 * h;
 #pragma unroll
         for (int db = 0; db < kDB; ++db)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const float x0 = o[db][g][4 * q] * mul, x1 = o[db][g][4 * q + 1] * mul;
-            const float x2 = o[db][g][4 * q + 2] * mul, x3 = o[db][g][4 * q + 3] * mul;
             uint2 w;
-            w.x = whole ? pack_bf16x2(x0, x1) : pack_f16x2(x0, x1);
-            w.y = whole ? pack_bf16x2(x2, x3) : pack_f16x2(x2, x3);
+            w.x = pack_bf16x2(o[db][g][4 * q] * mul, o[db][g][4 * q + 1] * mul);
+            w.y = pack_bf16x2(o[db][g][4 * q + 2] * mul, o[db][g][4 * q + 3] * mul);
             *reinterpret_cast<uint2*>(to + 64 * db + 16 * q) = w;
           }
         constexpr int kLanes = kCols / 8;  // of a row
         uint16_t* out = whole ? static_cast<uint16_t*>(in.out) + (static_cast<int64_t>(b) * in.Nmax * in.Hq + r0) * DL
-                              : reinterpret_cast<uint16_t*>(a.ws_o) + static_cast<int64_t>(slot) * kRows * DL;
+                              : a.ws_o + static_cast<int64_t>(slot) * kRows * DL;
 #pragma unroll
         for (int i = 0; i < 32 * kLanes / kWave; ++i) {
           const int row = i * (kWave / kLanes) + to_lane / kLanes, col = to_lane % kLanes * 8;
@@ -708,7 +701,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
 template <int DL>
 __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
   constexpr int kEach = DL / kWave;  // dims a lane
-  typedef _Float16 Dims __attribute__((ext_vector_type(DL / kWave)));
+  typedef __bf16 Dims __attribute__((ext_vector_type(DL / kWave)));
   const LatentAttn& in = a.in;
   if (halted(in.status)) return;
   const int lane = threadIdx.x % kWave;
@@ -740,12 +733,10 @@ __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
     constexpr int kUnroll = 8;
     for (int p = 0; p < count; p += kUnroll) {
       Dims d[kUnroll];
-      float f[kUnroll];
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         const int64_t s = slot(p0 + min(p + u, count - 1));
         d[u] = *reinterpret_cast<const Dims*>(a.ws_o + s * DL + lane * kEach);
-        f[u] = a.ws_row[s].factor[lane / (kWave / kWaves)];
       }
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
@@ -753,7 +744,7 @@ __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
         // (a piece of weight 0 has no rows to be read: it may hold anything)
         if (wu != 0.f) {
 #pragma unroll
-          for (int e = 0; e < kEach; ++e) acc[e] = __builtin_fmaf(wu * f[u], static_cast<float>(d[u][e]), acc[e]);
+          for (int e = 0; e < kEach; ++e) acc[e] = __builtin_fmaf(wu, static_cast<float>(d[u][e]), acc[e]);
         }
       }
     }
@@ -881,7 +872,7 @@ hipError_t launch_bf16(const LatentArgs& a, hipStream_t stream) {
 size_t latent_attn_workspace_bytes(const LatentAttn& s, int d_latent, int dtype, int cus) {
   if (dtype == LTD_DTYPE_F32 || s.B == 0) return 0;
   const size_t W = grid_of(s, cus);
-  return 2 * W * kRows * (d_latent * sizeof(_Float16) + sizeof(PieceRow)) + W * sizeof(CutUnit);
+  return 2 * W * kRows * (d_latent * sizeof(uint16_t) + sizeof(PieceRow)) + W * sizeof(CutUnit);
 }
 
 hipError_t launch_latent_attn(const LatentAttn& s, int d_latent, int dtype, void* workspace, int cus,
@@ -895,7 +886,7 @@ hipError_t launch_latent_attn(const LatentAttn& s, int d_latent, int dtype, void
   LatentArgs a{};
   a.in = s;
   a.W = grid_of(s, cus);
-  a.ws_o = static_cast<_Float16*>(workspace);
+  a.ws_o = static_cast<uint16_t*>(workspace);
   a.ws_cut = reinterpret_cast<CutUnit*>(a.ws_o + static_cast<int64_t>(2) * a.W * kRows * d_latent);
   a.ws_row = reinterpret_cast<PieceRow*>(a.ws_cut + a.W);
   a.scale_log2 = s.scale * kLog2e;

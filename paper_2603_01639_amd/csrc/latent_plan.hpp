@@ -23,9 +23,14 @@ constexpr int64_t tiles_of(int64_t P, int64_t n) { return (P + n + kKeyTile - 1)
 constexpr int64_t length_of(int64_t P, int64_t n, int64_t heads) {
   return units_of(n, heads) * (kUnitCost + tiles_of(P, n));
 }
+// floor(x / y) for 0 <= x < 2^52, by one division in float64 (a quotient just below an
+// integer is below it by 1 / x or more of itself, which float64 keeps apart).
+constexpr int64_t quotient(int64_t x, int64_t y) {
+  return static_cast<int64_t>(static_cast<double>(x) / static_cast<double>(y));
+}
 // Length of a share, for `total` and W workgroups.
 constexpr int64_t share_of(int64_t total, int W) {
-  const int64_t even = (total + W - 1) / W;
+  const int64_t even = quotient(total + W - 1, W);
   return even < kMinShare ? kMinShare : even;
 }
 // The tile that a unit's place `at` belongs to (its own cost comes first).
