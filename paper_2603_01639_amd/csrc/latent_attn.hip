@@ -190,6 +190,9 @@ __device__ __forceinline__ void mfma_next(f32x16& s, bf16x8 a, bf16x8 b) {
   asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void mfma_settle(f32x16& s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s)); }
+// The same after three further products: the last of them went out when the pipe had
+// been through the first two, 64 cycles after s was done.
+__device__ __forceinline__ void mfma_settled(f32x16& s) { asm volatile("s_nop 3" : "+v"(s)); }
 __device__ __forceinline__ void settled(f32x16& o) { asm volatile("" : "+a"(o)); }
 
 // A direct load of 16 bytes a lane (lane i's land at lds + 16 i) from kOff bytes past
@@ -301,13 +304,15 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
       if constexpr (kPaged)
         block = in.block_table[static_cast<int64_t>(b) * in.max_blocks + block_of(min(t * kKeys + load_key, last))];
     };
-    auto at = [&](int t, int32_t block) -> const unsigned char* {
-      const int row = min(t * kKeys + load_key, last);
+    auto place_of = [&](int row, int32_t block) -> uint32_t {
       // (rows of a cache are counted in 32 bits: 2^31 of them pass any memory)
-      const uint32_t place = kPaged ? block * in.kv_rows + (row - block_of(row) * in.kv_rows) : b * in.kv_rows + row;
+      return kPaged ? block * in.kv_rows + (row - block_of(row) * in.kv_rows) : b * in.kv_rows + row;
+    };
+    auto source = [&](uint32_t place) {
       return static_cast<const unsigned char*>(in.cache) +
              (static_cast<uint64_t>(place) * kRowBytes + ((lane & 7) ^ swz(load_key)) * 16);
     };
+    auto at = [&](int t, int32_t block) { return source(place_of(min(t * kKeys + load_key, last), block)); };
     auto issue_plane = [&](int t, const unsigned char* from, auto plane) {
       dma16_at<plane() * 128>(kv_lds + (t % kStages) * kTileBytes + wave * 1024 + plane() * kPlane, from);
     };
@@ -406,6 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     // (With two products and two weights a piece the vector operations of a piece
     // outlasted the second product: 1250 cycles a tile where the products take 670.)
     float alpha = 1.f, top, neg, ps, p0;
+    uint64_t moves;
     u32x4 pk[2];
     constexpr int kPieces = 23;
     auto weigh = [&](auto piece, const f32x16& s, int par) {
@@ -426,24 +432,25 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
         constexpr int j = (i - 6) / 2, q = j >> 2, r = 4 * q + 8 * ((j >> 1) & 1) + 2 * (j & 1);
         if constexpr ((i - 6) % 2 == 0) {
           p0 = exp2_fast(__builtin_fmaf(s[r], c, neg));
+          // (tells the other waves what the rows' sums so far are multiplied by)
+          if constexpr (j == 1) moves = __ballot(alpha != 1.f);
+          if constexpr (j == 2) {
+            if (moves != 0) sm.alpha[par][32 * wave + l32] = alpha;
+          }
+          if constexpr (j == 3) reinterpret_cast<int*>(&sm.moved[par])[wave] = moves != 0;  // (all lanes the same)
           if constexpr (j == 4) sm.p[par][h][32 * wave + l32] = pk[0];
         } else {
           const float p1 = exp2_fast(__builtin_fmaf(s[r + 1], c, neg));
           // (the sum is that of the rounded weights, the very ones that multiply the values)
           const bf16x2 w = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
           ps = __builtin_amdgcn_fdot2_f32_bf16(w, __builtin_bit_cast(bf16x2, 0x3F803F80u), ps, false);
+          asm volatile("" : "+v"(ps));  // (here, not all of them after the last product)
           pk[q][j & 3] = __builtin_bit_cast(uint32_t, w);
         }
       } else {
         sm.p[par][2 + h][32 * wave + l32] = pk[1];
         l_run = l_run * alpha + ps;
       }
-    };
-    // Tells the other waves what the rows' sums so far are multiplied by.
-    auto tell = [&](int par) {
-      const uint64_t any = __ballot(alpha != 1.f);
-      if (any != 0) sm.alpha[par][32 * wave + l32] = alpha;
-      if (lane == 0) reinterpret_cast<int*>(&sm.moved[par])[wave] = any != 0;
     };
     // Hides the keys that the lane's node does not see.  A tree key whose latent part
     // holds a NaN or an infinity (bad) gives NaN to the nodes that see it.
@@ -513,7 +520,13 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     constexpr int kHalf = 2 * kDB;  // products of two q
     // The last quarter of a tile's products waits in registers for the next step: it
     // fills the time that the step's first reads take.
-    auto last_products = [&] { for_each_index<kHalf>([&](auto i) { product(std::integral_constant<int, 3 * kHalf + i()>{}, vb, 0); }); };
+    auto last_products = [&](auto beside) {
+      for_each_index<kHalf>([&](auto i) {
+        product(std::integral_constant<int, 3 * kHalf + i()>{}, vb, 0);
+        beside(i);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
     auto load_values = [&](bf16x8(&v)[kDB], const unsigned char* kv, int ks) {
 #pragma unroll
       for (int db = 0; db < kDB; ++db) v[db] = load_v(kv, db, ks);
@@ -587,16 +600,21 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
       first_keys(kv);
       const i32x4 moved = sm.moved[par];
       __builtin_amdgcn_sched_barrier(0);
-      last_products();
-      __builtin_amdgcn_sched_barrier(0);
+      // (tile t + 2's addresses, a few instructions beside each product)
+      int row;
+      uint32_t place;
+      const unsigned char* from;
+      last_products([&](auto i) {
+        if constexpr (i() == 0) row = min((t + 2) * kKeys + load_key, last);
+        if constexpr (i() == 1) place = place_of(row, block);
+        if constexpr (i() == 2) from = source(place);
+        if constexpr (i() == 3) look_up(t + 3, block);
+      });
       catch_up(t, moved);
       bad = masked(t + 1) ? find_bad(t + 1) : 0;
-      const unsigned char* from;
       f32x16 s;
       scores(s, kv, [&](auto ix) {
         constexpr int kk = ix();
-        if constexpr (kk == 0) from = at(t + 2, block);
-        if constexpr (kk == 4) look_up(t + 3, block);
         // (tile t + 2's direct loads go out one by one; one tile past the piece's last
         // is loaded and not used)
         if constexpr (kk % 3 == 2 && kk / 3 < kPlanes) issue_plane(t + 2, from, std::integral_constant<int, kk / 3>{});
@@ -610,7 +628,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
       for_each_index<kApart>([&](auto i) { product(i, va, par); });
       load_values(vb, kv_old, 1);
       __builtin_amdgcn_sched_barrier(0);
-      mfma_settle(s);
+      mfma_settled(s);
       __builtin_amdgcn_sched_barrier(0);
       if (masked(t + 1)) mask(s, t + 1, bad);
       __builtin_amdgcn_sched_barrier(0);
@@ -624,7 +642,6 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
         weigh(ix, s, par ^ 1);
         __builtin_amdgcn_sched_barrier(0);
       });
-      tell(par ^ 1);
     }
     {
       const float l = l_run + xor32(l_run);
@@ -638,7 +655,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
         a.ws_cut[rank] = CutUnit{b, r0, valid, static_cast<int>(latent::quotient(start + length - 1, share))};
     }
     turn();
-    last_products();
+    last_products([](auto) {});
     catch_up(t1 - 1, sm.moved[(t1 - 1) & 1]);
     {
       const unsigned char* kv = sm.kv[(t1 - 1) % kStages];
