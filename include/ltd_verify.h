@@ -590,8 +590,8 @@ int ltd_tree_accept_processed(const float* logits, const int32_t* draft_tokens,
  *                for consecutive tokens (depth[b][i] = i).
  *   n_rows       [B] int32 in [0, Nmax]; rows i >= n_rows[b] are not written.
  *   rot_dim even, 2 <= rot_dim, rot_offset >= 0, rot_offset + rot_dim <= d <=
- *   LTD_ROPE_MAX_DIM, (Hq + Hk) * d <= 2^24, Nmax and positions up to
- *   LTD_MAX_LENGTH; Nmax may exceed LTD_MAX_NODES.  mscale is finite.
+ *   LTD_ROPE_MAX_DIM, (Hq + Hk) * d <= 2^24, B * Nmax < 2^31 - 1, Nmax and positions
+ *   up to LTD_MAX_LENGTH; Nmax may exceed LTD_MAX_NODES.  mscale is finite.
  * Any alignment is taken; 16-byte aligned rows and heads are faster.
  * With validate != 0: LTD_STATUS_BAD_NNODES (n_rows) and LTD_STATUS_BAD_PREFIX
  * (a position outside [0, LTD_MAX_LENGTH)).
@@ -614,8 +614,8 @@ int ltd_tree_rope(const void* q, int64_t q_row_stride, int64_t q_head_stride, vo
  *   + d_rope] (dtype), logical row r of sequence b in block
  *   block_table[b][r / kv_rows].
  * d_latent is 256 or 512, d_rope is LTD_LATENT_ROPE; anything else is
- * LTD_EUNSUPPORTED, as are more than LTD_MAX_LENGTH rows to append or max_prefix.
- * Caches are 16-byte aligned (LTD_EINVAL otherwise).
+ * LTD_EUNSUPPORTED, as are more than LTD_MAX_LENGTH rows to append or max_prefix,
+ * and B * Nmax >= 2^31 - 1 rows to append.  Caches are 16-byte aligned (LTD_EINVAL otherwise).
  */
 
 /*

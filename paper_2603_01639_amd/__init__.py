@@ -413,6 +413,9 @@ def _space(workspace):
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
+_calls = {}
+
+
 def _run(fn, args, tensors, stream):
     """Calls fn(*args, stream) on the GPU that holds the tensors, the last of
     which is the call's status."""
@@ -429,8 +432,10 @@ def _run(fn, args, tensors, stream):
     if stream is not None and stream.device.index != dev:
         raise ValueError(f"{fn}: tensors on {tensors[0].device}, a stream of {stream.device}")
     handle = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
-    call = getattr(lib(), fn)
-    if torch.cuda.current_device() == dev:
+    call = _calls.get(fn)
+    if call is None:
+        call = _calls[fn] = getattr(lib(), fn)
+    if torch._C._cuda_getDevice() == dev:
         rc = call(*args, handle)
     else:
         with torch.cuda.device(dev):
@@ -724,36 +729,65 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, *, scaling: Optional[s
     return f.to(device), mscale
 
 
-def _heads(name, t):
-    """Row and head strides, in elements, of t [B][Nmax][H][d]."""
-    B, N, H, d = t.shape
-    if d > 1 and t.stride(3) != 1:
+# (These calls' usual arguments pass their checks in a few microseconds of host
+# time: shapes and strides are read once, and what is wrong is told apart only
+# when something is.)
+
+def _rows_of(name, shape, stride):
+    """Row and head strides, in elements, of a [B][Nmax][H][d] tensor."""
+    B, N, H, d = shape
+    if stride[3] != 1 and d > 1:
         raise ValueError(f"{name}: a head's dims are not contiguous")
-    row = t.stride(1) if N > 1 else t.stride(0) if B > 1 else H * d
-    if B > 1 and t.stride(0) != N * row:
+    row = stride[1] if N > 1 else stride[0] if B > 1 else H * d
+    if B > 1 and stride[0] != N * row:
         raise ValueError(f"{name}: rows are not evenly spaced over the batch")
-    return row, t.stride(2) if H > 1 else d
+    return row, stride[2] if H > 1 else d
+
+
+_kinds = None
+
+
+def _kind(t):
+    """DTYPE_BF16, DTYPE_F32 or None."""
+    global _kinds
+    if _kinds is None:
+        import torch
+        _kinds = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32, torch.int32: "i32", torch.float64: "f64"}
+    return _kinds.get(t.dtype)
+
+
+def _ints(shape, names, tensors):
+    """Each tensor is int32, of the shape and contiguous, or None."""
+    for t in tensors:
+        if t is not None and not (_kind(t) == "i32" and t.shape == shape and t.is_contiguous()):
+            _int32(shape, **dict(zip(names, tensors)))
 
 
 def _frequencies(inv_freq):
-    import torch
-    _want("inv_freq", inv_freq, (torch.float64,), (_dims("inv_freq", inv_freq, 1)[0],))
+    if _kind(inv_freq) != "f64" or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        import torch
+        _want("inv_freq", inv_freq, (torch.float64,), (_dims("inv_freq", inv_freq, 1)[0],))
     return 2 * inv_freq.shape[0]
 
 
-def _span(t):
-    """First and past-the-last byte of a non-empty tensor's elements."""
-    size = t.element_size()
-    return t.data_ptr(), t.data_ptr() + size * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
-
-
-def _in_place_or_apart(name, t, out):
-    """out is t itself or overlaps it nowhere."""
-    if t.data_ptr() == out.data_ptr() and _heads(name, t) == _heads(name, out):
-        return
-    (a0, a1), (b0, b1) = _span(t), _span(out)
-    if a0 < b1 and b0 < a1:
-        raise ValueError(f"{name}_out overlaps {name}")
+def _rope_pair(name, t, out, kind, shape):
+    """Pointers and strides of a tensor and where it goes, which is the same places
+    or none of them."""
+    if _kind(t) != kind or _kind(out) != kind:
+        raise TypeError(f"{name} and {name}_out have types {t.dtype} and {out.dtype}, not q's")
+    if out.shape != shape:
+        raise ValueError(f"{name}_out has shape {tuple(out.shape)}, not {tuple(shape)}")
+    st, so = t.stride(), out.stride()
+    rt, ro = _rows_of(name, shape, st), _rows_of(name + "_out", shape, so)
+    p, po = t.data_ptr(), out.data_ptr()
+    if p != po or rt != ro:
+        size = 2 if kind == DTYPE_BF16 else 4
+        B, N, H, d = shape
+        end = p + size * ((B - 1) * st[0] + (N - 1) * st[1] + (H - 1) * st[2] + (d - 1) * st[3] + 1)
+        end_out = po + size * ((B - 1) * so[0] + (N - 1) * so[1] + (H - 1) * so[2] + (d - 1) * so[3] + 1)
+        if p < end_out and po < end:
+            raise ValueError(f"{name}_out overlaps {name}")
+    return (p, *rt, po, *ro)
 
 
 def tree_rope(q, q_out, inv_freq, prefix_len, n_rows, *, k=None, k_out=None, depth=None,
@@ -761,58 +795,50 @@ def tree_rope(q, q_out, inv_freq, prefix_len, n_rows, *, k=None, k_out=None, dep
               validate: bool = False, status=None, stream=None):
     """Rotary positions of queries ``[B][Nmax][Hq][d]`` and, if given, keys
     ``[B][Nmax][Hk][d]`` (bfloat16 or float32, views with evenly spaced rows
-    welcome; the outputs may be the inputs); see ``ltd_tree_rope``.  inv_freq
-    ``[rot_dim / 2]`` float64 from ``rope_frequencies``, depth ``[B][Nmax]`` int32 for
-    a draft tree's rows."""
-    dtype = _dtype_code(q)
-    B, Nmax, Hq, d = _dims("q", q, 4)
+    welcome; the outputs may be the inputs, and overlap nothing else); see
+    ``ltd_tree_rope``.  inv_freq ``[rot_dim / 2]`` float64 from
+    ``rope_frequencies``, depth ``[B][Nmax]`` int32 for a draft tree's rows."""
+    kind = _dtype_code(q)
+    shape = _dims("q", q, 4)
+    B, Nmax, Hq, d = shape
     rot_dim = _frequencies(inv_freq)
-    pairs = [("q", q, q_out)]
     if (k is None) != (k_out is None):
         raise ValueError("k and k_out come together")
-    Hk = 0
-    if k is not None:
-        Hk = _dims("k", k, 4)[2]
-        if tuple(k.shape) != (B, Nmax, Hk, d):
-            raise ValueError(f"k has shape {tuple(k.shape)}, q {tuple(q.shape)}")
-        pairs.append(("k", k, k_out))
-    args = []
-    for name, t, out in pairs:
-        if t.dtype != q.dtype or out.dtype != q.dtype:
-            raise TypeError(f"{name} and {name}_out have types {t.dtype} and {out.dtype}, not {q.dtype}")
-        if out.shape != t.shape:
-            raise ValueError(f"{name}_out has shape {tuple(out.shape)}, not {tuple(t.shape)}")
-        args += [t, *_heads(name, t), out, *_heads(name + "_out", out)]
     if rot_offset < 0 or rot_offset + rot_dim > d:
         raise ValueError(f"dims {rot_offset} to {rot_offset + rot_dim} of {d}")
-    _int32((B,), prefix_len=prefix_len, n_rows=n_rows)
-    _int32((B, Nmax), depth=depth)
+    args = _rope_pair("q", q, q_out, kind, shape)
+    Hk, k_args = 0, (None, 0, 0, None, 0, 0)
+    if k is not None:
+        k_shape = _dims("k", k, 4)
+        Hk = k_shape[2]
+        if k_shape[:2] != shape[:2] or k_shape[3] != d:
+            raise ValueError(f"k has shape {tuple(k_shape)}, q {tuple(shape)}")
+        k_args = _rope_pair("k", k, k_out, kind, k_shape)
+    _ints((B,), ("prefix_len", "n_rows"), (prefix_len, n_rows))
+    if depth is not None:
+        _ints((B, Nmax), ("depth",), (depth,))
     if B == 0 or Nmax == 0 or Hq == 0:
         return
-    for name, t, out in pairs:
-        if t.numel():
-            _in_place_or_apart(name, t, out)
-    if Hk == 0:
-        args = args[:6] + [None, 0, 0, None, 0, 0]
     _run("ltd_tree_rope",
-         (*(a if a is None or isinstance(a, int) else _p(a) for a in args), _p(inv_freq), _p(prefix_len),
-          _p(depth), _p(n_rows), B, Nmax, Hq, Hk, d, int(rot_offset), rot_dim, int(bool(interleaved)),
-          float(mscale), dtype, int(validate), _p(status)),
+         (*args, *k_args, inv_freq.data_ptr(), prefix_len.data_ptr(), _p(depth), n_rows.data_ptr(), B, Nmax,
+          Hq, Hk, d, int(rot_offset), rot_dim, bool(interleaved), float(mscale), kind, bool(validate), _p(status)),
          (q, q_out, k, k_out, inv_freq, prefix_len, depth, n_rows, status), stream)
 
 
 def _latent_cache(cache, block_table, num_blocks, lead):
     """The geometry of a latent cache of `lead` leading dimensions (layers):
     pages, rows of a page, row size, blocks a sequence."""
-    if cache.dim() != lead + 3:
-        raise ValueError(f"cache has {cache.dim()} dimensions, not {lead + 3}")
-    pages, kv_rows, d = cache.shape[lead:]
+    shape = cache.shape
+    if len(shape) != lead + 3:
+        raise ValueError(f"cache has {len(shape)} dimensions, not {lead + 3}")
+    pages, kv_rows, d = shape[lead:]
     if not cache.is_contiguous():
         raise ValueError("cache is not contiguous")
     max_blocks = 0
     if block_table is not None:
-        _int32(_dims("block_table", block_table, 2), block_table=block_table)
-        max_blocks = block_table.shape[1]
+        at = _dims("block_table", block_table, 2)
+        _ints(at, ("block_table",), (block_table,))
+        max_blocks = at[1]
         if num_blocks > pages:
             raise ValueError(f"num_blocks is {num_blocks}, the cache holds {pages}")
     return pages, kv_rows, d, max_blocks
@@ -827,8 +853,8 @@ def latent_append(kv_new, cache, inv_freq, prefix_len, n_rows, *, depth=None, no
     float32, a view with evenly spaced rows), cache ``[pages][rows][d_latent +
     d_rope]``, inv_freq ``[d_rope / 2]`` float64, norm_weight ``[d_latent]``."""
     pages, kv_rows, D, max_blocks = _latent_cache(cache, block_table, num_blocks, 0)
-    dtype = _dtype_code(kv_new)
-    if cache.dtype != kv_new.dtype:
+    kind = _dtype_code(kv_new)
+    if _kind(cache) != kind:
         raise TypeError(f"kv_new has type {kv_new.dtype}, cache {cache.dtype}")
     B, Nmax, d = _dims("kv_new", kv_new, 3)
     d_rope = _frequencies(inv_freq)
@@ -837,15 +863,17 @@ def latent_append(kv_new, cache, inv_freq, prefix_len, n_rows, *, depth=None, no
     if norm_weight is not None:
         _want("norm_weight", norm_weight, (kv_new.dtype,), (d - d_rope,))
     _batch_pages(B, pages, block_table)
-    _int32((B,), prefix_len=prefix_len, n_rows=n_rows)
-    _int32((B, Nmax), depth=depth)
+    _ints((B,), ("prefix_len", "n_rows"), (prefix_len, n_rows))
+    if depth is not None:
+        _ints((B, Nmax), ("depth",), (depth,))
     if B == 0 or Nmax == 0:
         return
-    row, _ = _heads("kv_new", kv_new.unsqueeze(2))
+    s0, s1, s2 = kv_new.stride()
+    row, _ = _rows_of("kv_new", (B, Nmax, 1, d), (s0, s1, d, s2))
     _run("ltd_latent_append",
-         (_p(kv_new), row, _p(norm_weight), float(norm_eps), _p(inv_freq), int(bool(interleaved)),
-          float(mscale), _p(cache), _p(block_table), _p(prefix_len), _p(depth), _p(n_rows), B, Nmax,
-          d - d_rope, d_rope, kv_rows, max_blocks, int(num_blocks), dtype, int(validate), _p(status)),
+         (kv_new.data_ptr(), row, _p(norm_weight), float(norm_eps), inv_freq.data_ptr(), bool(interleaved), float(mscale),
+          cache.data_ptr(), _p(block_table), prefix_len.data_ptr(), _p(depth), n_rows.data_ptr(), B, Nmax,
+          d - d_rope, d_rope, kv_rows, max_blocks, int(num_blocks), kind, bool(validate), _p(status)),
          (kv_new, cache, inv_freq, prefix_len, n_rows, depth, norm_weight, block_table, status), stream)
 
 
@@ -862,26 +890,29 @@ def tree_verify_attn_latent(q_latent, q_rope, cache, prefix_len, parents, n_node
     and head strides, out ``[B][Nmax][Hq][d_latent]``, the cache as for
     ``latent_append``."""
     pages, kv_rows, D, max_blocks = _latent_cache(cache, block_table, num_blocks, 0)
-    dtype = _dtype_code(q_latent)
-    B, Nmax, Hq, d_latent = _dims("q_latent", q_latent, 4)
-    d_rope = _dims("q_rope", q_rope, 4)[3]
-    if q_rope.dtype != q_latent.dtype or cache.dtype != q_latent.dtype:
+    kind = _dtype_code(q_latent)
+    ql_shape, qr_shape = _dims("q_latent", q_latent, 4), _dims("q_rope", q_rope, 4)
+    B, Nmax, Hq, d_latent = ql_shape
+    d_rope = qr_shape[3]
+    if _kind(q_rope) != kind or _kind(cache) != kind:
         raise TypeError(f"q_latent has type {q_latent.dtype}, q_rope {q_rope.dtype}, cache {cache.dtype}")
-    if tuple(q_rope.shape[:3]) != (B, Nmax, Hq) or d_latent + d_rope != D:
-        raise ValueError(f"q_latent {tuple(q_latent.shape)}, q_rope {tuple(q_rope.shape)}, cache rows of {D}")
-    _want("out", out, (q_latent.dtype,), (B, Nmax, Hq, d_latent))
+    if qr_shape[:3] != ql_shape[:3] or d_latent + d_rope != D:
+        raise ValueError(f"q_latent {tuple(ql_shape)}, q_rope {tuple(qr_shape)}, cache rows of {D}")
+    if _kind(out) != kind or out.shape != ql_shape or not out.is_contiguous():
+        _want("out", out, (q_latent.dtype,), ql_shape)
     _batch_pages(B, pages, block_table)
-    _int32((B,), prefix_len=prefix_len, n_nodes=n_nodes)
-    _int32((B, Nmax), parents=parents)
+    _ints((B,), ("prefix_len", "n_nodes"), (prefix_len, n_nodes))
+    _ints((B, Nmax), ("parents",), (parents,))
     if workspace is None:
         workspace = _workspace_for(
-            stream, attn_latent_workspace_size(B, Nmax, Hq, d_latent, d_rope, max_prefix, dtype),
+            stream, attn_latent_workspace_size(B, Nmax, Hq, d_latent, d_rope, max_prefix, kind),
             q_latent.device)
     _run("ltd_tree_verify_attn_latent",
-         (_p(q_latent), *_heads("q_latent", q_latent), _p(q_rope), *_heads("q_rope", q_rope), _p(cache),
-          _p(block_table), _p(prefix_len), _p(parents), _p(n_nodes), _p(out), B, Nmax, Hq, d_latent,
-          d_rope, int(max_prefix), kv_rows, max_blocks, int(num_blocks), float(scale), dtype,
-          *_space(workspace), int(validate), _p(status)),
+         (q_latent.data_ptr(), *_rows_of("q_latent", ql_shape, q_latent.stride()), q_rope.data_ptr(),
+          *_rows_of("q_rope", qr_shape, q_rope.stride()), cache.data_ptr(), _p(block_table),
+          prefix_len.data_ptr(), parents.data_ptr(), n_nodes.data_ptr(), out.data_ptr(), B, Nmax, Hq,
+          d_latent, d_rope, int(max_prefix), kv_rows, max_blocks, int(num_blocks), float(scale), kind, *_space(workspace),
+          bool(validate), _p(status)),
          (q_latent, q_rope, cache, block_table, prefix_len, parents, n_nodes, out, workspace, status),
          stream)
     return out
@@ -899,10 +930,11 @@ def latent_compact(cache, prefix_len, new_prefix_len, accepted_nodes, n_accepted
     layers = cache.shape[0] if lead else 1
     B, Nmax = _dims("accepted_nodes", accepted_nodes, 2)
     _batch_pages(B, pages, block_table)
-    _int32((B, Nmax), accepted_nodes=accepted_nodes)
-    _int32((B,), prefix_len=prefix_len, new_prefix_len=new_prefix_len, n_accepted=n_accepted)
+    _ints((B, Nmax), ("accepted_nodes",), (accepted_nodes,))
+    _ints((B,), ("prefix_len", "new_prefix_len", "n_accepted"), (prefix_len, new_prefix_len, n_accepted))
     _run("ltd_latent_compact",
-         (_p(cache), _p(block_table), _p(prefix_len), _p(new_prefix_len), _p(accepted_nodes),
-          _p(n_accepted), B, Nmax, D - d_rope, d_rope, kv_rows, max_blocks, int(num_blocks), layers,
-          cache.stride(0) if lead else 0, _dtype_code(cache), int(validate), _p(status)),
+         (cache.data_ptr(), _p(block_table), prefix_len.data_ptr(), new_prefix_len.data_ptr(),
+          accepted_nodes.data_ptr(), n_accepted.data_ptr(), B, Nmax, D - d_rope, d_rope, kv_rows,
+          max_blocks, int(num_blocks), layers, cache.stride(0) if lead else 0, _dtype_code(cache),
+          bool(validate), _p(status)),
          (cache, block_table, prefix_len, new_prefix_len, accepted_nodes, n_accepted, status), stream)

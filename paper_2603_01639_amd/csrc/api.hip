@@ -574,7 +574,7 @@ int ltd_tree_rope(const void* q, int64_t q_row_stride, int64_t q_head_stride, vo
       rot_offset < 0 || static_cast<int64_t>(rot_offset) + rot_dim > d || !std::isfinite(mscale))
     return LTD_EINVAL;
   if (!dtype_known(dtype) || d > LTD_ROPE_MAX_DIM || Nmax > LTD_MAX_LENGTH ||
-      (static_cast<int64_t>(Hq) + Hk) * d > (1 << 24))
+      (static_cast<int64_t>(Hq) + Hk) * d > (1 << 24) || static_cast<int64_t>(B) * Nmax >= INT32_MAX)
     return LTD_EUNSUPPORTED;
   if (validate && !status) return LTD_EINVAL;
   if (B == 0) return LTD_OK;
@@ -629,7 +629,8 @@ int ltd_latent_append(const void* kv_new, int64_t new_row_stride, const void* no
   if (B < 0 || Nmax < 1 || kv_rows < 1 || !(norm_eps >= 0.f) || !std::isfinite(norm_eps) ||
       !std::isfinite(mscale))
     return LTD_EINVAL;
-  if (!dtype_known(dtype) || !latent_supported(d_latent, d_rope) || Nmax > LTD_MAX_LENGTH)
+  if (!dtype_known(dtype) || !latent_supported(d_latent, d_rope) || Nmax > LTD_MAX_LENGTH ||
+      static_cast<int64_t>(B) * Nmax >= INT32_MAX)
     return LTD_EUNSUPPORTED;
   if (block_table && (max_blocks < 1 || num_blocks < 1)) return LTD_EINVAL;
   if (new_row_stride < d_latent + d_rope) return LTD_EINVAL;

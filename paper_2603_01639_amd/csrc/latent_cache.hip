@@ -5,10 +5,11 @@
 // A cache row holds one token's latent part (d_latent dims, the key and value
 // of every head) and its rotated part (d_rope dims, key alone).
 //
-// Append: a wave a row.  The latent part's mean square is a wave reduction over
-// registers, the rotated part's angles are computed by the lanes (a pair each)
-// and handed over by lane exchanges, so a row is read and written once and
-// nothing goes through LDS.  Bound: HBM, or the launch for a tree's rows.
+// Append: a wave takes four rows of a sequence, whose loads all go out first.  A row's
+// latent part lies across the wave, so that its mean square is a wave reduction
+// over registers; two angles a lane pass through LDS to the lanes that hold the
+// rotated parts.  A row is read and written once.  Bound: HBM, or the launch for a
+// tree's rows.
 #include "ltd_device.hpp"
 #include "ltd_launch.hpp"
 #include "rope.hpp"
@@ -32,80 +33,107 @@ struct Piece {  // 16 bytes
   __device__ __forceinline__ float get(int i) const { return static_cast<float>(v[i]); }
 };
 
+constexpr int kWaves = kThreads / kWave;
+constexpr int kRowsAtOnce = 4;
+constexpr int kGroupRows = kWaves * kRowsAtOnce;
+
 template <typename T, int DL>
 __global__ void __launch_bounds__(kThreads) latent_append_kernel(LatentAppendArgs a) {
   constexpr int N = Piece<T>::N;
   constexpr int D = DL + kRopeDims;
-  constexpr int kPieces = DL / N;                             // of the latent part
-  constexpr int kIter = (kPieces + kWave - 1) / kWave;        // a lane's
+  constexpr int kPieces = DL / N;                       // of the latent part
+  constexpr int kIter = (kPieces + kWave - 1) / kWave;  // a lane's
+  __shared__ float2 turn_s[kWaves][kRowsAtOnce][kPairs];
   if (halted(a.status)) return;
-  const int lane = threadIdx.x % kWave;
-  const int64_t waves = static_cast<int64_t>(gridDim.x) * (kThreads / kWave);
-  const int64_t all = static_cast<int64_t>(a.B) * a.Nmax;
-  for (int64_t at = static_cast<int64_t>(blockIdx.x) * (kThreads / kWave) + threadIdx.x / kWave; at < all; at += waves) {
-    const int b = static_cast<int>(at / a.Nmax), i = static_cast<int>(at % a.Nmax);
-    if (i >= a.n_rows[b]) continue;
-    const T* src = static_cast<const T*>(a.x) + at * a.x_row;
-    Piece<T> c[kIter], w[kIter], r0, r1;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  // The rotated parts: a lane has a piece of neighbouring pairs, or two pieces, the first
+  // and the second values of its pairs.
+  const int per_row = a.interleaved ? kRopeDims / N : kPairs / N;
+  const int turn_row = lane / per_row, turn_piece = lane % per_row;
+  const double freq = a.freq[lane % kPairs];
+  const int groups = (a.Nmax + kGroupRows - 1) / kGroupRows;  // of rows, a sequence
+  const uint32_t all = static_cast<uint32_t>(a.B) * groups;
+  for (uint32_t group = blockIdx.x; group < all; group += gridDim.x) {
+    const int b = static_cast<int>(group / groups);
+    const int i0 = static_cast<int>(group % groups) * kGroupRows + wave * kRowsAtOnce;
+    const int n = min(a.n_rows[b], a.Nmax), P = a.prefix_len[b];
+    const int rows = min(kRowsAtOnce, n - i0);  // (the same for the wave)
+    if (rows > 0) {
+      const T* src = static_cast<const T*>(a.x) + (static_cast<int64_t>(b) * a.Nmax + i0) * a.x_row;
+      Piece<T> c[kRowsAtOnce][kIter], r0, r1;
 #pragma unroll
-    for (int k = 0; k < kIter; ++k)
-      if (lane + k * kWave < kPieces) {
-        c[k].load(src + (lane + k * kWave) * N);
-        if (a.weight) w[k].load(static_cast<const T*>(a.weight) + (lane + k * kWave) * N);
+      for (int r = 0; r < kRowsAtOnce; ++r)
+#pragma unroll
+        for (int k = 0; k < kIter; ++k)
+          if (r < rows && lane + k * kWave < kPieces) c[r][k].load(src + r * a.x_row + (lane + k * kWave) * N);
+      const bool turns = turn_row < rows;
+      if (turns) {
+        r0.load(src + turn_row * a.x_row + DL + turn_piece * N);
+        if (!a.interleaved) r1.load(src + turn_row * a.x_row + DL + kPairs + turn_piece * N);
       }
-    // The rotated part: lanes below kRopeDims / N (neighbouring pairs) or half of
-    // that (halves: a lane has the first and the second values of its pairs).
-    const int turning = a.interleaved ? kRopeDims / N : kPairs / N;
-    if (lane < turning) {
-      r0.load(src + DL + lane * N);
-      if (!a.interleaved) r1.load(src + DL + kPairs + lane * N);
-    }
-    const int64_t P = a.prefix_len[b];
-    const int64_t pos = P + (a.depth ? a.depth[at] : i);
-    const float2 t = rope_turn(pos, a.freq[lane % kPairs], a.m);
-    const int row = static_cast<int>(P) + i;
-    T* dst = static_cast<T*>(a.cache) + cache_row(a.block_table, b, 0, row, 1, D, a.kv_rows, a.max_blocks);
-    if (a.weight) {
-      float ss = 0.f;
+      // the rows' places in the cache and their angles
+      T* dst[kRowsAtOnce];
 #pragma unroll
-      for (int k = 0; k < kIter; ++k)
-        if (lane + k * kWave < kPieces)
+      for (int r = 0; r < kRowsAtOnce; ++r)
+        dst[r] = static_cast<T*>(a.cache) +
+                 cache_row(a.block_table, b, 0, P + i0 + min(r, rows - 1), 1, D, a.kv_rows, a.max_blocks);
 #pragma unroll
-          for (int e = 0; e < N; ++e) ss = __builtin_fmaf(c[k].get(e), c[k].get(e), ss);
-      ss = wave_sum_dpp(ss);
-      const float rs = 1.f / __builtin_sqrtf(ss * (1.f / DL) + a.eps);
-#pragma unroll
-      for (int k = 0; k < kIter; ++k)
-        if (lane + k * kWave < kPieces)
-#pragma unroll
-          for (int e = 0; e < N; ++e) c[k].v[e] = static_cast<T>(c[k].get(e) * rs * w[k].get(e));
-    }
-#pragma unroll
-    for (int k = 0; k < kIter; ++k)
-      if (lane + k * kWave < kPieces) c[k].store(dst + (lane + k * kWave) * N);
-    // (every lane takes part in the exchanges)
-    if (a.interleaved) {
-#pragma unroll
-      for (int e = 0; e < N / 2; ++e) {
-        const int from = (lane * (N / 2) + e) % kPairs;
-        const float cs = __shfl(t.x, from, kWave), sn = __shfl(t.y, from, kWave);
-        const float p0 = r0.get(2 * e), p1 = r0.get(2 * e + 1);
-        r0.v[2 * e] = static_cast<T>(p0 * cs - p1 * sn);
-        r0.v[2 * e + 1] = static_cast<T>(p1 * cs + p0 * sn);
+      for (int r = 0; r < kRowsAtOnce; r += kWave / kPairs) {
+        const int row = r + lane / kPairs, i = i0 + min(row, rows - 1);
+        const int64_t pos = static_cast<int64_t>(P) + (a.depth ? a.depth[static_cast<int64_t>(b) * a.Nmax + i] : i);
+        turn_s[wave][row][lane % kPairs] = rope_turn(pos, freq, a.m);
       }
-    } else {
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const int from = (lane * N + e) % kPairs;
-        const float cs = __shfl(t.x, from, kWave), sn = __shfl(t.y, from, kWave);
-        const float p0 = r0.get(e), p1 = r1.get(e);
-        r0.v[e] = static_cast<T>(p0 * cs - p1 * sn);
-        r1.v[e] = static_cast<T>(p1 * cs + p0 * sn);
+      for (int r = 0; r < kRowsAtOnce; ++r) {
+        if (r >= rows) break;
+        if (a.weight) {
+          float ss = 0.f;
+#pragma unroll
+          for (int k = 0; k < kIter; ++k)
+            if (lane + k * kWave < kPieces)
+#pragma unroll
+              for (int e = 0; e < N; ++e) ss = __builtin_fmaf(c[r][k].get(e), c[r][k].get(e), ss);
+          ss = wave_sum_dpp(ss);
+          const float rs = 1.f / __builtin_sqrtf(ss * (1.f / DL) + a.eps);
+#pragma unroll
+          for (int k = 0; k < kIter; ++k)
+            if (lane + k * kWave < kPieces) {
+              Piece<T> w;
+              w.load(static_cast<const T*>(a.weight) + (lane + k * kWave) * N);
+#pragma unroll
+              for (int e = 0; e < N; ++e) c[r][k].v[e] = static_cast<T>(c[r][k].get(e) * rs * w.get(e));
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kIter; ++k)
+          if (lane + k * kWave < kPieces) c[r][k].store(dst[r] + (lane + k * kWave) * N);
       }
-    }
-    if (lane < turning) {
-      r0.store(dst + DL + lane * N);
-      if (!a.interleaved) r1.store(dst + DL + kPairs + lane * N);
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+      if (turns) {
+        T* to = dst[0];
+#pragma unroll
+        for (int r = 1; r < kRowsAtOnce; ++r)
+          if (turn_row == r) to = dst[r];
+        const float2* t = turn_s[wave][turn_row] + turn_piece * (a.interleaved ? N / 2 : N);
+        if (a.interleaved) {
+#pragma unroll
+          for (int e = 0; e < N / 2; ++e) {
+            const float p0 = r0.get(2 * e), p1 = r0.get(2 * e + 1);
+            r0.v[2 * e] = static_cast<T>(p0 * t[e].x - p1 * t[e].y);
+            r0.v[2 * e + 1] = static_cast<T>(p1 * t[e].x + p0 * t[e].y);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const float p0 = r0.get(e), p1 = r1.get(e);
+            r0.v[e] = static_cast<T>(p0 * t[e].x - p1 * t[e].y);
+            r1.v[e] = static_cast<T>(p1 * t[e].x + p0 * t[e].y);
+          }
+          r1.store(to + DL + kPairs + turn_piece * N);
+        }
+        r0.store(to + DL + turn_piece * N);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");  // (the angles are replaced)
     }
   }
 }
@@ -154,8 +182,7 @@ __global__ void __launch_bounds__(kThreads) latent_compact_kernel(LatentCompactA
 }  // namespace
 
 hipError_t launch_latent_append(const LatentAppendArgs& a, int d_latent, int dtype, hipStream_t stream) {
-  const int64_t all = static_cast<int64_t>(a.B) * a.Nmax;
-  const int64_t groups = (all + kThreads / kWave - 1) / (kThreads / kWave);
+  const int64_t groups = static_cast<int64_t>(a.B) * ((a.Nmax + kGroupRows - 1) / kGroupRows);
   const dim3 grid(static_cast<unsigned>(groups < (1 << 20) ? groups : (1 << 20)));
   if (dtype == LTD_DTYPE_F32) {
     if (d_latent == 512) hipLaunchKernelGGL((latent_append_kernel<float, 512>), grid, dim3(kThreads), 0, stream, a);

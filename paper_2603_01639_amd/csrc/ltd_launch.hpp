@@ -175,7 +175,9 @@ struct RopeArgs {
   int B, Nmax, d, off, rot;
   int interleaved;
   float m;
-  int rows, copies;  // set by the launcher: rows a workgroup, whether the other dims are copied
+  // set by the launcher: rows a workgroup, whether the other dims are copied, and how far
+  // a thread's next item lies
+  int rows, copies, step_p, step_head;
 };
 hipError_t launch_rope(RopeArgs a, int dtype, hipStream_t stream);
 hipError_t launch_validate_rows(const int32_t* prefix_len, const int32_t* depth,

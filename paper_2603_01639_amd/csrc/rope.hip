@@ -3,11 +3,11 @@
 // Pair j of a head's rotated dims (first, second) = (x0, x1) at position
 // p = P_b + depth turns by the angle p * f_j:
 //   y0 = m (x0 cos - x1 sin),  y1 = m (x1 cos + x0 sin).
-// A workgroup takes a few rows: it computes their angles' cosines and sines once
-// into LDS (every head of a row shares them) and then streams the heads through,
-// one 16-byte chunk of first and one of second values a step (a chunk of
-// neighbouring pairs in the interleaved layout), so every element is read and
-// written once.  Bound: HBM.
+// A workgroup takes a few rows: its first loads go out, their angles' cosines and sines
+// are computed once into LDS (every head of a row shares them), and the heads are
+// streamed through, one 16-byte chunk of first and one of second values a step (a
+// chunk of neighbouring pairs in the interleaved layout), so every element is read
+// and written once.  Bound: HBM; a tree's rows, the launch.
 #include "ltd_device.hpp"
 #include "ltd_launch.hpp"
 #include "rope.hpp"
@@ -18,6 +18,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTurns = 2048;  // angles in LDS
 constexpr int kAhead = 4;     // chunks a thread has in flight
+constexpr int kSteps = 4;     // times that, of a workgroup's rows
 
 template <typename T>
 __device__ __forceinline__ float widen(T x);
@@ -47,54 +48,66 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a) {
   const int turning = kInter ? a.rot / N : half / N;  // items of a head that turn ...
   constexpr int kCopy = kLoose ? 1 : N;
   const int per_head = turning + (a.copies ? (a.d - a.rot) / kCopy : 0);  // ... and that are copied
-  const int64_t total = static_cast<int64_t>(a.B) * groups;
-  for (int64_t group = blockIdx.x; group < total; group += gridDim.x) {
+  const uint32_t total = static_cast<uint32_t>(a.B) * groups;
+  for (uint32_t group = blockIdx.x; group < total; group += gridDim.x) {
     const int b = static_cast<int>(group / groups);
     const int i0 = static_cast<int>(group % groups) * a.rows;
     const int rows = min(a.rows, min(a.n_rows[b], a.Nmax) - i0);
     if (rows <= 0) continue;  // (the same for the whole workgroup)
     const int64_t row0 = static_cast<int64_t>(b) * a.Nmax + i0;
     const int64_t P = a.prefix_len[b];
+    // The thread's next item: row, head and piece, moved on without divisions.
+    int r = threadIdx.x / (heads * per_head), hh = threadIdx.x / per_head % heads, p = threadIdx.x % per_head;
+    Chunk<T, N> x0[kAhead], x1[kAhead];
+    T* to[kAhead];
+    int j0[kAhead];  // the chunk's first angle; -1: a copy; -2: none
+    auto load = [&] {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        j0[u] = -2;
+        if (r < rows) {
+          const int which = hh >= a.H[0];
+          const int h = which ? hh - a.H[0] : hh;
+          const T* x = static_cast<const T*>(a.x[which]) + (row0 + r) * a.x_row[which] + h * a.x_head[which];
+          int at;  // first element
+          if (p < turning) {
+            at = a.off + p * N;
+            j0[u] = r * half + (kInter ? p * (N / 2) : p * N);
+          } else {
+            at = (p - turning) * kCopy;
+            if (at >= a.off) at += a.rot;
+            j0[u] = -1;
+          }
+          to[u] = static_cast<T*>(a.y[which]) + (row0 + r) * a.y_row[which] + h * a.y_head[which] + at;
+          if constexpr (kLoose) {
+            x0[u].v[0] = x[at];
+            if (kInter && j0[u] >= 0) x0[u].v[N - 1] = x[at + 1];
+            if (!kInter && j0[u] >= 0) x1[u].v[0] = x[at + half];
+          } else {
+            x0[u].load(x + at);
+            if (!kInter && j0[u] >= 0) x1[u].load(x + at + half);
+          }
+          p += a.step_p;
+          hh += a.step_head;
+          if (p >= per_head) {
+            p -= per_head;
+            ++hh;
+          }
+          while (hh >= heads) {
+            hh -= heads;
+            ++r;
+          }
+        }
+      }
+    };
+    load();
     for (int e = threadIdx.x; e < rows * half; e += kThreads) {
-      const int r = e / half, j = e % half;
-      const int64_t pos = P + (a.depth ? a.depth[row0 + r] : i0 + r);
+      const int row = e / half, j = e % half;
+      const int64_t pos = P + (a.depth ? a.depth[row0 + row] : i0 + row);
       turn_s[e] = rope_turn(pos, a.freq[j], a.m);
     }
     __syncthreads();
-    const int items = rows * heads * per_head;
-    for (int it0 = threadIdx.x; it0 < items; it0 += kThreads * kAhead) {
-      Chunk<T, N> x0[kAhead], x1[kAhead];
-      T* to[kAhead];
-      int j0[kAhead];  // the chunk's first angle, or -1: a copy
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int it = it0 + u * kThreads;
-        j0[u] = -2;
-        if (it >= items) continue;
-        const int head = it / per_head, p = it % per_head;
-        const int r = head / heads, hh = head % heads;
-        const int which = hh >= a.H[0];
-        const int h = which ? hh - a.H[0] : hh;
-        const T* x = static_cast<const T*>(a.x[which]) + (row0 + r) * a.x_row[which] + h * a.x_head[which];
-        int at;  // first element
-        if (p < turning) {
-          at = a.off + p * N;
-          j0[u] = r * half + (kInter ? p * (N / 2) : p * N);
-        } else {
-          at = (p - turning) * kCopy;
-          if (at >= a.off) at += a.rot;
-          j0[u] = -1;
-        }
-        to[u] = static_cast<T*>(a.y[which]) + (row0 + r) * a.y_row[which] + h * a.y_head[which] + at;
-        if constexpr (kLoose) {
-          x0[u].v[0] = x[at];
-          if (kInter && j0[u] >= 0) x0[u].v[N - 1] = x[at + 1];
-          if (!kInter && j0[u] >= 0) x1[u].v[0] = x[at + half];
-        } else {
-          x0[u].load(x + at);
-          if (!kInter && j0[u] >= 0) x1[u].load(x + at + half);
-        }
-      }
+    while (j0[0] != -2) {
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
         if (j0[u] == -2) continue;
@@ -126,6 +139,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a) {
           if (!kInter && j0[u] >= 0) x1[u].store(to[u] + half);
         }
       }
+      load();
     }
     __syncthreads();  // the angles are replaced
   }
@@ -159,7 +173,20 @@ __global__ void __launch_bounds__(kThreads) validate_rows_kernel(const int32_t* 
 }
 
 template <typename T, int N, bool kLoose>
-void launch_typed(const RopeArgs& a, int grid, hipStream_t stream) {
+void launch_typed(RopeArgs a, hipStream_t stream) {
+  const int turning = a.interleaved ? a.rot / (kLoose ? 2 : N) : a.rot / 2 / N;
+  const int per_head = turning + (a.copies ? (a.d - a.rot) / (kLoose ? 1 : N) : 0);
+  a.step_p = kThreads % per_head;
+  a.step_head = kThreads / per_head;
+  // Rows a workgroup: a few steps of every thread where there are rows for many
+  // workgroups, one row otherwise.
+  const int64_t all = static_cast<int64_t>(a.B) * a.Nmax;
+  const int64_t row_items = static_cast<int64_t>(a.H[0] + a.H[1]) * per_head;
+  int64_t rows = all < 8192 ? 1 : (kSteps * kAhead * kThreads + row_items - 1) / row_items;
+  const int64_t most = kTurns / (a.rot / 2);
+  a.rows = static_cast<int>(rows < most ? rows : most);
+  const int64_t groups = static_cast<int64_t>(a.B) * ((a.Nmax + a.rows - 1) / a.rows);
+  const int grid = static_cast<int>(groups < (1 << 20) ? groups : (1 << 20));
   if (a.interleaved)
     hipLaunchKernelGGL((rope_kernel<T, kLoose ? 2 : N, true, kLoose>), dim3(grid), dim3(kThreads), 0, stream, a);
   else
@@ -188,22 +215,12 @@ hipError_t launch_rope(RopeArgs a, int dtype, hipStream_t stream) {
            a.x_row[w] % N == 0 && a.x_head[w] % N == 0 && a.y_row[w] % N == 0 && a.y_head[w] % N == 0;
     if (a.x[w] != a.y[w]) a.copies = 1;  // (in place the other dims stay where they are)
   }
-  const int per_head = a.d / (2 * (wide ? N : 1)) + 1;
-  const int64_t row_items = static_cast<int64_t>(a.H[0] + a.H[1]) * per_head;
-  // Rows a workgroup: enough work for a few steps of every thread where there
-  // are rows for many workgroups, one row otherwise.
-  const int64_t all = static_cast<int64_t>(a.B) * a.Nmax;
-  int64_t rows = all < 4096 ? 1 : (kAhead * kThreads + row_items - 1) / row_items;
-  rows = rows < 1 ? 1 : rows > kTurns / (a.rot / 2) ? kTurns / (a.rot / 2) : rows;
-  a.rows = static_cast<int>(rows);
-  const int64_t groups = static_cast<int64_t>(a.B) * ((a.Nmax + a.rows - 1) / a.rows);
-  const int grid = static_cast<int>(groups < (1 << 20) ? groups : (1 << 20));
   if (dtype == LTD_DTYPE_F32) {
-    if (wide) launch_typed<float, 4, false>(a, grid, stream);
-    else launch_typed<float, 1, true>(a, grid, stream);
+    if (wide) launch_typed<float, 4, false>(a, stream);
+    else launch_typed<float, 1, true>(a, stream);
   } else {
-    if (wide) launch_typed<__bf16, 8, false>(a, grid, stream);
-    else launch_typed<__bf16, 1, true>(a, grid, stream);
+    if (wide) launch_typed<__bf16, 8, false>(a, stream);
+    else launch_typed<__bf16, 1, true>(a, stream);
   }
   return hipGetLastError();
 }
