@@ -14,127 +14,17 @@
 // then passes through LDS once, and a tile's rows are read 1.9 times a wave
 // row less than if a wave kept its 32 rows over all dims, which would need every
 // byte that LDS can give during the products' time.
-#include "ltd_device.hpp"
-#include "ltd_launch.hpp"
-#include "latent_plan.hpp"
-#include "mfma_tiles.hpp"
+#include "latent_attn.hpp"
 #include "tree_walk.hpp"
 
 namespace ltd {
 namespace {
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * kWave;
-constexpr int kRows = latent::kUnitRows;
 constexpr int kKeys = latent::kKeyTile;
-constexpr int kRopeDims = 64;
-constexpr int kStages = 3;                     // tiles in the LDS ring
-constexpr int kAncWords = LTD_MAX_NODES / 32;  // 256 bits a node
-constexpr int kPlane = kKeys * 128;             // bytes of a tile's plane in LDS
-// A row's reference maximum moves when a score passes it by 2^16: weights up to that
-// and their sums have as many bits in float32 and bfloat16 as small ones, and
-// moving it costs 256 accumulators a lane.  (At 2^8 two tiles in ten moved some
-// row's, 1400 cycles a tile; 8 sequences of 128 heads 774 us.)
-constexpr float kLazyMax = 16.f;
-constexpr int kAhead = 6;                      // key fragments in flight
-constexpr float kNoMax = -__FLT_MAX__;
-
-// A piece's row beside its O / l: the maximum (log2 units) and the sum.
-struct PieceRow {
-  float m, l;
-};
-// A unit that was cut: its rows, and the workgroups that have the other pieces.
-struct CutUnit {
-  int b, r0, valid, last;
-};
-
-struct LatentArgs {
-  LatentAttn in;
-  uint16_t* ws_o;    // [2 W][128][DL] bf16: pieces' O / l
-  PieceRow* ws_row;  // [2 W][128]
-  CutUnit* ws_cut;   // [W]: the cut unit that begins in a workgroup's share (valid 0: none)
-  int W;         // workgroups
-  float scale_log2, lazy_gap;
-  uint32_t row_magic;  // block_of's multiplier and shift
-  int row_shift;
-};
-
-// Where a place of the laid-out units falls.
-struct Place {
-  int b;
-  int64_t before;  // length before sequence b
-};
-
-// Nodes and prefix of sequence b (none past the batch; what is out of range is clamped).
-struct Seq {
-  int n, P;
-};
-__device__ __forceinline__ Seq seq_of(const LatentAttn& a, int b) {
-  if (b >= a.B) return Seq{0, 0};
-  return Seq{min(max(a.n_nodes[b], 0), a.Nmax), max(a.prefix_len[b], 0)};
-}
-__device__ __forceinline__ int64_t seq_length(const LatentAttn& a, const Seq& s) {
-  return s.n > 0 ? latent::length_of(s.P, s.n, a.Hq) : 0;
-}
-
-// x moved between lanes by DPP (0 where there is none to take).
-template <int kCtrl, int kRowMask>
-__device__ __forceinline__ int64_t dpp64(int64_t x) {
-  const uint64_t u = static_cast<uint64_t>(x);
-  const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), kCtrl, kRowMask, 0xF, kRowMask == 0xF);
-  const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), kCtrl, kRowMask, 0xF, kRowMask == 0xF);
-  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
-}
-__device__ __forceinline__ int64_t wave_scan(int64_t v) {  // inclusive
-  v += dpp64<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8
-  v += dpp64<0x112, 0xF>(v);
-  v += dpp64<0x114, 0xF>(v);
-  v += dpp64<0x118, 0xF>(v);
-  v += dpp64<0x142, 0xA>(v);  // row_bcast 15 into rows 1 and 3
-  v += dpp64<0x143, 0xC>(v);  // row_bcast 31 into rows 2 and 3
-  return v;
-}
-__device__ __forceinline__ int64_t read_lane(int64_t v, int l) {
-  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(v), l);
-  const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(static_cast<uint64_t>(v) >> 32), l);
-  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
-}
-
-// A value that is the same in all lanes, in scalar registers.
-__device__ __forceinline__ int64_t uniform(int64_t v) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v));
-  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(static_cast<uint64_t>(v) >> 32));
-  return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
-}
-
-// The length of all sequences' units, and the sequence that place pos(length) falls
-// into (B past the end); every wave works it out by itself.  seq: sequence `lane`.
-template <class Pos>
-__device__ __forceinline__ Place find_place(const LatentAttn& a, int lane, const Seq& seq, int64_t* total_out, Pos pos) {
-  const int64_t mine = seq_length(a, seq), upto = wave_scan(mine);
-  const int64_t first = read_lane(upto, kWave - 1);
-  int64_t total = first;
-  for (int b0 = kWave; b0 < a.B; b0 += kWave) total += read_lane(wave_scan(seq_length(a, seq_of(a, b0 + lane))), kWave - 1);
-  *total_out = total;
-  const int64_t at = pos(total);
-  if (at < first) {
-    const int l = __ffsll(static_cast<long long>(__ballot(at < upto))) - 1;
-    return Place{l, read_lane(upto - mine, l)};
-  }
-  int64_t before = first;
-  for (int b0 = kWave; b0 < a.B; b0 += kWave) {
-    const int64_t here = seq_length(a, seq_of(a, b0 + lane)), past = wave_scan(here) + before;
-    const uint64_t hit = __ballot(at < past);
-    if (hit != 0) {
-      const int l = __ffsll(static_cast<long long>(hit)) - 1;
-      return Place{b0 + l, read_lane(past - here, l)};
-    }
-    before = read_lane(past, kWave - 1);
-  }
-  return Place{a.B, total};
-}
+constexpr int kStages = 3;           // tiles in the LDS ring
+constexpr int kAhead = 6;            // key fragments in flight
+constexpr int kPlane = kKeys * 128;  // bytes of a tile's plane in LDS
+constexpr latent::Cut kCut = latent::kMany;
 
 template <int DL>
 struct Smem {
@@ -195,13 +85,6 @@ __device__ __forceinline__ void mfma_settle(f32x16& s) { asm volatile("s_nop 15\
 __device__ __forceinline__ void mfma_settled(f32x16& s) { asm volatile("s_nop 3" : "+v"(s)); }
 __device__ __forceinline__ void settled(f32x16& o) { asm volatile("" : "+a"(o)); }
 
-// A direct load of 16 bytes a lane (lane i's land at lds + 16 i) from kOff bytes past
-// p.  (The instruction's offset moves its place in LDS as well, so that is taken back.)
-template <int kOff>
-__device__ __forceinline__ void dma16_at(uint32_t lds, const void* p) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off offset:%2" ::"s"(lds - kOff), "v"(p), "n"(kOff) : "memory");
-}
-
 // o *= f in the accumulation registers.
 __device__ __forceinline__ void rescale(f32x16& o, float f) {
 #pragma unroll
@@ -239,8 +122,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
   const int rank = a.W % 8 == 0 ? static_cast<int>(blockIdx.x % 8) * (a.W / 8) + static_cast<int>(blockIdx.x / 8)
                                 : static_cast<int>(blockIdx.x);
   const Seq first_seqs = seq_of(in, lane);
-  const Place place = find_place(in, lane, first_seqs, &total, [&](int64_t t) {
-    share = latent::share_of(t, a.W);
+  const Place place = find_place(in, kCut, lane, first_seqs, &total, [&](int64_t t) {
+    share = latent::share_of(t, a.W, kCut);
     return rank * share;
   });
   share = uniform(share);
@@ -263,17 +146,12 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
   int v_rd = wave * (kCols / 64) * kPlane + v_key * 128 +
              (((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ swz(v_key)) << 4) + (lane & 1) * 8;
   const uint32_t kv_lds = lds_addr(sm.kv[0]);
-  // a row's block, by a multiplication (row_magic)
-  auto block_of = [&](int row) {
-    return static_cast<int>(__umulhi(2u * static_cast<uint32_t>(row), a.row_magic) >> a.row_shift);
-  };
-
   while (pos < end) {
     // ---- the unit's piece in this share
     const Seq seq = b < kWave ? first_seqs : seq_of(in, b);
     const int n = __builtin_amdgcn_readlane(seq.n, b % kWave), P = __builtin_amdgcn_readlane(seq.P, b % kWave);
-    const int64_t length = latent::kUnitCost + latent::tiles_of(P, n);
-    const int64_t all = latent::units_of(n, in.Hq) * length;
+    const int64_t length = kCut.cost + latent::tiles_of(P, n);
+    const int64_t all = latent::units_of(n, in.Hq, kCut) * length;
     if (pos >= before + all) {
       before += all;
       ++b;
@@ -282,8 +160,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     const int unit = __builtin_amdgcn_readfirstlane(static_cast<int>(latent::quotient(pos - before, length)));
     const int64_t start = before + unit * length;
     const int64_t stop = uniform(min(start + length, end));
-    const int t0 = __builtin_amdgcn_readfirstlane(static_cast<int>(latent::tile_at(pos - start)));
-    const int t1 = __builtin_amdgcn_readfirstlane(static_cast<int>(latent::tile_at(stop - start)));
+    const int t0 = __builtin_amdgcn_readfirstlane(static_cast<int>(latent::tile_at(pos - start, kCut)));
+    const int t1 = __builtin_amdgcn_readfirstlane(static_cast<int>(latent::tile_at(stop - start, kCut)));
     if (t1 == t0) {  // (a share that ends within a unit's own cost)
       pos = stop;
       continue;
@@ -302,17 +180,13 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     int32_t block = 0;
     auto look_up = [&](int t, int32_t& block) {
       if constexpr (kPaged)
-        block = in.block_table[static_cast<int64_t>(b) * in.max_blocks + block_of(min(t * kKeys + load_key, last))];
-    };
-    auto place_of = [&](int row, int32_t block) -> uint32_t {
-      // (rows of a cache are counted in 32 bits: 2^31 of them pass any memory)
-      return kPaged ? block * in.kv_rows + (row - block_of(row) * in.kv_rows) : b * in.kv_rows + row;
+        block = in.block_table[static_cast<int64_t>(b) * in.max_blocks + block_of(a, min(t * kKeys + load_key, last))];
     };
     auto source = [&](uint32_t place) {
       return static_cast<const unsigned char*>(in.cache) +
              (static_cast<uint64_t>(place) * kRowBytes + ((lane & 7) ^ swz(load_key)) * 16);
     };
-    auto at = [&](int t, int32_t block) { return source(place_of(min(t * kKeys + load_key, last), block)); };
+    auto at = [&](int t, int32_t block) { return source(row_place<kPaged>(a, b, min(t * kKeys + load_key, last), block)); };
     auto issue_plane = [&](int t, const unsigned char* from, auto plane) {
       dma16_at<plane() * 128>(kv_lds + (t % kStages) * kTileBytes + wave * 1024 + plane() * kPlane, from);
     };
@@ -606,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
       const unsigned char* from;
       last_products([&](auto i) {
         if constexpr (i() == 0) row = min((t + 2) * kKeys + load_key, last);
-        if constexpr (i() == 1) place = place_of(row, block);
+        if constexpr (i() == 1) place = row_place<kPaged>(a, b, row, block);
         if constexpr (i() == 2) from = source(place);
         if constexpr (i() == 3) look_up(t + 3, block);
       });
@@ -874,13 +748,20 @@ int grid_of(const LatentAttn& s, int cus) {
 
 template <int DL>
 hipError_t launch_bf16(const LatentArgs& a, hipStream_t stream) {
-  if (a.in.block_table)
-    hipLaunchKernelGGL((latent_attn_kernel<DL, true>), dim3(a.W), dim3(kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL((latent_attn_kernel<DL, false>), dim3(a.W), dim3(kThreads), 0, stream, a);
-  const hipError_t rc = hipGetLastError();
+  hipError_t rc;
+  const bool few = a.in.Nmax * static_cast<int64_t>(a.in.Hq) <= latent::kFewRows;
+  if (few) {
+    rc = launch_latent_few(&a, DL, stream);
+  } else {
+    if (a.in.block_table)
+      hipLaunchKernelGGL((latent_attn_kernel<DL, true>), dim3(a.W), dim3(kThreads), 0, stream, a);
+    else
+      hipLaunchKernelGGL((latent_attn_kernel<DL, false>), dim3(a.W), dim3(kThreads), 0, stream, a);
+    rc = hipGetLastError();
+  }
   if (rc != hipSuccess || a.W < 2) return rc;
-  hipLaunchKernelGGL((latent_merge_kernel<DL>), dim3(a.W - 1, kRows / kWaves), dim3(kThreads), 0, stream, a);
+  const int rows = few ? latent::kFew.rows : kRows;
+  hipLaunchKernelGGL((latent_merge_kernel<DL>), dim3(a.W - 1, rows / kWaves), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 
