@@ -55,14 +55,6 @@ __device__ __forceinline__ int swz(int key) {
   return ((key >> 1) & 1) << 2 | ((key >> 3) & 1) << 1 | ((key >> 4) & 1);
 }
 
-// x, made anew: constants of rare branches and what they derive from the thread's
-// index would be hoisted out of the tile loop into registers that the loop does
-// not have.
-template <typename T>
-__device__ __forceinline__ T rare(T x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
 __device__ __forceinline__ int rare_thread() { return rare(static_cast<int>(threadIdx.x)); }
 
 // The products by hand: O's accumulators take all 256 accumulation registers, and S's

@@ -45,6 +45,15 @@ struct LatentArgs {
   int row_shift;
 };
 
+// x, made anew: constants of rare branches, and what they and a piece's end derive from
+// the thread's index, would be hoisted out of the loops into registers that these do
+// not have.
+template <typename T>
+__device__ __forceinline__ T rare(T x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Where a place of the laid-out units falls.
 struct Place {
   int b;

@@ -30,6 +30,21 @@ __device__ __forceinline__ int swz(int key) {
   return ((key >> 1) & 1) << 1 | ((key >> 2) & 1) << 2 | ((key >> 3) & 1);
 }
 
+// The products by hand, sums in vector registers (the compiler would keep them in the
+// accumulation registers and move all of O out and in for every tile).  What else reads a
+// sum waits: 16 wait states are more than either product takes.
+__device__ __forceinline__ void mfma_s(f32x4& s, bf16x8 a, bf16x8 b) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void mfma_o(f32x4& o, bf16x4 a, bf16x4 b) {
+  asm volatile("v_mfma_f32_16x16x16_bf16 %0, %1, %2, %0" : "+v"(o) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void mfma_first(f32x4& s, bf16x8 a, bf16x8 b) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void mfma_settle(f32x4& s) { asm volatile("s_nop 15" : "+v"(s)); }
+__device__ __forceinline__ void settled(f32x4& o) { asm volatile("" : "+v"(o)); }
+
 template <int DL>
 struct Smem {
   static constexpr int kTileBytes = (DL + kRopeDims) / 64 * kPlane;
@@ -95,7 +110,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
       ++b;
       continue;
     }
-    const int unit = __builtin_amdgcn_readfirstlane(static_cast<int>(latent::quotient(pos - before, length)));
+    int unit = 0;  // (of at most two)
+    while (pos >= before + (unit + 1) * length) ++unit;
     const int64_t start = before + unit * length;
     const int64_t stop = uniform(min(start + length, end));
     const int t0 = __builtin_amdgcn_readfirstlane(static_cast<int>(latent::tile_at(pos - start, kCut))) * kTilesPer;
@@ -197,12 +213,14 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
         any |= lane_xor<32>(any, lane);
         bad = __builtin_amdgcn_readfirstlane(any);
       }
-      f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+      f32x4 s;
 #pragma unroll
       for (int kk = 0; kk < kSteps; ++kk) {
         const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kv + (k_rd ^ ((kk & 1) << 6)) + (kk >> 1) * kPlane);
-        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[kk], s, 0, 0, 0);
+        if (kk == 0) mfma_first(s, kf, qf[0]);
+        else mfma_s(s, kf, qf[kk]);
       }
+      mfma_settle(s);
       if (masked) {
         // bit j: tree key t * 16 - P + 4 quad + j (earlier ones are the prefix, later ones none)
         const int base = t * kKeys - P + 4 * quad;
@@ -242,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
 #pragma unroll
       for (int d = 0; d < kBlocks; ++d) {
         const bf16x4 vf = __builtin_bit_cast(bf16x4, lds_read_tr(kv + (v_rd ^ ((d & 3) << 5)) + (d >> 2) * kPlane));
-        o[d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, pf, o[d], 0, 0, 0);
+        mfma_o(o[d], vf, pf);
       }
       if (t + 2 * kWaves < t1) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the buffer's last reads are done
@@ -251,34 +269,38 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
     }
 
     // ---- the waves' results joined
+    asm volatile("s_nop 15");
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d) settled(o[d]);
+    const int jl = rare(lane), row16 = jl & 15, part = jl >> 4;
     l_run = rows_reduce(l_run, [](float x, float y) { return x + y; });
-    if (quad == 0) {
-      sm.m[wave][l16] = m_run * c;
-      sm.l[wave][l16] = l_run;
+    if (part == 0) {
+      sm.m[wave][row16] = m_run * c;
+      sm.l[wave][row16] = l_run;
     }
     __syncthreads();  // (all waves are done with their tiles, too)
     float M = kNoMax * __FLT_MAX__, L = 0.f;  // (-inf)
 #pragma unroll
     for (int w = 0; w < kWaves; ++w)
-      if (sm.l[w][l16] != 0.f) M = fmaxf(M, sm.m[w][l16]);
+      if (sm.l[w][row16] != 0.f) M = fmaxf(M, sm.m[w][row16]);
 #pragma unroll
     for (int w = 0; w < kWaves; ++w)
-      if (sm.l[w][l16] != 0.f) L += exp2_fast(sm.m[w][l16] - M) * sm.l[w][l16];
+      if (sm.l[w][row16] != 0.f) L += exp2_fast(sm.m[w][row16] - M) * sm.l[w][row16];
     // (a wave without a visible key has weight 0 and adds nothing, as does such a piece)
     const bool none = l_run == 0.f && (L != 0.f || !whole);
     const float f = none ? 0.f : exp2_fast(m_run * c - M) / L;
-    if (!whole && wave == 0 && quad == 0 && l16 < valid)
-      a.ws_row[static_cast<int64_t>(slot) * kRows + l16] = PieceRow{M, L};
+    if (!whole && wave == 0 && part == 0 && row16 < valid)
+      a.ws_row[static_cast<int64_t>(slot) * kRows + row16] = PieceRow{M, L};
     if (!whole && t0 == 0 && threadIdx.x == 0)
       a.ws_cut[rank] = CutUnit{b, r0, valid, static_cast<int>(latent::quotient(start + length - 1, share))};
 #pragma unroll
     for (int d = 0; d < kBlocks; ++d)
-      sm.o[wave][l16][(4 * d + quad) ^ (l16 & 7)] = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[d] * f;
+      sm.o[wave][row16][(4 * d + part) ^ (row16 & 7)] = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[d] * f;
     __syncthreads();
     uint16_t* out = whole ? static_cast<uint16_t*>(in.out) + (static_cast<int64_t>(b) * in.Nmax * in.Hq + r0) * DL
                           : a.ws_o + static_cast<int64_t>(slot) * kRows * DL;
 #pragma unroll 2
-    for (int e = threadIdx.x; e < 16 * DL / 8; e += kThreads) {
+    for (int e = rare(static_cast<int>(threadIdx.x)); e < 16 * DL / 8; e += kThreads) {
       const int row = e / (DL / 8), col = e % (DL / 8);
       f32x4 x0 = f32x4{0.f, 0.f, 0.f, 0.f}, x1 = x0;
 #pragma unroll
