@@ -150,7 +150,7 @@ __device__ __forceinline__ uint32_t row_place(const LatentArgs& a, int b, int ro
 
 }  // namespace
 
-// latent_few.hip: the kernel for up to 32 stacked rows a sequence (args: a LatentArgs).
+// latent_few.hip: the kernel for up to 16 stacked rows a sequence (args: a LatentArgs).
 hipError_t launch_latent_few(const void* args, int d_latent, hipStream_t stream);
 
 }  // namespace ltd

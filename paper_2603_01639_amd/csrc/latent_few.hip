@@ -1,18 +1,22 @@
-// Tree attention over a latent cache for calls of up to 32 stacked query rows a sequence
+// Tree attention over a latent cache for calls of up to 16 stacked query rows a sequence
 // (one token, or a few nodes, of a few heads), in bf16 on the matrix cores.
 //
-// The cache's bytes bound these calls, so the split follows the stream: a unit is 16 of
-// a sequence's rows, and the four waves of a workgroup take every fourth tile of 16
-// keys of its share, each with a double buffer of its own in LDS, rows in registers,
-// and no barrier until the share ends.
+// The cache's bytes bound these calls, so the split follows the stream: the four waves
+// of a workgroup take every fourth tile of 16 keys of its share, each with a double
+// buffer of its own in LDS that direct loads fill, rows in registers, and no barrier
+// until the share ends.
 //   S^T[key][row] = X Q^T         (v_mfma_f32_16x16x32_bf16, 18 a tile)
 //   O^T[dim][row] += C^T P^T      (v_mfma_f32_16x16x16_bf16, 32 a tile)
 // A lane's four accumulators of S^T are four keys of its row and as they are, rounded,
 // its operand P^T; C^T comes from the same tile by transposed reads.  The waves' results
 // are joined through LDS at the end.
 //
-// 16 sequences of 16 heads, one token each, over 1024 to 8192 keys: the kernel for many
-// rows (128 of them padded) 35 us a call.
+// 16 heads, this kernel and the one for many rows (which pads them to 128), both with
+// the merge: one token of a sequence over 1000 keys 20 us, 25; of 16 sequences 23, 28;
+// of 16 over 8192 keys 46, 45; of 128 over 2048 keys 70, 93.  With 32 rows, in two units
+// that each read the cache, 16 sequences over 8192 keys took 58 us, 48 there, hence the
+// rule.  16 sequences over 1024 to 8192 keys (85 MB) take 28 us before the merge, half
+// of it the stream at 6 TB/s, the rest the search, the first loads and the join.
 #include "latent_attn.hpp"
 
 namespace ltd {
@@ -53,6 +57,7 @@ struct Smem {
     f32x4 o[kWaves][16][DL / 4];  // the waves' results of 16 rows
   };
   float m[kWaves][16], l[kWaves][16];
+  int32_t ids[kWaves][2][kWave];  // block ids of the tile that follows a buffer's, key i % 16 at i
 };
 
 template <int DL, bool kPaged>
@@ -96,7 +101,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
   // C^T operand: keys 4 quad + .., 16 dims from 16 block on
   const int v_key = 4 * quad + (l16 >> 2);
   const int v_rd = v_key * 128 + ((((l16 & 3) >> 1) ^ swz(v_key)) << 4) + (l16 & 1) * 8;
-  const uint32_t ring = lds_addr(sm.kv[wave][0]);
+  const uint32_t ring = lds_addr(sm.kv[wave][0]), ids = lds_addr(sm.ids[wave][0]);
   const float c = a.scale_log2;
 
   while (pos < end) {
@@ -104,56 +109,49 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
     const Seq seq = b < kWave ? first_seqs : seq_of(in, b);
     const int n = __builtin_amdgcn_readlane(seq.n, b % kWave), P = __builtin_amdgcn_readlane(seq.P, b % kWave);
     const int64_t length = kCut.cost + latent::tiles_of(P, n);
-    const int64_t all = latent::units_of(n, in.Hq, kCut) * length;
-    if (pos >= before + all) {
-      before += all;
+    if (n == 0 || pos >= before + length) {
+      if (n != 0) before += length;
       ++b;
       continue;
     }
-    int unit = 0;  // (of at most two)
-    while (pos >= before + (unit + 1) * length) ++unit;
-    const int64_t start = before + unit * length;
+    const int64_t start = before;  // (its one unit)
     const int64_t stop = uniform(min(start + length, end));
     const int t0 = __builtin_amdgcn_readfirstlane(static_cast<int>(latent::tile_at(pos - start, kCut))) * kTilesPer;
     const int t1 = __builtin_amdgcn_readfirstlane(static_cast<int>(latent::tile_at(stop - start, kCut))) * kTilesPer;
     const bool whole = t0 == 0 && stop == start + length;
     const int slot = 2 * rank + (t0 == 0);  // (one piece that goes on, one that begins)
-    const int r0 = unit * kCut.rows;
-    const int valid = min(kCut.rows, n * in.Hq - r0);
+    const int valid = n * in.Hq;
     const int last = P + n - 1;
     pos = stop;
     if (t1 == t0) continue;  // (a share that ends within a unit's own cost)
 
-    // block ids of the lane's two keys of a tile, and the tile's direct loads from there
-    auto look_up = [&](int t, int32_t (&block)[2]) {
-      if constexpr (kPaged)
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-          block[k] = in.block_table[static_cast<int64_t>(b) * in.max_blocks + block_of(a, min(t * kKeys + load_key + 8 * k, last))];
+    // a tile's direct loads, by the block ids of the lane's two keys; behind them those of the
+    // ids of the tile that will follow in the buffer, so that one wait covers both
+    const auto table_at = [&](int key) {
+      return in.block_table + (static_cast<int64_t>(b) * in.max_blocks + block_of(a, min(key, last)));
     };
-    auto issue = [&](int t, int buffer, const int32_t (&block)[2]) {
+    auto issue = [&](int t, int buffer, int id0, int id1) {
       const unsigned char* from[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k)
         from[k] = static_cast<const unsigned char*>(in.cache) +
-                  (static_cast<uint64_t>(row_place<kPaged>(a, b, min(t * kKeys + load_key + 8 * k, last), block[k])) * kRowBytes +
+                  (static_cast<uint64_t>(row_place<kPaged>(a, b, min(t * kKeys + load_key + 8 * k, last), k == 0 ? id0 : id1)) * kRowBytes +
                    (k == 0 ? off0 : off1));
       const uint32_t dst = ring + buffer * kTileBytes;
       for_each_index<kPlanes>([&](auto g) {
         dma16_at<g() * 128>(dst + g() * kPlane, from[0]);
         dma16_at<g() * 128>(dst + g() * kPlane + 1024, from[1]);
       });
+      if constexpr (kPaged) dma4(ids + buffer * kWave * 4, table_at((t + 2 * kWaves) * kKeys + l16));
     };
+    constexpr int kLoads = 2 * kPlanes + (kPaged ? 1 : 0);
 
-    // ---- queries: lane holds row l16 of each 16, dims 32 kk + 8 quad ..; tiles t0 + wave and
-    // every fourth from there are this wave's
-    int32_t block[2] = {0, 0}, block1[2] = {0, 0};
-    look_up(t0 + wave, block);
-    look_up(t0 + wave + kWaves, block1);
+    // ---- the queries (lane: row l16, dims 32 kk + 8 quad ..) and the tree's links, then the
+    // first two of the wave's tiles, which are t0 + wave and every fourth from there
     bf16x8 qf[kSteps];
     int node;
     {
-      const uint32_t r = r0 + min(l16, valid - 1), heads = in.Hq;
+      const uint32_t r = min(l16, valid - 1), heads = in.Hq;
       node = static_cast<int>(r / heads);
       const int head = static_cast<int>(r % heads);
       const int64_t row = static_cast<int64_t>(b) * in.Nmax + node;
@@ -164,10 +162,24 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
 #pragma unroll
       for (int kk = 0; kk < kRopeDims / 32; ++kk) qf[DL / 32 + kk] = *reinterpret_cast<const bf16x8*>(qr + 32 * kk);
     }
-    // the lane's node's ancestors: at most 32 nodes, whose links lie across the wave
+    int par = -1;
+    if (lane < n) par = min(in.parents[static_cast<int64_t>(b) * in.Nmax + lane], lane - 1);
+    int first_ids[2][2] = {{0, 0}, {0, 0}};
+    if constexpr (kPaged) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        first_ids[i / 2][i % 2] = *table_at((t0 + wave + i / 2 * kWaves) * kKeys + load_key + 8 * (i % 2));
+    }
+    // (asked for before the tiles: a later wait for one of these would wait for tiles too)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int kk = 0; kk < kSteps; ++kk) asm volatile("" : "+v"(qf[kk]));
+    asm volatile("" : "+v"(par));
+    if (t0 + wave < t1) issue(t0 + wave, 0, first_ids[0][0], first_ids[0][1]);
+    if (t0 + wave + kWaves < t1) issue(t0 + wave + kWaves, 1, first_ids[1][0], first_ids[1][1]);
+    // the lane's node's ancestors: at most 16 nodes, whose links lie across the wave
     uint32_t anc = 0;
-    if (t1 * kKeys > P) {
-      const int par = lane < n ? min(in.parents[static_cast<int64_t>(b) * in.Nmax + lane], lane - 1) : -1;
+    if (t1 * static_cast<int64_t>(kKeys) > P) {
       int j = node;
       while (__ballot(j >= 0) != 0) {  // (every link goes down, so at most n steps)
         if (j >= 0) anc |= 1u << j;
@@ -175,8 +187,6 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
         j = j > 0 ? up : -1;
       }
     }
-    if (t0 + wave < t1) issue(t0 + wave, 0, block);
-    if (t0 + wave + kWaves < t1) issue(t0 + wave + kWaves, 1, block1);
 
     float m_run = kNoMax, l_run = 0.f;
     f32x4 o[kBlocks];
@@ -185,9 +195,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
     int buffer = 0;
 #pragma unroll 1
     for (int t = t0 + wave; t < t1; t += kWaves, buffer ^= 1) {
-      look_up(t + 2 * kWaves, block);
-      // (the table's ids were asked for after the tile in flight)
-      if (t + kWaves < t1) wait_vmcnt<2 * kPlanes + (kPaged ? 2 : 0)>();
+      if (t + kWaves < t1) wait_vmcnt<kLoads>();
       else wait_vmcnt<0>();
       unsigned char* kv = sm.kv[wave][buffer];
       // A tree key whose latent part holds a NaN or an infinity: the nodes that see it get
@@ -224,8 +232,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
       if (masked) {
         // bit j: tree key t * 16 - P + 4 quad + j (earlier ones are the prefix, later ones none)
         const int base = t * kKeys - P + 4 * quad;
-        const uint32_t vis = base >= 32 ? 0u : base >= 0 ? anc >> base
-                             : base > -32 ? (anc << -base) | ((1u << -base) - 1u) : 0xFFFFFFFFu;
+        const uint32_t vis = base >= 16 ? 0u : base >= 0 ? anc >> base
+                             : base > -16 ? (anc << -base) | ((1u << -base) - 1u) : 0xFFFFFFFFu;
         const uint32_t nan = bad >> (4 * quad);
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[j] = !((vis >> j) & 1u) ? -INFINITY : (nan >> j) & 1u ? NAN : s[j];
@@ -263,8 +271,9 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
         mfma_o(o[d], vf, pf);
       }
       if (t + 2 * kWaves < t1) {
+        const int id0 = kPaged ? sm.ids[wave][buffer][load_key] : 0, id1 = kPaged ? sm.ids[wave][buffer][load_key + 8] : 0;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the buffer's last reads are done
-        issue(t + 2 * kWaves, buffer, block);
+        issue(t + 2 * kWaves, buffer, id0, id1);
       }
     }
 
@@ -292,12 +301,12 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
     if (!whole && wave == 0 && part == 0 && row16 < valid)
       a.ws_row[static_cast<int64_t>(slot) * kRows + row16] = PieceRow{M, L};
     if (!whole && t0 == 0 && threadIdx.x == 0)
-      a.ws_cut[rank] = CutUnit{b, r0, valid, static_cast<int>(latent::quotient(start + length - 1, share))};
+      a.ws_cut[rank] = CutUnit{b, 0, valid, static_cast<int>(latent::quotient(start + length - 1, share))};
 #pragma unroll
     for (int d = 0; d < kBlocks; ++d)
       sm.o[wave][row16][(4 * d + part) ^ (row16 & 7)] = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[d] * f;
     __syncthreads();
-    uint16_t* out = whole ? static_cast<uint16_t*>(in.out) + (static_cast<int64_t>(b) * in.Nmax * in.Hq + r0) * DL
+    uint16_t* out = whole ? static_cast<uint16_t*>(in.out) + static_cast<int64_t>(b) * in.Nmax * in.Hq * DL
                           : a.ws_o + static_cast<int64_t>(slot) * kRows * DL;
 #pragma unroll 2
     for (int e = rare(static_cast<int>(threadIdx.x)); e < 16 * DL / 8; e += kThreads) {

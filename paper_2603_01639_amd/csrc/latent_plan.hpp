@@ -14,15 +14,15 @@ namespace latent {
 
 constexpr int kKeyTile = 32;
 constexpr int kRows = 128;    // stacked rows of a unit ...
-constexpr int kFewRows = 32;  // ... and the most of a call that takes the kernel for few rows
+constexpr int kFewRows = 16;  // ... and the most of a call that takes the kernel for few rows
 // How a kernel's calls are cut: rows of a unit, what a unit costs beside its tiles (in
 // tiles), and the shortest share.
 struct Cut {
   int rows, cost, min_share;
 };
 constexpr Cut kMany{kRows, 6, 10};
-constexpr Cut kFew{16, 4, 8};
-// Calls of up to 32 stacked rows a sequence (one token of a few heads) have a kernel of
+constexpr Cut kFew{kFewRows, 4, 8};
+// Calls of up to 16 stacked rows a sequence (one token of a few heads) have a kernel of
 // their own.
 constexpr Cut cut_of(int64_t Nmax, int64_t heads) {
   return Nmax * heads <= kFewRows ? kFew : kMany;
