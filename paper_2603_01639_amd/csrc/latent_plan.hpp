@@ -49,6 +49,7 @@ constexpr int64_t tile_at(int64_t at, const Cut& c) { return at < c.cost ? 0 : a
 // Workgroups a call can use at most.
 constexpr int workgroups(int64_t B, int64_t Nmax, int64_t heads, int64_t max_prefix, int cus) {
   const Cut c = cut_of(Nmax, heads);
+  if (B >= static_cast<int64_t>(cus) * c.min_share) return cus;  // (the product below could pass 2^63)
   const int64_t total = B * length_of(max_prefix, Nmax, heads, c);
   const int64_t most = (total + c.min_share - 1) / c.min_share;
   return static_cast<int>(most < cus ? most : cus);

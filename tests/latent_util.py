@@ -4,9 +4,16 @@ from __future__ import annotations
 
 import numpy as np
 
-from q8_util import to_dev, trees  # noqa: F401  (parent arrays of several kinds)
+import q8_util
+from q8_util import to_dev  # noqa: F401
 
 ROPE = 64
+
+
+def trees(rng, sizes, kind="random"):
+    """parents [B][max] (-1 past a tree, and for an empty one)."""
+    par = q8_util.trees(rng, [max(n, 1) for n in sizes], kind)
+    return par[:, :max(sizes)]
 
 
 def frequencies(rot, base=10000.0):
