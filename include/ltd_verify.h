@@ -582,8 +582,10 @@ int ltd_tree_accept_processed(const float* logits, const int32_t* draft_tokens,
  *   q, q_out     [B][Nmax] rows of Hq heads of d elements (dtype): row (b, i) starts
  *                at (b * Nmax + i) * q_row_stride, its head h q_head_stride elements
  *                after head h - 1; a head's elements follow one another.  q_out has
- *                strides of its own.  q_out may be q, with the same strides (in
- *                place); other overlaps give undefined results.
+ *                strides of its own, with whole rows, or all rows of a head, one after
+ *                another (LTD_EINVAL otherwise: no two heads may share memory).
+ *                q_out may be q, with the same strides (in place); other overlaps give
+ *                undefined results.
  *   k, k_out     the same with Hk heads, or Hk = 0 and NULL.
  *   inv_freq     [rot_dim / 2] float64: radians a position.
  *   depth        [B][Nmax] int32 >= 0 (as ltd_select_candidates writes it), or NULL

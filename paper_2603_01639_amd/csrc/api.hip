@@ -563,6 +563,17 @@ bool latent_supported(int d_latent, int d_rope) {
 
 }  // namespace
 
+namespace {
+// Whether the heads of `rows` rows lie apart: whole rows one after another, or whole heads.
+bool heads_apart(int64_t rows, int64_t heads, int d, int64_t row, int64_t head) {
+  if (row < 0 || head < 0) return false;
+  const bool inner = heads == 1 || head >= d, outer = rows == 1 || row >= d;
+  return inner && outer &&
+         (rows == 1 || heads == 1 || row >= static_cast<__int128>(heads - 1) * head + d ||
+          head >= static_cast<__int128>(rows - 1) * row + d);
+}
+}  // namespace
+
 int ltd_tree_rope(const void* q, int64_t q_row_stride, int64_t q_head_stride, void* q_out,
                   int64_t q_out_row_stride, int64_t q_out_head_stride, const void* k,
                   int64_t k_row_stride, int64_t k_head_stride, void* k_out,
@@ -584,6 +595,10 @@ int ltd_tree_rope(const void* q, int64_t q_row_stride, int64_t q_head_stride, vo
   if (q == q_out && (q_row_stride != q_out_row_stride || q_head_stride != q_out_head_stride))
     return LTD_EINVAL;
   if (Hk > 0 && k == k_out && (k_row_stride != k_out_row_stride || k_head_stride != k_out_head_stride))
+    return LTD_EINVAL;
+  const int64_t rows = static_cast<int64_t>(B) * Nmax;
+  if (!heads_apart(rows, Hq, d, q_out_row_stride, q_out_head_stride) ||
+      (Hk > 0 && !heads_apart(rows, Hk, d, k_out_row_stride, k_out_head_stride)))
     return LTD_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (validate) {

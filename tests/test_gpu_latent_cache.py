@@ -162,3 +162,64 @@ def test_compact_validation():
         ltd.latent_compact(cache, i(P), new, i(*path)[None], i(n), validate=True, status=st)
         torch.cuda.synchronize()
         assert int(st) == code and int(new) == -1 and torch.equal(cache, was)
+
+
+# ---- caches that 32 bits do not reach: only the rows of the case are filled
+
+@pytest.mark.parametrize("block", [0, 1, 48])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_append_past_32_bits(dtype, block):
+    import torch
+    c = make(21, 512, (40, 3, 100), (9, 30, 1), block=block, dtype=dtype)
+    size = c["cache"].element_size()
+    if block:
+        pages, used = 5 * 10 ** 9 // (576 * block * size), c["cache"].shape[0]
+        big = torch.empty((pages, block, 576), dtype=c["cache"].dtype, device="cuda")
+        view = big[pages - used:]
+        c["moved"] = dict(c, table=np.where(c["table"] < 0, c["table"], c["table"] + pages - used).astype(np.int32))
+    else:
+        R, used = 5 * 10 ** 9 // (2 * 576 * size) + 3, c["cache"].shape[1]
+        big = torch.empty((3, R, 576), dtype=c["cache"].dtype, device="cuda")
+        view = big[:, :used]
+        c["moved"] = c
+    view.copy_(c["cache"])
+    call(c["moved"], big)
+    y, tol = want(c)
+    assert (np.abs(view.double().cpu().numpy() - y) <= tol).all()
+
+
+@pytest.mark.parametrize("block", [0, 16])
+def test_compact_past_32_bits(block):
+    """The second of two layers begins past 2^32 bytes, and the pages in use are a layer's last."""
+    import torch
+    rng = np.random.default_rng(22)
+    P, n, acc = 45, 20, [0, 3, 4, 11, 19]
+    R = block or 2_000_003
+    pages = 250_000 if block else 1
+    cache = torch.empty((2, pages, R, 576), dtype=torch.bfloat16, device="cuda")
+    cache = cache if block else torch.empty((2, 2, R, 576), dtype=torch.bfloat16, device="cuda")
+    assert cache[1].data_ptr() - cache.data_ptr() > 2 ** 32
+    rows = torch.from_numpy(rng.normal(size=(2, 64 + 16, 576))).bfloat16().cuda()
+    if block:
+        table = (pages - 1 - rng.permutation(5)).astype(np.int32)[None]
+        for k, page in enumerate(table[0]):
+            cache[:, page] = rows[:, 16 * k:16 * k + 16]
+        one = lambda v: L.to_dev(np.array([v], np.int32))  # noqa: E731
+    else:
+        table = None
+        cache[:, 1, :80] = rows
+        cache[:, 0, :80] = 0
+        one = lambda v: L.to_dev(np.array([0, v], np.int32))  # noqa: E731
+    B = 1 if block else 2
+    path = np.zeros((B, n), np.int32)
+    path[B - 1, :len(acc)] = acc
+    new = torch.zeros((B,), dtype=torch.int32, device="cuda")
+    nacc = one(len(acc)) if block else L.to_dev(np.array([1, len(acc)], np.int32))
+    ltd.latent_compact(cache, one(P), new, L.to_dev(path), nacc, block_table=L.to_dev(table), num_blocks=pages if block else 0)
+    torch.cuda.synchronize()
+    want = rows.clone()
+    for j, a in enumerate(acc):
+        want[:, P + j] = rows[:, P + a]
+    got = torch.cat([cache[:, p] for p in table[0]], 1) if block else cache[:, 1, :80]
+    assert torch.equal(got, want)
+    assert int(new[-1]) == P + len(acc)

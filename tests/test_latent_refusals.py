@@ -43,7 +43,9 @@ def compact(**kw):
     (dict(off=-2), BAD), (dict(off=2), BAD), (dict(off=2**31 - 1), BAD), (dict(m=float("nan")), BAD), (dict(m=float("inf")), BAD),
     (dict(dtype=2), NO), (dict(d=4098, rot=2), NO), (dict(N=TOP + 1), NO), (dict(Hq=2**31 - 1), NO), (dict(q=None), BAD),
     (dict(qo=None), BAD), (dict(k=None), BAD), (dict(freq=None), BAD), (dict(prefix=None), BAD), (dict(n=None), BAD),
-    (dict(qo=X, qor=640), BAD), (dict(ko=X, koh=128), BAD), (dict(validate=1), BAD), (dict(B=0, q=None), 0)])
+    (dict(qo=X, qor=640), BAD), (dict(ko=X, koh=128), BAD), (dict(validate=1), BAD), (dict(B=0, q=None), 0),
+    (dict(qor=511), BAD), (dict(qoh=0), BAD), (dict(qor=0), BAD), (dict(qor=-512), BAD), (dict(koh=63), BAD), (dict(kor=127), BAD),
+    (dict(qor=64, qoh=255), BAD), (dict(qor=2**62, qoh=2**62, Hq=100), BAD), (dict(q=2 * X, qr=512, qh=0), BAD)])
 def test_rope(kw, code):
     assert rope(**kw) == code
 
