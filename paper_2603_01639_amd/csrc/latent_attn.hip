@@ -781,10 +781,7 @@ hipError_t launch_latent_attn(const LatentAttn& s, int d_latent, int dtype, void
   a.ws_row = reinterpret_cast<PieceRow*>(a.ws_cut + a.W);
   a.scale_log2 = s.scale * kLog2e;
   a.lazy_gap = kLazyMax / a.scale_log2;
-  // row / kv_rows = floor(2 row * magic / 2^(32 + shift)): with kv_rows <= 2^shift and magic =
-  // floor(2^(31 + shift) / kv_rows) + 1 it is exact for every row below 2^31.
-  while (a.row_shift < 31 && (1u << a.row_shift) < static_cast<uint32_t>(s.kv_rows)) ++a.row_shift;
-  a.row_magic = static_cast<uint32_t>((uint64_t{1} << (31 + a.row_shift)) / s.kv_rows + 1);
+  a.block = latent::row_divisor(s.kv_rows);
   return d_latent == 512 ? launch_bf16<512>(a, stream) : launch_bf16<256>(a, stream);
 }
 

@@ -41,8 +41,7 @@ struct LatentArgs {
   CutUnit* ws_cut;   // [W]: the cut unit that begins in a workgroup's share (valid 0: none)
   int W;         // workgroups
   float scale_log2, lazy_gap;
-  uint32_t row_magic;  // block_of's multiplier and shift
-  int row_shift;
+  latent::RowDivisor block;  // of kv_rows
 };
 
 // x, made anew: constants of rare branches, and what they and a piece's end derive from
@@ -137,9 +136,9 @@ __device__ __forceinline__ void dma16_at(uint32_t lds, const void* p) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off offset:%2" ::"s"(lds - kOff), "v"(p), "n"(kOff) : "memory");
 }
 
-// A row of a cache: its block, by a multiplication with row_magic.
+// A row's block.
 __device__ __forceinline__ int block_of(const LatentArgs& a, int row) {
-  return static_cast<int>(__umulhi(2u * static_cast<uint32_t>(row), a.row_magic) >> a.row_shift);
+  return static_cast<int>(__umulhi(2u * static_cast<uint32_t>(row), a.block.magic) >> a.block.shift);
 }
 // Its place among the cache's rows, which are counted in 32 bits: 2^31 of them pass any
 // memory.

@@ -46,6 +46,18 @@ constexpr int64_t share_of(int64_t total, int W, const Cut& c) {
 }
 // The tile that a unit's place `at` belongs to (its own cost comes first).
 constexpr int64_t tile_at(int64_t at, const Cut& c) { return at < c.cost ? 0 : at - c.cost; }
+// row / kv_rows by a multiplication: floor(2 row * magic / 2^(32 + shift)).  With kv_rows <=
+// 2^shift and magic = floor(2^(31 + shift) / kv_rows) + 1 it is exact for every row below
+// 2^31.
+struct RowDivisor {
+  uint32_t magic;
+  int shift;
+};
+constexpr RowDivisor row_divisor(int kv_rows) {
+  int shift = 0;
+  while (shift < 31 && (uint32_t{1} << shift) < static_cast<uint32_t>(kv_rows)) ++shift;
+  return {static_cast<uint32_t>((uint64_t{1} << (31 + shift)) / static_cast<uint32_t>(kv_rows) + 1), shift};
+}
 // Workgroups a call can use at most.
 constexpr int workgroups(int64_t B, int64_t Nmax, int64_t heads, int64_t max_prefix, int cus) {
   const Cut c = cut_of(Nmax, heads);
