@@ -24,6 +24,7 @@ constexpr int kKeys = latent::kKeyTile;
 constexpr int kStages = 3;           // tiles in the LDS ring
 constexpr int kAhead = 6;            // key fragments in flight
 constexpr int kPlane = kKeys * 128;  // bytes of a tile's plane in LDS
+constexpr int kQPlane = 32 * 128;    // and of a wave's queries'
 constexpr latent::Cut kCut = latent::kMany;
 
 template <int DL>
@@ -32,7 +33,7 @@ struct Smem {
   u32x4 p[2][kKeys / 8][kRows];              // weights: 8 keys of a row
   float alpha[2][kRows];                     // what a row's sums so far are multiplied by
   i32x4 moved[2];                            // whether a wave's rows have such factors
-  float row_l[kRows];                        // sums
+  float row_f[kRows];                        // 1 / sum
   uint32_t anc[kAncWords][LTD_MAX_NODES];    // word w of every node's ancestor set
   int jump[LTD_MAX_NODES];
   uint32_t bad[2];                           // tree keys of a tile with a NaN or an infinity
@@ -67,6 +68,10 @@ __device__ __forceinline__ void mfma_acc(f32x16& o, bf16x8 a, bf16x8 b) {
 }
 __device__ __forceinline__ void mfma_first(f32x16& s, bf16x8 a, bf16x8 b) {
   asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
+}
+// o = 0 (a product takes 8 bytes of code, 16 moves 128).
+__device__ __forceinline__ void mfma_zero(f32x16& o, bf16x8 zero) {
+  asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %1, 0" : "=a"(o) : "v"(zero));
 }
 __device__ __forceinline__ void mfma_next(f32x16& s, bf16x8 a, bf16x8 b) {
   asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
@@ -180,7 +185,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     };
     auto at = [&](int t, int32_t block) { return source(row_place<kPaged>(a, b, min(t * kKeys + load_key, last), block)); };
     auto issue_plane = [&](int t, const unsigned char* from, auto plane) {
-      dma16_at<plane() * 128>(kv_lds + (t % kStages) * kTileBytes + wave * 1024 + plane() * kPlane, from);
+      dma16_at<plane() * 128>(kv_lds + ((t - t0) % kStages) * kTileBytes + wave * 1024 + plane() * kPlane, from);
     };
     auto issue = [&](int t, int32_t block) {
       const unsigned char* from = at(t, block);
@@ -190,24 +195,52 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     look_up(t0, block0);
     look_up(t0 + 1, block1);
     look_up(t0 + 2, block);
-    // ---- queries: lane holds row l32 of the wave's 32, dims 16 kk + 8 h ..
+    // ---- queries: lane holds row l32 of the wave's 32, dims 16 kk + 8 h ..  They come
+    // through LDS, in two runs of planes of 64 dims through the wave's part of what the
+    // first tile leaves free: loaded from where they lie, 16 bytes of 32 rows an
+    // instruction, they took 7100 cycles, and the tile behind them waited.
     bf16x8 qf[kSteps];
     int node;
+    constexpr int kRun = (2 * kTileBytes + static_cast<int>(sizeof(sm.p))) / (kWaves * kQPlane);
+    static_assert(2 * kRun >= kPlanes && offsetof(Smem<DL>, p) == kStages * kTileBytes, "the queries come in two runs");
+    constexpr int kFirst = kRun < kPlanes ? kRun : kPlanes;
+    const unsigned char* q_from[2][4];  // row 8 i + lane / 8: its chunk of the first plane, and of the rotated part
     {
       const uint32_t r = r0 + min(32 * wave + l32, valid - 1), heads = rare(in.Hq);
       node = static_cast<int>(r / heads);
       const int head = static_cast<int>(r % heads);
       const int64_t row = static_cast<int64_t>(b) * in.Nmax + node;
-      const uint16_t* ql = static_cast<const uint16_t*>(in.q_latent) + row * in.ql_row + head * in.ql_head + 8 * h;
-      const uint16_t* qr = static_cast<const uint16_t*>(in.q_rope) + row * in.qr_row + head * in.qr_head + 8 * h;
+      const int64_t ql = 2 * (row * in.ql_row + head * in.ql_head), qr = 2 * (row * in.qr_row + head * in.qr_head);
 #pragma unroll
-      for (int kk = 0; kk < DL / 16; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(ql + 16 * kk);
-#pragma unroll
-      for (int kk = 0; kk < kRopeDims / 16; ++kk) qf[DL / 16 + kk] = *reinterpret_cast<const bf16x8*>(qr + 16 * kk);
+      for (int i = 0; i < 4; ++i) {
+        const int of = 8 * i + (lane >> 3), chunk = ((lane & 7) ^ (of >> 1 & 7)) * 16;
+        q_from[0][i] = static_cast<const unsigned char*>(in.q_latent) + (__shfl(ql, of, kWave) + chunk);
+        q_from[1][i] = static_cast<const unsigned char*>(in.q_rope) + (__shfl(qr, of, kWave) + chunk);
+      }
     }
-
+    unsigned char* q_lds = sm.kv[1] + wave * (kFirst * kQPlane);
+    auto load_queries = [&](auto from, auto to) {
+      for_each_index<to() - from()>([&](auto ix) {
+        constexpr int g = from() + ix();
+        for_each_index<4>([&](auto i) {
+          const uint32_t dst = lds_addr(q_lds) + ix() * kQPlane + i() * 1024;
+          if constexpr (g < DL / 64) dma16_at<g * 128>(dst, q_from[0][i()]);
+          else dma16_at<0>(dst, q_from[1][i()]);
+        });
+      });
+    };
+    auto take_queries = [&](auto from, auto to) {
+      wait_vmcnt<0>();
+      for_each_index<4 * (to() - from())>([&](auto ix) {
+        qf[4 * from() + ix()] = *reinterpret_cast<const bf16x8*>(
+            q_lds + (ix() >> 2) * kQPlane + l32 * 128 + (((2 * (ix() & 3) + h) ^ (l32 >> 1 & 7)) << 4));
+      });
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
+    using First = std::integral_constant<int, kFirst>;
+    using All = std::integral_constant<int, kPlanes>;
     issue(t0, block0);
-    if (t0 + 1 < t1) issue(t0 + 1, block1);
+    load_queries(std::integral_constant<int, 0>{}, First{});
 
     // ---- ancestor sets (256 bits a node) by pointer doubling: anc(i) |= anc(jump(i)),
     // jump(i) = jump(jump(i)); thread i has node i
@@ -240,16 +273,23 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
         }
       }
     }
+    take_queries(std::integral_constant<int, 0>{}, First{});
+    if constexpr (kFirst < kPlanes) {
+      load_queries(First{}, All{});
+      take_queries(First{}, All{});
+    }
     __syncthreads();
+    if (t0 + 1 < t1) issue(t0 + 1, block1);
 
     float m_run = rare(kNoMax), l_run = 0.f;
     f32x16 o[kDB][kGroups];
+    bf16x8 zero = bf16x8{};
+    asm volatile("s_nop 1" : "+v"(zero));
 #pragma unroll
     for (int db = 0; db < kDB; ++db)
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
-        o[db][g] = f32x16{};
-        asm volatile("" : "+a"(o[db][g]));
+        mfma_zero(o[db][g], zero);
       }
     const float c = a.scale_log2;
     auto settle_all = [&] {
@@ -336,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     // The keys of tile t (landed) whose latent part is not finite; the whole
     // workgroup looks.
     auto find_bad = [&](int t) -> uint32_t {
-      const unsigned char* kv = sm.kv[t % kStages];
+      const unsigned char* kv = sm.kv[(t - t0) % kStages];
       if (threadIdx.x == 0) sm.bad[t & 1] = 0;
       __syncthreads();
 #pragma unroll 1
@@ -353,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     };
     // 0 times a NaN would be one in the rows that do not see it.
     auto clear_bad = [&](int t, uint32_t bad) {
-      unsigned char* kv = sm.kv[t % kStages];
+      unsigned char* kv = sm.kv[(t - t0) % kStages];
 #pragma unroll 1
       for (int e = rare_thread(); e < kKeys * DL / 8; e += kThreads)
         if ((bad >> (e / 8 % kKeys)) & 1u) {
@@ -418,12 +458,10 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     // weights of tile t + 1 and multiplies tile t's weights and values.  A quarter of
     // those products runs in front of the scores', and three beside the weights'
     // vector operations.
-    wait_vmcnt<0>();
-    barrier_only();
     uint32_t bad = masked(t0) ? find_bad(t0) : 0;
     {
       f32x16 s;
-      const unsigned char* kv = sm.kv[t0 % kStages];
+      const unsigned char* kv = sm.kv[0];
       first_keys(kv);
       scores(s, kv, [](auto) {});
       mfma_settle(s);
@@ -459,8 +497,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
       // (opaque to the compiler, which would keep every address that follows from
       // these in registers of its own over the loop)
       asm volatile("" : "+v"(k_rd), "+v"(v_rd), "+v"(l32), "+v"(h), "+v"(load_key));
-      const unsigned char* kv = sm.kv[(t + 1) % kStages];
-      const unsigned char* kv_old = sm.kv[t % kStages];
+      const unsigned char* kv = sm.kv[(t + 1 - t0) % kStages];
+      const unsigned char* kv_old = sm.kv[(t - t0) % kStages];
       const int par = t & 1;
       turn();
       first_keys(kv);
@@ -511,7 +549,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     }
     {
       const float l = l_run + xor32(l_run);
-      if (h == 0) sm.row_l[32 * wave + l32] = l;
+      // (a piece without a visible key has weight 0 in the merge, and O = 0)
+      if (h == 0) sm.row_f[32 * wave + l32] = !whole && l == 0.f ? 0.f : 1.f / l;
       if (!whole && h == 0 && 32 * wave + l32 < valid) {
         PieceRow& row = a.ws_row[static_cast<int64_t>(slot) * kRows + 32 * wave + l32];
         row.m = m_run * c;
@@ -524,7 +563,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     last_products([](auto) {});
     catch_up(t1 - 1, sm.moved[(t1 - 1) & 1]);
     {
-      const unsigned char* kv = sm.kv[(t1 - 1) % kStages];
+      const unsigned char* kv = sm.kv[(t1 - 1 - t0) % kStages];
       const int par = (t1 - 1) & 1;
       load_values(va, kv, 0);
       load_values(vb, kv, 1);
@@ -535,44 +574,46 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     settle_all();
 
     // ---- results, 32 rows at a time: O / l in bf16, of a whole unit to `out`, as a piece
-    // to the workspace.  (Rounding a piece costs at most 2^-9 of its own weight; in fp16
-    // under a power of two a row they were a third of the kernel's code, read but once a
-    // unit: 15600 cycles each.)  They pass through LDS, a part of the ring that no wave
-    // reads any more, so that a row's dims of a wave go out in one run.
-    constexpr int kPitch = kCols * 2 + 16;
-    unsigned char* stage = sm.kv[t1 % kStages] + wave * 32 * kPitch;
-    static_assert(kWaves * 32 * kPitch <= kTileBytes, "rows fit a tile");
+    // to the workspace.  (Rounding a piece costs at most 2^-9 of its own weight.)  The sums
+    // pass through LDS, in the stages that no wave reads any more (two waves in each), so
+    // that a row's dims of a wave go out in one run and the code is that of one row.
+    constexpr int kPitch = kCols * 4 + 16;
+    unsigned char* stage = sm.kv[(t1 - t0 + (wave >> 1)) % kStages] + (wave & 1) * 32 * kPitch;
+    static_assert(2 * 32 * kPitch <= kTileBytes, "rows of two waves fit a tile");
     {
-      for_each_index<kGroups>([&](auto gx) {
-        constexpr int g = gx();
-        if (32 * g >= valid) return;
-        __builtin_amdgcn_sched_barrier(0);
-        asm volatile("" : "+v"(l32), "+v"(h));
-        const int to_lane = rare(lane);
-        const float l = sm.row_l[32 * g + l32];
-        // (a piece without a visible key has weight 0 in the merge, and O = 0)
-        const float mul = !whole && l == 0.f ? 0.f : 1.f / l;
-        unsigned char* to = stage + l32 * kPitch + 8 * h;
+      uint16_t* out = (whole ? static_cast<uint16_t*>(in.out) + (static_cast<int64_t>(b) * in.Nmax * in.Hq + r0) * DL
+                             : a.ws_o + static_cast<int64_t>(slot) * kRows * DL) + wave * kCols;
+      asm volatile("" : "+v"(l32), "+v"(h));
+      const int to_lane = rare(lane);
+      constexpr int kLanes = kCols / 8;  // of a row
+      const int col = to_lane % kLanes * 8;
+      const auto put = [&](auto g) {
+        f32x4* to = reinterpret_cast<f32x4*>(stage + l32 * kPitch + 16 * h);
 #pragma unroll
         for (int db = 0; db < kDB; ++db)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            uint2 w;
-            w.x = pack_bf16x2(o[db][g][4 * q] * mul, o[db][g][4 * q + 1] * mul);
-            w.y = pack_bf16x2(o[db][g][4 * q + 2] * mul, o[db][g][4 * q + 3] * mul);
-            *reinterpret_cast<uint2*>(to + 64 * db + 16 * q) = w;
+            const f32x16& x = o[db][g()];
+            to[8 * db + 2 * q] = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
           }
-        constexpr int kLanes = kCols / 8;  // of a row
-        uint16_t* out = whole ? static_cast<uint16_t*>(in.out) + (static_cast<int64_t>(b) * in.Nmax * in.Hq + r0) * DL
-                              : a.ws_o + static_cast<int64_t>(slot) * kRows * DL;
+      };
+#pragma unroll 1
+      for (int r = 0; r < valid; r += 32) {
+        if (r == 0) put(std::integral_constant<int, 0>{});
+        else if (r == 32) put(std::integral_constant<int, 1>{});
+        else if (r == 64) put(std::integral_constant<int, 2>{});
+        else put(std::integral_constant<int, 3>{});
 #pragma unroll
         for (int i = 0; i < 32 * kLanes / kWave; ++i) {
-          const int row = i * (kWave / kLanes) + to_lane / kLanes, col = to_lane % kLanes * 8;
-          const u32x4 x = *reinterpret_cast<const u32x4*>(stage + row * kPitch + col * 2);
-          if (32 * g + row < valid)
-            *reinterpret_cast<u32x4*>(out + static_cast<int64_t>(32 * g + row) * DL + wave * kCols + col) = x;
+          const int row = i * (kWave / kLanes) + to_lane / kLanes;
+          const f32x4* from = reinterpret_cast<const f32x4*>(stage + row * kPitch + col * 4);
+          const float f = sm.row_f[r + row];
+          const f32x4 x0 = from[0] * f, x1 = from[1] * f;
+          if (r + row < valid)
+            *reinterpret_cast<u32x4*>(out + static_cast<int64_t>(r + row) * DL + col) =
+                u32x4{pack_bf16x2(x0[0], x0[1]), pack_bf16x2(x0[2], x0[3]), pack_bf16x2(x1[0], x1[1]), pack_bf16x2(x1[2], x1[3])};
         }
-      });
+      }
     }
     pos = stop;
   }
