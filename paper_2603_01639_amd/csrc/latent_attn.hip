@@ -573,8 +573,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     }
     settle_all();
 
-    // ---- results, 32 rows at a time: O / l in bf16, of a whole unit to `out`, as a piece
-    // to the workspace.  (Rounding a piece costs at most 2^-9 of its own weight.)  The sums
+    // ---- results, 32 rows at a time: O / l of a whole unit to `out`, as a piece to the
+    // workspace.  (256 workgroups' pieces are 33 MB, which bound this part.)  The sums
     // pass through LDS, in the stages that no wave reads any more (two waves in each), so
     // that a row's dims of a wave go out in one run and the code is that of one row.
     constexpr int kPitch = kCols * 4 + 16;
@@ -603,15 +603,32 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
         else if (r == 32) put(std::integral_constant<int, 1>{});
         else if (r == 64) put(std::integral_constant<int, 2>{});
         else put(std::integral_constant<int, 3>{});
-#pragma unroll
-        for (int i = 0; i < 32 * kLanes / kWave; ++i) {
-          const int row = i * (kWave / kLanes) + to_lane / kLanes;
-          const f32x4* from = reinterpret_cast<const f32x4*>(stage + row * kPitch + col * 4);
-          const float f = sm.row_f[r + row];
-          const f32x4 x0 = from[0] * f, x1 = from[1] * f;
-          if (r + row < valid)
-            *reinterpret_cast<u32x4*>(out + static_cast<int64_t>(r + row) * DL + col) =
-                u32x4{pack_bf16x2(x0[0], x0[1]), pack_bf16x2(x0[2], x0[3]), pack_bf16x2(x1[0], x1[1]), pack_bf16x2(x1[2], x1[3])};
+        // (a lane's rows side by side: one after another they wait for themselves)
+        constexpr int kEach = 32 * kLanes / kWave, kStep = kWave / kLanes;  // rows a lane, and to the next
+        const int first = to_lane / kLanes;
+        uint16_t* to = out + static_cast<int64_t>(r + first) * DL + col;
+        const auto row = [&](int i, auto pack) {
+          const f32x4* from = reinterpret_cast<const f32x4*>(stage + (first + i * kStep) * kPitch + col * 4);
+          return pack(from[0], from[1], sm.row_f[r + first + i * kStep]);
+        };
+        if (whole) {
+          for_each_index<kEach>([&](auto i) {
+            const u32x4 x = row(i(), [](f32x4 x0, f32x4 x1, float f) {
+              return u32x4{pack_bf16x2(x0[0] * f, x0[1] * f), pack_bf16x2(x0[2] * f, x0[3] * f),
+                           pack_bf16x2(x1[0] * f, x1[1] * f), pack_bf16x2(x1[2] * f, x1[3] * f)};
+            });
+            if (r + first + i() * kStep < valid) *reinterpret_cast<u32x4*>(to + i() * kStep * DL) = x;
+          });
+        } else {  // (a slot has room for all 128 rows)
+          float mine = 0.f;  // lane i of a row's first ones: the factor of the i-th row
+          for_each_index<kEach>([&](auto i) {
+            float factor;
+            const u32x4 x = row(i(), [&](f32x4 x0, f32x4 x1, float f) { return pack_piece<DL>(x0, x1, f, &factor); });
+            *reinterpret_cast<u32x4*>(to + i() * kStep * DL) = x;
+            mine = to_lane % kLanes == i() ? factor : mine;
+          });
+          if (to_lane % kLanes < kEach)
+            a.ws_factor[(static_cast<int64_t>(slot) * kRows + r + first + to_lane % kLanes * kStep) * 4 + wave] = mine;
         }
       }
     }
@@ -619,13 +636,14 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
   }
 }
 
-// Joins the pieces of the cut unit that begins in workgroup x's share, a wave a row:
-// lane p takes piece p's maximum and sum for the weights, then each lane its dims of
-// every piece.
+// Joins the pieces of the cut unit that begins in workgroup x's share, a wave a row, 16
+// pieces at a time: lane 16 g + p takes piece p's maximum and sum for the weights, with the
+// factor of quarter g of its dims, then each lane its dims of every piece.
 template <int DL>
 __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
-  constexpr int kEach = DL / kWave;  // dims a lane
-  typedef __bf16 Dims __attribute__((ext_vector_type(DL / kWave)));
+  constexpr int kEach = DL / kWave;  // dims a lane: lanes 16 g .. have quarter g
+  constexpr int kBatch = 16;
+  typedef _Float16 Dims __attribute__((ext_vector_type(DL / kWave)));
   const LatentAttn& in = a.in;
   if (halted(in.status)) return;
   const int lane = threadIdx.x % kWave;
@@ -640,20 +658,23 @@ __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
   float acc[kEach];
 #pragma unroll
   for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
-  for (int p0 = 0; p0 < pieces; p0 += kWave) {
-    const int count = min(kWave, pieces - p0);
-    float m = kNoMax, l = 0.f;
-    if (lane < count) {
-      const PieceRow& r = a.ws_row[slot(p0 + lane)];
+  for (int p0 = 0; p0 < pieces; p0 += kBatch) {
+    const int count = min(kBatch, pieces - p0);
+    float m = kNoMax, l = 0.f, factor = 0.f;
+    if (lane % kBatch < count) {
+      const int64_t s = slot(p0 + lane % kBatch);
+      const PieceRow& r = a.ws_row[s];
       l = r.l;
+      factor = a.ws_factor[s * 4 + lane / kBatch];
       if (l != 0.f) m = r.m;
     }
-    const float m_new = fmaxf(M, wave_max_dpp(m));
+    const float m_new = fmaxf(M, row_reduce(m, [](float u, float v) { return fmaxf(u, v); }));
     const float old = exp2_fast(M - m_new), w = l != 0.f ? exp2_fast(m - m_new) * l : 0.f;
-    L = L * old + wave_sum_dpp(w);
+    L = L * old + row_reduce(w, [](float u, float v) { return u + v; });
     M = m_new;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) acc[e] *= old;
+    const float wf = w != 0.f ? w * factor : 0.f;
     constexpr int kUnroll = 8;
     for (int p = 0; p < count; p += kUnroll) {
       Dims d[kUnroll];
@@ -664,7 +685,7 @@ __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
       }
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        const float wu = p + u < count ? __shfl(w, p + u, kWave) : 0.f;
+        const float wu = p + u < count ? __shfl(wf, p + u, kBatch) : 0.f;
         // (a piece of weight 0 has no rows to be read: it may hold anything)
         if (wu != 0.f) {
 #pragma unroll
@@ -803,7 +824,7 @@ hipError_t launch_bf16(const LatentArgs& a, hipStream_t stream) {
 size_t latent_attn_workspace_bytes(const LatentAttn& s, int d_latent, int dtype, int cus) {
   if (dtype == LTD_DTYPE_F32 || s.B == 0) return 0;
   const size_t W = grid_of(s, cus);
-  return 2 * W * kRows * (d_latent * sizeof(uint16_t) + sizeof(PieceRow)) + W * sizeof(CutUnit);
+  return 2 * W * kRows * (d_latent * sizeof(uint16_t) + 4 * sizeof(float) + sizeof(PieceRow)) + W * sizeof(CutUnit);
 }
 
 hipError_t launch_latent_attn(const LatentAttn& s, int d_latent, int dtype, void* workspace, int cus,
@@ -818,7 +839,8 @@ hipError_t launch_latent_attn(const LatentAttn& s, int d_latent, int dtype, void
   a.in = s;
   a.W = grid_of(s, cus);
   a.ws_o = static_cast<uint16_t*>(workspace);
-  a.ws_cut = reinterpret_cast<CutUnit*>(a.ws_o + static_cast<int64_t>(2) * a.W * kRows * d_latent);
+  a.ws_factor = reinterpret_cast<float*>(a.ws_o + static_cast<int64_t>(2) * a.W * kRows * d_latent);
+  a.ws_cut = reinterpret_cast<CutUnit*>(a.ws_factor + static_cast<int64_t>(2) * a.W * kRows * 4);
   a.ws_row = reinterpret_cast<PieceRow*>(a.ws_cut + a.W);
   a.scale_log2 = s.scale * kLog2e;
   a.lazy_gap = kLazyMax / a.scale_log2;

@@ -317,9 +317,15 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
         x0 += sm.o[w][row][(2 * col) ^ (row & 7)];
         x1 += sm.o[w][row][(2 * col + 1) ^ (row & 7)];
       }
-      if (row < valid)
-        *reinterpret_cast<u32x4*>(out + static_cast<int64_t>(row) * DL + col * 8) =
-            u32x4{pack_bf16x2(x0[0], x0[1]), pack_bf16x2(x0[2], x0[3]), pack_bf16x2(x1[0], x1[1]), pack_bf16x2(x1[2], x1[3])};
+      float factor;
+      const u32x4 packed = whole ? u32x4{pack_bf16x2(x0[0], x0[1]), pack_bf16x2(x0[2], x0[3]),
+                                         pack_bf16x2(x1[0], x1[1]), pack_bf16x2(x1[2], x1[3])}
+                                 : pack_piece<DL>(x0, x1, 1.f, &factor);
+      if (row < valid) {
+        *reinterpret_cast<u32x4*>(out + static_cast<int64_t>(row) * DL + col * 8) = packed;
+        if (!whole && col % (DL / 32) == 0)
+          a.ws_factor[(static_cast<int64_t>(slot) * kRows + row) * 4 + col / (DL / 32)] = factor;
+      }
     }
     __syncthreads();
   }

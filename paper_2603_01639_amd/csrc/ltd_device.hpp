@@ -73,13 +73,17 @@ __device__ __forceinline__ float rows_reduce(float v, Op op) {
   const uint32_t c = r32[0], e = r32[1];
   return op(__builtin_bit_cast(float, c), __builtin_bit_cast(float, e));
 }
+// op over a row of 16 lanes.
 template <class Op>
-__device__ __forceinline__ float wave_reduce(float v, Op op) {
+__device__ __forceinline__ float row_reduce(float v, Op op) {
   v = op(v, dpp<0xB1>(v));   // quad_perm [1, 0, 3, 2]
   v = op(v, dpp<0x4E>(v));   // quad_perm [2, 3, 0, 1]
   v = op(v, dpp<0x141>(v));  // row_half_mirror
-  v = op(v, dpp<0x140>(v));  // row_mirror
-  return rows_reduce(v, op);
+  return op(v, dpp<0x140>(v));  // row_mirror
+}
+template <class Op>
+__device__ __forceinline__ float wave_reduce(float v, Op op) {
+  return rows_reduce(row_reduce(v, op), op);
 }
 __device__ __forceinline__ float wave_max_dpp(float v) {
   return wave_reduce(v, [](float x, float y) { return fmaxf(x, y); });

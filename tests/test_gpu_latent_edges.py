@@ -289,3 +289,18 @@ def test_a_long_prefix(H):
     m = dict(cache=cache, table=table, par=np.array([[-1]], np.int32), q=q, ql=q[..., :DL], qr=q[..., DL:], layout="rows",
              prefix=np.array([P], np.int32), n=np.array([1], np.int32), scale=192 ** -0.5, DL=DL)
     check(m, run(m))
+
+
+@pytest.mark.parametrize("H, sizes", [(16, [1, 1]), (16, [20, 1])])
+@pytest.mark.parametrize("DL", [256, 512])
+def test_dims_of_different_sizes(DL, H, sizes):
+    """Latent dims from 2^-12 to 2^12 in turn, rows of sequences from 2^-60 to 2^60: split rows keep every dim's bits."""
+    import torch
+    m = make(16, H, DL, [3000, 700], sizes, 0)
+    by_dim = 2.0 ** torch.from_numpy(np.random.default_rng(2).integers(-12, 13, DL)).double()
+    by_seq = torch.tensor([2.0 ** 60, 2.0 ** -60]).double()
+    lat = m["cache"][..., :DL].double() * by_dim
+    m["cache"][..., :DL] = (lat * by_seq[:, None, None]).bfloat16()
+    m["q"][..., :DL] = (m["q"][..., :DL].double() / by_dim / by_seq[:, None, None, None]).bfloat16()
+    m.update(ql=m["q"][..., :DL], qr=m["q"][..., DL:], layout="rows")
+    check(m, run(m))
