@@ -718,6 +718,7 @@ __global__ void __launch_bounds__(kThreads) latent_vector_kernel(LatentAttn a) {
   __shared__ __attribute__((aligned(16))) float q_s[kWaves][DK];
   __shared__ float p_s[kWaves][kKeys];
   __shared__ int path_s[LTD_MAX_NODES];
+  __shared__ int32_t parents_s[LTD_MAX_NODES];
   __shared__ int path_len_s;
   if (halted(a.status)) return;
   const int i = blockIdx.x, b = blockIdx.z;
@@ -726,7 +727,7 @@ __global__ void __launch_bounds__(kThreads) latent_vector_kernel(LatentAttn a) {
   const int head = blockIdx.y * kWaves + w;
   const bool live = head < a.Hq;
   const int P = max(a.prefix_len[b], 0);
-  if (t == 0) path_len_s = root_path(a.parents + static_cast<int64_t>(b) * a.Nmax, i, path_s);
+  if (t <= i) parents_s[t] = a.parents[static_cast<int64_t>(b) * a.Nmax + t];
   const int64_t row = static_cast<int64_t>(b) * a.Nmax + i;
   for (int e = lane; e < DK; e += kWave) {
     float v = 0.f;
@@ -736,34 +737,45 @@ __global__ void __launch_bounds__(kThreads) latent_vector_kernel(LatentAttn a) {
     q_s[w][e] = v;
   }
   __syncthreads();
+  if (t == 0) path_len_s = root_path(parents_s, i, path_s);
+  __syncthreads();
   const int n_keys = P + path_len_s;
   float m = -INFINITY, l = 0.f;
   float acc[DL / kWave];
 #pragma unroll
   for (int e = 0; e < DL / kWave; ++e) acc[e] = 0.f;
   const float c = a.scale;
+  // Eight threads load a key, into registers a tile ahead: the loads run beside the last
+  // tile's products.
+  constexpr int kPerKey = kThreads / kKeys, kLoads = kQuads / kPerKey;
+  static_assert(kQuads % kPerKey == 0, "whole loads");
+  const int my_key = t / kPerKey, my_col = t % kPerKey * 4;
+  f32x4 next[kLoads];
+  auto load = [&](int base) {
+    const int kt = min(base + my_key, n_keys - 1);
+    const int r = kt < P ? kt : P + path_s[kt - P];
+    const float* src = static_cast<const float*>(a.cache) + cache_row(a.block_table, b, 0, r, 1, DK, a.kv_rows, a.max_blocks) + my_col;
+    for_each_index<kLoads>([&](auto j) { next[j()] = *reinterpret_cast<const f32x4*>(src + j() * kPerKey * 4); });
+  };
+  load(0);
   for (int base = 0; base < n_keys; base += kKeys) {
     const int cnt = min(kKeys, n_keys - base);
-    for (int e = t; e < cnt * kQuads; e += kThreads) {
-      const int k = e / kQuads, col = e % kQuads * 4;
-      const int kt = base + k;
-      const int r = kt < P ? kt : P + path_s[kt - P];
-      const float* src = static_cast<const float*>(a.cache) + cache_row(a.block_table, b, 0, r, 1, DK, a.kv_rows, a.max_blocks);
-      *reinterpret_cast<float4*>(&x_s[k][col]) = *reinterpret_cast<const float4*>(src + col);
-    }
+    for_each_index<kLoads>([&](auto j) { *reinterpret_cast<f32x4*>(&x_s[my_key][my_col + j() * kPerKey * 4]) = next[j()]; });
     __syncthreads();
+    if (base + kKeys < n_keys) load(base + kKeys);
     const int key = lane & 31, half = lane >> 5;
-    float s = 0.f;
+    float s4[4] = {0.f, 0.f, 0.f, 0.f};
     const float* xr = &x_s[min(key, cnt - 1)][half * (DK / 2)];
     const float* qr = &q_s[w][half * (DK / 2)];
-#pragma unroll 4
+#pragma unroll 8
     for (int e = 0; e < DK / 2; e += 4) {
       const float4 x = *reinterpret_cast<const float4*>(xr + e), q = *reinterpret_cast<const float4*>(qr + e);
-      s = __builtin_fmaf(x.x, q.x, s);
-      s = __builtin_fmaf(x.y, q.y, s);
-      s = __builtin_fmaf(x.z, q.z, s);
-      s = __builtin_fmaf(x.w, q.w, s);
+      s4[0] = __builtin_fmaf(x.x, q.x, s4[0]);
+      s4[1] = __builtin_fmaf(x.y, q.y, s4[1]);
+      s4[2] = __builtin_fmaf(x.z, q.z, s4[2]);
+      s4[3] = __builtin_fmaf(x.w, q.w, s4[3]);
     }
+    float s = (s4[0] + s4[1]) + (s4[2] + s4[3]);
     s = (s + xor32(s)) * c;
     if (key >= cnt) s = -INFINITY;
     const float m_new = fmaxf(m, wave_max_dpp(s));
@@ -776,7 +788,9 @@ __global__ void __launch_bounds__(kThreads) latent_vector_kernel(LatentAttn a) {
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
 #pragma unroll
     for (int e = 0; e < DL / kWave; ++e) acc[e] *= alpha;
-    for (int k = 0; k < cnt; ++k) {
+    // (a row past the last key is the last one again, of weight 0)
+#pragma unroll 8
+    for (int k = 0; k < kKeys; ++k) {
       const float pk = p_s[w][k];
 #pragma unroll
       for (int e = 0; e < DL / kWave; e += 4) {

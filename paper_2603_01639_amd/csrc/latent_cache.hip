@@ -5,7 +5,7 @@
 // A cache row holds one token's latent part (d_latent dims, the key and value
 // of every head) and its rotated part (d_rope dims, key alone).
 //
-// Append: a wave takes four rows of a sequence, whose loads all go out first.  A row's
+// Append: a wave takes two or four rows of a sequence, whose loads all go out first.  A row's
 // latent part lies across the wave, so that its mean square is a wave reduction
 // over registers; two angles a lane pass through LDS to the lanes that hold the
 // rotated parts.  A row is read and written once.  Bound: HBM, or the launch for a
@@ -34,11 +34,10 @@ struct Piece {  // 16 bytes
 };
 
 constexpr int kWaves = kThreads / kWave;
-constexpr int kRowsAtOnce = 4;
-constexpr int kGroupRows = kWaves * kRowsAtOnce;
 
-template <typename T, int DL>
+template <typename T, int DL, int kRowsAtOnce>
 __global__ void __launch_bounds__(kThreads) latent_append_kernel(LatentAppendArgs a) {
+  constexpr int kGroupRows = kWaves * kRowsAtOnce;
   constexpr int N = Piece<T>::N;
   constexpr int D = DL + kRopeDims;
   constexpr int kPieces = DL / N;                       // of the latent part
@@ -181,17 +180,31 @@ __global__ void __launch_bounds__(kThreads) latent_compact_kernel(LatentCompactA
 
 }  // namespace
 
-hipError_t launch_latent_append(const LatentAppendArgs& a, int d_latent, int dtype, hipStream_t stream) {
+namespace {
+
+template <typename T, int kRowsAtOnce>
+hipError_t launch_append(const LatentAppendArgs& a, int d_latent, hipStream_t stream) {
+  constexpr int kGroupRows = kWaves * kRowsAtOnce;
   const int64_t groups = static_cast<int64_t>(a.B) * ((a.Nmax + kGroupRows - 1) / kGroupRows);
   const dim3 grid(static_cast<unsigned>(groups < (1 << 20) ? groups : (1 << 20)));
-  if (dtype == LTD_DTYPE_F32) {
-    if (d_latent == 512) hipLaunchKernelGGL((latent_append_kernel<float, 512>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((latent_append_kernel<float, 256>), grid, dim3(kThreads), 0, stream, a);
-  } else {
-    if (d_latent == 512) hipLaunchKernelGGL((latent_append_kernel<__bf16, 512>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((latent_append_kernel<__bf16, 256>), grid, dim3(kThreads), 0, stream, a);
-  }
+  if (d_latent == 512) hipLaunchKernelGGL((latent_append_kernel<T, 512, kRowsAtOnce>), grid, dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((latent_append_kernel<T, 256, kRowsAtOnce>), grid, dim3(kThreads), 0, stream, a);
   return hipGetLastError();
+}
+
+// Rows a wave: two where that leaves fewer than eight waves a SIMD, which are not all
+// filled anyhow (60 rows 3.2 us, with four 4.0), four past that (16 prompts of 1024 to
+// 8192 rows 41.3 us, with two 42.8).
+template <typename T>
+hipError_t launch_append(const LatentAppendArgs& a, int d_latent, hipStream_t stream) {
+  if (static_cast<int64_t>(a.B) * a.Nmax < 16384) return launch_append<T, 2>(a, d_latent, stream);
+  return launch_append<T, 4>(a, d_latent, stream);
+}
+
+}  // namespace
+
+hipError_t launch_latent_append(const LatentAppendArgs& a, int d_latent, int dtype, hipStream_t stream) {
+  return dtype == LTD_DTYPE_F32 ? launch_append<float>(a, d_latent, stream) : launch_append<__bf16>(a, d_latent, stream);
 }
 
 hipError_t launch_latent_compact(const LatentCompactArgs& a, int B, int num_layers, hipStream_t stream) {
