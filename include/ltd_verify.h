@@ -585,7 +585,8 @@ int ltd_tree_accept_processed(const float* logits, const int32_t* draft_tokens,
  *                strides of its own, with whole rows, or all rows of a head, one after
  *                another (LTD_EINVAL otherwise: no two heads may share memory).
  *                q_out may be q, with the same strides (in place); other overlaps give
- *                undefined results.
+ *                undefined results (LTD_EINVAL where queries and keys begin at one
+ *                place and either is written there).
  *   k, k_out     the same with Hk heads, or Hk = 0 and NULL.
  *   inv_freq     [rot_dim / 2] float64: radians a position.
  *   depth        [B][Nmax] int32 >= 0 (as ltd_select_candidates writes it), or NULL
@@ -632,7 +633,8 @@ int ltd_tree_rope(const void* q, int64_t q_row_stride, int64_t q_head_stride, vo
  *
  *   kv_new       [B][Nmax][d_latent + d_rope] (dtype), row (b, i) at (b * Nmax + i) *
  *                new_row_stride (at least d_latent + d_rope: rows may be views into
- *                a fused projection's output); rows are 16-byte aligned.
+ *                a fused projection's output); rows are 16-byte aligned and lie
+ *                outside the cache (LTD_EINVAL).
  *   norm_weight  [d_latent] (dtype), 16-byte aligned, or NULL; norm_eps finite, >= 0.
  *   inv_freq     [d_rope / 2] float64; interleaved, mscale, depth and n_rows as for
  *                ltd_tree_rope.
@@ -669,7 +671,8 @@ int ltd_latent_append(const void* kv_new, int64_t new_row_stride, const void* no
  *                [Hq][B][Nmax][d_latent], as a product per head leaves it).
  *                With bfloat16 rows and heads are 16-byte aligned (LTD_EINVAL).
  *   out          [B][Nmax][Hq][d_latent] (dtype), 16-byte aligned; rows i >=
- *                n_nodes[b] are not written.
+ *                n_nodes[b] are not written.  It overlaps neither queries (LTD_EINVAL
+ *                where the two ranges of bytes meet) nor the cache.
  *   scale        finite and > 0 (that of the expanded heads, which the latent size
  *                does not tell).
  *   prefix_len, max_prefix, parents, n_nodes, block_table as for

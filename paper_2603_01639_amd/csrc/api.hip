@@ -572,6 +572,20 @@ bool heads_apart(int64_t rows, int64_t heads, int d, int64_t row, int64_t head) 
          (rows == 1 || heads == 1 || row >= static_cast<__int128>(heads - 1) * head + d ||
           head >= static_cast<__int128>(rows - 1) * row + d);
 }
+
+// The bytes from a tensor's first element to its last one's end: `rows` rows of `heads` runs
+// of d elements.
+struct Span {
+  __int128 from, to;
+};
+Span span_of(const void* p, int64_t rows, int64_t row, int64_t heads, int64_t head, int d, int elem) {
+  const __int128 base = static_cast<__int128>(reinterpret_cast<uintptr_t>(p));
+  const __int128 by_row = static_cast<__int128>(rows - 1) * row, by_head = static_cast<__int128>(heads - 1) * head;
+  const __int128 low = (by_row < 0 ? by_row : 0) + (by_head < 0 ? by_head : 0);
+  const __int128 high = (by_row > 0 ? by_row : 0) + (by_head > 0 ? by_head : 0) + d;
+  return {base + low * elem, base + high * elem};
+}
+bool meet(const Span& x, const Span& y) { return x.from < y.to && y.from < x.to; }
 }  // namespace
 
 int ltd_tree_rope(const void* q, int64_t q_row_stride, int64_t q_head_stride, void* q_out,
@@ -596,6 +610,8 @@ int ltd_tree_rope(const void* q, int64_t q_row_stride, int64_t q_head_stride, vo
     return LTD_EINVAL;
   if (Hk > 0 && k == k_out && (k_row_stride != k_out_row_stride || k_head_stride != k_out_head_stride))
     return LTD_EINVAL;
+  // (nor may queries and keys be exchanged, or written to one place)
+  if (Hk > 0 && (q_out == k_out || q_out == k || k_out == q)) return LTD_EINVAL;
   const int64_t rows = static_cast<int64_t>(B) * Nmax;
   if (!heads_apart(rows, Hq, d, q_out_row_stride, q_out_head_stride) ||
       (Hk > 0 && !heads_apart(rows, Hk, d, k_out_row_stride, k_out_head_stride)))
@@ -654,6 +670,10 @@ int ltd_latent_append(const void* kv_new, int64_t new_row_stride, const void* no
   if (!kv_new || !inv_freq || !cache || !prefix_len || !n_rows) return LTD_EINVAL;
   if (!aligned16(kv_new) || new_row_stride * (dtype == LTD_DTYPE_F32 ? 4 : 2) % 16 != 0 ||
       !aligned16(cache) || !aligned16(norm_weight))
+    return LTD_EINVAL;
+  const int D = d_latent + d_rope, elem = dtype == LTD_DTYPE_F32 ? 4 : 2;
+  if (meet(span_of(kv_new, static_cast<int64_t>(B) * Nmax, new_row_stride, 1, 0, D, elem),
+           span_of(cache, static_cast<int64_t>(block_table ? num_blocks : B) * kv_rows, D, 1, 0, D, elem)))
     return LTD_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (validate) {
@@ -716,6 +736,13 @@ int ltd_tree_verify_attn_latent(const void* q_latent, int64_t ql_row_stride,
   const int cus = device_cu_count();
   const size_t need = ltd::latent_attn_workspace_bytes(s, d_latent, dtype, cus);
   if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return LTD_EWORKSPACE;
+  // (several workgroups read a row's queries, at times when others have their outputs)
+  const int64_t rows = static_cast<int64_t>(B) * Nmax;
+  const int elem = dtype == LTD_DTYPE_F32 ? 4 : 2;
+  const Span to = span_of(out, rows, static_cast<int64_t>(Hq) * d_latent, Hq, d_latent, d_latent, elem);
+  if (meet(to, span_of(q_latent, rows, ql_row_stride, Hq, ql_head_stride, d_latent, elem)) ||
+      meet(to, span_of(q_rope, rows, qr_row_stride, Hq, qr_head_stride, d_rope, elem)))
+    return LTD_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (validate) {
     if (ltd::launch_validate_tree(block_table, prefix_len, parents, n_nodes, B, Nmax, max_prefix,

@@ -256,7 +256,8 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
       const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
       l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w0), ones, l_run, false);
       l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w1), ones, l_run, false);
-      const bf16x4 pf = __builtin_bit_cast(bf16x4, (static_cast<uint64_t>(w1) << 32) | w0);
+      bf16x4 pf = __builtin_bit_cast(bf16x4, (static_cast<uint64_t>(w1) << 32) | w0);
+      asm volatile("s_nop 1" : "+v"(pf));  // (a product reads what vector operations wrote two wait states later)
       if (bad != 0) {
 #pragma unroll 1
         for (int e = 0; e < kKeys * DL * 2 / 16 / kWave; ++e) {

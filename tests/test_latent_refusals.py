@@ -81,6 +81,34 @@ def test_compact(kw, code):
     assert compact(**kw) == code
 
 
+F = 1 << 20  # bytes that no case below reaches
+
+
+@pytest.mark.parametrize("kw", [
+    dict(qo=F, ko=F), dict(qo=X, q=F, k=X, ko=2 * F), dict(ko=X, q=X, qo=F, k=2 * F)])
+def test_rope_refuses_queries_and_keys_in_one_place(kw):
+    assert rope(**kw) == BAD
+
+
+# rows of 576 bfloat16 elements are 1152 bytes: 4 of them 4608; a cache of one sequence is 64 rows, 73728
+@pytest.mark.parametrize("kw", [
+    dict(x=F, cache=F), dict(x=F, cache=F + 4608 - 16), dict(x=F + 73728 - 16, cache=F),
+    dict(x=F + 73728 * 3 - 16, cache=F, table=X, mb=1, nb=3), dict(x=F, cache=F + 3 * 1152, stride=1152),
+    dict(x=F + 147456 - 16, cache=F, dtype=0)])
+def test_append_refuses_rows_of_the_cache(kw):
+    assert append(**kw) == BAD
+
+
+# four rows of 16 heads of 512 float32 elements are 131072 bytes, those of 64 dims 16384
+@pytest.mark.parametrize("kw", [
+    dict(ql=F, out=F), dict(ql=F, out=F + 131072 - 16), dict(ql=F + 131072 - 16, out=F),
+    dict(qr=F, out=F + 16384 - 16, ql=8 * F), dict(qr=F + 131072 - 16, out=F, ql=8 * F),
+    dict(ql=F, qlr=512, qlh=4 * 512, out=F + 65536), dict(ql=F, qlr=0, qlh=0, out=F + 2048 - 16),
+    dict(ql=F, qlr=-8192, out=F - 3 * 32768)])
+def test_attention_refuses_outputs_over_its_queries(kw):
+    assert attn(**kw) == BAD
+
+
 def test_workspace_query():
     size = ltd.attn_latent_workspace_size
     assert size(1, 60, 16, 384, 64, 2048, ltd.DTYPE_BF16) == 0
