@@ -14,6 +14,8 @@
 // then passes through LDS once, and a tile's rows are read 1.9 times a wave
 // row less than if a wave kept its 32 rows over all dims, which would need every
 // byte that LDS can give during the products' time.
+#include <algorithm>
+
 #include "latent_attn.hpp"
 #include "tree_walk.hpp"
 
@@ -636,62 +638,120 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
   }
 }
 
-// Joins the pieces of the cut unit that begins in workgroup x's share, a wave a row, 16
-// pieces at a time: lane 16 g + p takes piece p's maximum and sum for the weights, with the
-// factor of quarter g of its dims, then each lane its dims of every piece.
-template <int DL>
+// Joins the pieces of cut unit blockIdx.x (in the order of the shares that they begin in), a
+// wave a row, kBatch pieces at a time: lane 16 g + p takes piece p's maximum and sum for the
+// weights, with the factor of quarter g of its dims, then each lane its dims of every piece.
+// The pieces are asked for before their weights are known, and with kAhead those of the
+// next batch before the last one's are summed up.
+//
+// Bound: the pieces' bytes where there are many rows (256 workgroups' 33 MB in about 10 us),
+// one row's chain of loads where there are few.  (With a workgroup per share that looked
+// up whether a cut begins there, and pieces' loads behind their weights, one token of 128
+// heads over 4096 keys took 28.3 us a call instead of 27.4, 8 nodes over 2048 keys 32.4
+// instead of 31.4.)
+template <int DL, int kBatch, bool kAhead>
 __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
   constexpr int kEach = DL / kWave;  // dims a lane: lanes 16 g .. have quarter g
-  constexpr int kBatch = 16;
+  constexpr int kGroup = 4;          // pieces whose loads go out together
+  static_assert(kBatch % kGroup == 0 && kBatch <= 16, "a batch's pieces lie across 16 lanes");
   typedef _Float16 Dims __attribute__((ext_vector_type(DL / kWave)));
   const LatentAttn& in = a.in;
   if (halted(in.status)) return;
   const int lane = threadIdx.x % kWave;
-  const int x = blockIdx.x;
-  const CutUnit cut = a.ws_cut[x];
-  const int row = blockIdx.y * kWaves + threadIdx.x / kWave;
-  if (row >= cut.valid) return;
+  // ---- which share the cut unit begins in
+  int x = -1;
+  CutUnit cut{};
+  int rank = blockIdx.x;  // among the cuts from share `base` on
+  for (int base = 0; base < a.W && x < 0; base += 4 * kWave) {
+    CutUnit c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = a.ws_cut[min(base + i * kWave + lane, a.W - 1)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint64_t cuts = __ballot(base + i * kWave + lane < a.W && c[i].valid > 0);
+      const int below = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(cuts >> 32),
+                                                  __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(cuts), 0));
+      const uint64_t hit = __ballot((cuts >> lane & 1) != 0 && below == rank);
+      if (x < 0 && hit != 0) {
+        const int l = __ffsll(static_cast<long long>(hit)) - 1;
+        x = base + i * kWave + l;
+        cut = CutUnit{__builtin_amdgcn_readlane(c[i].b, l), __builtin_amdgcn_readlane(c[i].r0, l),
+                      __builtin_amdgcn_readlane(c[i].valid, l), __builtin_amdgcn_readlane(c[i].last, l)};
+      }
+      rank -= __popcll(cuts);
+    }
+  }
+  const int row = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  if (x < 0 || row >= cut.valid) return;
   const int pieces = cut.last - x + 1;
   // (the first piece begins in share x, the others go on in the next ones)
   auto slot = [&](int p) { return static_cast<int64_t>(p == 0 ? 2 * x + 1 : 2 * (x + p)) * kRows + row; };
+  struct Batch {
+    float m, l, factor;
+    Dims d[kBatch];
+  };
+  auto fetch = [&](Batch& t, int p0) {
+    const int count = min(kBatch, pieces - p0);
+    t.m = kNoMax;
+    t.l = t.factor = 0.f;
+    if (lane % 16 < count) {
+      const int64_t s = slot(p0 + lane % 16);
+      const PieceRow r = a.ws_row[s];
+      t.m = r.m;
+      t.l = r.l;
+      t.factor = a.ws_factor[s * 4 + lane / 16];
+    }
+#pragma unroll
+    for (int g = 0; g < kBatch; g += kGroup)
+      if (g < count) {
+#pragma unroll
+        for (int u = g; u < g + kGroup; ++u)
+          t.d[u] = *reinterpret_cast<const Dims*>(a.ws_o + slot(p0 + min(u, count - 1)) * DL + lane * kEach);
+      }
+  };
   float M = kNoMax, L = 0.f;
   float acc[kEach];
 #pragma unroll
   for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
-  for (int p0 = 0; p0 < pieces; p0 += kBatch) {
+  auto add = [&](const Batch& t, int p0) {
     const int count = min(kBatch, pieces - p0);
-    float m = kNoMax, l = 0.f, factor = 0.f;
-    if (lane % kBatch < count) {
-      const int64_t s = slot(p0 + lane % kBatch);
-      const PieceRow& r = a.ws_row[s];
-      l = r.l;
-      factor = a.ws_factor[s * 4 + lane / kBatch];
-      if (l != 0.f) m = r.m;
-    }
+    const float m = t.l != 0.f ? t.m : kNoMax;
     const float m_new = fmaxf(M, row_reduce(m, [](float u, float v) { return fmaxf(u, v); }));
-    const float old = exp2_fast(M - m_new), w = l != 0.f ? exp2_fast(m - m_new) * l : 0.f;
+    const float old = exp2_fast(M - m_new), w = t.l != 0.f ? exp2_fast(m - m_new) * t.l : 0.f;
     L = L * old + row_reduce(w, [](float u, float v) { return u + v; });
     M = m_new;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) acc[e] *= old;
-    const float wf = w != 0.f ? w * factor : 0.f;
-    constexpr int kUnroll = 8;
-    for (int p = 0; p < count; p += kUnroll) {
-      Dims d[kUnroll];
+    const float wf = w != 0.f ? w * t.factor : 0.f;
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int64_t s = slot(p0 + min(p + u, count - 1));
-        d[u] = *reinterpret_cast<const Dims*>(a.ws_o + s * DL + lane * kEach);
-      }
+    for (int g = 0; g < kBatch; g += kGroup)
+      if (g < count) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const float wu = p + u < count ? __shfl(wf, p + u, kBatch) : 0.f;
-        // (a piece of weight 0 has no rows to be read: it may hold anything)
-        if (wu != 0.f) {
+        for (int u = g; u < g + kGroup; ++u) {
+          const float wu = u < count ? __shfl(wf, u, 16) : 0.f;
+          // (a piece of weight 0 has no rows to be read: it may hold anything)
+          if (wu != 0.f) {
 #pragma unroll
-          for (int e = 0; e < kEach; ++e) acc[e] = __builtin_fmaf(wu, static_cast<float>(d[u][e]), acc[e]);
+            for (int e = 0; e < kEach; ++e) acc[e] = __builtin_fmaf(wu, static_cast<float>(t.d[u][e]), acc[e]);
+          }
         }
       }
+  };
+  Batch t0, t1;
+  fetch(t0, 0);
+  for (int p = 0; p < pieces; p += 2 * kBatch) {
+    if constexpr (kAhead) {
+      if (p + kBatch < pieces) fetch(t1, p + kBatch);
+      add(t0, p);
+      if (p + 2 * kBatch < pieces) fetch(t0, p + 2 * kBatch);
+      if (p + kBatch < pieces) add(t1, p + kBatch);
+    } else {
+      add(t0, p);
+      if (p + kBatch < pieces) {
+        fetch(t0, p + kBatch);
+        add(t0, p + kBatch);
+      }
+      if (p + 2 * kBatch < pieces) fetch(t0, p + 2 * kBatch);
     }
   }
   const float inv = 1.f / L;
@@ -828,8 +888,14 @@ hipError_t launch_bf16(const LatentArgs& a, hipStream_t stream) {
     rc = hipGetLastError();
   }
   if (rc != hipSuccess || a.W < 2) return rc;
-  const int rows = few ? latent::kFew.rows : kRows;
-  hipLaunchKernelGGL((latent_merge_kernel<DL>), dim3(a.W - 1, rows / kWaves), dim3(kThreads), 0, stream, a);
+  // At most so many units are cut.  Where that leaves a unit 16 pieces or more, a wave has 32
+  // of a row's on the way; where there are more units, and rows, more waves fit a compute
+  // unit (64 units of 128 rows 68.2 us a call, 71.7 the other way).
+  const latent::Cut cut = few ? latent::kFew : latent::kMany;
+  const int64_t units = a.in.B * latent::units_of(a.in.Nmax, a.in.Hq, cut);
+  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(a.W - 1, units)), cut.rows / kWaves);
+  if (a.W >= 16 * units) hipLaunchKernelGGL((latent_merge_kernel<DL, 16, true>), grid, dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((latent_merge_kernel<DL, 8, false>), grid, dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

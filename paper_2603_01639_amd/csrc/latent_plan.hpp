@@ -16,12 +16,19 @@ constexpr int kKeyTile = 32;
 constexpr int kRows = 128;    // stacked rows of a unit ...
 constexpr int kFewRows = 16;  // ... and the most of a call that takes the kernel for few rows
 // How a kernel's calls are cut: rows of a unit, what a unit costs beside its tiles (in
-// tiles), and the shortest share.
+// tiles: the workgroup that begins one behind another's last piece loads queries, and
+// stores a piece, twice), and the shortest share.  A share may lie within a unit's own
+// cost and has nothing to do then.  (With a cost of 6 and shares of 10, 4 and 8 for few
+// rows, the workgroups with two units' pieces ended last, 52 us after the launch where
+// the others took 43: 60 nodes of 16 heads over 16384 keys 62.4 us a call, 58.5 so, over 2041
+// keys 40.0 and 35.0, 8 nodes of 128 heads over 2048 keys 37.2 and 31.0, one token of 16
+// sequences of 16 heads over 1024 to 8192 keys 37.2 and 33.9, over 500 to 1500 29.4 and 22.7.
+// Shares of 3, or costs of 16 and 20, changed nothing beyond 2%.)
 struct Cut {
   int rows, cost, min_share;
 };
-constexpr Cut kMany{kRows, 6, 10};
-constexpr Cut kFew{kFewRows, 4, 8};
+constexpr Cut kMany{kRows, 12, 4};
+constexpr Cut kFew{kFewRows, 8, 4};
 // Calls of up to 16 stacked rows a sequence (one token of a few heads) have a kernel of
 // their own.
 constexpr Cut cut_of(int64_t Nmax, int64_t heads) {
@@ -62,6 +69,8 @@ constexpr RowDivisor row_divisor(int kv_rows) {
 constexpr int workgroups(int64_t B, int64_t Nmax, int64_t heads, int64_t max_prefix, int cus) {
   const Cut c = cut_of(Nmax, heads);
   if (B >= static_cast<int64_t>(cus) * c.min_share) return cus;  // (the product below could pass 2^63)
+  // (one unit that is too short for two shares needs no merge)
+  if (B * units_of(Nmax, heads, c) == 1 && tiles_of(max_prefix, Nmax) <= c.min_share) return 1;
   const int64_t total = B * length_of(max_prefix, Nmax, heads, c);
   const int64_t most = (total + c.min_share - 1) / c.min_share;
   return static_cast<int>(most < cus ? most : cus);
