@@ -15,8 +15,9 @@
 // the merge, in a graph: one token of a sequence over 1000 keys 19 us, 19; of 16
 // sequences 22, 22; of 16 over 1024 to 8192 keys 34, 38; of 16 over 8192 keys 48, 54; of 128
 // over 2048 keys 78, 100.  With 32 rows, in two units that each read the cache, 16
-// sequences over 8192 keys took 58 us, 48 there, hence the rule.  16 sequences over 1024 to 8192 keys (85 MB) take 28 us before the merge, half
-// of it the stream at 6 TB/s, the rest the search, the first loads and the join.
+// sequences over 8192 keys took 58 us where the other kernel took 48, hence the rule.
+// 16 sequences over 1024 to 8192 keys (85 MB) take 26 to 28 us before the merge, half of it the
+// stream at 6 TB/s, the rest the search, the first loads and the join.
 #include "latent_attn.hpp"
 
 namespace ltd {
