@@ -304,3 +304,22 @@ def test_dims_of_different_sizes(DL, H, sizes):
     m["q"][..., :DL] = (m["q"][..., :DL].double() / by_dim / by_seq[:, None, None, None]).bfloat16()
     m.update(ql=m["q"][..., :DL], qr=m["q"][..., DL:], layout="rows")
     check(m, run(m))
+
+
+@pytest.mark.parametrize("H, n", [(16, 1), (128, 1), (16, 12)])
+@pytest.mark.parametrize("others", [1, 17, 40])
+def test_one_long_sequence_among_short_ones(others, H, n):
+    """Rows that many workgroups have pieces of, beside rows of one: up to a hundred pieces are joined."""
+    prefix = [40, 12000] + [int(p) for p in np.random.default_rng(others).choice([0, 3, 31, 64, 90], size=others)]
+    m = make(others + H, H, 512, prefix, [n] * len(prefix), 16)
+    check(m, run(m), label=f"{H} heads, {n} nodes, {others} others")
+
+
+@pytest.mark.parametrize("DL", [256, 512])
+@pytest.mark.parametrize("H", [16, 20])
+def test_prefixes_around_the_shortest_share(DL, H):
+    """Shares that lie within a unit's own cost, end with it, or have one tile."""
+    for tiles in (1, 2, 3, 4, 5, 8, 9, 12, 13, 16, 17, 20):
+        for prefix in ([32 * tiles - 1], [32 * tiles], [32 * tiles - 1, 32 * tiles + 100, 5]):
+            m = make(tiles + H, H, DL, prefix, [1] * len(prefix), 0)
+            check(m, run(m), label=f"{H} heads over {prefix}")
