@@ -169,7 +169,9 @@ __device__ __forceinline__ Place find_place(const LatentAttn& a, const latent::C
 // p.  (The instruction's offset moves its place in LDS as well, so that is taken back.)
 template <int kOff>
 __device__ __forceinline__ void dma16_at(uint32_t lds, const void* p) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off offset:%2" ::"s"(lds - kOff), "v"(p), "n"(kOff) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off offset:%2"
+               ::"s"(lds - kOff), "v"(p), "n"(kOff)
+               : "memory");
 }
 
 // A row's block.

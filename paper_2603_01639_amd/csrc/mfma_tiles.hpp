@@ -84,7 +84,9 @@ __device__ __forceinline__ void wait_vmcnt() {
 // vector-memory wait in front of every later LDS read (which would drain the
 // prefetch ring every tile).  The kernel waits for them itself (wait_vmcnt)
 // and orders them across waves with bare barriers.  Nothing else in these
-// kernels uses M0.
+// kernels uses M0.  A load that takes its place in LDS from M0 comes one wait state
+// after the write (s_nop 0), which nobody else sees to inside the assembly: without it
+// the load may take the last place.
 __device__ __forceinline__ uint32_t lds_addr(const void* p) {
   return __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(as_lds(p))));
 }
@@ -97,22 +99,22 @@ __device__ __forceinline__ const void* scalar_ptr(const void* p) {
   return reinterpret_cast<const void*>((static_cast<uint64_t>(hi) << 32) | lo);
 }
 __device__ __forceinline__ void dma16(uint32_t lds, const void* uniform_base, uint32_t lane_off) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                ::"s"(lds), "v"(lane_off), "s"(scalar_ptr(uniform_base))
                : "memory");
 }
 __device__ __forceinline__ void dma16(uint32_t lds, const void* lane_ptr) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(lane_ptr)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(lane_ptr)
                : "memory");
 }
 // Direct global->LDS load of a byte per lane (lane i's byte lands as a word at M0 + 4*i).
 __device__ __forceinline__ void dma1(uint32_t lds, const void* lane_ptr) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_ubyte %1, off" ::"s"(lds), "v"(lane_ptr)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, off" ::"s"(lds), "v"(lane_ptr)
                : "memory");
 }
 // Direct global->LDS load of 4 bytes per lane (lane i's word lands at M0 + 4*i).
 __device__ __forceinline__ void dma4(uint32_t lds, const void* lane_ptr) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(lane_ptr)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(lane_ptr)
                : "memory");
 }
 // Workgroup barrier without the memory fence __syncthreads() adds (that fence
