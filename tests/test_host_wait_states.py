@@ -81,3 +81,40 @@ def test_direct_loads(library):
 def test_scalar_bases(library):
     """A memory instruction reads scalar registers that a vector instruction wrote five wait states before or earlier."""
     assert found_in(library, W.scalar_base) == []
+
+
+BIG, SMALL = "v_mfma_f32_32x32x16_bf16 v[0:15], v[20:23], v[24:27], v[0:15]", "v_mfma_f32_16x16x32_bf16 v[0:3], v[20:23], v[24:27], 0"
+AGPR = "v_mfma_f32_32x32x16_bf16 a[0:15], v[20:23], v[24:27], a[0:15]"
+OTHER = "v_mfma_f32_32x32x16_bf16 a[16:31], v[20:23], v[24:27], a[16:31]"
+
+
+@pytest.mark.parametrize("lines, hits", [
+    ((BIG, "s_nop 10", "v_add_f32_e32 v30, v3, v4"), 1), ((BIG, "s_nop 11", "v_add_f32_e32 v30, v3, v4"), 0),
+    ((SMALL, "s_nop 6", "v_add_f32_e32 v30, v3, v4"), 1), ((SMALL, "s_nop 7", "v_add_f32_e32 v30, v3, v4"), 0),
+    ((BIG, "v_mov_b32_e32 v15, 0"), 1), ((BIG, "ds_write_b128 v30, v[12:15]"), 1), ((BIG, "v_add_f32_e32 v30, v16, v17"), 0),
+    ((BIG, BIG), 0), ((SMALL, SMALL), 0), ((AGPR, OTHER), 0), ((AGPR, "v_accvgpr_read_b32 v30, a7"), 1),
+    ((BIG, "v_mfma_f32_32x32x16_bf16 a[0:15], v[4:7], v[24:27], a[0:15]"), 1),
+    ((BIG, "v_mfma_f32_16x16x32_bf16 v[0:3], v[20:23], v[24:27], v[0:3]"), 1),
+    ((AGPR, OTHER, OTHER, OTHER, "s_nop 3", "v_accvgpr_read_b32 v30, a7"), 1),
+    (("loop:", "v_add_f32_e32 v30, v3, v4", "s_nop 7", BIG, "s_cbranch_scc1 loop", "s_endpgm"), 1)])
+def test_reader_of_sums(lines, hits):
+    assert len(list(W.sums(code(*lines)))) == hits
+
+
+@pytest.mark.parametrize("lines, hits", [
+    (("v_mov_b32_e32 v20, 0", BIG), 1), (("v_mov_b32_e32 v20, 0", "s_nop 0", BIG), 1), (("v_mov_b32_e32 v20, 0", "s_nop 1", BIG), 0),
+    (("v_mov_b32_e32 v30, 0", BIG), 0), (("v_mov_b32_e32 v0, 0", BIG), 1), (("v_accvgpr_write_b32 a3, v9", AGPR), 1),
+    (("ds_read_b128 v[20:23], v40", BIG), 0), (("v_dot2c_f32_bf16_e32 v20, v30, v31", BIG), 0)])
+def test_reader_of_factors(lines, hits):
+    assert len(list(W.factors(code(*lines)))) == hits
+
+
+def test_sums_of_products(library):
+    """A matrix product's sums are there when something else than a product that adds to them touches them: the kernels over a
+    latent cache write their products in assembly, where the compiler keeps no distance by itself."""
+    assert found_in(library, W.sums) == []
+
+
+def test_factors_of_products(library):
+    """A matrix product reads what a vector instruction wrote two wait states before or earlier."""
+    assert found_in(library, W.factors) == []

@@ -147,3 +147,34 @@ def scalar_base(code):
             for j, states in after(code, at, 5):
                 if j.memory and j.reads & written:
                     yield i, j, states
+
+
+# Passes of the matrix products in use.  What reads or writes a product's sums, but a product that adds to the same ones,
+# comes passes + 4 wait states later; so does a product that takes them as factors.  (What hipcc keeps for its own products
+# on gfx950: 12 behind one of 8 passes, 8 behind one of 4.)
+PASSES = {"v_mfma_f32_32x32x16_bf16": 8, "v_mfma_f32_16x16x32_bf16": 4, "v_mfma_f32_16x16x16_bf16": 4}
+
+
+def sums(code):
+    """What touches a product's sums before they are there."""
+    for at, i in enumerate(code):
+        if not i.mfma:
+            continue
+        need = PASSES[i.name] + 4
+        for j, states in after(code, at, need):
+            if j.mfma:
+                same = i.writes == j.writes and (j.operands[3] == i.writes or not j.operands[3])
+                if (j.operands[1] | j.operands[2]) & i.writes or (not same and (j.operands[3] | j.writes) & i.writes):
+                    yield i, j, states
+            elif (j.reads | j.writes) & i.writes:
+                yield i, j, states
+
+
+def factors(code):
+    """A product that reads what a vector instruction (but a dot product) wrote: two wait states."""
+    for at, i in enumerate(code):
+        written = {r for r in i.writes if r[0] in "va"} if i.valu and not i.name.startswith("v_dot") else ()
+        if written:
+            for j, states in after(code, at, 2):
+                if j.mfma and j.reads & written:
+                    yield i, j, states
