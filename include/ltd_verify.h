@@ -661,8 +661,7 @@ int ltd_latent_append(const void* kv_new, int64_t new_row_stride, const void* no
  * node i, i included}.  Statistics and accumulation are float32; with bfloat16 the
  * weights are rounded to bfloat16 before they multiply the values, and the sum that
  * normalises them is that of the rounded ones; partial results of a row that the call
- * splits over its keys are float16 relative to the largest of their quarter of the
- * dims (what is 2^28 times smaller loses bits).  Latent values may be as large as 2^80:
+ * splits over its keys are float32.  Latent values may be as large as 2^80:
  * weights of up to 2^16 multiply them before the sum divides.
  *
  *   q_latent     rows of Hq heads of d_latent elements, q_rope of d_rope elements

@@ -576,19 +576,16 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     settle_all();
 
     // ---- results, 32 rows at a time: O / l of a whole unit to `out`, as a piece to the
-    // workspace.  (256 workgroups' pieces are 33 MB, which bound this part.)  The sums
+    // workspace.  (256 workgroups' pieces are 67 MB, which bound this part.)  The sums
     // pass through LDS, in the stages that no wave reads any more (two waves in each), so
     // that a row's dims of a wave go out in one run and the code is that of one row.
     constexpr int kPitch = kCols * 4 + 16;
     unsigned char* stage = sm.kv[(t1 - t0 + (wave >> 1)) % kStages] + (wave & 1) * 32 * kPitch;
     static_assert(2 * 32 * kPitch <= kTileBytes, "rows of two waves fit a tile");
     {
-      uint16_t* out = (whole ? static_cast<uint16_t*>(in.out) + (static_cast<int64_t>(b) * in.Nmax * in.Hq + r0) * DL
-                             : a.ws_o + static_cast<int64_t>(slot) * kRows * DL) + wave * kCols;
       asm volatile("" : "+v"(l32), "+v"(h));
       const int to_lane = rare(lane);
       constexpr int kLanes = kCols / 8;  // of a row
-      const int col = to_lane % kLanes * 8;
       const auto put = [&](auto g) {
         f32x4* to = reinterpret_cast<f32x4*>(stage + l32 * kPitch + 16 * h);
 #pragma unroll
@@ -607,30 +604,25 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
         else put(std::integral_constant<int, 3>{});
         // (a lane's rows side by side: one after another they wait for themselves)
         constexpr int kEach = 32 * kLanes / kWave, kStep = kWave / kLanes;  // rows a lane, and to the next
-        const int first = to_lane / kLanes;
-        uint16_t* to = out + static_cast<int64_t>(r + first) * DL + col;
-        const auto row = [&](int i, auto pack) {
-          const f32x4* from = reinterpret_cast<const f32x4*>(stage + (first + i * kStep) * kPitch + col * 4);
-          return pack(from[0], from[1], sm.row_f[r + first + i * kStep]);
+        const int first = to_lane / kLanes, piece = to_lane % kLanes;
+        const auto sums = [&](int i, int col) {  // dims 4 col .. of the i-th row
+          return *reinterpret_cast<const f32x4*>(stage + (first + i * kStep) * kPitch + col * 16) * sm.row_f[r + first + i * kStep];
         };
         if (whole) {
+          uint16_t* to = static_cast<uint16_t*>(in.out) +
+                         (static_cast<int64_t>(b) * in.Nmax * in.Hq + r0 + r + first) * DL + wave * kCols + piece * 8;
           for_each_index<kEach>([&](auto i) {
-            const u32x4 x = row(i(), [](f32x4 x0, f32x4 x1, float f) {
-              return u32x4{pack_bf16x2(x0[0] * f, x0[1] * f), pack_bf16x2(x0[2] * f, x0[3] * f),
-                           pack_bf16x2(x1[0] * f, x1[1] * f), pack_bf16x2(x1[2] * f, x1[3] * f)};
-            });
-            if (r + first + i() * kStep < valid) *reinterpret_cast<u32x4*>(to + i() * kStep * DL) = x;
+            const f32x4 x0 = sums(i(), 2 * piece), x1 = sums(i(), 2 * piece + 1);
+            if (r + first + i() * kStep < valid)
+              *reinterpret_cast<u32x4*>(to + i() * kStep * DL) =
+                  u32x4{pack_bf16x2(x0[0], x0[1]), pack_bf16x2(x0[2], x0[3]), pack_bf16x2(x1[0], x1[1]), pack_bf16x2(x1[2], x1[3])};
           });
         } else {  // (a slot has room for all 128 rows)
-          float mine = 0.f;  // lane i of a row's first ones: the factor of the i-th row
+          float* to = a.ws_o + (static_cast<int64_t>(slot) * kRows + r + first) * DL + wave * kCols + piece * 4;
           for_each_index<kEach>([&](auto i) {
-            float factor;
-            const u32x4 x = row(i(), [&](f32x4 x0, f32x4 x1, float f) { return pack_piece<DL>(x0, x1, f, &factor); });
-            *reinterpret_cast<u32x4*>(to + i() * kStep * DL) = x;
-            mine = to_lane % kLanes == i() ? factor : mine;
+            *reinterpret_cast<f32x4*>(to + i() * kStep * DL) = sums(i(), piece);
+            *reinterpret_cast<f32x4*>(to + i() * kStep * DL + kCols / 2) = sums(i(), kLanes + piece);
           });
-          if (to_lane % kLanes < kEach)
-            a.ws_factor[(static_cast<int64_t>(slot) * kRows + r + first + to_lane % kLanes * kStep) * 4 + wave] = mine;
         }
       }
     }
@@ -640,21 +632,19 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
 
 // Joins the pieces of cut unit blockIdx.x (in the order of the shares that they begin in), a
 // wave a row, kBatch pieces at a time: lane 16 g + p takes piece p's maximum and sum for the
-// weights, with the factor of quarter g of its dims, then each lane its dims of every piece.
-// The pieces are asked for before their weights are known, and with kAhead those of the
-// next batch before the last one's are summed up.
+// weights, then each lane its dims of every piece.  The pieces are asked for before their
+// weights are known, and with kAhead those of the next batch before the last one's are
+// summed up.
 //
-// Bound: the pieces' bytes where there are many rows (256 workgroups' 33 MB in about 10 us),
+// Bound: the pieces' bytes where there are many rows (256 workgroups' 67 MB),
 // one row's chain of loads where there are few.  (With a workgroup per share that looked
 // up whether a cut begins there, and pieces' loads behind their weights, one token of 128
-// heads over 4096 keys took 28.3 us a call instead of 27.4, 8 nodes over 2048 keys 32.4
-// instead of 31.4.)
+// heads over 4096 keys took 1 us more.)
 template <int DL, int kBatch, bool kAhead>
 __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
-  constexpr int kEach = DL / kWave;  // dims a lane: lanes 16 g .. have quarter g
-  constexpr int kGroup = 4;          // pieces whose loads go out together
+  constexpr int kRuns = DL / (4 * kWave);  // of 4 dims a lane, 256 dims apart
+  constexpr int kGroup = 4;                // pieces whose loads go out together
   static_assert(kBatch % kGroup == 0 && kBatch <= 16, "a batch's pieces lie across 16 lanes");
-  typedef _Float16 Dims __attribute__((ext_vector_type(DL / kWave)));
   const LatentAttn& in = a.in;
   if (halted(in.status)) return;
   const int lane = threadIdx.x % kWave;
@@ -687,32 +677,32 @@ __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
   // (the first piece begins in share x, the others go on in the next ones)
   auto slot = [&](int p) { return static_cast<int64_t>(p == 0 ? 2 * x + 1 : 2 * (x + p)) * kRows + row; };
   struct Batch {
-    float m, l, factor;
-    Dims d[kBatch];
+    float m, l;
+    f32x4 d[kBatch][kRuns];
   };
   auto fetch = [&](Batch& t, int p0) {
     const int count = min(kBatch, pieces - p0);
     t.m = kNoMax;
-    t.l = t.factor = 0.f;
+    t.l = 0.f;
     if (lane % 16 < count) {
-      const int64_t s = slot(p0 + lane % 16);
-      const PieceRow r = a.ws_row[s];
+      const PieceRow r = a.ws_row[slot(p0 + lane % 16)];
       t.m = r.m;
       t.l = r.l;
-      t.factor = a.ws_factor[s * 4 + lane / 16];
     }
 #pragma unroll
     for (int g = 0; g < kBatch; g += kGroup)
       if (g < count) {
 #pragma unroll
         for (int u = g; u < g + kGroup; ++u)
-          t.d[u] = *reinterpret_cast<const Dims*>(a.ws_o + slot(p0 + min(u, count - 1)) * DL + lane * kEach);
+#pragma unroll
+          for (int i = 0; i < kRuns; ++i)
+            t.d[u][i] = reinterpret_cast<const f32x4*>(a.ws_o + slot(p0 + min(u, count - 1)) * DL)[i * kWave + lane];
       }
   };
   float M = kNoMax, L = 0.f;
-  float acc[kEach];
+  f32x4 acc[kRuns];
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
+  for (int i = 0; i < kRuns; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   auto add = [&](const Batch& t, int p0) {
     const int count = min(kBatch, pieces - p0);
     const float m = t.l != 0.f ? t.m : kNoMax;
@@ -721,18 +711,19 @@ __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
     L = L * old + row_reduce(w, [](float u, float v) { return u + v; });
     M = m_new;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) acc[e] *= old;
-    const float wf = w != 0.f ? w * t.factor : 0.f;
+    for (int i = 0; i < kRuns; ++i) acc[i] *= old;
 #pragma unroll
     for (int g = 0; g < kBatch; g += kGroup)
       if (g < count) {
 #pragma unroll
         for (int u = g; u < g + kGroup; ++u) {
-          const float wu = u < count ? __shfl(wf, u, 16) : 0.f;
+          const float wu = u < count ? __shfl(w, u, 16) : 0.f;
           // (a piece of weight 0 has no rows to be read: it may hold anything)
           if (wu != 0.f) {
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) acc[e] = __builtin_fmaf(wu, static_cast<float>(t.d[u][e]), acc[e]);
+            for (int i = 0; i < kRuns; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[i][e] = __builtin_fmaf(wu, t.d[u][i][e], acc[i][e]);
           }
         }
       }
@@ -755,13 +746,11 @@ __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
     }
   }
   const float inv = 1.f / L;
-  uint16_t* out = static_cast<uint16_t*>(in.out) +
-                  (static_cast<int64_t>(cut.b) * in.Nmax * in.Hq + cut.r0 + row) * DL + lane * kEach;
-  uint32_t w[kEach / 2];
+  uint16_t* out = static_cast<uint16_t*>(in.out) + (static_cast<int64_t>(cut.b) * in.Nmax * in.Hq + cut.r0 + row) * DL;
 #pragma unroll
-  for (int e = 0; e < kEach / 2; ++e) w[e] = pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-#pragma unroll
-  for (int e = 0; e < kEach / 2; ++e) reinterpret_cast<uint32_t*>(out)[e] = w[e];
+  for (int i = 0; i < kRuns; ++i)
+    reinterpret_cast<uint2*>(out)[i * kWave + lane] =
+        make_uint2(pack_bf16x2(acc[i][0] * inv, acc[i][1] * inv), pack_bf16x2(acc[i][2] * inv, acc[i][3] * inv));
 }
 
 // The float32 path, on the vector ALUs: a workgroup per (sequence, node, four
@@ -894,7 +883,7 @@ hipError_t launch_bf16(const LatentArgs& a, hipStream_t stream) {
   const latent::Cut cut = few ? latent::kFew : latent::kMany;
   const int64_t units = a.in.B * latent::units_of(a.in.Nmax, a.in.Hq, cut);
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>(a.W - 1, units)), cut.rows / kWaves);
-  if (a.W >= 16 * units) hipLaunchKernelGGL((latent_merge_kernel<DL, 16, true>), grid, dim3(kThreads), 0, stream, a);
+  if (a.W >= 16 * units) hipLaunchKernelGGL((latent_merge_kernel<DL, 8, true>), grid, dim3(kThreads), 0, stream, a);
   else hipLaunchKernelGGL((latent_merge_kernel<DL, 8, false>), grid, dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
@@ -904,7 +893,7 @@ hipError_t launch_bf16(const LatentArgs& a, hipStream_t stream) {
 size_t latent_attn_workspace_bytes(const LatentAttn& s, int d_latent, int dtype, int cus) {
   if (dtype == LTD_DTYPE_F32 || s.B == 0) return 0;
   const size_t W = grid_of(s, cus);
-  return 2 * W * kRows * (d_latent * sizeof(uint16_t) + 4 * sizeof(float) + sizeof(PieceRow)) + W * sizeof(CutUnit);
+  return 2 * W * kRows * (d_latent * sizeof(float) + sizeof(PieceRow)) + W * sizeof(CutUnit);
 }
 
 hipError_t launch_latent_attn(const LatentAttn& s, int d_latent, int dtype, void* workspace, int cus,
@@ -918,9 +907,8 @@ hipError_t launch_latent_attn(const LatentAttn& s, int d_latent, int dtype, void
   LatentArgs a{};
   a.in = s;
   a.W = grid_of(s, cus);
-  a.ws_o = static_cast<uint16_t*>(workspace);
-  a.ws_factor = reinterpret_cast<float*>(a.ws_o + static_cast<int64_t>(2) * a.W * kRows * d_latent);
-  a.ws_cut = reinterpret_cast<CutUnit*>(a.ws_factor + static_cast<int64_t>(2) * a.W * kRows * 4);
+  a.ws_o = static_cast<float*>(workspace);
+  a.ws_cut = reinterpret_cast<CutUnit*>(a.ws_o + static_cast<int64_t>(2) * a.W * kRows * d_latent);
   a.ws_row = reinterpret_cast<PieceRow*>(a.ws_cut + a.W);
   a.scale_log2 = s.scale * kLog2e;
   a.lazy_gap = kLazyMax / a.scale_log2;

@@ -25,11 +25,11 @@ constexpr int kAncWords = LTD_MAX_NODES / 32;  // 256 bits a node
 constexpr float kLazyMax = 16.f;
 constexpr float kNoMax = -__FLT_MAX__;
 
-// A piece's row beside its O / l: the maximum (log2 units) and the sum.  O / l is held in
-// float16, each quarter of the dims under a power of two of its own (factor): in bfloat16
-// the pieces' rounding was as large as the output's (root mean square error 0.0025 of the
-// output; so 0.0020, and 0.0017 for rounding the output alone), and in float32 it would be
-// twice the bytes.  128 heads' decoding of 16 sequences 47.3 us with bfloat16, 49.6 so.
+// A piece's row beside its O / l, which is float32 as every sum here: the maximum (log2 units)
+// and the sum.  (Half the bytes, in float16 under powers of two and rounded towards 0, moved
+// outputs by up to an eighth of their own rounding step: one token of 16 sequences of 128 heads
+// over 1024 to 8192 keys took 48.1 us so, takes 53.8 us; 60 nodes of 16 heads over 16384 56.6 and
+// 60.9; 8 sequences' trees of 128 heads are as fast.)
 struct PieceRow {
   float m, l;
 };
@@ -40,8 +40,7 @@ struct CutUnit {
 
 struct LatentArgs {
   LatentAttn in;
-  uint16_t* ws_o;    // [2 W][128][DL] float16: pieces' O / l
-  float* ws_factor;  // [2 W][128][4]: and what their quarters are multiplied by
+  float* ws_o;       // [2 W][128][DL]: pieces' O / l
   PieceRow* ws_row;  // [2 W][128]
   CutUnit* ws_cut;   // [W]: the cut unit that begins in a workgroup's share (valid 0: none)
   int W;         // workgroups
@@ -56,37 +55,6 @@ template <typename T>
 __device__ __forceinline__ T rare(T x) {
   asm volatile("" : "+v"(x));
   return x;
-}
-
-// x of the lane that DPP control kCtrl names (within 16; every lane has one).
-template <int kCtrl>
-__device__ __forceinline__ uint32_t from_lane(uint32_t x) {
-  return __builtin_amdgcn_update_dpp(0, static_cast<int>(x), kCtrl, 0xF, 0xF, true);
-}
-
-// 8 values of each of the lanes that hold a quarter of a row, times f, in float16 under
-// the power of two (*factor) that brings the quarter's largest to 2^14 or more.  Rounded
-// towards 0, by the instruction that takes two at once: at most 2^-10 of a value, a
-// quarter of bfloat16's half step.  (Infinities and NaN stay what they are.)
-template <int DL>
-__device__ __forceinline__ u32x4 pack_piece(f32x4 x0, f32x4 x1, float f, float* factor) {
-  float top = fabsf(x0[0]);
-#pragma unroll
-  for (int i = 1; i < 4; ++i) top = fmaxf(top, fabsf(x0[i]));
-#pragma unroll
-  for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(x1[i]));
-  // (on the bits, which are in the values' order: no instruction for a signalling NaN)
-  uint32_t bits = __builtin_bit_cast(uint32_t, top * f) & 0x7FFFFFFFu;
-  bits = max(bits, from_lane<0xB1>(bits));
-  bits = max(bits, from_lane<0x4E>(bits));
-  bits = max(bits, from_lane<0x141>(bits));
-  if constexpr (DL == 512) bits = max(bits, from_lane<0x140>(bits));
-  const uint32_t e = max(bits >> 23, 15u);
-  const float up = __builtin_bit_cast(float, (268u - e) << 23) * f;  // 2^(14 - (e - 127)) f
-  *factor = __builtin_bit_cast(float, (e - 14u) << 23);
-  const f32x4 y0 = x0 * up, y1 = x1 * up;
-  const auto two = [](float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y)); };
-  return u32x4{two(y0[0], y0[1]), two(y0[2], y0[3]), two(y1[0], y1[1]), two(y1[2], y1[3])};
 }
 
 // Where a place of the laid-out units falls.

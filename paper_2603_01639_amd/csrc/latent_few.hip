@@ -308,26 +308,26 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
     for (int d = 0; d < kBlocks; ++d)
       sm.o[wave][row16][(4 * d + part) ^ (row16 & 7)] = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[d] * f;
     __syncthreads();
-    uint16_t* out = whole ? static_cast<uint16_t*>(in.out) + static_cast<int64_t>(b) * in.Nmax * in.Hq * DL
-                          : a.ws_o + static_cast<int64_t>(slot) * kRows * DL;
-#pragma unroll 2
-    for (int e = rare(static_cast<int>(threadIdx.x)); e < 16 * DL / 8; e += kThreads) {
-      const int row = e / (DL / 8), col = e % (DL / 8);
-      f32x4 x0 = f32x4{0.f, 0.f, 0.f, 0.f}, x1 = x0;
+    const auto sum_of = [&](int row, int col) {  // dims 4 col ..
+      f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        x0 += sm.o[w][row][(2 * col) ^ (row & 7)];
-        x1 += sm.o[w][row][(2 * col + 1) ^ (row & 7)];
+      for (int w = 0; w < kWaves; ++w) x += sm.o[w][row][col ^ (row & 7)];
+      return x;
+    };
+    if (whole) {
+      uint16_t* out = static_cast<uint16_t*>(in.out) + static_cast<int64_t>(b) * in.Nmax * in.Hq * DL;
+#pragma unroll 2
+      for (int e = rare(static_cast<int>(threadIdx.x)); e < valid * (DL / 8); e += kThreads) {
+        const int row = e / (DL / 8), col = e % (DL / 8);
+        const f32x4 x0 = sum_of(row, 2 * col), x1 = sum_of(row, 2 * col + 1);
+        *reinterpret_cast<u32x4*>(out + static_cast<int64_t>(row) * DL + col * 8) =
+            u32x4{pack_bf16x2(x0[0], x0[1]), pack_bf16x2(x0[2], x0[3]), pack_bf16x2(x1[0], x1[1]), pack_bf16x2(x1[2], x1[3])};
       }
-      float factor;
-      const u32x4 packed = whole ? u32x4{pack_bf16x2(x0[0], x0[1]), pack_bf16x2(x0[2], x0[3]),
-                                         pack_bf16x2(x1[0], x1[1]), pack_bf16x2(x1[2], x1[3])}
-                                 : pack_piece<DL>(x0, x1, 1.f, &factor);
-      if (row < valid) {
-        *reinterpret_cast<u32x4*>(out + static_cast<int64_t>(row) * DL + col * 8) = packed;
-        if (!whole && col % (DL / 32) == 0)
-          a.ws_factor[(static_cast<int64_t>(slot) * kRows + row) * 4 + col / (DL / 32)] = factor;
-      }
+    } else {
+      float* out = a.ws_o + static_cast<int64_t>(slot) * kRows * DL;
+#pragma unroll 2
+      for (int e = rare(static_cast<int>(threadIdx.x)); e < valid * (DL / 4); e += kThreads)
+        *reinterpret_cast<f32x4*>(out + e * 4) = sum_of(e / (DL / 4), e % (DL / 4));
     }
     __syncthreads();
   }
