@@ -717,9 +717,10 @@ __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
       if (g < count) {
 #pragma unroll
         for (int u = g; u < g + kGroup; ++u) {
-          const float wu = u < count ? __shfl(w, u, 16) : 0.f;
-          // (a piece of weight 0 has no rows to be read: it may hold anything)
-          if (wu != 0.f) {
+          const float wu = __shfl(w, u, 16);
+          // (a piece of weight 0 is added too: it has 0, or NaN where an infinity stood
+          // behind weights of 0, which has to reach the output however the row is cut)
+          if (u < count) {
 #pragma unroll
             for (int i = 0; i < kRuns; ++i)
 #pragma unroll

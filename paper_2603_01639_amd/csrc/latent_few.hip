@@ -297,16 +297,16 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
 #pragma unroll
     for (int w = 0; w < kWaves; ++w)
       if (sm.l[w][row16] != 0.f) L += exp2_fast(sm.m[w][row16] - M) * sm.l[w][row16];
-    // (a wave without a visible key has weight 0 and adds nothing, as does such a piece)
-    const bool none = l_run == 0.f && (L != 0.f || !whole);
-    const float f = none ? 0.f : exp2_fast(m_run * c - M) / L;
+    // (a wave without a visible key has weight 0, as has such a piece, and O = 0, or NaN where
+    // an infinity stood behind weights of 0)
+    const float f = l_run == 0.f && (L != 0.f || !whole) ? 0.f : exp2_fast(m_run * c - M) / L;
     if (!whole && wave == 0 && part == 0 && row16 < valid)
       a.ws_row[static_cast<int64_t>(slot) * kRows + row16] = PieceRow{M, L};
     if (!whole && t0 == 0 && threadIdx.x == 0)
       a.ws_cut[rank] = CutUnit{b, 0, valid, static_cast<int>(latent::quotient(start + length - 1, share))};
 #pragma unroll
     for (int d = 0; d < kBlocks; ++d)
-      sm.o[wave][row16][(4 * d + part) ^ (row16 & 7)] = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[d] * f;
+      sm.o[wave][row16][(4 * d + part) ^ (row16 & 7)] = o[d] * f;
     __syncthreads();
     const auto sum_of = [&](int row, int col) {  // dims 4 col ..
       f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};

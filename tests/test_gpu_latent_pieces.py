@@ -64,3 +64,28 @@ def test_infinities_leave_the_other_dims(shape):
     for b, n in enumerate(sizes):
         assert np.isfinite(got[b, :n][..., rest]).all()
         assert (got[b, :n][..., rest] == clean[b, :n][..., rest]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("rows", ["one far below", "the first half", "the first tile"])
+@pytest.mark.parametrize("shape", CUT + [(16, 512, [40], [1], 0), (2, 256, [45, 70], [5, 1], 16), (20, 512, [70], [1], 0)], ids=named)
+def test_infinities_of_no_weight_reach_the_outputs(shape, rows, dtype):
+    """Rows of the prefix with infinite dims and a score of minus infinity, on a workgroup (or a wave) all of whose other
+    weights are 0 beside the row's largest: the infinite dims of the outputs have no number, cut or not."""
+    H, DL, prefix, sizes, block = shape
+    m = make(sum(prefix) + 7, H, DL, prefix, sizes, block, dtype)
+    m["q"][..., 8:16] = -m["q"][..., 8:16].abs() - 0.5
+    m["q"][..., DL] = 16.0
+    m.update(ql=m["q"][..., :DL], qr=m["q"][..., DL:], layout="rows")
+    for b, P in enumerate(prefix):
+        poison = {"one far below": [P // 5], "the first half": range(P // 2), "the first tile": range(16)}[rows]
+        for r in range(P // 2):
+            page, at = L.place(m["table"], b, r, m["cache"].shape[1])
+            m["cache"][page, at, DL] = -1024.0  # (2^-1700 of the others' weight)
+            if r in poison:
+                m["cache"][page, at, 8:16] = float("inf")
+    out = run(m)
+    for b, n in enumerate(sizes):
+        got = out[b, :n].float().cpu().numpy()
+        assert not np.isfinite(got[..., 8:16]).any(), b
+        assert np.isfinite(got[..., 16:]).all() and np.isfinite(got[..., :8]).all(), b
