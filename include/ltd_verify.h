@@ -584,9 +584,11 @@ int ltd_tree_accept_processed(const float* logits, const int32_t* draft_tokens,
  *                after head h - 1; a head's elements follow one another.  q_out has
  *                strides of its own, with whole rows, or all rows of a head, one after
  *                another (LTD_EINVAL otherwise: no two heads may share memory).
- *                q_out may be q, with the same strides (in place); other overlaps give
- *                undefined results (LTD_EINVAL where queries and keys begin at one
- *                place and either is written there).
+ *                q_out may be q, with the same strides (in place).  Otherwise neither
+ *                output shares memory with an input, or with the other output
+ *                (LTD_EINVAL).  Interleaved heads of one buffer are apart where the
+ *                two have the same strides, or their rows lie in different parts of the
+ *                same row stride; ranges of other strides may not meet.
  *   k, k_out     the same with Hk heads, or Hk = 0 and NULL.
  *   inv_freq     [rot_dim / 2] float64: radians a position.
  *   depth        [B][Nmax] int32 >= 0 (as ltd_select_candidates writes it), or NULL

@@ -770,6 +770,22 @@ def _frequencies(inv_freq):
     return 2 * inv_freq.shape[0]
 
 
+def _heads_meet(off, rows, row, row_out, heads, head, head_out, d):
+    """Whether heads of d bytes share some with the same heads at other strides, `off`
+    bytes on (the binding's form of the call's own check, for tensors whose ranges meet)."""
+    if row != row_out or row < 1:
+        return True
+    if head != head_out:
+        at, wide, wide_out = off % row, (heads - 1) * head + d, (heads - 1) * head_out + d
+        return not (at >= wide and at + wide_out <= row)
+    for v in range(1 - heads, heads):
+        at = off + v * head
+        u = max(1 - rows, (-at - d) // row + 1)  # the first row that begins past d bytes before
+        if u < rows and at + u * row < d:
+            return True
+    return False
+
+
 def _rope_pair(name, t, out, kind, shape):
     """Pointers and strides of a tensor and where it goes, which is the same places
     or none of them."""
@@ -785,7 +801,8 @@ def _rope_pair(name, t, out, kind, shape):
         B, N, H, d = shape
         end = p + size * ((B - 1) * st[0] + (N - 1) * st[1] + (H - 1) * st[2] + (d - 1) * st[3] + 1)
         end_out = po + size * ((B - 1) * so[0] + (N - 1) * so[1] + (H - 1) * so[2] + (d - 1) * so[3] + 1)
-        if p < end_out and po < end:
+        if p < end_out and po < end and _heads_meet(po - p, B * N, rt[0] * size, ro[0] * size, H, rt[1] * size,
+                                                    ro[1] * size, d * size):
             raise ValueError(f"{name}_out overlaps {name}")
     return (p, *rt, po, *ro)
 
@@ -795,7 +812,8 @@ def tree_rope(q, q_out, inv_freq, prefix_len, n_rows, *, k=None, k_out=None, dep
               validate: bool = False, status=None, stream=None):
     """Rotary positions of queries ``[B][Nmax][Hq][d]`` and, if given, keys
     ``[B][Nmax][Hk][d]`` (bfloat16 or float32, views with evenly spaced rows
-    welcome; the outputs may be the inputs, and overlap nothing else); see
+    welcome, other parts of one buffer among them; the outputs may be the inputs,
+    and share memory with nothing else); see
     ``ltd_tree_rope``.  inv_freq ``[rot_dim / 2]`` float64 from
     ``rope_frequencies``, depth ``[B][Nmax]`` int32 for a draft tree's rows."""
     kind = _dtype_code(q)

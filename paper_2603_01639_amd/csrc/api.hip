@@ -8,6 +8,7 @@
 
 #include "ltd_launch.hpp"
 #include "ltd_verify.h"
+#include "runs.hpp"
 
 namespace {
 
@@ -610,12 +611,23 @@ int ltd_tree_rope(const void* q, int64_t q_row_stride, int64_t q_head_stride, vo
     return LTD_EINVAL;
   if (Hk > 0 && k == k_out && (k_row_stride != k_out_row_stride || k_head_stride != k_out_head_stride))
     return LTD_EINVAL;
-  // (nor may queries and keys be exchanged, or written to one place)
-  if (Hk > 0 && (q_out == k_out || q_out == k || k_out == q)) return LTD_EINVAL;
   const int64_t rows = static_cast<int64_t>(B) * Nmax;
   if (!heads_apart(rows, Hq, d, q_out_row_stride, q_out_head_stride) ||
       (Hk > 0 && !heads_apart(rows, Hk, d, k_out_row_stride, k_out_head_stride)))
     return LTD_EINVAL;
+  // (workgroups write heads at times when others still read theirs)
+  const auto runs = [&](const void* p, int64_t row, int H, int64_t head) {
+    const int64_t elem = dtype == LTD_DTYPE_F32 ? 4 : 2;
+    return ltd::Runs{reinterpret_cast<uintptr_t>(p), rows, static_cast<ltd::Wide>(row) * elem, H, static_cast<ltd::Wide>(head) * elem, d * elem};
+  };
+  const ltd::Runs q_in = runs(q, q_row_stride, Hq, q_head_stride), q_to = runs(q_out, q_out_row_stride, Hq, q_out_head_stride);
+  if (q != q_out && ltd::runs_meet(q_in, q_to)) return LTD_EINVAL;
+  if (Hk > 0) {
+    const ltd::Runs k_in = runs(k, k_row_stride, Hk, k_head_stride), k_to = runs(k_out, k_out_row_stride, Hk, k_out_head_stride);
+    if ((k != k_out && ltd::runs_meet(k_in, k_to)) || ltd::runs_meet(q_to, k_in) || ltd::runs_meet(k_to, q_in) ||
+        ltd::runs_meet(q_to, k_to))
+      return LTD_EINVAL;
+  }
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (validate) {
     if (ltd::launch_validate_rows(prefix_len, depth, n_rows, B, Nmax, status, st) != hipSuccess)
