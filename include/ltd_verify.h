@@ -672,15 +672,16 @@ int ltd_latent_append(const void* kv_new, int64_t new_row_stride, const void* no
  *                [Hq][B][Nmax][d_latent], as a product per head leaves it).
  *                With bfloat16 rows and heads are 16-byte aligned (LTD_EINVAL).
  *   out          [B][Nmax][Hq][d_latent] (dtype), 16-byte aligned; rows i >=
- *                n_nodes[b] are not written.  It overlaps neither queries (LTD_EINVAL
- *                where the two ranges of bytes meet) nor the cache.
+ *                n_nodes[b] are not written.  It overlaps neither queries nor the cache
+ *                (LTD_EINVAL where the two ranges of bytes meet).
  *   scale        finite and > 0 (that of the expanded heads, which the latent size
  *                does not tell).
  *   prefix_len, max_prefix, parents, n_nodes, block_table as for
  *   ltd_tree_verify_attn; a single token a sequence is a tree of one node.
  *   workspace    at least ltd_tree_verify_attn_latent_workspace_size() bytes for the
  *                same (B, Nmax, Hq, d_latent, d_rope, max_prefix, dtype), 16-byte
- *                aligned; needs no initialisation.
+ *                aligned; needs no initialisation.  The bytes that the query tells lie
+ *                outside queries, cache and out (LTD_EINVAL).
  * A NaN or an infinity in a row's latent part, or a NaN score, reaches the outputs
  * of the nodes that see the row (where it may make every dimension NaN), and no
  * others.  Hq <= LTD_LATENT_MAX_HEADS; B <= 65535 with float32.

@@ -755,6 +755,17 @@ int ltd_tree_verify_attn_latent(const void* q_latent, int64_t ql_row_stride,
   if (meet(to, span_of(q_latent, rows, ql_row_stride, Hq, ql_head_stride, d_latent, elem)) ||
       meet(to, span_of(q_rope, rows, qr_row_stride, Hq, qr_head_stride, d_rope, elem)))
     return LTD_EINVAL;
+  // (nor may outputs or pieces be written where keys, queries or each other lie)
+  const int D = d_latent + d_rope;
+  const Span keys = span_of(cache, static_cast<int64_t>(block_table ? num_blocks : B) * kv_rows, D, 1, 0, D, elem);
+  if (meet(to, keys)) return LTD_EINVAL;
+  if (need > 0) {
+    const __int128 at = static_cast<__int128>(reinterpret_cast<uintptr_t>(workspace));
+    const Span pieces{at, at + need};
+    if (meet(pieces, to) || meet(pieces, keys) || meet(pieces, span_of(q_latent, rows, ql_row_stride, Hq, ql_head_stride, d_latent, elem)) ||
+        meet(pieces, span_of(q_rope, rows, qr_row_stride, Hq, qr_head_stride, d_rope, elem)))
+      return LTD_EINVAL;
+  }
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (validate) {
     if (ltd::launch_validate_tree(block_table, prefix_len, parents, n_nodes, B, Nmax, max_prefix,

@@ -3,7 +3,7 @@ the binding lets other parts of one buffer through (to its refusal of CPU tensor
 import pytest
 
 import paper_2603_01639_amd as ltd
-from test_latent_refusals import BAD, rope
+from test_latent_refusals import BAD, attn, rope
 
 F = 1 << 20  # bytes that no case reaches by chance
 
@@ -60,3 +60,30 @@ def test_binding_takes_other_parts_of_one_buffer():
         run(buf[:, :, :8], buf[:, :, 7:15])
     with pytest.raises(ValueError, match="q_out overlaps q"):  # heads two apart and one apart
         run(buf[:, :, 0:16:2], buf[:, :, 8:16])
+
+
+# A sequence's 64 cache rows of 576 float32 elements are 147456 bytes, four rows of 16 heads of 512 131072, of 64 16384.
+APART = dict(ql=F, qr=2 * F, cache=3 * F, out=4 * F)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(out=3 * F), dict(out=3 * F + 147456 - 16), dict(out=3 * F - 131072 + 16), dict(out=3 * F + 1024),
+    dict(B=2, out=3 * F + 2 * 147456 - 16), dict(table=F, mb=1, nb=5, out=3 * F + 5 * 147456 - 16)])
+def test_attention_refuses_outputs_over_its_cache(kw):
+    assert attn(**{**APART, **kw}) == BAD
+
+
+def size():
+    n = ltd.attn_latent_workspace_size(1, 60, 16, 512, 64, 4096, ltd.DTYPE_BF16)
+    assert n > 0
+    return n
+
+
+# bfloat16, 60 nodes, one sequence of 8192 rows: out and q_latent 983040 bytes, q_rope 122880, cache 9437184
+@pytest.mark.parametrize("over, at", [("ql", 0), ("ql", 983040 - 16), ("qr", 0), ("qr", 122880 - 16), ("cache", 0),
+                                      ("cache", 9437184 - 16), ("out", 0), ("out", 983040 - 16), ("ql", None), ("out", None)])
+def test_attention_refuses_a_workspace_over_its_tensors(over, at):
+    """From byte `at` of the tensor on, or with its last 16 bytes over the tensor's first."""
+    place = dict(ql=1 << 40, qr=2 << 40, cache=3 << 40, out=4 << 40)
+    ws = place[over] + (16 - size() // 16 * 16 if at is None else at)
+    assert attn(**place, dtype=1, N=60, mp=4096, rows=8192, qlr=8192, ws=ws, wsb=1 << 38) == BAD
