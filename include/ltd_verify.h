@@ -577,7 +577,8 @@ int ltd_tree_accept_processed(const float* logits, const int32_t* draft_tokens,
  *     (mscale (x0 cos t - x1 sin t), mscale (x1 cos t + x0 sin t)),  t = p * inv_freq[j].
  * The angle is formed and reduced in float64, so that a position a million tokens
  * out is as exact as the first; the rest is float32, rounded once.  Other dims
- * are copied.
+ * are copied: a factor that scores as a whole are to have (YaRN's, squared) goes into
+ * mscale only where all dims turn, and into the attention's scale otherwise.
  *
  *   q, q_out     [B][Nmax] rows of Hq heads of d elements (dtype): row (b, i) starts
  *                at (b * Nmax + i) * q_row_stride, its head h q_head_stride elements
@@ -639,7 +640,8 @@ int ltd_tree_rope(const void* q, int64_t q_row_stride, int64_t q_head_stride, vo
  *                outside the cache (LTD_EINVAL).
  *   norm_weight  [d_latent] (dtype), 16-byte aligned, or NULL; norm_eps finite, >= 0.
  *   inv_freq     [d_rope / 2] float64; interleaved, mscale, depth and n_rows as for
- *                ltd_tree_rope.
+ *                ltd_tree_rope (a factor for whole scores goes into the attention's
+ *                scale: mscale would multiply the rotated part alone).
  * Other rows keep their bytes.  No two sequences may append to the same row.  With
  * validate != 0: LTD_STATUS_BAD_NNODES, LTD_STATUS_BAD_PREFIX (P_b < 0, rows past the
  * capacity or LTD_MAX_LENGTH) and LTD_STATUS_BAD_BLOCK (ids of the blocks that are
@@ -675,7 +677,7 @@ int ltd_latent_append(const void* kv_new, int64_t new_row_stride, const void* no
  *                n_nodes[b] are not written.  It overlaps neither queries nor the cache
  *                (LTD_EINVAL where the two ranges of bytes meet).
  *   scale        finite and > 0 (that of the expanded heads, which the latent size
- *                does not tell).
+ *                does not tell, times the square of a context scaling's factor).
  *   prefix_len, max_prefix, parents, n_nodes, block_table as for
  *   ltd_tree_verify_attn; a single token a sequence is a tree of one node.
  *   workspace    at least ltd_tree_verify_attn_latent_workspace_size() bytes for the

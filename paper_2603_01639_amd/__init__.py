@@ -690,6 +690,11 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, *, scaling: Optional[s
     - ``"yarn"``: a pair that turns more than beta_fast times within trained_len keeps
       f_j, one that turns less than beta_slow times gets f_j / factor, with a
       linear ramp over the pair's index between; mscale = 0.1 ln(factor) + 1.
+      This factor is meant for whole queries and keys: it multiplies every
+      score by mscale^2.  ``mscale=`` of the rotations does so where all dims of a
+      head turn.  Where only a part does (a latent cache's rows, part of a head)
+      it would raise that part of the score alone: leave ``mscale=`` at 1 there
+      and multiply the attention's scale by mscale^2.
     - ``"bands"``: a pair whose wavelength is below trained_len / high_factor keeps
       f_j, one above trained_len / low_factor gets f_j / factor, and between them
       the two are blended by trained_len / wavelength.
@@ -815,7 +820,8 @@ def tree_rope(q, q_out, inv_freq, prefix_len, n_rows, *, k=None, k_out=None, dep
     welcome, other parts of one buffer among them; the outputs may be the inputs,
     and share memory with nothing else); see
     ``ltd_tree_rope``.  inv_freq ``[rot_dim / 2]`` float64 from
-    ``rope_frequencies``, depth ``[B][Nmax]`` int32 for a draft tree's rows."""
+    ``rope_frequencies``, depth ``[B][Nmax]`` int32 for a draft tree's rows.
+    mscale multiplies the turned dims alone (see ``rope_frequencies``)."""
     kind = _dtype_code(q)
     shape = _dims("q", q, 4)
     B, Nmax, Hq, d = shape
@@ -869,7 +875,10 @@ def latent_append(kv_new, cache, inv_freq, prefix_len, n_rows, *, depth=None, no
     """Rows of a prompt or a draft tree into a latent cache; see
     ``ltd_latent_append``.  kv_new ``[B][Nmax][d_latent + d_rope]`` (bfloat16 or
     float32, a view with evenly spaced rows), cache ``[pages][rows][d_latent +
-    d_rope]``, inv_freq ``[d_rope / 2]`` float64, norm_weight ``[d_latent]``."""
+    d_rope]``, inv_freq ``[d_rope / 2]`` float64, norm_weight ``[d_latent]``.
+    mscale multiplies the turned dims alone: 1 for a model that scales its
+    contexts by YaRN, whose factor's square goes into the attention's scale
+    (see ``rope_frequencies``)."""
     pages, kv_rows, D, max_blocks = _latent_cache(cache, block_table, num_blocks, 0)
     kind = _dtype_code(kv_new)
     if _kind(cache) != kind:
