@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
       const bool masked = (t + 1) * static_cast<int64_t>(kKeys) > P;
       uint32_t bad = 0;
       if (masked) {
-        uint32_t any = 0;  // of key lane / 4: a lane looks at its 16 bytes of every 64
+        uint32_t any = 0;  // bits of keys: 64 lanes look at 128 bytes of eight of them at a time
 #pragma unroll 1
         for (int e = 0; e < kKeys * DL * 2 / 16 / kWave; ++e) {
           const int at = (e * kWave + lane) * 16;
