@@ -662,11 +662,11 @@ int ltd_latent_append(const void* kv_new, int64_t new_row_stride, const void* no
  * of the cache:
  *     out[b][i][h] = softmax_t(scale * (<q_latent[b][i][h], c_t> + <q_rope[b][i][h], k_t>)) . c_t
  * over the visible rows t = {0, ..., P_b - 1} u {P_b + j : j on the root path of
- * node i, i included}.  Statistics and accumulation are float32; with bfloat16 the
- * weights are rounded to bfloat16 before they multiply the values, and the sum that
- * normalises them is that of the rounded ones; partial results of a row that the call
- * splits over its keys are float32.  Latent values may be as large as 2^80:
- * weights of up to 2^16 multiply them before the sum divides.
+ * node i, i included}.  Statistics and accumulation are float32, and so are partial
+ * results of a row that the call splits over its keys; with bfloat16 the weights are
+ * rounded to bfloat16 before they multiply the values (to 16 bits where Nmax * Hq <= 16),
+ * and the sum that normalises them is that of the rounded ones.  Latent values may be
+ * as large as 2^80: weights of up to 2^16 multiply them before the sum divides.
  *
  *   q_latent     rows of Hq heads of d_latent elements, q_rope of d_rope elements
  *                (dtype): row (b, i) at (b * Nmax + i) * row stride, head h at h * head

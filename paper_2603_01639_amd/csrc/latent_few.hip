@@ -6,10 +6,10 @@
 // buffer of its own in LDS that direct loads fill, rows in registers, and no barrier
 // until the share ends.
 //   S^T[key][row] = X Q^T         (v_mfma_f32_16x16x32_bf16, 18 a tile)
-//   O^T[dim][row] += C^T P^T      (v_mfma_f32_16x16x16_bf16, 32 a tile)
-// A lane's four accumulators of S^T are four keys of its row and as they are, rounded,
-// its operand P^T; C^T comes from the same tile by transposed reads.  The waves' results
-// are joined through LDS at the end.
+//   O^T[dim][row] += C^T P^T      (the same with both parts of 16 weights, 32 a tile)
+// A lane's four accumulators of S^T are four keys of its row and as they are, in two parts,
+// its operand P^T; C^T comes from the same tile by transposed reads, each value twice.  The
+// waves' results are joined through LDS at the end.
 //
 // 16 heads, this kernel and the one for many rows (which pads them to 128), both with
 // the merge, in a graph: one token of a sequence over 1000 keys 19 us, 19; of 16
@@ -26,8 +26,6 @@ namespace {
 constexpr int kKeys = 16;            // of a tile
 constexpr int kPlane = kKeys * 128;  // 64 dims of a tile in LDS
 
-typedef short bf16x4 __attribute__((ext_vector_type(4)));
-
 // A tile's 16-byte chunks within a plane trade places by their key: neither 16 lanes of
 // an S^T operand's read (one chunk of 16 keys; even and odd ones lie in different halves
 // of the banks) nor 32 lanes of a transposed read (32 bytes of eight keys) meet on a bank.
@@ -40,9 +38,6 @@ __device__ __forceinline__ int swz(int key) {
 // sum waits: 16 wait states are more than either product takes.
 __device__ __forceinline__ void mfma_s(f32x4& s, bf16x8 a, bf16x8 b) {
   asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
-}
-__device__ __forceinline__ void mfma_o(f32x4& o, bf16x4 a, bf16x4 b) {
-  asm volatile("v_mfma_f32_16x16x16_bf16 %0, %1, %2, %0" : "+v"(o) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void mfma_first(f32x4& s, bf16x8 a, bf16x8 b) {
   asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
@@ -251,14 +246,25 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
         for (int d = 0; d < kBlocks; ++d) o[d] *= alpha;
         m_run = m_new;
       }
-      const uint32_t w0 = pack_bf16x2(exp2_fast(__builtin_fmaf(s[0], c, neg)), exp2_fast(__builtin_fmaf(s[1], c, neg)));
-      const uint32_t w1 = pack_bf16x2(exp2_fast(__builtin_fmaf(s[2], c, neg)), exp2_fast(__builtin_fmaf(s[3], c, neg)));
-      // (the sum is that of the rounded weights, the very ones that multiply the values)
+      // Weights in two parts, rounded and what that left, 16 bits in all: a product of 32
+      // factors takes the time of one of 16, and with one part the outputs' error was 0.0019
+      // of them where their own rounding gives 0.0017 (one token of 16 sequences of 16 heads 32.1
+      // us a call, with one part 32.6).
+      u32x4 w;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float p0 = exp2_fast(__builtin_fmaf(s[2 * j], c, neg)), p1 = exp2_fast(__builtin_fmaf(s[2 * j + 1], c, neg));
+        w[j] = pack_bf16x2(p0, p1);
+        w[2 + j] = pack_bf16x2(p0 - __builtin_bit_cast(float, w[j] << 16), p1 - __builtin_bit_cast(float, w[j] & 0xFFFF0000u));
+      }
+      // (the sum is that of the very weights that multiply the values)
       const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
-      l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w0), ones, l_run, false);
-      l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w1), ones, l_run, false);
-      bf16x4 pf = __builtin_bit_cast(bf16x4, (static_cast<uint64_t>(w1) << 32) | w0);
-      asm volatile("s_nop 1" : "+v"(pf));  // (a product reads what vector operations wrote two wait states later)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t two = w[j];
+        l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), ones, l_run, false);
+      }
+      bf16x8 pf = __builtin_bit_cast(bf16x8, w);
       if (bad != 0) {
 #pragma unroll 1
         for (int e = 0; e < kKeys * DL * 2 / 16 / kWave; ++e) {
@@ -267,11 +273,18 @@ __global__ void __launch_bounds__(kThreads, 1) latent_few_kernel(LatentArgs a) {
         }
         __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
       }
+      for_each_index<kBlocks / 4>([&](auto plane) {
+        bf16x8 vf[4];
 #pragma unroll
-      for (int d = 0; d < kBlocks; ++d) {
-        const bf16x4 vf = __builtin_bit_cast(bf16x4, lds_read_tr(kv + (v_rd ^ ((d & 3) << 5)) + (d >> 2) * kPlane));
-        mfma_o(o[d], vf, pf);
-      }
+        for (int d = 0; d < 4; ++d) {
+          const s16x4 v = lds_read_tr(kv + (v_rd ^ (d << 5)) + plane() * kPlane);
+          vf[d] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v, v, 0, 1, 2, 3, 0, 1, 2, 3));
+        }
+        // (a product reads what vector operations wrote two wait states later)
+        asm volatile("s_nop 1" : "+v"(vf[0]), "+v"(vf[1]), "+v"(vf[2]), "+v"(vf[3]), "+v"(pf));
+#pragma unroll
+        for (int d = 0; d < 4; ++d) mfma_s(o[4 * plane() + d], vf[d], pf);
+      });
       if (t + 2 * kWaves < t1) {
         const int id0 = kPaged ? sm.ids[wave][buffer][load_key] : 0, id1 = kPaged ? sm.ids[wave][buffer][load_key + 8] : 0;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the buffer's last reads are done

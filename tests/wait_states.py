@@ -152,7 +152,7 @@ def scalar_base(code):
 # Passes of the matrix products in use.  What reads or writes a product's sums, but a product that adds to the same ones,
 # comes passes + 4 wait states later; so does a product that takes them as factors.  (What hipcc keeps for its own products
 # on gfx950: 12 behind one of 8 passes, 8 behind one of 4.)
-PASSES = {"v_mfma_f32_32x32x16_bf16": 8, "v_mfma_f32_16x16x32_bf16": 4, "v_mfma_f32_16x16x16_bf16": 4}
+PASSES = {"v_mfma_f32_32x32x16_bf16": 8, "v_mfma_f32_16x16x32_bf16": 4}
 
 
 def sums(code):
