@@ -63,8 +63,9 @@ __device__ __forceinline__ int rare_thread() { return rare(static_cast<int>(thre
 // The products by hand: O's accumulators take all 256 accumulation registers, and S's
 // go to vector registers (the compiler would keep both in the former, and move O out
 // and in for every tile).  A product may follow one that it adds to at once; what
-// else reads a sum waits for it, 18 wait states at most after a product of 8 passes
-// (mfma_settle), which nobody else sees to.
+// else touches a sum waits for it, 12 wait states behind a product of 8 passes.  The
+// compiler does not see to that here: mfma_settle does, and a test reads the distances
+// from the listing.
 __device__ __forceinline__ void mfma_acc(f32x16& o, bf16x8 a, bf16x8 b) {
   asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o) : "v"(a), "v"(b));
 }
@@ -318,6 +319,12 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
     // score passes it by 2^kLazyMax, a weight a piece, and what follows from them.
     // (With two products and two weights a piece the vector operations of a piece
     // outlasted the second product: 1250 cycles a tile where the products take 670.)
+    //
+    // They are rounded to bfloat16, as one factor of the products: outputs are off by 0.0020 of
+    // them where their own rounding gives 0.0017.  With what the rounding left as a second
+    // part, 32 more products a tile beside 68, the difference was gone and 8 sequences of
+    // 128 heads took 731 us instead of 556, 60 nodes of 16 heads over 16384 keys 68 instead of 58,
+    // one token of 16 sequences of 128 heads 58 instead of 53.
     float alpha = 1.f, top, neg, ps, p0;
     uint64_t moves;
     u32x4 pk[2];
@@ -633,17 +640,18 @@ __global__ void __launch_bounds__(kThreads, 1) latent_attn_kernel(LatentArgs a) 
 // Joins the pieces of cut unit blockIdx.x (in the order of the shares that they begin in), a
 // wave a row, kBatch pieces at a time: lane 16 g + p takes piece p's maximum and sum for the
 // weights, then each lane its dims of every piece.  The pieces are asked for before their
-// weights are known, and with kAhead those of the next batch before the last one's are
-// summed up.
+// weights are known, and those of the next batch before the last one's are summed up (one token
+// of a sequence of 16 heads over 8192 keys 24.4 us a call, 26.4 otherwise; where units have few
+// pieces it changes nothing).
 //
-// Bound: the pieces' bytes where there are many rows (256 workgroups' 67 MB),
+// Bound: the pieces' bytes where there are many rows (256 workgroups' 67 MB in about 13 us),
 // one row's chain of loads where there are few.  (With a workgroup per share that looked
 // up whether a cut begins there, and pieces' loads behind their weights, one token of 128
 // heads over 4096 keys took 1 us more.)
-template <int DL, int kBatch, bool kAhead>
+template <int DL>
 __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
   constexpr int kRuns = DL / (4 * kWave);  // of 4 dims a lane, 256 dims apart
-  constexpr int kGroup = 4;                // pieces whose loads go out together
+  constexpr int kBatch = 8, kGroup = 4;    // pieces, and those whose loads go out together
   static_assert(kBatch % kGroup == 0 && kBatch <= 16, "a batch's pieces lie across 16 lanes");
   const LatentAttn& in = a.in;
   if (halted(in.status)) return;
@@ -732,19 +740,10 @@ __global__ void __launch_bounds__(kThreads) latent_merge_kernel(LatentArgs a) {
   Batch t0, t1;
   fetch(t0, 0);
   for (int p = 0; p < pieces; p += 2 * kBatch) {
-    if constexpr (kAhead) {
-      if (p + kBatch < pieces) fetch(t1, p + kBatch);
-      add(t0, p);
-      if (p + 2 * kBatch < pieces) fetch(t0, p + 2 * kBatch);
-      if (p + kBatch < pieces) add(t1, p + kBatch);
-    } else {
-      add(t0, p);
-      if (p + kBatch < pieces) {
-        fetch(t0, p + kBatch);
-        add(t0, p + kBatch);
-      }
-      if (p + 2 * kBatch < pieces) fetch(t0, p + 2 * kBatch);
-    }
+    if (p + kBatch < pieces) fetch(t1, p + kBatch);
+    add(t0, p);
+    if (p + 2 * kBatch < pieces) fetch(t0, p + 2 * kBatch);
+    if (p + kBatch < pieces) add(t1, p + kBatch);
   }
   const float inv = 1.f / L;
   uint16_t* out = static_cast<uint16_t*>(in.out) + (static_cast<int64_t>(cut.b) * in.Nmax * in.Hq + cut.r0 + row) * DL;
@@ -878,14 +877,11 @@ hipError_t launch_bf16(const LatentArgs& a, hipStream_t stream) {
     rc = hipGetLastError();
   }
   if (rc != hipSuccess || a.W < 2) return rc;
-  // At most so many units are cut.  Where that leaves a unit 16 pieces or more, a wave has 32
-  // of a row's on the way; where there are more units, and rows, more waves fit a compute
-  // unit (64 units of 128 rows 68.2 us a call, 71.7 the other way).
+  // At most so many units are cut.
   const latent::Cut cut = few ? latent::kFew : latent::kMany;
   const int64_t units = a.in.B * latent::units_of(a.in.Nmax, a.in.Hq, cut);
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>(a.W - 1, units)), cut.rows / kWaves);
-  if (a.W >= 16 * units) hipLaunchKernelGGL((latent_merge_kernel<DL, 8, true>), grid, dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((latent_merge_kernel<DL, 8, false>), grid, dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL((latent_merge_kernel<DL>), grid, dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -12,11 +12,11 @@
 // waves' results are joined through LDS at the end.
 //
 // 16 heads, this kernel and the one for many rows (which pads them to 128), both with
-// the merge, in a graph: one token of a sequence over 1000 keys 19 us, 19; of 16
-// sequences 22, 22; of 16 over 1024 to 8192 keys 34, 38; of 16 over 8192 keys 48, 54; of 128
-// over 2048 keys 78, 100.  With 32 rows, in two units that each read the cache, 16
-// sequences over 8192 keys took 58 us where the other kernel took 48, hence the rule.
-// 16 sequences over 1024 to 8192 keys (85 MB) take 26 to 28 us before the merge, half of it the
+// the merge, in a graph: one token of a sequence over 1000 keys 17.8 us, 18.9; of 16
+// sequences 21, 22; of 16 over 1024 to 8192 keys 33, 40; of 16 over 8192 keys 47, 55; of 128
+// over 2048 keys 79, 100.  With 32 rows, in two units that each read the cache, 16
+// sequences over 8192 keys took 58 us where the other kernel takes 55, hence the rule.
+// 16 sequences over 1024 to 8192 keys (85 MB) take 25 to 26 us before the merge, half of it the
 // stream at 6 TB/s, the rest the search, the first loads and the join.
 #include "latent_attn.hpp"
 
@@ -35,7 +35,7 @@ __device__ __forceinline__ int swz(int key) {
 
 // The products by hand, sums in vector registers (the compiler would keep them in the
 // accumulation registers and move all of O out and in for every tile).  What else reads a
-// sum waits: 16 wait states are more than either product takes.
+// sum waits: 16 wait states are more than a product takes.
 __device__ __forceinline__ void mfma_s(f32x4& s, bf16x8 a, bf16x8 b) {
   asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
 }

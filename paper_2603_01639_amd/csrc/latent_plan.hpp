@@ -19,11 +19,10 @@ constexpr int kFewRows = 16;  // ... and the most of a call that takes the kerne
 // tiles: the workgroup that begins one behind another's last piece loads queries, and
 // stores a piece, twice), and the shortest share.  A share may lie within a unit's own
 // cost and has nothing to do then.  (With a cost of 6 and shares of 10, 4 and 8 for few
-// rows, the workgroups with two units' pieces ended last, 52 us after the launch where
-// the others took 43: 60 nodes of 16 heads over 16384 keys 62.4 us a call, 58.5 so, over 2041
-// keys 40.0 and 35.0, 8 nodes of 128 heads over 2048 keys 37.2 and 31.0, one token of 16
-// sequences of 16 heads over 1024 to 8192 keys 37.2 and 33.9, over 500 to 1500 29.4 and 22.7.
-// Shares of 3, or costs of 16 and 20, changed nothing beyond 2%.)
+// rows, the workgroups with two units' pieces end last: one token of 16 sequences of 16 heads
+// over 1024 to 8192 keys 35.8 us a call, 33.0 so, over 500 to 1500 27.8 and 22.4; 8 nodes of 128
+// heads over 2048 keys 36.8 and 31.9, 60 nodes of 16 heads over 2041 40.0 and 35.8, over 16384 64.1
+// and 61.9.  Shares of 3, or costs of 16 and 20, changed nothing beyond 2%.)
 struct Cut {
   int rows, cost, min_share;
 };
