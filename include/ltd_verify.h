@@ -49,7 +49,7 @@
  *   `stream` (a hipStream_t passed as void*, NULL = the default stream).
  * - Return value: LTD_OK, or a negative LTD_E* code when the call itself is
  *   malformed (nothing is launched then).  These checks use only the scalar
- *   arguments and pointer nullness.
+ *   arguments and the pointers themselves (null, aligned, apart where a call says so).
  * - Data-dependent checks (tree shape, prefix bounds, block ids, paths) run on
  *   the device only when `validate != 0`: a validation kernel writes an
  *   LTD_STATUS_* code to `*status` (0 when the data is well formed) and, when
